@@ -68,6 +68,7 @@ enum {
                                     next on the stream (e.g. the backward) instead of in front of it; out_host is complete
                                     once a LATER call on the context -- moe_ffn_bwd_host, the next moe_ffn_fwd_host,
                                     moe_get_status -- has completed, not yet when this call's stream work has */
+  MOE_FLAG_W4 = 64u,           /* room in the workspace for moe_ffn_fwd_w4: T_max * (k + n_shared) + 127 (E + n_shared) fp32 rows of d */
   MOE_FLAG_TRACE = 8u,         /* the persistent launches record a per-tile trace (role, phase, item,
                                   start and end time) into the workspace; read it with
                                   moe_debug_trace (moe_b200_debug.h).  Costs 8 MB of workspace and one
@@ -242,6 +243,63 @@ int moe_router_fwd(moe_ctx* ctx, const uint16_t* x, const uint16_t* W_r, int32_t
                    float* topk_w, float* logits, int32_t* counts, void* stream);
 int moe_router_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, const float* d_topk_w, int32_t T,
                    float* d_logits, void* stream);
+
+/* ---- Balance losses of the router -------------------------------------------------------------------------
+ * What keeps the experts evenly used while the router is trained, with the counts it is computed from:
+ *   p[t][e] = softmax(logits[t])_e, or with MOE_FLAG_SIGMOID_GATE sigmoid(logits[t][e]) / sum_e' sigmoid(logits[t][e'])
+ *   counts[s][e] = slots of sequence s that name expert e;  tokens[s] = its tokens, tokens[n_seq] = all sequences' together
+ *   prob[s][e] = mean of p[t][e] over the sequence's tokens (0 for a sequence without tokens)
+ *   losses[0] = 1/n_seq * sum_s E / (k tokens[s]) * sum_e counts[s][e] prob[s][e]      (1 where everything is even)
+ *   losses[1] = mean over all sequences' tokens of logsumexp(logits[t])^2              (the z loss)
+ * Sequence s is the tokens [seq_offsets[s], seq_offsets[s + 1]) (device int32[n_seq + 1], ascending, within [0, T]; NULL with
+ * n_seq = 1: the whole batch); tokens outside of all sequences take no part, nor do tokens whose token_mask (device uint8[T], may be
+ * NULL) is 0.  Ids out of range are not counted.  A token whose logits are all -infinity has p = 0 and a z loss of 0.
+ * losses[2] fp32, counts[n_seq][E] int32, prob[n_seq][E] fp32, tokens[n_seq + 1] int32: overwritten.  The sums' order is fixed.
+ *
+ * moe_balance_bwd: d_logits[T][E] fp32 (overwritten; may be the logits themselves) = d_losses[0] * d losses[0] / d logits +
+ * d_losses[1] * d losses[1] / d logits (the counts pass no gradient) + what moe_router_bwd gives for d_topk_w[T][k] (NULL: without;
+ * then topk_ids may be NULL too).  An expert that a token names twice gets both gradients.  counts and tokens as the forward left them,
+ * d_losses[2] on the device.  Tokens that take no part get the scores' gradient alone.
+ * Offsets that do not ascend give unspecified values.  Both calls are asynchronous on `stream`. */
+int moe_balance_fwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, int32_t T, const int32_t* seq_offsets, int32_t n_seq,
+                    const uint8_t* token_mask, float* losses, int32_t* counts, float* prob, int32_t* tokens, void* stream);
+int moe_balance_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, const int32_t* counts, const int32_t* tokens, const float* d_losses,
+                    const float* d_topk_w, int32_t T, const int32_t* seq_offsets, int32_t n_seq, const uint8_t* token_mask, float* d_logits,
+                    void* stream);
+
+/* ---- Experts with 4-bit weights ---------------------------------------------------------------------------
+ * A weight is w = s (q - z): codes q in 0..15, a bf16 scale s and, in matrices with zero points, z in 0..15 for every `group` (32, 64
+ * or 128) consecutive columns of a row; without zero points z = 8.  cols need not be a multiple of the group.
+ *
+ * Weights are laid out once for the kernels: n matrices [rows][cols] (cols % 8 == 0) become codes (n * code_bytes), scales (n *
+ * group_elems bf16) and zeros (n * group_elems bytes; NULL: no zero points), all 16-byte aligned, the sizes from moe_w4_sizes.  The
+ * layout is the library's; flags = MOE_W4_GATE_UP for W_gate_up (rows = 2F, gate rows first, F % 8 == 0), 0 for W_down.
+ *   moe_w4_quantize   from bf16 W[n][rows][cols] (finite values).  Without zero points s = bf16(max|w| / 7), q = round(w / s) + 8;
+ *                     with them s = bf16((max(w, 0) - min(w, 0)) / 15), z = round(-min(w, 0) / s), q = round(w / s) + z; both kept in 0..15
+ *   moe_w4_pack       from codes q[n][rows][cols / 2], the even column in the low half of each byte, with q_scales[n][rows][ceil(cols /
+ *                     group)] bf16 and q_zeros[same] bytes (NULL: no zero points; then zeros must be NULL too); q 4-byte aligned
+ *   moe_w4_dequantize back to bf16 W[n][rows][cols] = bf16(s (q - z))
+ * These three need no context and are asynchronous on `stream`.
+ *
+ * moe_ffn_fwd_w4: moe_ffn_fwd's layer over such weights (W_gate_up: E + S matrices [2F][d], W_down: E + S matrices [d][F]), any T up to
+ * T_max, on a context with MOE_FLAG_W4 (MOE_ERR_STATE otherwise).  bf16 x and out, fp32 sums, scales applied in fp32; the activations
+ * between the two products are bf16.  It uses the context's layout: a forward saved for moe_ffn_bwd is given up.
+ * MOE_ERR_TOO_LARGE: a row of d or F elements does not fit shared memory (about 90000). */
+#define MOE_W4_GATE_UP 1u
+typedef struct {
+  const uint32_t* codes;
+  const uint16_t* scales;
+  const uint8_t* zeros; /* NULL: no zero points */
+  int32_t group;
+} moe_w4_weights;
+int moe_w4_sizes(int32_t rows, int32_t cols, int32_t group, uint32_t flags, size_t* code_bytes, size_t* group_elems);
+int moe_w4_quantize(const uint16_t* W, int32_t n, int32_t rows, int32_t cols, int32_t group, uint32_t flags, uint32_t* codes, uint16_t* scales,
+                    uint8_t* zeros, void* stream);
+int moe_w4_pack(const uint8_t* q, const uint16_t* q_scales, const uint8_t* q_zeros, int32_t n, int32_t rows, int32_t cols, int32_t group, uint32_t flags,
+                uint32_t* codes, uint16_t* scales, uint8_t* zeros, void* stream);
+int moe_w4_dequantize(const moe_w4_weights* w, int32_t n, int32_t rows, int32_t cols, uint32_t flags, uint16_t* W, void* stream);
+int moe_ffn_fwd_w4(moe_ctx* ctx, const uint16_t* x, const int32_t* topk_ids, const float* topk_w, const moe_w4_weights* W_gate_up,
+                   const moe_w4_weights* W_down, uint16_t* out, int32_t T, void* stream);
 
 /* ---- Scheduling microbenchmark: SwiGLU + Add operator pair (Section 6.1, Section 6.2) -------------
  * The two element-wise operators the paper uses to study scheduling in isolation, on

@@ -17,7 +17,8 @@ import threading
 import torch
 
 MOE_FLAG_RENORM_TOPK, MOE_FLAG_SAVE_FOR_BWD, MOE_FLAG_SERIAL_LAUNCH, MOE_FLAG_TRACE, MOE_FLAG_SIGMOID_GATE = 1, 2, 4, 8, 16
-MOE_FLAG_DEFER_OUT_COPY = 32
+MOE_FLAG_DEFER_OUT_COPY, MOE_FLAG_W4 = 32, 64
+MOE_W4_GATE_UP = 1
 MOE_BUF = {"counts": 0, "offsets": 1, "row_of": 2, "src_of": 3, "prow_of": 4, "pad_off": 5, "Xp": 6, "H": 7,
            "A": 8, "Y": 9, "dOutp": 10, "dH": 11, "dXp": 12, "meta": 13, "trace": 14, "event_counters": 15}
 _BUF_DTYPE = {k: (torch.bfloat16 if k in ("Xp", "H", "A", "Y", "dOutp", "dH", "dXp") else torch.int32)
@@ -31,7 +32,8 @@ EXPORTS = ["moe_workspace_bytes", "moe_create", "moe_destroy", "moe_route", "moe
            "moe_debug_host_direct", "moe_debug_layout_blocks", "moe_debug_ring",
            "moe_sched_study_workspace_bytes", "moe_sched_study", "moe_sched_study_stats", "moe_router_fwd",
            "moe_router_bwd", "moe_taskflow_compile", "moe_taskflow_workspace_bytes", "moe_taskflow_run",
-           "moe_taskflow_status", "moe_ep_plan", "moe_ep_dispatch", "moe_ep_combine"]
+           "moe_taskflow_status", "moe_ep_plan", "moe_ep_dispatch", "moe_ep_combine", "moe_balance_fwd", "moe_balance_bwd",
+           "moe_w4_sizes", "moe_w4_quantize", "moe_w4_pack", "moe_w4_dequantize", "moe_ffn_fwd_w4"]
 PHASES = ["route", "layout", "gather", "gemm_gate_up", "gemm_down", "combine", "bwd_gather", "act_grad",
           "dw_reduce", "wgrad_down", "gate_grad", "wgrad_gate_up", "bwd_combine", "fused_fwd", "fused_bwd"]
 
@@ -68,6 +70,10 @@ class MoeEpLocal(ctypes.Structure):
 class MoeEpLocalCombine(ctypes.Structure):
     _fields_ = [("rank", ctypes.c_int32), ("T", ctypes.c_int32), ("recv_rows", ctypes.c_int32), ("pad", ctypes.c_int32),
                 ("y", ctypes.c_void_p), ("out", ctypes.c_void_p), ("ticket", ctypes.c_void_p)]
+
+
+class _W4(ctypes.Structure):   # moe_w4_weights
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p), ("group", ctypes.c_int32)]
 
 
 class MoeTfTensor(ctypes.Structure):
@@ -177,6 +183,13 @@ def load_library() -> ctypes.CDLL:
                                 ctypes.POINTER(i32), ctypes.POINTER(i32)]
     lib.moe_ep_dispatch.argtypes = [ctypes.POINTER(MoeEpPeer), ctypes.POINTER(MoeEpLocal), i32, i32, i32, i32, vp, vp]
     lib.moe_ep_combine.argtypes = [ctypes.POINTER(MoeEpPeer), ctypes.POINTER(MoeEpLocalCombine), i32, i32, i32, i32, vp, vp]
+    lib.moe_balance_fwd.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.moe_balance_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp]
+    lib.moe_w4_sizes.argtypes = [i32, i32, i32, ctypes.c_uint32, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    lib.moe_w4_quantize.argtypes = [vp, i32, i32, i32, i32, ctypes.c_uint32, vp, vp, vp, vp]
+    lib.moe_w4_pack.argtypes = [vp, vp, vp, i32, i32, i32, i32, ctypes.c_uint32, vp, vp, vp, vp]
+    lib.moe_w4_dequantize.argtypes = [ctypes.POINTER(_W4), i32, i32, i32, ctypes.c_uint32, vp, vp]
+    lib.moe_ffn_fwd_w4.argtypes = [vp, vp, vp, vp, ctypes.POINTER(_W4), ctypes.POINTER(_W4), vp, i32, vp]
     lib.moe_sched_study_workspace_bytes.restype = sz
     lib.moe_sched_study_workspace_bytes.argtypes = [i32, i32]
     lib.moe_sched_study.argtypes = [i32, vp, vp, vp, vp, i32, i32, i32, vp, sz, vp]
@@ -187,7 +200,8 @@ def load_library() -> ctypes.CDLL:
     lib.moe_last_cuda_error.restype = ctypes.c_char_p
     if _fast is not None:
         _fast.setup(*(ctypes.cast(getattr(lib, f), vp).value for f in (
-            "moe_route", "moe_router_fwd", "moe_router_bwd", "moe_layout_noalloc", "moe_ffn_fwd", "moe_ffn_bwd")))
+            "moe_route", "moe_router_fwd", "moe_router_bwd", "moe_layout_noalloc", "moe_ffn_fwd", "moe_ffn_bwd",
+            "moe_balance_fwd", "moe_balance_bwd", "moe_ffn_fwd_w4")))
     _lib = lib
     return lib
 
@@ -410,6 +424,89 @@ def _moe_ffn_bwd(ctx, dout, x, topk_ids, topk_w, W_gate_up, W_down, dx, dW_gate_
                                       _dev(dx, _BF, "dx", td), _dev(dW_gate_up, _BF, "dW_gate_up", 2 * nw),
                                       _dev(dW_down, _BF, "dW_down", nw), _dev(d_topk_w, _F32, "d_topk_w", tk),
                                       T, _stream()), "moe_ffn_bwd")
+
+
+def _here(t, dtype, name, n=0):
+    """_dev for a tensor on the current device, where the call runs."""
+    p = _dev(t, dtype, name, n)
+    if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
+        _fault(name, f"CUDA device {torch.cuda.current_device()}", dtype)
+    return p
+
+
+@_sizes_first
+def moe_balance_fwd(ctx, logits, topk_ids, T, seq_offsets, n_seq, token_mask, losses, counts, prob, tokens):
+    _, _, E, k, _, _, _ = _shape_of(ctx)
+    _check(load_library().moe_balance_fwd(ctx, _here(logits, _F32, "logits", T * E), _here(topk_ids, _I32, "topk_ids", T * k), T,
+                                          _here(seq_offsets, _I32, "seq_offsets", n_seq + 1), n_seq,
+                                          _here(token_mask, torch.uint8, "token_mask", T), _here(losses, _F32, "losses", 2),
+                                          _here(counts, _I32, "counts", n_seq * E), _here(prob, _F32, "prob", n_seq * E),
+                                          _here(tokens, _I32, "tokens", n_seq + 1), _stream()), "moe_balance_fwd")
+
+
+@_sizes_first
+def moe_balance_bwd(ctx, logits, topk_ids, counts, tokens, d_losses, d_topk_w, T, seq_offsets, n_seq, token_mask, d_logits):
+    _, _, E, k, _, _, _ = _shape_of(ctx)
+    _check(load_library().moe_balance_bwd(ctx, _here(logits, _F32, "logits", T * E), _here(topk_ids, _I32, "topk_ids", T * k),
+                                          _here(counts, _I32, "counts", n_seq * E), _here(tokens, _I32, "tokens", n_seq + 1),
+                                          _here(d_losses, _F32, "d_losses", 2), _here(d_topk_w, _F32, "d_topk_w", T * k), T,
+                                          _here(seq_offsets, _I32, "seq_offsets", n_seq + 1), n_seq,
+                                          _here(token_mask, torch.uint8, "token_mask", T), _here(d_logits, _F32, "d_logits", T * E),
+                                          _stream()), "moe_balance_bwd")
+
+
+def moe_w4_sizes(rows, cols, group, flags=0):
+    """(bytes of codes, elements of scales and of zero points) of one matrix."""
+    code_bytes, elems = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load_library().moe_w4_sizes(int(rows), int(cols), int(group), int(flags), ctypes.byref(code_bytes), ctypes.byref(elems)),
+           "moe_w4_sizes")
+    return code_bytes.value, elems.value
+
+
+@_sizes_first
+def moe_w4_quantize(W, n, rows, cols, group, flags, codes, scales, zeros):
+    nb, ne = moe_w4_sizes(rows, cols, group, flags)
+    _check(load_library().moe_w4_quantize(_here(W, _BF, "W", n * rows * cols), n, rows, cols, group, flags,
+                                          _here(codes, _I32, "codes", n * nb // 4), _here(scales, _BF, "scales", n * ne),
+                                          _here(zeros, torch.uint8, "zeros", n * ne), _stream()), "moe_w4_quantize")
+
+
+@_sizes_first
+def moe_w4_pack(q, q_scales, q_zeros, n, rows, cols, group, flags, codes, scales, zeros):
+    nb, ne = moe_w4_sizes(rows, cols, group, flags)
+    nq = n * rows * -(-cols // group)
+    _check(load_library().moe_w4_pack(_here(q, torch.uint8, "q", n * rows * cols // 2), _here(q_scales, _BF, "q_scales", nq),
+                                      _here(q_zeros, torch.uint8, "q_zeros", nq), n, rows, cols, group, flags,
+                                      _here(codes, _I32, "codes", n * nb // 4), _here(scales, _BF, "scales", n * ne),
+                                      _here(zeros, torch.uint8, "zeros", n * ne), _stream()), "moe_w4_pack")
+
+
+@_sizes_first
+def moe_w4_dequantize(codes, scales, zeros, group, n, rows, cols, flags, W):
+    nb, ne = moe_w4_sizes(rows, cols, group, flags)
+    w = _W4(_here(codes, _I32, "codes", n * nb // 4), _here(scales, _BF, "scales", n * ne), _here(zeros, torch.uint8, "zeros", n * ne), group)
+    _check(load_library().moe_w4_dequantize(ctypes.byref(w), n, rows, cols, flags, _here(W, _BF, "W", n * rows * cols), _stream()),
+           "moe_w4_dequantize")
+
+
+def _w4_of_shape(W, n, rows, cols, gate_up, name):
+    if not isinstance(W, MoeW4Weights) or (W.n, W.rows, W.cols, W.gate_up) != (n, rows, cols, gate_up):
+        raise MoeError(f"{name}: expected MoeW4Weights of {n} matrices {rows} x {cols}" + (", gate_up=True" if gate_up else ""))
+
+
+@_sizes_first
+def moe_ffn_fwd_w4(ctx, x, topk_ids, topk_w, W_gate_up, W_down, out, T):
+    """W_gate_up, W_down: MoeW4Weights."""
+    _, d, E, k, S, F, _ = _shape_of(ctx)
+    _w4_of_shape(W_gate_up, E + S, 2 * F, d, True, "W_gate_up")
+    _w4_of_shape(W_down, E + S, d, F, False, "W_down")
+    ws = []
+    for W, name in ((W_gate_up, "W_gate_up"), (W_down, "W_down")):
+        ws.append(_W4(_here(W.codes, _I32, name + ".codes", W.n * W.words), _here(W.scales, _BF, name + ".scales", W.n * W.elems),
+                      _here(W.zeros, torch.uint8, name + ".zeros", W.n * W.elems), W.group))
+    _check(load_library().moe_ffn_fwd_w4(ctx, _here(x, _BF, "x", T * d), _here(topk_ids, _I32, "topk_ids", T * k),
+                                         _here(topk_w, _F32, "topk_w", T * k), ctypes.byref(ws[0]), ctypes.byref(ws[1]),
+                                         _here(out, _BF, "out", T * d), T, _stream()), "moe_ffn_fwd_w4")
 
 
 @_sizes_first
@@ -710,15 +807,56 @@ def moe_debug_buffer(ctx, which: str) -> torch.Tensor:
     return raw.view(torch.bfloat16).clone()
 
 
+class MoeW4Weights:
+    """n matrices [rows][cols] in 4 bits, laid out for the kernels: w = scale * (code - zero) with a scale, and a zero point if there
+    are any, for every `group` columns of a row.  gate_up: rows are 2F, gate rows first (W_gate_up)."""
+
+    def __init__(self, n, rows, cols, group, gate_up, asymmetric, device):
+        self.n, self.rows, self.cols, self.group, self.gate_up = int(n), int(rows), int(cols), int(group), bool(gate_up)
+        self.flags = MOE_W4_GATE_UP if gate_up else 0
+        nb, self.elems = moe_w4_sizes(rows, cols, group, self.flags)
+        self.words = nb // 4
+        self.codes = torch.empty(self.n, self.words, dtype=_I32, device=device)
+        self.scales = torch.empty(self.n, self.elems, dtype=_BF, device=device)
+        self.zeros = torch.empty(self.n, self.elems, dtype=torch.uint8, device=device) if asymmetric else None
+
+    @classmethod
+    def quantize(cls, W, group=128, asymmetric=False, gate_up=False):
+        """From bf16 W [n][rows][cols]."""
+        if W.dim() != 3:
+            raise MoeError("W: expected n matrices [n][rows][cols]")
+        w = cls(*W.shape, group, gate_up, asymmetric, W.device)
+        moe_w4_quantize(W, w.n, w.rows, w.cols, w.group, w.flags, w.codes, w.scales, w.zeros)
+        return w
+
+    @classmethod
+    def pack(cls, q, scales, zeros=None, group=128, gate_up=False):
+        """From a checkpoint's codes q uint8 [n][rows][cols / 2] (the even column in the low half), scales bf16 [n][rows][ceil(cols /
+        group)] and zero points uint8 of the same shape."""
+        if q.dim() != 3:
+            raise MoeError("q: expected codes [n][rows][cols / 2]")
+        w = cls(q.shape[0], q.shape[1], 2 * q.shape[2], group, gate_up, zeros is not None, q.device)
+        moe_w4_pack(q, scales, zeros, w.n, w.rows, w.cols, w.group, w.flags, w.codes, w.scales, w.zeros)
+        return w
+
+    def dequantize(self, out=None):
+        """The values they stand for, bf16 [n][rows][cols]."""
+        if out is None:
+            out = torch.empty(self.n, self.rows, self.cols, dtype=_BF, device=self.codes.device)
+        moe_w4_dequantize(self.codes, self.scales, self.zeros, self.group, self.n, self.rows, self.cols, self.flags, out)
+        return out
+
+
 class MoeLayer:
     """Owns a context and its workspace (a torch allocation); allocates outputs; same calls as the C ABI."""
 
     def __init__(self, T_max, d, E, k, n_shared, F, renorm=False, save_for_bwd=False, serial=False, trace=False,
-                 sigmoid_gate=False, defer_out_copy=False):
+                 sigmoid_gate=False, defer_out_copy=False, w4=False):
         self.T_max, self.d, self.E, self.k, self.S, self.F = T_max, d, E, k, n_shared, F
         self.flags = ((MOE_FLAG_RENORM_TOPK if renorm else 0) | (MOE_FLAG_SAVE_FOR_BWD if save_for_bwd else 0) |
                       (MOE_FLAG_SERIAL_LAUNCH if serial else 0) | (MOE_FLAG_TRACE if trace else 0) |
-                      (MOE_FLAG_SIGMOID_GATE if sigmoid_gate else 0) | (MOE_FLAG_DEFER_OUT_COPY if defer_out_copy else 0))
+                      (MOE_FLAG_SIGMOID_GATE if sigmoid_gate else 0) | (MOE_FLAG_DEFER_OUT_COPY if defer_out_copy else 0) |
+                      (MOE_FLAG_W4 if w4 else 0))
         nbytes = moe_workspace_bytes(T_max, d, E, k, n_shared, F, self.flags)
         if nbytes == 0:
             raise MoeError("invalid shape")
@@ -784,6 +922,53 @@ class MoeLayer:
             d_topk_w = torch.empty(T, self.k, dtype=_F32, device=x.device)
         moe_ffn_bwd(self.ctx, dout, x, topk_ids, topk_w, W_gate_up, W_down, dx, dW_gate_up, dW_down, d_topk_w, T)
         return dx, dW_gate_up, dW_down, d_topk_w
+
+    def balance_fwd(self, logits, topk_ids, seq_offsets=None, token_mask=None):
+        """-> losses [2] (balance, z), counts [n_seq][E], prob [n_seq][E], tokens [n_seq + 1]"""
+        if _fast is not None:
+            r = _fast.balance_fwd_new(self.ctx, logits, topk_ids, seq_offsets, token_mask)
+            if r is not None:
+                if r[0]:
+                    _check(r[0], "moe_balance_fwd")
+                return r[1:]
+        T, dev = logits.shape[0], logits.device
+        n = 1 if seq_offsets is None else seq_offsets.numel() - 1
+        losses, prob = torch.empty(2, dtype=_F32, device=dev), torch.empty(max(n, 0), self.E, dtype=_F32, device=dev)
+        counts, tokens = torch.empty(max(n, 0), self.E, dtype=_I32, device=dev), torch.empty(max(n, 0) + 1, dtype=_I32, device=dev)
+        moe_balance_fwd(self.ctx, logits, topk_ids, T, seq_offsets, n, token_mask, losses, counts, prob, tokens)
+        return losses, counts, prob, tokens
+
+    def balance_bwd(self, logits, topk_ids, counts, tokens, d_losses, d_topk_w=None, seq_offsets=None, token_mask=None, d_logits=None):
+        if d_logits is None and _fast is not None:
+            r = _fast.balance_bwd_new(self.ctx, logits, topk_ids, counts, tokens, d_losses, d_topk_w, seq_offsets, token_mask)
+            if r is not None:
+                if r[0]:
+                    _check(r[0], "moe_balance_bwd")
+                return r[1]
+        T = logits.shape[0]
+        n = 1 if seq_offsets is None else seq_offsets.numel() - 1
+        if d_logits is None:
+            d_logits = torch.empty(T, self.E, dtype=_F32, device=logits.device)
+        moe_balance_bwd(self.ctx, logits, topk_ids, counts, tokens, d_losses, d_topk_w, T, seq_offsets, n, token_mask, d_logits)
+        return d_logits
+
+    def ffn_fwd_w4(self, x, topk_ids, topk_w, W_gate_up, W_down, out=None):
+        """ffn_fwd over MoeW4Weights (the layer made with w4=True)."""
+        if out is None and _fast is not None:
+            _w4_of_shape(W_gate_up, self.E + self.S, 2 * self.F, self.d, True, "W_gate_up")
+            _w4_of_shape(W_down, self.E + self.S, self.d, self.F, False, "W_down")
+            r = _fast.ffn_fwd_w4_new(self.ctx, x, topk_ids, topk_w, W_gate_up.words, W_gate_up.elems, W_gate_up.codes, W_gate_up.scales,
+                                     W_gate_up.zeros, W_gate_up.group, W_down.words, W_down.elems, W_down.codes, W_down.scales,
+                                     W_down.zeros, W_down.group)
+            if r is not None:
+                if r[0]:
+                    _check(r[0], "moe_ffn_fwd_w4")
+                return r[1]
+        T = x.shape[0]
+        if out is None:
+            out = torch.empty(T, self.d, dtype=_BF, device=x.device)
+        moe_ffn_fwd_w4(self.ctx, x, topk_ids, topk_w, W_gate_up, W_down, out, T)
+        return out
 
     def status(self):
         return moe_get_status(self.ctx)

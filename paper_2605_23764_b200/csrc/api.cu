@@ -1,6 +1,7 @@
 // C ABI of libmoe_b200: context, workspace carving, tensor-map encoding and the launch
 // sequences of the forward and backward layer.  Argument marshalling and planning only; every
-// step of the layer runs in the kernels of route_layout.cu, permute.cu, gemm_tc3.cu, gemm_wgrad.cu and fused.cu.
+// step of the layer runs in the kernels of route_layout.cu, permute.cu, gemm_tc3.cu, gemm_wgrad.cu and fused.cu; over 4-bit
+// weights in those of w4_vec.cu.
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
@@ -12,6 +13,7 @@
 #include "../../include/moe_b200.h"
 #include "../../include/moe_b200_debug.h"
 #include "moe_internal.h"
+#include "w4.cuh"
 
 using namespace moe;
 
@@ -133,7 +135,7 @@ struct Carve {
 // Byte offsets of every workspace tensor.
 struct WsPlan {
   size_t status, meta, counts, offsets, pad_off, mb_start, mblk_expert, work_start, wblk_expert, blk_hist, row_of, src_of, prow_of, combine_order, tok_last, wg_order, group_start, group_row, group_slot, prow_w,
-      dw_partial, Xp, H, A, Y, dOutp, dH, st_x[2], st_dout, st_ids, st_w, st_out, st_dx, st_dw, st_logits, ctr, trace, total;
+      dw_partial, Xp, H, A, Y, dOutp, dH, st_x[2], st_dout, st_ids, st_w, st_out, st_dx, st_dw, st_logits, ctr, trace, balance, tickets, Y4, total;
   int cap_rows, nblk_max, ntn_act, ctr_count, trace_cap;
 };
 
@@ -187,6 +189,9 @@ WsPlan plan_workspace(const moe_shape& s) {
   p.ctr = c.take(sizeof(int) * (size_t)p.ctr_count * (train ? 2 : 1));   // forward, backward
   p.trace_cap = (s.flags & MOE_FLAG_TRACE) ? TRACE_RECORDS : 0;
   p.trace = c.take((size_t)p.trace_cap * 32);
+  p.balance = c.take(balance_scratch_bytes(s.T_max, s.E));
+  p.tickets = c.take(sizeof(int) * (BAL_MAX_BLOCKS + 1));
+  p.Y4 = c.take((s.flags & MOE_FLAG_W4) ? sizeof(float) * cap * s.d : 0);
   p.total = c.off;
   return p;
 }
@@ -764,6 +769,95 @@ int run_bwd(moe_ctx* c, const uint16_t* dout, const uint16_t* W1, const uint16_t
   return MOE_OK;
 }
 
+// A context's calls run on its device.
+bool on_its_device(const moe_ctx* c) {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
+}
+
+bool w4_group_ok(int group) { return group == 32 || group == 64 || group == 128; }
+bool w4_ok(const moe_w4_weights* w) {
+  return w && w->codes && w->scales && w4_group_ok(w->group) && aligned16(w->codes) && aligned16(w->scales) && aligned16(w->zeros);
+}
+W4VecArgs w4_vec_args(const moe_ctx* c, const moe_w4_weights& w, int rows, int cols, int paired, int T, const int32_t* ids) {
+  const moe_shape& s = c->shape;
+  const W4Shape ws{rows, cols, w.group, paired};
+  W4VecArgs a;
+  memset(&a, 0, sizeof a);
+  a.codes = reinterpret_cast<const uint4*>(w.codes);
+  a.scales = reinterpret_cast<const uint32_t*>(w.scales);
+  a.zeros = reinterpret_cast<const uint16_t*>(w.zeros);
+  a.K = cols;
+  a.KB = ws.k_tiles();
+  a.NG = ws.groups();
+  a.RT = ws.row_tiles();
+  a.group = w.group;
+  a.A = c->at<uint16_t>(c->plan.A);
+  a.a_ld = row_ld(s.F);
+  a.Y = c->at<float>(c->plan.Y4);
+  a.y_ld = s.d;
+  a.ids = ids;
+  a.T = T; a.k = s.k; a.kp = s.k + s.n_shared; a.E = s.E; a.Ep = s.E + s.n_shared;
+  a.rows_most = INT32_MAX;
+  a.status = c->status();
+  const LayoutView lv = c->layout();
+  if ((long)T * a.kp > W4_SMALL_SLOTS) {
+    a.counts = lv.counts;
+    a.offsets = lv.offsets;
+    a.pad_off = lv.pad_off;
+    a.src_of = lv.src_of;
+  }
+  a.prow_of = lv.prow_of;
+  return a;
+}
+
+int run_fwd_w4(moe_ctx* c, const uint16_t* x, const int32_t* ids, const float* w, const moe_w4_weights& W1, const moe_w4_weights& W2, uint16_t* out,
+               int T, cudaStream_t st) {
+  const moe_shape& s = c->shape;
+  const Dims dm = c->dims(T);
+  const LayoutView lv = c->layout();
+  c->saved_T = -1;
+  W4VecArgs up = w4_vec_args(c, W1, 2 * s.F, s.d, 1, T, ids), down = w4_vec_args(c, W2, s.d, s.F, 0, T, ids);
+  up.n_out = s.F;
+  up.in = x;
+  up.in_ld = s.d;
+  up.w = w;
+  down.down = 1;
+  down.n_out = s.d;
+  down.in = up.A;
+  down.in_ld = up.a_ld;
+  if (up.counts) {
+    Phase ph(c, MOE_PHASE_LAYOUT, st);
+    MOE_CUDA(launch_layout(ids, dm, lv, false, 0, nullptr, 0, c->status(), st, &c->launches));
+  }
+  {
+    Phase ph(c, MOE_PHASE_GEMM_GATE_UP, st);
+    MOE_CUDA(launch_w4_vec(up, c->num_sms, st, &c->launches));
+  }
+  {
+    Phase ph(c, MOE_PHASE_GEMM_DOWN, st);
+    MOE_CUDA(launch_w4_vec(down, c->num_sms, st, &c->launches));
+  }
+  Phase ph(c, MOE_PHASE_COMBINE, st);
+  MOE_CUDA(launch_w4_combine(up.Y, up.y_ld, lv.prow_of, T, s.d, dm.kp(), out, st, &c->launches));
+  return MOE_OK;
+}
+
+BalanceArgs balance_args(const moe_ctx* c, const float* logits, const int32_t* topk_ids, int32_t T, const int32_t* seq_offsets, int32_t n_seq,
+                         const uint8_t* token_mask) {
+  BalanceArgs a;
+  memset(&a, 0, sizeof a);
+  a.logits = logits;
+  a.topk_ids = topk_ids;
+  a.seq_offsets = seq_offsets;
+  a.token_mask = token_mask;
+  a.T = T; a.E = c->shape.E; a.k = c->shape.k; a.n_seq = n_seq;
+  a.mode = gate_mode(c);
+  a.scratch = c->at<uint8_t>(c->plan.balance);
+  a.tickets = c->at<int>(c->plan.tickets);
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -811,6 +905,7 @@ int moe_create(moe_ctx** out, const moe_shape* shape, void* workspace, size_t wo
   const uint64_t ld_d = row_ld(s.d), ld_F = row_ld(s.F), ld_2F = row_ld(2 * s.F);
   int rc = MOE_OK;
   cudaError_t e = cudaMemset(c->ws, 0, p.Xp);  // status, tables and small arrays start at zero
+  if (e == cudaSuccess) e = cudaMemset(c->ws + p.tickets, 0, sizeof(int) * (BAL_MAX_BLOCKS + 1));
   if (e != cudaSuccess) rc = cuda_fail(e, "cudaMemset(workspace)");
   if (!rc && train) rc = encode_2d(&c->tm_dOutp_mn, c->ws + p.dOutp, cap, s.d, 64, 64, ld_d);
   if (!rc && train) rc = encode_2d(&c->tm_A_mn, c->ws + p.A, cap, s.F, 64, 64, ld_F);
@@ -905,6 +1000,49 @@ int moe_router_bwd(moe_ctx* c, const float* logits, const int32_t* topk_ids, con
   return MOE_OK;
 }
 
+int moe_balance_fwd(moe_ctx* c, const float* logits, const int32_t* topk_ids, int32_t T, const int32_t* seq_offsets, int32_t n_seq,
+                    const uint8_t* token_mask, float* losses, int32_t* counts, float* prob, int32_t* tokens, void* stream) {
+  if (!c || T < 0 || T > c->shape.T_max || n_seq < 1 || (n_seq > 1 && !seq_offsets) || !losses || !counts || !prob || !tokens)
+    return MOE_ERR_INVALID_ARG;
+  if (T > 0 && (!logits || !topk_ids)) return MOE_ERR_INVALID_ARG;
+  if (!on_its_device(c)) return MOE_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  c->begin_call(st);
+  if (T == 0) {
+    const size_t n = (size_t)n_seq * c->shape.E;
+    MOE_CUDA(cudaMemsetAsync(losses, 0, 2 * sizeof(float), st));
+    MOE_CUDA(cudaMemsetAsync(counts, 0, n * sizeof(int), st));
+    MOE_CUDA(cudaMemsetAsync(prob, 0, n * sizeof(float), st));
+    MOE_CUDA(cudaMemsetAsync(tokens, 0, ((size_t)n_seq + 1) * sizeof(int), st));
+    return MOE_OK;
+  }
+  BalanceArgs a = balance_args(c, logits, topk_ids, T, seq_offsets, n_seq, token_mask);
+  a.losses = losses; a.counts = counts; a.prob = prob; a.tokens = tokens;
+  Phase ph(c, MOE_PHASE_ROUTE, st);
+  MOE_CUDA(launch_balance_fwd(a, st, &c->launches));
+  return MOE_OK;
+}
+
+int moe_balance_bwd(moe_ctx* c, const float* logits, const int32_t* topk_ids, const int32_t* counts, const int32_t* tokens, const float* d_losses,
+                    const float* d_topk_w, int32_t T, const int32_t* seq_offsets, int32_t n_seq, const uint8_t* token_mask, float* d_logits,
+                    void* stream) {
+  if (!c || T < 0 || T > c->shape.T_max || n_seq < 1 || (n_seq > 1 && !seq_offsets)) return MOE_ERR_INVALID_ARG;
+  if (T > 0 && (!logits || !counts || !tokens || !d_losses || !d_logits || (d_topk_w && !topk_ids))) return MOE_ERR_INVALID_ARG;
+  if (!on_its_device(c)) return MOE_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  c->begin_call(st);
+  if (T == 0) return MOE_OK;
+  BalanceArgs a = balance_args(c, logits, topk_ids, T, seq_offsets, n_seq, token_mask);
+  a.counts = const_cast<int32_t*>(counts);
+  a.tokens = const_cast<int32_t*>(tokens);
+  a.d_losses = d_losses;
+  a.d_topk_w = d_topk_w;
+  a.d_logits = d_logits;
+  Phase ph(c, MOE_PHASE_ROUTE, st);
+  MOE_CUDA(launch_balance_bwd(a, st, &c->launches));
+  return MOE_OK;
+}
+
 int moe_route_host(moe_ctx* c, const float* logits_host, int32_t T, int32_t* topk_ids_host, float* topk_w_host,
                    void* stream) {
   if (!c || !logits_host || !topk_ids_host || !topk_w_host || T < 0 || T > c->shape.T_max)
@@ -961,6 +1099,57 @@ int moe_ffn_fwd(moe_ctx* c, const uint16_t* x, const int32_t* topk_ids, const fl
   if (!x || !topk_ids || !topk_w || !W_gate_up || !W_down || !out) return MOE_ERR_INVALID_ARG;
   if (!aligned16(x) || !aligned16(W_gate_up) || !aligned16(W_down) || !aligned16(out)) return MOE_ERR_INVALID_ARG;
   return run_fwd(c, x, topk_ids, topk_w, W_gate_up, W_down, out, T, c->last_stream);
+}
+
+int moe_w4_sizes(int32_t rows, int32_t cols, int32_t group, uint32_t flags, size_t* code_bytes, size_t* group_elems) {
+  const int paired = (flags & MOE_W4_GATE_UP) ? 1 : 0;
+  if (rows < 1 || cols < 8 || cols % 8 || !w4_group_ok(group) || (flags & ~MOE_W4_GATE_UP) || (paired && rows % 16)) return MOE_ERR_INVALID_ARG;
+  const W4Shape s{rows, cols, group, paired};
+  if (code_bytes) *code_bytes = (size_t)s.row_tiles() * s.k_tiles() * W4_TILE_BYTES;
+  if (group_elems) *group_elems = (size_t)s.row_tiles() * s.groups() * W4_TILE_ROWS;
+  return MOE_OK;
+}
+
+int moe_w4_quantize(const uint16_t* W, int32_t n, int32_t rows, int32_t cols, int32_t group, uint32_t flags, uint32_t* codes, uint16_t* scales,
+                    uint8_t* zeros, void* stream) {
+  if (n < 0 || moe_w4_sizes(rows, cols, group, flags, nullptr, nullptr)) return MOE_ERR_INVALID_ARG;
+  if (n == 0) return MOE_OK;
+  if (!W || !codes || !scales || !aligned16(W) || !aligned16(codes) || !aligned16(scales) || !aligned16(zeros)) return MOE_ERR_INVALID_ARG;
+  MOE_CUDA(launch_w4_quantize(W, n, W4Shape{rows, cols, group, (flags & MOE_W4_GATE_UP) ? 1 : 0}, codes, scales, zeros, static_cast<cudaStream_t>(stream)));
+  return MOE_OK;
+}
+
+int moe_w4_pack(const uint8_t* q, const uint16_t* q_scales, const uint8_t* q_zeros, int32_t n, int32_t rows, int32_t cols, int32_t group, uint32_t flags,
+                uint32_t* codes, uint16_t* scales, uint8_t* zeros, void* stream) {
+  if (n < 0 || moe_w4_sizes(rows, cols, group, flags, nullptr, nullptr) || (q_zeros == nullptr) != (zeros == nullptr)) return MOE_ERR_INVALID_ARG;
+  if (n == 0) return MOE_OK;
+  if (!q || !q_scales || !codes || !scales || (reinterpret_cast<uintptr_t>(q) & 3) || (reinterpret_cast<uintptr_t>(q_scales) & 1) || !aligned16(codes) ||
+      !aligned16(scales) || !aligned16(zeros))
+    return MOE_ERR_INVALID_ARG;
+  MOE_CUDA(launch_w4_pack(q, q_scales, q_zeros, n, W4Shape{rows, cols, group, (flags & MOE_W4_GATE_UP) ? 1 : 0}, codes, scales, zeros,
+                          static_cast<cudaStream_t>(stream)));
+  return MOE_OK;
+}
+
+int moe_w4_dequantize(const moe_w4_weights* w, int32_t n, int32_t rows, int32_t cols, uint32_t flags, uint16_t* W, void* stream) {
+  if (!w || n < 0 || moe_w4_sizes(rows, cols, w->group, flags, nullptr, nullptr)) return MOE_ERR_INVALID_ARG;
+  if (n == 0) return MOE_OK;
+  if (!w4_ok(w) || !W || !aligned16(W)) return MOE_ERR_INVALID_ARG;
+  MOE_CUDA(launch_w4_dequantize(w->codes, w->scales, w->zeros, n, W4Shape{rows, cols, w->group, (flags & MOE_W4_GATE_UP) ? 1 : 0}, W,
+                                static_cast<cudaStream_t>(stream)));
+  return MOE_OK;
+}
+
+int moe_ffn_fwd_w4(moe_ctx* c, const uint16_t* x, const int32_t* topk_ids, const float* topk_w, const moe_w4_weights* W_gate_up,
+                   const moe_w4_weights* W_down, uint16_t* out, int32_t T, void* stream) {
+  if (!c || T < 0 || T > c->shape.T_max) return MOE_ERR_INVALID_ARG;
+  if (!(c->shape.flags & MOE_FLAG_W4)) return MOE_ERR_STATE;
+  if (w4_vec_rows(c->shape.d) < 1 || w4_vec_rows(c->shape.F) < 1) return MOE_ERR_TOO_LARGE;
+  c->begin_call(static_cast<cudaStream_t>(stream));
+  if (T == 0) return MOE_OK;
+  if (!x || !topk_ids || !topk_w || !out || !w4_ok(W_gate_up) || !w4_ok(W_down) || !aligned16(x) || !aligned16(out)) return MOE_ERR_INVALID_ARG;
+  if (!on_its_device(c)) return MOE_ERR_INVALID_ARG;
+  return run_fwd_w4(c, x, topk_ids, topk_w, *W_gate_up, *W_down, out, T, c->last_stream);
 }
 
 int moe_ffn_bwd(moe_ctx* c, const uint16_t* dout, const uint16_t* x, const int32_t* topk_ids, const float* topk_w,

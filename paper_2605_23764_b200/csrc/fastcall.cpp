@@ -11,12 +11,15 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
 #include <stdexcept>
 #include <unordered_map>
+
+#include "../../include/moe_b200.h"
 
 namespace {
 
@@ -30,6 +33,9 @@ int (*f_router_bwd)(P, const P, const P, const P, int32_t, P, P);
 int (*f_layout_noalloc)(const P, int32_t, int32_t, int32_t, int32_t, P, P, P, P, P, P);
 int (*f_ffn_fwd)(P, const P, const P, const P, const P, const P, P, int32_t, P);
 int (*f_ffn_bwd)(P, const P, const P, const P, const P, const P, const P, P, P, P, P, int32_t, P);
+decltype(&moe_balance_fwd) f_balance_fwd;
+decltype(&moe_balance_bwd) f_balance_bwd;
+decltype(&moe_ffn_fwd_w4) f_ffn_fwd_w4;
 
 struct Slow {};   // not for this path
 
@@ -96,9 +102,9 @@ PyObject* guarded(F body) {
 void want(Py_ssize_t n, Py_ssize_t need) { if (n != need) throw Slow(); }
 
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 6) { PyErr_SetString(PyExc_TypeError, "setup: six addresses"); return nullptr; }
-  void* p[6];
-  for (int i = 0; i < 6; ++i) {
+  if (n != 9) { PyErr_SetString(PyExc_TypeError, "setup: nine addresses"); return nullptr; }
+  void* p[9];
+  for (int i = 0; i < 9; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "setup: null address");
@@ -111,6 +117,9 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
   f_layout_noalloc = reinterpret_cast<decltype(f_layout_noalloc)>(p[3]);
   f_ffn_fwd = reinterpret_cast<decltype(f_ffn_fwd)>(p[4]);
   f_ffn_bwd = reinterpret_cast<decltype(f_ffn_bwd)>(p[5]);
+  f_balance_fwd = reinterpret_cast<decltype(f_balance_fwd)>(p[6]);
+  f_balance_bwd = reinterpret_cast<decltype(f_balance_bwd)>(p[7]);
+  f_ffn_fwd_w4 = reinterpret_cast<decltype(f_ffn_fwd_w4)>(p[8]);
   Py_RETURN_NONE;
 }
 PyObject* add(PyObject*, PyObject* const* a, Py_ssize_t n) {   // handle, T_max, d, E, k, S, F
@@ -232,9 +241,96 @@ PyObject* ffn_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// a tensor on the current device
+template <class T>
+T* here(PyObject* o, at::ScalarType type, int64_t n) {
+  const at::Tensor& t = tensor(o);
+  T* p = static_cast<T*>(check(t, type, n));
+  if (t.get_device() != c10::cuda::current_device()) throw Slow();
+  return p;
+}
+template <class T>
+T* here_or_null(PyObject* o, at::ScalarType type, int64_t n) { return o == Py_None ? nullptr : here<T>(o, type, n); }
+int64_t sequences(PyObject* o) {   // of an offsets tensor
+  if (o == Py_None) return 1;
+  const int64_t n = tensor(o).numel() - 1;
+  if (n < 1 || n > INT32_MAX - 1) throw Slow();
+  return n;
+}
+PyObject* balance_fwd_new(PyObject*, PyObject* const* a, Py_ssize_t n) {   // ctx, logits, ids, offsets, mask -> (code, losses, counts, prob, tokens)
+  return guarded([&]() -> PyObject* {
+    want(n, 5);
+    moe_ctx* c = static_cast<moe_ctx*>(handle(a[0]));
+    const Shape& s = shape_of(c);
+    const at::Tensor& l = tensor(a[1]);
+    if (l.dim() != 2) throw Slow();
+    const int64_t T = l.size(0), ns = sequences(a[3]);
+    const float* logits = here<float>(a[1], F32, T * s.E);
+    const int32_t *ids = here<int32_t>(a[2], I32, T * s.k), *off = here_or_null<int32_t>(a[3], I32, ns + 1);
+    const uint8_t* mask = here_or_null<uint8_t>(a[4], at::kByte, T);
+    at::Tensor losses = empty({2}, F32, l), counts = empty({ns, s.E}, I32, l), prob = empty({ns, s.E}, F32, l), tokens = empty({ns + 1}, I32, l);
+    float *p0 = losses.data_ptr<float>(), *p2 = prob.data_ptr<float>();
+    int32_t *p1 = counts.data_ptr<int32_t>(), *p3 = tokens.data_ptr<int32_t>();
+    void* st = stream();
+    const int rc = unlocked([&] { return f_balance_fwd(c, logits, ids, (int32_t)T, off, (int32_t)ns, mask, p0, p1, p2, p3, st); });
+    return Py_BuildValue("(iNNNN)", rc, THPVariable_Wrap(losses), THPVariable_Wrap(counts), THPVariable_Wrap(prob), THPVariable_Wrap(tokens));
+  });
+}
+// ctx, logits, ids, counts, tokens, d_losses, d_topk_w, offsets, mask -> (code, d_logits)
+PyObject* balance_bwd_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    want(n, 9);
+    moe_ctx* c = static_cast<moe_ctx*>(handle(a[0]));
+    const Shape& s = shape_of(c);
+    const at::Tensor& l = tensor(a[1]);
+    if (l.dim() != 2) throw Slow();
+    const int64_t T = l.size(0), ns = sequences(a[7]);
+    const float* logits = here<float>(a[1], F32, T * s.E);
+    const float* dw = here_or_null<float>(a[6], F32, T * s.k);
+    const int32_t *ids = dw ? here<int32_t>(a[2], I32, T * s.k) : nullptr, *counts = here<int32_t>(a[3], I32, ns * s.E),
+                  *tokens = here<int32_t>(a[4], I32, ns + 1), *off = here_or_null<int32_t>(a[7], I32, ns + 1);
+    const float* dl = here<float>(a[5], F32, 2);
+    const uint8_t* mask = here_or_null<uint8_t>(a[8], at::kByte, T);
+    at::Tensor out = empty({T, s.E}, F32, l);
+    float* po = out.data_ptr<float>();
+    void* st = stream();
+    const int rc = unlocked([&] { return f_balance_bwd(c, logits, ids, counts, tokens, dl, dw, (int32_t)T, off, (int32_t)ns, mask, po, st); });
+    return Py_BuildValue("(iN)", rc, THPVariable_Wrap(out));
+  });
+}
+// ctx, x, ids, w, W_gate_up's (words, group elements of a matrix, codes, scales, zeros, group), W_down's -> (code, out)
+PyObject* ffn_fwd_w4_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    want(n, 16);
+    moe_ctx* c = static_cast<moe_ctx*>(handle(a[0]));
+    const Shape& s = shape_of(c);
+    const at::Tensor& xt = tensor(a[1]);
+    if (xt.dim() != 2) throw Slow();
+    const int64_t T = xt.size(0);
+    const uint16_t* x = here<uint16_t>(a[1], BF, T * s.d);
+    const int32_t* ids = here<int32_t>(a[2], I32, T * s.k);
+    const float* w = here<float>(a[3], F32, T * s.k);
+    moe_w4_weights W[2];
+    for (int i = 0; i < 2; ++i) {
+      PyObject* const* m = a + 4 + 6 * i;
+      const int64_t words = integer(m[0]), elems = integer(m[1]), Ep = s.E + s.S;   // of one matrix
+      W[i].codes = here<uint32_t>(m[2], I32, Ep * words);
+      W[i].scales = here<uint16_t>(m[3], BF, Ep * elems);
+      W[i].zeros = here_or_null<uint8_t>(m[4], at::kByte, Ep * elems);
+      W[i].group = (int32_t)integer(m[5]);
+    }
+    at::Tensor out = empty({T, s.d}, BF, xt);
+    uint16_t* po = static_cast<uint16_t*>(out.data_ptr());
+    void* st = stream();
+    const int rc = unlocked([&] { return f_ffn_fwd_w4(c, x, ids, w, &W[0], &W[1], po, (int32_t)T, st); });
+    return Py_BuildValue("(iN)", rc, THPVariable_Wrap(out));
+  });
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(setup), FAST(add), FAST(drop), FAST(route), FAST(route_new), FAST(router_fwd), FAST(router_bwd),
-                         FAST(layout_noalloc), FAST(ffn_fwd), FAST(ffn_fwd_new), FAST(ffn_bwd), {nullptr, nullptr, 0, nullptr}};
+                         FAST(layout_noalloc), FAST(ffn_fwd), FAST(ffn_fwd_new), FAST(ffn_bwd), FAST(balance_fwd_new),
+                         FAST(balance_bwd_new), FAST(ffn_fwd_w4_new), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -5,8 +5,10 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <stdint.h>
 #include <string.h>
 
+#include <atomic>
 #include <mutex>
 
 namespace moe {
@@ -18,6 +20,20 @@ struct PairLaunchState {
   bool attr_set[MAX_DEVICES] = {};
   int max_pairs[MAX_DEVICES] = {};
 };
+
+// Opt-in shared memory of a kernel, once per device.
+template <auto Kernel>
+cudaError_t opt_in_smem(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
+  if (done.load(std::memory_order_acquire) >> dev & 1) return cudaSuccess;
+  e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(1ull << dev, std::memory_order_release);
+  return e;
+}
 
 template <class Kernel, class Args>
 cudaError_t launch_on_pairs(PairLaunchState& st, Kernel kernel, const Args& args, int threads, size_t smem_bytes,

@@ -212,6 +212,33 @@ cudaError_t launch_router_fwd(const RouterArgs& a, int num_sms, cudaStream_t s, 
 cudaError_t launch_router_bwd(const float* logits, const int* ids, const float* g, int T, int E, int k, int gate_mode,
                               float* dlogits, cudaStream_t s, int* launches);
 
+// Balance losses of the router (balance.cu)
+constexpr int BAL_BLOCK_BYTES = 64 * 1024;   // logits of a block, at least
+constexpr int BAL_MAX_BLOCKS = 2 * 148;
+constexpr int BAL_BWD_MAX_BLOCKS = 4 * 148;
+struct BalanceArgs {
+  const float* logits;         // [T][E]
+  const int* topk_ids;         // [T][k]
+  const int* seq_offsets;      // [n_seq + 1]; NULL: the batch is one sequence
+  const uint8_t* token_mask;   // [T]; NULL: every token counts
+  int T, E, k, n_seq, mode;    // mode: GATE_RENORM | GATE_SIGMOID
+  // forward's outputs; counts and tokens are the backward's inputs
+  float* losses;               // [2] balance, z
+  int* counts;                 // [n_seq][E]
+  float* prob;                 // [n_seq][E]
+  int* tokens;                 // [n_seq + 1]: of each sequence, of all
+  uint8_t* scratch;            // balance_scratch_bytes()
+  int* tickets;                // [BAL_MAX_BLOCKS + 1], zero between calls
+  // backward
+  const float* d_losses;       // [2]
+  const float* d_topk_w;       // [T][k]; NULL: without the scores' gradient
+  float* d_logits;             // [T][E]
+};
+int balance_fwd_blocks(int T, int E);
+size_t balance_scratch_bytes(int T_max, int E);
+cudaError_t launch_balance_fwd(const BalanceArgs& a, cudaStream_t s, int* launches);
+cudaError_t launch_balance_bwd(const BalanceArgs& a, cudaStream_t s, int* launches);
+
 int vector_warps();   // vector warps per CTA of the persistent launch
 // Not a cooperative launch: that attribute holds a launch back until the one in front of it has ended (2 us each: the smallest
 // training step 57 -> 52 us), and co-residency is not needed (schedule.h).  The grid is sized to what can be resident.

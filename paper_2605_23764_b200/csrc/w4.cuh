@@ -1,0 +1,90 @@
+// Expert weights in 4 bits with a scale -- and a zero point, where there are any -- for each group of 32, 64 or 128 reduction
+// elements: w = s (q - z), q and z in 0 .. 15 (z = 8 without zero points), s in bf16.
+//
+// Layout.  A matrix of R rows (output features) and K columns (reduction) is cut into tiles of 16 rows x 64 columns, 512 bytes
+// each, row tile major.  The 32 lanes of a warp own 16 bytes of a tile side by side: word j of lane 4 g + c holds, of the 16
+// columns 16 j .., what the lane is given of a 16 x 16 bf16 operand of a matrix instruction -- the pairs of columns
+// {2 c, 2 c + 1} and {2 c + 8, 2 c + 9} of rows g and g + 8:
+//   pair r (0: row g, first pair; 1: row g + 8, first; 2: row g, second; 3: row g + 8, second)
+//   has its even column in bits 4 r .. 4 r + 3 and its odd column in bits 16 + 4 r ..
+// so that (word >> 4 r) & 0x000F000F is a pair in the place of two bf16 mantissas.  The same fragment is what a warp writes to
+// TMEM for 16 lanes x 8 columns (two bf16 each), so matrix-vector and tensor-core kernels read one layout.
+// Scales [row tile][group][8][2] bf16 and zero points [..][8][2] bytes: {row g, row g + 8} side by side.
+// Rows of W_gate_up: tile rows 0 .. 7 are gate rows, 8 .. 15 the up rows of the same features (SwiGLU needs no exchange).
+// Rows behind the last and columns behind K are codes of value 0 with scale 0.
+#pragma once
+
+#include "moe_internal.h"
+
+namespace moe {
+
+constexpr int W4_TILE_ROWS = 16, W4_TILE_K = 64, W4_TILE_BYTES = 512;
+
+struct W4Shape {
+  int rows, cols, group, paired;
+  __host__ __device__ int row_tiles() const { return (rows + W4_TILE_ROWS - 1) / W4_TILE_ROWS; }
+  __host__ __device__ int k_tiles() const { return (cols + W4_TILE_K - 1) / W4_TILE_K; }
+  __host__ __device__ int groups() const { return (k_tiles() * W4_TILE_K + group - 1) / group; }   // whole tiles
+  // row of the matrix that is row r of tile rt; -1: behind the last
+  __host__ __device__ int row_at(int rt, int r) const {
+    if (paired) return (r & 8 ? rows / 2 : 0) + rt * 8 + (r & 7);
+    const int i = rt * W4_TILE_ROWS + r;
+    return i < rows ? i : -1;
+  }
+};
+
+// The four registers of a 16 x 16 bf16 operand from a word of codes: q - z exactly, q and z in the low mantissa bits of 128 + ..
+__device__ __forceinline__ uint32_t w4_bias(uint32_t z) { return 0x43004300u | z * 0x00010001u; }
+__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ void w4_fragment(uint32_t word, uint32_t bias_lo, uint32_t bias_hi, uint32_t (&a)[4]) {
+  a[0] = sub_bf16x2((word & 0x000F000Fu) | 0x43004300u, bias_lo);
+  a[1] = sub_bf16x2(((word >> 4) & 0x000F000Fu) | 0x43004300u, bias_hi);
+  a[2] = sub_bf16x2(((word >> 8) & 0x000F000Fu) | 0x43004300u, bias_lo);
+  a[3] = sub_bf16x2(((word >> 12) & 0x000F000Fu) | 0x43004300u, bias_hi);
+}
+
+// One expert product of the layer over experts with few rows (w4_vec.cu).
+struct W4VecArgs {
+  const uint4* codes;
+  const uint32_t* scales;     // bf16 pairs
+  const uint16_t* zeros;      // byte pairs; NULL: 8
+  int K, KB, NG, RT, group;
+  int down;                   // 0: x -> A = w silu(gate) up; 1: A -> Y
+  int n_out;                  // features of the result
+  const uint16_t* in;         // x [T][in_ld] or A [rows][in_ld]
+  int in_ld;
+  uint16_t* A;                // rows a_ld apart
+  int a_ld;
+  float* Y;                   // rows y_ld apart
+  int y_ld;
+  const int* ids;             // [T][k]
+  const float* w;             // [T][k]
+  int T, k, kp, E, Ep;
+  const int *counts, *offsets, *pad_off, *src_of;   // the layout; counts NULL: few slots, each block orders them itself
+  int* prow_of;               // few slots, first product: filled here for the combine
+  int rows_most;              // experts with more rows are left to the tile kernel
+  int rows_cap, group_rows;   // filled by the launch: staged rows, rows of a pass over an expert's weights
+  DevStatus* status;
+};
+constexpr int W4_SMALL_SLOTS = 128;   // up to here the blocks order the slots themselves
+
+cudaError_t launch_w4_quantize(const uint16_t* W, int n, const W4Shape& s, uint32_t* codes, uint16_t* scales, uint8_t* zeros, cudaStream_t st);
+cudaError_t launch_w4_pack(const uint8_t* q, const uint16_t* qs, const uint8_t* qz, int n, const W4Shape& s, uint32_t* codes, uint16_t* scales,
+                           uint8_t* zeros, cudaStream_t st);
+cudaError_t launch_w4_dequantize(const uint32_t* codes, const uint16_t* scales, const uint8_t* zeros, int n, const W4Shape& s, uint16_t* W, cudaStream_t st);
+// rows the vector kernel can stage at reduction K; 0: too long
+int w4_vec_rows(int K);
+cudaError_t launch_w4_vec(W4VecArgs a, int num_sms, cudaStream_t st, int* launches);
+// out[t] = sum_j Y[prow_of[t kp + j]], j ascending
+cudaError_t launch_w4_combine(const float* Y, int y_ld, const int* prow_of, int T, int d, int kp, uint16_t* out, cudaStream_t st, int* launches);
+
+}  // namespace moe
