@@ -1,63 +1,59 @@
 // Expert weights in 4 bits with a scale -- and a zero point, where there are any -- for each group of 32, 64 or 128 reduction
 // elements: w = s (q - z), q and z in 0 .. 15 (z = 8 without zero points), s in bf16.
 //
-// Layout.  A matrix of R rows (output features) and K columns (reduction) is cut into tiles of 16 rows x 64 columns, 512 bytes
-// each, row tile major.  The 32 lanes of a warp own 16 bytes of a tile side by side: word j of lane 4 g + c holds, of the 16
-// columns 16 j .., what the lane is given of a 16 x 16 bf16 operand of a matrix instruction -- the pairs of columns
-// {2 c, 2 c + 1} and {2 c + 8, 2 c + 9} of rows g and g + 8:
+// Layout.  A matrix of R rows (output features) and K columns (reduction) is cut into units of 32 rows x 128 columns, 2 KB each,
+// row tile major; a unit into quarters of 16 rows x 64 columns (columns slow: first half's two, second half's two).  The 32 lanes of
+// a warp own 16 bytes of a quarter side by side: word j of lane 4 g + c holds, of the quarter's columns 16 j .., what the lane is
+// given of a 16 x 16 bf16 operand of a matrix instruction -- the pairs of columns {2 c, 2 c + 1} and {2 c + 8, 2 c + 9} of rows g
+// and g + 8:
 //   pair r (0: row g, first pair; 1: row g + 8, first; 2: row g, second; 3: row g + 8, second)
 //   has its even column in bits 4 r .. 4 r + 3 and its odd column in bits 16 + 4 r ..
 // so that (word >> 4 r) & 0x000F000F is a pair in the place of two bf16 mantissas.  The same fragment is what a warp writes to
 // TMEM for 16 lanes x 8 columns (two bf16 each), so matrix-vector and tensor-core kernels read one layout.
-// Scales [row tile][group][8][2] bf16 and zero points [..][8][2] bytes: {row g, row g + 8} side by side.
-// Rows of W_gate_up: tile rows 0 .. 7 are gate rows, 8 .. 15 the up rows of the same features (SwiGLU needs no exchange).
-// Rows behind the last and columns behind K are codes of value 0 with scale 0.
+// Scales [unit][8][groups of a unit][4] bf16 and zero points [..] bytes: lanes 4 g + c need rows {g, g + 8, g + 16, g + 24} of the unit's
+// 1, 2 or 4 groups, side by side.  Units follow one another, so a warp's addresses only ever grow by a constant.
+// Rows of W_gate_up: of 16 rows, 0 .. 7 are gate rows, 8 .. 15 the up rows of the same features (SwiGLU needs no exchange).
+// Rows behind the last are codes of value 0 with scale 0, columns behind K codes of value 0.
 #pragma once
 
 #include "moe_internal.h"
 
 namespace moe {
 
-constexpr int W4_TILE_ROWS = 16, W4_TILE_K = 64, W4_TILE_BYTES = 512;
+constexpr int W4_TILE_ROWS = 32, W4_UNIT_K = 128, W4_UNIT_BYTES = 2048;
 
 struct W4Shape {
   int rows, cols, group, paired;
   __host__ __device__ int row_tiles() const { return (rows + W4_TILE_ROWS - 1) / W4_TILE_ROWS; }
-  __host__ __device__ int k_tiles() const { return (cols + W4_TILE_K - 1) / W4_TILE_K; }
-  __host__ __device__ int groups() const { return (k_tiles() * W4_TILE_K + group - 1) / group; }   // whole tiles
+  __host__ __device__ int units() const { return (cols + W4_UNIT_K - 1) / W4_UNIT_K; }   // of a row tile
+  __host__ __device__ int unit_groups() const { return W4_UNIT_K / group; }
   // row of the matrix that is row r of tile rt; -1: behind the last
   __host__ __device__ int row_at(int rt, int r) const {
-    if (paired) return (r & 8 ? rows / 2 : 0) + rt * 8 + (r & 7);
-    const int i = rt * W4_TILE_ROWS + r;
+    const int sub = 2 * rt + (r >> 4);   // sixteen rows
+    const int i = paired ? (sub * 8 < rows / 2 ? (r & 8 ? rows / 2 : 0) + sub * 8 + (r & 7) : rows) : sub * 16 + (r & 15);
     return i < rows ? i : -1;
   }
 };
 
-// The four registers of a 16 x 16 bf16 operand from a word of codes: q - z exactly, q and z in the low mantissa bits of 128 + ..
-__device__ __forceinline__ uint32_t w4_bias(uint32_t z) { return 0x43004300u | z * 0x00010001u; }
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
+// The four registers of a 16 x 16 bf16 operand from a word of codes: 128 + q, the codes being the low mantissa bits.
+constexpr uint32_t W4_MAGIC = 0x43004300u;
+__device__ __forceinline__ uint32_t w4_pair(uint32_t word) {
   uint32_t r;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(r) : "r"(word), "r"(W4_MAGIC));   // (word & mask) | magic
   return r;
 }
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
+__device__ __forceinline__ void w4_fragment(uint32_t word, uint32_t (&a)[4]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) a[r] = w4_pair(word >> (4 * r));
 }
-__device__ __forceinline__ void w4_fragment(uint32_t word, uint32_t bias_lo, uint32_t bias_hi, uint32_t (&a)[4]) {
-  a[0] = sub_bf16x2((word & 0x000F000Fu) | 0x43004300u, bias_lo);
-  a[1] = sub_bf16x2(((word >> 4) & 0x000F000Fu) | 0x43004300u, bias_hi);
-  a[2] = sub_bf16x2(((word >> 8) & 0x000F000Fu) | 0x43004300u, bias_lo);
-  a[3] = sub_bf16x2(((word >> 12) & 0x000F000Fu) | 0x43004300u, bias_hi);
-}
+__device__ __forceinline__ float w4_offset(uint32_t z) { return __uint_as_float(0x43000000u | (z & 0xFFu) << 16); }   // 128 + z, z < 128
 
 // One expert product of the layer over experts with few rows (w4_vec.cu).
 struct W4VecArgs {
   const uint4* codes;
   const uint32_t* scales;     // bf16 pairs
   const uint16_t* zeros;      // byte pairs; NULL: 8
-  int K, KB, NG, RT, group;
+  int K, KU, RT, group;       // reduction, units of a row tile, row tiles of an expert
   int down;                   // 0: x -> A = w silu(gate) up; 1: A -> Y
   int n_out;                  // features of the result
   const uint16_t* in;         // x [T][in_ld] or A [rows][in_ld]

@@ -1,6 +1,6 @@
 // Weights into 4 bits, from a checkpoint's natural codes into the layout of w4.cuh, and back to the values they stand for.
-// A warp takes 16 rows x 128 columns: lanes 16 h + m have columns 8 m .. of rows 2 i + h, and change places with the layout's
-// lanes through 1 KB of shared memory.  Bound by the bytes of the matrices.
+// A warp takes 16 rows x 128 columns, half a unit: lanes 16 h + m have columns 8 m .. of rows 2 i + h, and change places with the
+// layout's lanes through 1 KB of shared memory.  Bound by the bytes of the matrices.
 #include "launch_pairs.cuh"
 #include "topk.cuh"
 #include "w4.cuh"
@@ -11,17 +11,19 @@ namespace {
 
 constexpr int CODE_WARPS = 8, CODE_LD = 17;   // words of a staged row: 16 of codes, one so that rows fall into different banks
 
-struct CodeTask { int64_t rt_index; int m, rt, chunk; };   // row tile over all matrices, matrix, row tile, 128-column chunk
+struct CodeTask { int64_t unit; int m, rt, chunk, t; };   // unit of all, matrix, row tile, unit of the tile, upper or lower 16 rows
 __device__ __forceinline__ CodeTask code_task(int64_t i, int RT, int chunks) {
   CodeTask t;
-  t.rt_index = i / chunks;
-  t.chunk = (int)(i - t.rt_index * chunks);
-  t.m = (int)(t.rt_index / RT);
-  t.rt = (int)(t.rt_index - (int64_t)t.m * RT);
+  t.unit = i >> 1;
+  t.t = (int)(i & 1);
+  const int64_t tile = t.unit / chunks;
+  t.chunk = (int)(t.unit - tile * chunks);
+  t.m = (int)(tile / RT);
+  t.rt = (int)(tile - (int64_t)t.m * RT);
   return t;
 }
 
-// natural words [16][CODE_LD] <-> the lane's words of k-tile b of the chunk
+// natural words [16][CODE_LD] <-> the lane's words of half b of the unit
 __device__ __forceinline__ uint4 gather_words(const uint32_t* st, int b, int lane) {
   const int g = lane >> 2, c8 = (lane & 3) * 8;
   uint32_t out[4];
@@ -69,19 +71,19 @@ __global__ void __launch_bounds__(32 * CODE_WARPS) w4_encode_kernel(const void* 
   __shared__ uint32_t stage[CODE_WARPS][16 * CODE_LD];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = lane >> 4, m = lane & 15;
   uint32_t* const st = stage[warp];
-  const int RT = s.row_tiles(), KB = s.k_tiles(), NG = s.groups(), ng_src = (s.cols + s.group - 1) / s.group;
+  const int RT = s.row_tiles(), ng = s.unit_groups(), ng_src = (s.cols + s.group - 1) / s.group;
   const int gl = s.group >> 3;   // lanes of a group
   const bool asym = zeros != nullptr;
   pdl_wait();
   pdl_trigger();
   for (int64_t i = (int64_t)blockIdx.x * CODE_WARPS + warp; i < tasks; i += (int64_t)gridDim.x * CODE_WARPS) {
     const CodeTask t = code_task(i, RT, chunks);
-    const int col = t.chunk * 128 + m * 8, grp = t.chunk * (128 / s.group) + m / gl;
-    const bool leads = m % gl == 0 && grp < NG;
+    const int col = t.chunk * 128 + m * 8, grp = t.chunk * ng + m / gl;
+    const bool leads = m % gl == 0;
     uint4 in[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      const int row = s.row_at(t.rt, 2 * q + h);
+      const int row = s.row_at(t.rt, 16 * t.t + 2 * q + h);
       in[q] = make_uint4(0, 0, 0, 0);
       if (row >= 0 && col < s.cols) {
         const size_t at = ((size_t)t.m * s.rows + row) * s.cols + col;
@@ -91,7 +93,7 @@ __global__ void __launch_bounds__(32 * CODE_WARPS) w4_encode_kernel(const void* 
     }
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      const int r = 2 * q + h, row = s.row_at(t.rt, r);
+      const int r = 2 * q + h, row = s.row_at(t.rt, 16 * t.t + r);
       uint32_t word;
       float scale = 0.f, zero = 8.f;
       if (QUANT) {
@@ -123,15 +125,14 @@ __global__ void __launch_bounds__(32 * CODE_WARPS) w4_encode_kernel(const void* 
       }
       st[r * CODE_LD + m] = word;
       if (leads) {
-        const size_t at = ((size_t)t.rt_index * NG + grp) * 16 + (r & 7) * 2 + (r >> 3);
+        const size_t at = (((size_t)t.unit * 8 + (r & 7)) * ng + m / gl) * 4 + 2 * t.t + (r >> 3);
         scales[at] = (uint16_t)(__float_as_uint(scale) >> 16);
         if (asym) zeros[at] = (uint8_t)zero;
       }
     }
     __syncwarp();
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-      if (t.chunk * 2 + b < KB) codes[((size_t)t.rt_index * KB + t.chunk * 2 + b) * 32 + lane] = gather_words(st, b, lane);
+    for (int b = 0; b < 2; ++b) codes[((size_t)t.unit * 4 + 2 * b + t.t) * 32 + lane] = gather_words(st, b, lane);
     __syncwarp();
   }
 }
@@ -142,31 +143,29 @@ __global__ void __launch_bounds__(32 * CODE_WARPS) w4_decode_kernel(const uint4*
   __shared__ uint32_t stage[CODE_WARPS][16 * CODE_LD];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = lane >> 4, m = lane & 15;
   uint32_t* const st = stage[warp];
-  const int RT = s.row_tiles(), KB = s.k_tiles(), NG = s.groups();
+  const int RT = s.row_tiles(), ng = s.unit_groups();
   pdl_wait();
   pdl_trigger();
   for (int64_t i = (int64_t)blockIdx.x * CODE_WARPS + warp; i < tasks; i += (int64_t)gridDim.x * CODE_WARPS) {
     const CodeTask t = code_task(i, RT, chunks);
-    const int col = t.chunk * 128 + m * 8, grp = (t.chunk * 128 + m * 8) / s.group;
+    const int col = t.chunk * 128 + m * 8, grp = m * 8 / s.group;
     uint4 w[2];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-      if (t.chunk * 2 + b < KB) w[b] = __ldcs(&codes[((size_t)t.rt_index * KB + t.chunk * 2 + b) * 32 + lane]);
+    for (int b = 0; b < 2; ++b) w[b] = __ldcs(&codes[((size_t)t.unit * 4 + 2 * b + t.t) * 32 + lane]);
     float sc[8], z[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       const int r = 2 * q + h;
-      const size_t at = ((size_t)t.rt_index * NG + min(grp, NG - 1)) * 16 + (r & 7) * 2 + (r >> 3);
+      const size_t at = (((size_t)t.unit * 8 + (r & 7)) * ng + grp) * 4 + 2 * t.t + (r >> 3);
       sc[q] = __uint_as_float((uint32_t)scales[at] << 16);
       z[q] = zeros ? (float)zeros[at] : 8.f;
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-      if (t.chunk * 2 + b < KB) scatter_words(st, b, lane, w[b]);
+    for (int b = 0; b < 2; ++b) scatter_words(st, b, lane, w[b]);
     __syncwarp();
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      const int r = 2 * q + h, row = s.row_at(t.rt, r);
+      const int r = 2 * q + h, row = s.row_at(t.rt, 16 * t.t + r);
       const uint32_t word = st[r * CODE_LD + m];
       uint32_t o[4];
 #pragma unroll
@@ -183,21 +182,21 @@ static dim3 code_grid(int64_t tasks) {
 }
 
 cudaError_t launch_w4_quantize(const uint16_t* W, int n, const W4Shape& s, uint32_t* codes, uint16_t* scales, uint8_t* zeros, cudaStream_t st) {
-  const int chunks = (s.k_tiles() + 1) / 2;
-  const int64_t tasks = (int64_t)n * s.row_tiles() * chunks;
+  const int chunks = s.units();
+  const int64_t tasks = (int64_t)n * s.row_tiles() * chunks * 2;
   return launch_dependent(w4_encode_kernel<true>, code_grid(tasks), dim3(32 * CODE_WARPS), 0, st, W, nullptr, nullptr, tasks, chunks, s,
                           reinterpret_cast<uint4*>(codes), scales, zeros);
 }
 cudaError_t launch_w4_pack(const uint8_t* q, const uint16_t* qs, const uint8_t* qz, int n, const W4Shape& s, uint32_t* codes, uint16_t* scales,
                            uint8_t* zeros, cudaStream_t st) {
-  const int chunks = (s.k_tiles() + 1) / 2;
-  const int64_t tasks = (int64_t)n * s.row_tiles() * chunks;
+  const int chunks = s.units();
+  const int64_t tasks = (int64_t)n * s.row_tiles() * chunks * 2;
   return launch_dependent(w4_encode_kernel<false>, code_grid(tasks), dim3(32 * CODE_WARPS), 0, st, q, qs, qz, tasks, chunks, s,
                           reinterpret_cast<uint4*>(codes), scales, zeros);
 }
 cudaError_t launch_w4_dequantize(const uint32_t* codes, const uint16_t* scales, const uint8_t* zeros, int n, const W4Shape& s, uint16_t* W, cudaStream_t st) {
-  const int chunks = (s.k_tiles() + 1) / 2;
-  const int64_t tasks = (int64_t)n * s.row_tiles() * chunks;
+  const int chunks = s.units();
+  const int64_t tasks = (int64_t)n * s.row_tiles() * chunks * 2;
   return launch_dependent(w4_decode_kernel, code_grid(tasks), dim3(32 * CODE_WARPS), 0, st, reinterpret_cast<const uint4*>(codes), scales, zeros,
                           tasks, chunks, s, W);
 }

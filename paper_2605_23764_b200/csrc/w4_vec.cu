@@ -2,13 +2,17 @@
 //
 //   h[i] = sum_groups s_g sum_k (q - z) x[i][k];   A = w silu(h_gate) h_up;   Y = the same over A;   out[t] = sum_j Y of its slots
 //
-// What bounds it: the weights' bytes, read once.  Every warp streams its share of the row tiles straight into registers (16 bytes
-// a lane and tile, eight tiles in flight), widens the codes to bf16 -- q - z is a small whole number, exact -- and multiplies 16 rows
-// by up to 8 rows of x at a time (mma.m16n8k16, which a matrix-vector product needs as a dot-product unit, not for its rate).
-// A group's sum is scaled in fp32: the only rounding to fewer bits on the way is that of A to bf16.
+// What bounds it: the weights' bytes, read once.  Every warp streams its share of the units (2 KB) through a ring of its own in shared
+// memory (loads kept in registers instead did not overlap: a unit then cost a memory latency, 2.7 TB/s), widens the codes to bf16
+// 128 + q -- a mask and an exponent -- and multiplies 32 rows by up to 8 rows of x at a time (mma.m16n8k16, which a matrix-vector
+// product needs as a dot-product unit, not for its rate).  A third operand of ones gives the sums of x, of which 128 + z is taken off:
+//   sum (q - z) x = sum (128 + q) x - (128 + z) sum x,
+// exact products, fp32 sums; a subtraction for each pair of codes instead kept the pipe that multiplies at 40 % and the kernel at
+// 3.5 TB/s.  A group's sum is scaled in fp32: the only rounding to fewer bits on the way is that of A to bf16.  32 rows because the
+// operand rows of x are read from shared memory once for all of them.
 //
-// Split.  Blocks take consecutive row tiles of the hit experts, one block an SM; inside a block the warps share the (row tile, 64
-// columns) units evenly, whatever the tile boundaries: a row tile that several warps have a piece of is put together from shared
+// Split.  Blocks take consecutive row tiles of the hit experts, one block an SM; inside a block the warps share the units (32 rows x 128
+// columns) evenly, whatever the tile boundaries: a row tile that several warps have a piece of is put together from shared
 // memory in the warps' order.  So few experts and long reductions keep all warps at work, and results do not depend on timing.
 #include "launch_pairs.cuh"
 #include "topk.cuh"
@@ -20,21 +24,23 @@ namespace {
 
 constexpr int VEC_WARPS = 16, VEC_THREADS = 32 * VEC_WARPS;
 constexpr int VEC_ROWS = 8;          // rows of x that a pass over an expert's weights takes
-constexpr int VEC_SEG_TILES = 64;    // row tiles between two joins
+constexpr int VEC_SEG_TILES = 16;    // row tiles between two joins
 constexpr int VEC_SEG_GROUPS = 32;   // passes a segment may touch: a lane each
-constexpr int VEC_DEPTH = 8;         // units in flight per warp
+constexpr int VEC_DEPTH = 3;         // slots of a warp's ring: two units in flight, 50 KB an SM
 constexpr int VEC_SMEM = 222 * 1024;
+constexpr int VEC_PIECE_BYTES = W4_TILE_ROWS * VEC_ROWS * 4;   // sums of a row tile
 constexpr int VEC_ROWS_MOST = 64;    // staged rows, at most
 
-__host__ __device__ constexpr int vec_ld(int KB) { return KB * W4_TILE_K * 2 + 16; }   // bytes from row to row: ldmatrix rows in different banks
-__host__ __device__ constexpr size_t vec_fixed_smem(int Ep) {
-  return (size_t)(VEC_SEG_TILES + VEC_WARPS) * W4_TILE_BYTES + sizeof(int) * (3 * (size_t)Ep + 4);
+__host__ __device__ constexpr int vec_ld(int KU) { return KU * W4_UNIT_K * 2 + 16; }   // bytes from row to row: ldmatrix rows in different banks
+__host__ __device__ constexpr int vec_slot(int ng, bool asym) { return W4_UNIT_BYTES + 64 * ng + (asym ? 32 * ng : 0); }   // codes, scales, zero points
+__host__ __device__ constexpr size_t vec_fixed_smem(int Ep, int ng, bool asym) {
+  return (size_t)VEC_WARPS * VEC_DEPTH * vec_slot(ng, asym) +
+         (size_t)(VEC_SEG_TILES + VEC_WARPS) * VEC_PIECE_BYTES + sizeof(int) * (3 * (size_t)Ep + 4);
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t* r) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -44,11 +50,30 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
+// the first product of a chain: no accumulator goes in
+__device__ __forceinline__ void mma16816_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
   return v;
 }
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Exclusive scan of v over the block, n <= 3 values a thread; returns the total.
 __device__ __forceinline__ int block_scan3(int (&v)[3], int* warp_sums) {
@@ -75,12 +100,12 @@ __device__ __forceinline__ int block_scan3(int (&v)[3], int* warp_sums) {
   for (int i = 0; i < 3; ++i) { const int x = v[i]; v[i] = at; at += x; }
   return total;
 }
-static_assert(3 * VEC_THREADS >= 1024 + 64, "an expert for each scanned value");
+static_assert(3 * VEC_THREADS >= 1024 + 64 && VEC_THREADS >= W4_SMALL_SLOTS, "an expert for each scanned value");
 
 }  // namespace
 
-// G32: groups of 32, two to a unit of 64 columns; else a unit lies in one group.
-template <bool ASYM, bool G32>
+// NG groups of 128 / NG columns to a unit.
+template <bool ASYM, int NG>
 __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs a) {
   extern __shared__ __align__(16) uint8_t vsm[];
   __shared__ int warp_sums[VEC_WARPS];
@@ -89,13 +114,14 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
   __shared__ int sg_e[VEC_SEG_GROUPS], sg_x[VEC_SEG_GROUPS], sg_n[VEC_SEG_GROUPS], seg_end, seg_rows;
   __shared__ int row_p[VEC_ROWS_MOST], row_t[VEC_ROWS_MOST];
   __shared__ float row_w[VEC_ROWS_MOST];
-  float* const acc_s = reinterpret_cast<float*>(vsm);                                  // [VEC_SEG_TILES][16][8]
-  float* const head_s = acc_s + VEC_SEG_TILES * W4_TILE_BYTES / 4;                     // [VEC_WARPS][16][8]
-  int* const cnt = reinterpret_cast<int*>(head_s + VEC_WARPS * W4_TILE_BYTES / 4);     // [Ep] rows of the expert
+  constexpr int SLOT = vec_slot(NG, ASYM), PIECE = VEC_PIECE_BYTES / 4;
+  float* const acc_s = reinterpret_cast<float*>(vsm + VEC_WARPS * VEC_DEPTH * SLOT);   // [VEC_SEG_TILES][32][8]
+  float* const head_s = acc_s + VEC_SEG_TILES * PIECE;                                 // [VEC_WARPS][32][8]
+  int* const cnt = reinterpret_cast<int*>(head_s + VEC_WARPS * PIECE);                     // [Ep] rows of the expert
   int* const first = cnt + a.Ep;                                                       // [Ep] first row of the expert (few slots)
   int* const gstart = first + a.Ep;                                                    // [Ep + 1] first pass of the expert
-  const int ld = vec_ld(a.KB);
-  uint8_t* const xs = vsm + ((vec_fixed_smem(a.Ep) + 15) & ~size_t(15));               // [rows_cap][ld]
+  const int ld = vec_ld(a.KU);
+  uint8_t* const xs = vsm + ((vec_fixed_smem(a.Ep, NG, ASYM) + 15) & ~size_t(15));               // [rows_cap][ld]
   const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x, g = lane >> 2, c = lane & 3;
   const bool small = a.counts == nullptr;
 
@@ -209,44 +235,47 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
     }
     __syncthreads();
     const int ntiles = seg_end, rt0 = (int)(t0 - (int64_t)p0 * a.RT);
-    const int units = ntiles * a.KB;
+    const int units = ntiles * a.KU;
     const int u0 = (int)((int64_t)units * warp / VEC_WARPS), u1 = (int)((int64_t)units * (warp + 1) / VEC_WARPS);
+    int tile = u0 / a.KU, ku = u0 - tile * a.KU;   // row tile of the segment, unit of it
+    int pass = (rt0 + tile) / a.RT, rt = rt0 + tile - pass * a.RT;
 
-    // ---- the stream: unit u of the segment is k-tile u % KB of row tile u / KB
-    uint4 q[VEC_DEPTH];
-    uint32_t sc[VEC_DEPTH][G32 ? 2 : 1];
-    uint32_t zp[VEC_DEPTH][ASYM ? (G32 ? 2 : 1) : 1];
-    int f_tile = u0 / a.KB, f_kb = u0 - f_tile * a.KB, f_rt, f_pass;   // of the next unit to fetch
-    {
-      const int at = rt0 + f_tile;
-      f_pass = at / a.RT;
-      f_rt = at - f_pass * a.RT;
+    // ---- the stream: from unit to unit of an expert the addresses grow by a constant
+    const uint8_t *f_codes = nullptr, *f_scales = nullptr, *f_zeros = nullptr;
+    int f_pass = pass, f_left = u1 - u0, f_run = 0;   // units to fetch, of them in this pass
+    auto seek = [&](size_t unit) {   // of all experts' units; lane l copies 16 bytes at 16 l
+      f_codes = reinterpret_cast<const uint8_t*>(a.codes) + unit * W4_UNIT_BYTES + lane * 16;
+      f_scales = reinterpret_cast<const uint8_t*>(a.scales) + unit * (64 * NG) + lane * 16;
+      if (ASYM) f_zeros = reinterpret_cast<const uint8_t*>(a.zeros) + unit * (32 * NG) + lane * 16;
+    };
+    if (u0 < u1) {
+      const int at = rt * a.KU + ku;
+      seek((size_t)sg_e[pass] * a.RT * a.KU + at);
+      f_run = min(f_left, a.RT * a.KU - at);
     }
-    size_t f_row = 0;   // row tile over all experts
-    if (u0 < u1) f_row = (size_t)sg_e[f_pass] * a.RT + f_rt;
-    const int glog = a.group == 128 ? 7 : 6;
-    auto fetch = [&](int i, bool on) {
-      if (!on) return;
-      q[i] = ld_stream(a.codes + (f_row * a.KB + f_kb) * 32 + lane);
-      const size_t sg = f_row * a.NG + (G32 ? 2 * f_kb : (f_kb * W4_TILE_K) >> glog);
-      sc[i][0] = __ldg(a.scales + sg * 8 + g);
-      if (G32) sc[i][G32 ? 1 : 0] = __ldg(a.scales + (sg + 1) * 8 + g);
-      if (ASYM) {
-        zp[i][0] = __ldg(a.zeros + sg * 8 + g);
-        if (G32) zp[i][ASYM && G32 ? 1 : 0] = __ldg(a.zeros + (sg + 1) * 8 + g);
+    const uint32_t ring = smem_u32(vsm) + warp * VEC_DEPTH * SLOT, ring_end = ring + VEC_DEPTH * SLOT;
+    auto fetch = [&](uint32_t slot) {
+      if (f_run == 0 && f_left > 0) {
+        ++f_pass;
+        seek((size_t)sg_e[f_pass] * a.RT * a.KU);
+        f_run = min(f_left, a.RT * a.KU);
       }
-      if (++f_kb == a.KB) {
-        f_kb = 0;
-        ++f_row;
-        if (++f_rt == a.RT) {
-          f_rt = 0;
-          ++f_pass;
-          if (f_pass < VEC_SEG_GROUPS) f_row = (size_t)sg_e[f_pass] * a.RT;
-        }
+      if (f_run > 0) {
+        --f_run;
+        --f_left;
+        const uint32_t to = slot + lane * 16;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) cp_async16(to + 512 * h, f_codes + 512 * h);
+        if (lane < 4 * NG) cp_async16(to + W4_UNIT_BYTES, f_scales);
+        if (ASYM && lane < 2 * NG) cp_async16(to + W4_UNIT_BYTES + 64 * NG, f_zeros);
+        f_codes += W4_UNIT_BYTES;
+        f_scales += 64 * NG;
+        if (ASYM) f_zeros += 32 * NG;
       }
+      cp_async_commit();
     };
 #pragma unroll
-    for (int i = 0; i < VEC_DEPTH; ++i) fetch(i, u0 + i < u1);
+    for (int i = 0; i < VEC_DEPTH - 1; ++i) fetch(ring + i * SLOT);
 
     // ---- the rows of x, zeros behind K
     if (!waited) {
@@ -255,96 +284,140 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
       waited = true;
     }
     {
-      const int pieces = a.KB * (W4_TILE_K / 8), full = a.K >> 3, rows = seg_rows;
+      const int pieces = a.KU * (W4_UNIT_K / 8), full = a.K >> 3, rows = seg_rows;
       for (int i = tid; i < rows * pieces; i += VEC_THREADS) {
         const int r = i / pieces, v = i - r * pieces;
         uint8_t* dst = xs + (size_t)r * ld + v * 16;
         if (v < full) cp_async16(smem_u32(dst), a.in + (size_t)row_t[r] * a.in_ld + v * 8);
         else *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
       }
-      cp_async_wait_all();
+      cp_async_commit();
+      cp_async_wait<0>();   // (the first units as well)
     }
     __syncthreads();
 
     // ---- the products
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    int tile = u0 / a.KB, kb = u0 - tile * a.KB;
-    bool began = kb == 0;   // this warp has the tile from its first unit on
-    uint32_t x_addr = 0;
-    int rt = 0, pass = 0;
+    float acc[2][4] = {};
+    bool began = ku == 0;   // this warp has the tile from its first unit on
+    uint32_t x_row = 0;
     auto enter_pass = [&]() {   // operand rows: lane l gives row l % 8 of matrix l / 8; rows that are not there are computed and dropped
       const int r = min(lane & 7, sg_n[pass] - 1);
-      x_addr = smem_u32(xs + (size_t)(sg_x[pass] + r) * ld) + (lane >> 3) * 16;
+      x_row = smem_u32(xs + (size_t)(sg_x[pass] + r) * ld) + (lane >> 3) * 16;
     };
-    if (u0 < u1) {
-      const int at = rt0 + tile;
-      pass = at / a.RT;
-      rt = at - pass * a.RT;
-      enter_pass();
-    }
-    auto put = [&](float* to) {
-      *reinterpret_cast<float2*>(to + g * 8 + 2 * c) = make_float2(acc[0], acc[1]);
-      *reinterpret_cast<float2*>(to + (g + 8) * 8 + 2 * c) = make_float2(acc[2], acc[3]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = 0.f;
-    };
+    if (u0 < u1) enter_pass();
+    uint32_t rd = ring, wr = ring + (VEC_DEPTH - 1) * SLOT;
+    for (int u = u0; u < u1;) {
+      // the warp's piece of a row tile
+      const int n = min(a.KU - ku, u1 - u);
+      uint32_t x_addr = x_row + ku * (W4_UNIT_K * 2);
 #pragma unroll 1
-    for (int u = u0; u < u1; u += VEC_DEPTH) {
+      for (int i = 0; i < n; ++i) {
+        fetch(wr);
+        cp_async_wait<VEC_DEPTH - 1>();
+        __syncwarp();   // the lanes' copies of scales are everybody's
+        uint32_t b[16];
 #pragma unroll
-      for (int i = 0; i < VEC_DEPTH; ++i) {
-        if (u + i < u1) {
-          uint32_t b[8];
-          ldmatrix4(x_addr + kb * (W4_TILE_K * 2), b);
-          ldmatrix4(x_addr + kb * (W4_TILE_K * 2) + 64, b + 4);
-          const uint32_t words[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+        for (int h = 0; h < 4; ++h) ldmatrix4(x_addr + 64 * h, b + 4 * h);
+        x_addr += W4_UNIT_K * 2;
+        // rows {g, g + 8} and {g + 16, g + 24} of each group
+        uint32_t sc[2][NG], zp[ASYM ? NG : 1];
+        {
+          const uint32_t at = rd + W4_UNIT_BYTES + g * (8 * NG);
+          if constexpr (NG == 1) {
+            const uint2 v = lds64(at);
+            sc[0][0] = v.x; sc[1][0] = v.y;
+          } else {
 #pragma unroll
-          for (int h = 0; h < (G32 ? 2 : 1); ++h) {
-            const uint32_t z = ASYM ? zp[i][ASYM && G32 ? h : 0] : 0x0808u;
-            const uint32_t blo = w4_bias(z & 0xFFu), bhi = w4_bias(z >> 8);
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < (G32 ? 2 : 4); ++j) {
-              const int jj = (G32 ? 2 * h : 0) + j;
-              uint32_t f[4];
-              w4_fragment(words[jj], blo, bhi, f);
-              mma16816(part, f, b[2 * jj], b[2 * jj + 1]);
+            for (int h = 0; h < NG; h += 2) {
+              const uint4 v = lds128(at + 8 * h);
+              sc[0][h] = v.x; sc[1][h] = v.y; sc[0][h + 1] = v.z; sc[1][h + 1] = v.w;
             }
-            const float slo = bf16lo(sc[i][G32 ? h : 0]), shi = bf16hi(sc[i][G32 ? h : 0]);
-            acc[0] = fmaf(slo, part[0], acc[0]);
-            acc[1] = fmaf(slo, part[1], acc[1]);
-            acc[2] = fmaf(shi, part[2], acc[2]);
-            acc[3] = fmaf(shi, part[3], acc[3]);
           }
-          fetch(i, u + i + VEC_DEPTH < u1);
-          if (++kb == a.KB) {
-            put(began ? acc_s + tile * 128 : head_s + warp * 128);
-            began = true;
-            kb = 0;
-            ++tile;
-            if (++rt == a.RT) {
-              rt = 0;
-              ++pass;
-              if (u + i + 1 < u1) enter_pass();
+          if constexpr (ASYM) {
+            const uint32_t zat = rd + W4_UNIT_BYTES + 64 * NG + g * (4 * NG);
+            if constexpr (NG == 1) {
+              zp[0] = lds32(zat);
+            } else if constexpr (NG == 2) {
+              const uint2 v = lds64(zat);
+              zp[0] = v.x; zp[1] = v.y;
+            } else {
+              const uint4 v = lds128(zat);
+              zp[0] = v.x; zp[1] = v.y; zp[2] = v.z; zp[3] = v.w;
             }
           }
         }
+        constexpr int STEPS = 8 / NG;   // 16-column steps of a group
+        constexpr uint32_t ONES[4] = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+        float part[2][4], sums[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {   // halves of 64 columns
+          const uint4 q0 = lds128(rd + lane * 16 + 1024 * h), q1 = lds128(rd + lane * 16 + 1024 * h + 512);
+          const uint32_t words[2][4] = {{q0.x, q0.y, q0.z, q0.w}, {q1.x, q1.y, q1.z, q1.w}};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int at = 4 * h + j, grp = at / STEPS;
+            if (at % STEPS == 0) mma16816_first(sums, ONES, b[2 * at], b[2 * at + 1]);
+            else mma16816(sums, ONES, b[2 * at], b[2 * at + 1]);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              uint32_t f[4];
+              w4_fragment(words[t][j], f);
+              if (at % STEPS == 0) mma16816_first(part[t], f, b[2 * at], b[2 * at + 1]);
+              else mma16816(part[t], f, b[2 * at], b[2 * at + 1]);
+            }
+            if (at % STEPS == STEPS - 1)
+#pragma unroll
+              for (int t = 0; t < 2; ++t) {
+                const float zlo = ASYM ? w4_offset(zp[ASYM ? grp : 0] >> (16 * t)) : 136.f;
+                const float zhi = ASYM ? w4_offset(zp[ASYM ? grp : 0] >> (16 * t + 8)) : 136.f;
+                const float slo = bf16lo(sc[t][grp]), shi = bf16hi(sc[t][grp]);
+                acc[t][0] = fmaf(slo, fmaf(-zlo, sums[0], part[t][0]), acc[t][0]);
+                acc[t][1] = fmaf(slo, fmaf(-zlo, sums[1], part[t][1]), acc[t][1]);
+                acc[t][2] = fmaf(shi, fmaf(-zhi, sums[0], part[t][2]), acc[t][2]);
+                acc[t][3] = fmaf(shi, fmaf(-zhi, sums[1], part[t][3]), acc[t][3]);
+              }
+          }
+        }
+        __syncwarp();   // everybody has read the slot that the next copy fills
+        wr = rd;
+        rd = rd + SLOT == ring_end ? ring : rd + SLOT;
+      }
+      u += n;
+      ku += n;
+      float* const to = began ? acc_s + tile * PIECE : head_s + warp * PIECE;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        *reinterpret_cast<float2*>(to + (16 * t + g) * 8 + 2 * c) = make_float2(acc[t][0], acc[t][1]);
+        *reinterpret_cast<float2*>(to + (16 * t + g + 8) * 8 + 2 * c) = make_float2(acc[t][2], acc[t][3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[t][i] = 0.f;
+      }
+      if (ku == a.KU) {
+        began = true;
+        ku = 0;
+        ++tile;
+        if (++rt == a.RT) {
+          rt = 0;
+          ++pass;
+          if (u < u1) enter_pass();
+        }
       }
     }
-    if (u0 < u1 && kb != 0) put(began ? acc_s + tile * 128 : head_s + warp * 128);
+    cp_async_wait<0>();
     __syncthreads();
 
-    // ---- pieces of a tile in the warps' order, then the result.  Threads: features fastest, 8 (gate and up) or 16 to a tile
+    // ---- pieces of a tile in the warps' order, then the result.  Threads: features fastest, 16 (gate and up) or 32 to a tile
     auto total = [&](int tl, int r, int col) {
-      float v = acc_s[tl * 128 + r * 8 + col];
-      const int lo = tl * a.KB, hi = lo + a.KB;   // units of the tile
+      float v = acc_s[tl * PIECE + r * 8 + col];
+      const int lo = tl * a.KU, hi = lo + a.KU;   // units of the tile
       for (int w = (int)((int64_t)lo * VEC_WARPS / units); w < VEC_WARPS; ++w) {
         const int b0 = (int)((int64_t)units * w / VEC_WARPS), b1 = (int)((int64_t)units * (w + 1) / VEC_WARPS);
         if (b0 >= hi) break;
-        if (b0 > lo && b1 > b0) v += head_s[w * 128 + r * 8 + col];
+        if (b0 > lo && b1 > b0) v += head_s[w * PIECE + r * 8 + col];
       }
       return v;
     };
-    const int per = a.down ? 16 : 8;
+    const int per = a.down ? 32 : 16;
     for (int i = tid; i < ntiles * per * VEC_ROWS; i += VEC_THREADS) {
       const int f = i % per, rest = i / per, tl = rest % ntiles, col = rest / ntiles;
       const int at = rt0 + tl, ps = at / a.RT, feature = (at - ps * a.RT) * per + f;
@@ -353,7 +426,8 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
       if (a.down) {
         a.Y[(size_t)row_p[xr] * a.y_ld + feature] = total(tl, f, col);
       } else {
-        const float gate = total(tl, f, col), up = total(tl, f + 8, col);
+        const int r = (f & 8) * 2 + (f & 7);   // of the two sixteens of rows
+        const float gate = total(tl, r, col), up = total(tl, r + 8, col);
         const float act = row_w[xr] * (gate / (1.0f + __expf(-gate)) * up);
         a.A[(size_t)row_p[xr] * a.a_ld + feature] = (uint16_t)(pack_bf16x2(act, 0.f) & 0xFFFFu);
       }
@@ -367,32 +441,38 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
   }
 }
 
-int w4_vec_rows(int K) {
-  const int KB = (K + W4_TILE_K - 1) / W4_TILE_K;
-  const long room = (long)VEC_SMEM - (long)((vec_fixed_smem(1024 + 64) + 15) & ~size_t(15));
-  const long rows = room / vec_ld(KB);
+static int vec_rows(int K, int Ep, int ng, bool asym) {
+  const long room = (long)VEC_SMEM - (long)((vec_fixed_smem(Ep, ng, asym) + 15) & ~size_t(15));
+  const long rows = room / vec_ld((K + W4_UNIT_K - 1) / W4_UNIT_K);
   return (int)(rows < VEC_ROWS_MOST ? rows : VEC_ROWS_MOST);
 }
+int w4_vec_rows(int K) { return vec_rows(K, 1024 + 64, 4, true); }
 
 cudaError_t launch_w4_vec(W4VecArgs a, int num_sms, cudaStream_t st, int* launches) {
-  const size_t fixed = (vec_fixed_smem(a.Ep) + 15) & ~size_t(15);
-  a.rows_cap = w4_vec_rows(a.K);
+  const int ng = W4_UNIT_K / a.group;
+  const bool asym = a.zeros != nullptr;
+  const size_t fixed = (vec_fixed_smem(a.Ep, ng, asym) + 15) & ~size_t(15);
+  a.rows_cap = vec_rows(a.K, a.Ep, ng, asym);
   const long slots = (long)a.T * a.kp;
   if (a.rows_cap > slots) a.rows_cap = (int)slots;
   a.group_rows = a.rows_cap < VEC_ROWS ? a.rows_cap : VEC_ROWS;
-  const size_t smem = fixed + (size_t)a.rows_cap * vec_ld(a.KB);
+  const size_t smem = fixed + (size_t)a.rows_cap * vec_ld(a.KU);
   ++*launches;
-#define MOE_W4_VEC(ASYM, G32)                                                                  \
-  do {                                                                                         \
-    if (cudaError_t e = opt_in_smem<w4_vec_kernel<ASYM, G32>>(VEC_SMEM)) return e;              \
-    return launch_dependent(w4_vec_kernel<ASYM, G32>, dim3(num_sms), dim3(VEC_THREADS), smem, st, a); \
+#define MOE_W4_VEC(ASYM, NG)                                                                  \
+  do {                                                                                        \
+    if (cudaError_t e = opt_in_smem<w4_vec_kernel<ASYM, NG>>(VEC_SMEM)) return e;             \
+    return launch_dependent(w4_vec_kernel<ASYM, NG>, dim3(num_sms), dim3(VEC_THREADS), smem, st, a); \
   } while (0)
   if (a.group == 32) {
-    if (a.zeros) MOE_W4_VEC(true, true);
-    MOE_W4_VEC(false, true);
+    if (asym) MOE_W4_VEC(true, 4);
+    MOE_W4_VEC(false, 4);
   }
-  if (a.zeros) MOE_W4_VEC(true, false);
-  MOE_W4_VEC(false, false);
+  if (a.group == 64) {
+    if (asym) MOE_W4_VEC(true, 2);
+    MOE_W4_VEC(false, 2);
+  }
+  if (asym) MOE_W4_VEC(true, 1);
+  MOE_W4_VEC(false, 1);
 #undef MOE_W4_VEC
 }
 
