@@ -810,6 +810,34 @@ W4VecArgs w4_vec_args(const moe_ctx* c, const moe_w4_weights& w, int rows, int c
   return a;
 }
 
+W4TileArgs w4_tile_args(const moe_ctx* c, const moe_w4_weights& w, int rows, int cols, int paired, const CUtensorMap* tok) {
+  const W4Shape ws{rows, cols, w.group, paired};
+  const LayoutView lv = c->layout();
+  W4TileArgs a;
+  memset(&a, 0, sizeof a);
+  memcpy(a.tok, tok, sizeof a.tok);   // the first four: boxes of 16 to 64 rows
+  a.codes = reinterpret_cast<const uint8_t*>(w.codes);
+  a.scales = reinterpret_cast<const uint8_t*>(w.scales);
+  a.zeros = w.zeros;
+  a.K = cols;
+  a.KU = ws.units();
+  a.RT = ws.row_tiles();
+  a.group = w.group;
+  a.ntn = (a.RT + 7) / 8;
+  a.A = c->at<uint16_t>(c->plan.A);
+  a.a_ld = row_ld(c->shape.F);
+  a.Y = c->at<float>(c->plan.Y4);
+  a.y_ld = c->shape.d;
+  a.prow_w = c->at<float>(c->plan.prow_w);
+  a.mblk_expert = lv.mblk_expert;
+  a.mb_start = lv.mb_start;
+  a.counts = lv.counts;
+  a.meta = lv.meta;
+  a.status = c->status();
+  a.budget_ns = c->budget_ns;
+  return a;
+}
+
 int run_fwd_w4(moe_ctx* c, const uint16_t* x, const int32_t* ids, const float* w, const moe_w4_weights& W1, const moe_w4_weights& W2, uint16_t* out,
                int T, cudaStream_t st) {
   const moe_shape& s = c->shape;
@@ -826,14 +854,30 @@ int run_fwd_w4(moe_ctx* c, const uint16_t* x, const int32_t* ids, const float* w
   down.in = up.A;
   down.in_ld = up.a_ld;
   if (up.counts) {
-    Phase ph(c, MOE_PHASE_LAYOUT, st);
-    MOE_CUDA(launch_layout(ids, dm, lv, false, 0, nullptr, 0, c->status(), st, &c->launches));
-  }
-  {
-    Phase ph(c, MOE_PHASE_GEMM_GATE_UP, st);
-    MOE_CUDA(launch_w4_vec(up, c->num_sms, st, &c->launches));
-  }
-  {
+    {
+      Phase ph(c, MOE_PHASE_LAYOUT, st);
+      MOE_CUDA(launch_layout(ids, dm, lv, false, 0, nullptr, 0, c->status(), st, &c->launches));
+    }
+    {
+      Phase ph(c, MOE_PHASE_GATHER, st);
+      MOE_CUDA(launch_gather(x, w, dm, lv, c->at<uint16_t>(c->plan.Xp), c->at<float>(c->plan.prow_w), c->plan.cap_rows, st, &c->launches, c->status(),
+                             c->budget_ns));
+    }
+    W4TileArgs tu = w4_tile_args(c, W1, 2 * s.F, s.d, 1, c->tk_Xp), td = w4_tile_args(c, W2, s.d, s.F, 0, c->tk_A);
+    tu.n_out = s.F;
+    td.n_out = s.d;
+    td.down = 1;
+    {
+      Phase ph(c, MOE_PHASE_GEMM_GATE_UP, st);
+      MOE_CUDA(launch_w4_tile(tu, c->num_sms, st, &c->launches));
+    }
+    Phase ph(c, MOE_PHASE_GEMM_DOWN, st);
+    MOE_CUDA(launch_w4_tile(td, c->num_sms, st, &c->launches));
+  } else {
+    {
+      Phase ph(c, MOE_PHASE_GEMM_GATE_UP, st);
+      MOE_CUDA(launch_w4_vec(up, c->num_sms, st, &c->launches));
+    }
     Phase ph(c, MOE_PHASE_GEMM_DOWN, st);
     MOE_CUDA(launch_w4_vec(down, c->num_sms, st, &c->launches));
   }

@@ -46,6 +46,13 @@ __device__ __forceinline__ void w4_fragment(uint32_t word, uint32_t (&a)[4]) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) a[r] = w4_pair(word >> (4 * r));
 }
+// 128 + q less 128 + z: a whole number, exact.  A fused multiply-add by one: the subtraction of bf16 pairs is not one instruction here.
+__host__ __device__ __forceinline__ uint32_t w4_bias(uint32_t z) { return 0xC300C300u | z * 0x00010001u; }   // - (128 + z), twice
+__device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(0x3F803F80u), "r"(b));
+  return r;
+}
 __device__ __forceinline__ float w4_offset(uint32_t z) { return __uint_as_float(0x43000000u | (z & 0xFFu) << 16); }   // 128 + z, z < 128
 
 // One expert product of the layer over experts with few rows (w4_vec.cu).
@@ -72,6 +79,24 @@ struct W4VecArgs {
   DevStatus* status;
 };
 constexpr int W4_SMALL_SLOTS = 128;   // up to here the blocks order the slots themselves
+
+// The same for a batch, on the tensor cores (w4_tile.cu): M-blocks of the padded row space, x gathered into it.
+struct W4TileArgs {
+  CUtensorMap tok[4];         // Xp or A, boxes of 16, 32, 48, 64 rows x 64 columns
+  const uint8_t *codes, *scales, *zeros;   // zeros NULL: 8
+  int K, KU, RT, group;
+  int ntn;                    // tiles of 256 weight rows
+  int down, n_out;
+  uint16_t* A;
+  int a_ld;
+  float* Y;
+  int y_ld;
+  const float* prow_w;
+  const int *mblk_expert, *mb_start, *counts, *meta;
+  DevStatus* status;
+  uint64_t budget_ns;
+};
+cudaError_t launch_w4_tile(const W4TileArgs& a, int num_sms, cudaStream_t st, int* launches);
 
 cudaError_t launch_w4_quantize(const uint16_t* W, int n, const W4Shape& s, uint32_t* codes, uint16_t* scales, uint8_t* zeros, cudaStream_t st);
 cudaError_t launch_w4_pack(const uint8_t* q, const uint16_t* qs, const uint8_t* qz, int n, const W4Shape& s, uint32_t* codes, uint16_t* scales,
