@@ -790,6 +790,7 @@ W4VecArgs w4_vec_args(const moe_ctx* c, const moe_w4_weights& w, int rows, int c
   a.K = cols;
   a.KU = ws.units();
   a.RT = ws.row_tiles();
+  a.RTS = ws.stored_tiles();
   a.group = w.group;
   a.A = c->at<uint16_t>(c->plan.A);
   a.a_ld = row_ld(s.F);
@@ -822,6 +823,7 @@ W4TileArgs w4_tile_args(const moe_ctx* c, const moe_w4_weights& w, int rows, int
   a.K = cols;
   a.KU = ws.units();
   a.RT = ws.row_tiles();
+  a.RTS = ws.stored_tiles();
   a.group = w.group;
   a.ntn = (a.RT + 7) / 8;
   a.A = c->at<uint16_t>(c->plan.A);
@@ -1148,8 +1150,8 @@ int moe_w4_sizes(int32_t rows, int32_t cols, int32_t group, uint32_t flags, size
   const int paired = (flags & MOE_W4_GATE_UP) ? 1 : 0;
   if (rows < 1 || cols < 8 || cols % 8 || !w4_group_ok(group) || (flags & ~MOE_W4_GATE_UP) || (paired && rows % 16)) return MOE_ERR_INVALID_ARG;
   const W4Shape s{rows, cols, group, paired};
-  if (code_bytes) *code_bytes = (size_t)s.row_tiles() * s.units() * W4_UNIT_BYTES;
-  if (group_elems) *group_elems = (size_t)s.row_tiles() * s.units() * s.unit_groups() * W4_TILE_ROWS;
+  if (code_bytes) *code_bytes = (size_t)s.stored_tiles() * s.units() * W4_UNIT_BYTES;
+  if (group_elems) *group_elems = (size_t)s.stored_tiles() * s.units() * s.unit_groups() * W4_TILE_ROWS;
   return MOE_OK;
 }
 

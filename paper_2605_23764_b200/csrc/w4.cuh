@@ -1,8 +1,9 @@
 // Expert weights in 4 bits with a scale -- and a zero point, where there are any -- for each group of 32, 64 or 128 reduction
 // elements: w = s (q - z), q and z in 0 .. 15 (z = 8 without zero points), s in bf16.
 //
-// Layout.  A matrix of R rows (output features) and K columns (reduction) is cut into units of 32 rows x 128 columns, 2 KB each,
-// row tile major; a unit into quarters of 16 rows x 64 columns (columns slow: first half's two, second half's two).  The 32 lanes of
+// Layout.  A matrix of R rows (output features) and K columns (reduction) is cut into units of 32 rows x 128 columns, 2 KB each;
+// four units below one another (128 rows, one copy for the tensor-core kernel) lie side by side, then the next 128 columns, then the
+// next 128 rows.  A unit is cut into quarters of 16 rows x 64 columns (columns slow: first half's two, second half's two).  The 32 lanes of
 // a warp own 16 bytes of a quarter side by side: word j of lane 4 g + c holds, of the quarter's columns 16 j .., what the lane is
 // given of a 16 x 16 bf16 operand of a matrix instruction -- the pairs of columns {2 c, 2 c + 1} and {2 c + 8, 2 c + 9} of rows g
 // and g + 8:
@@ -11,7 +12,7 @@
 // so that (word >> 4 r) & 0x000F000F is a pair in the place of two bf16 mantissas.  The same fragment is what a warp writes to
 // TMEM for 16 lanes x 8 columns (two bf16 each), so matrix-vector and tensor-core kernels read one layout.
 // Scales [unit][8][groups of a unit][4] bf16 and zero points [..] bytes: lanes 4 g + c need rows {g, g + 8, g + 16, g + 24} of the unit's
-// 1, 2 or 4 groups, side by side.  Units follow one another, so a warp's addresses only ever grow by a constant.
+// 1, 2 or 4 groups, side by side, in the same order of units.
 // Rows of W_gate_up: of 16 rows, 0 .. 7 are gate rows, 8 .. 15 the up rows of the same features (SwiGLU needs no exchange).
 // Rows behind the last are codes of value 0 with scale 0, columns behind K codes of value 0.
 #pragma once
@@ -24,7 +25,8 @@ constexpr int W4_TILE_ROWS = 32, W4_UNIT_K = 128, W4_UNIT_BYTES = 2048;
 
 struct W4Shape {
   int rows, cols, group, paired;
-  __host__ __device__ int row_tiles() const { return (rows + W4_TILE_ROWS - 1) / W4_TILE_ROWS; }
+  __host__ __device__ int row_tiles() const { return (rows + W4_TILE_ROWS - 1) / W4_TILE_ROWS; }   // that hold rows
+  __host__ __device__ int stored_tiles() const { return (row_tiles() + 3) & ~3; }
   __host__ __device__ int units() const { return (cols + W4_UNIT_K - 1) / W4_UNIT_K; }   // of a row tile
   __host__ __device__ int unit_groups() const { return W4_UNIT_K / group; }
   // row of the matrix that is row r of tile rt; -1: behind the last
@@ -46,6 +48,9 @@ __device__ __forceinline__ void w4_fragment(uint32_t word, uint32_t (&a)[4]) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) a[r] = w4_pair(word >> (4 * r));
 }
+// Unit ku of row tile rt of a matrix of KU units a row tile.
+__host__ __device__ __forceinline__ int64_t w4_unit(int rt, int ku, int KU) { return ((int64_t)(rt >> 2) * KU + ku) * 4 + (rt & 3); }
+
 // 128 + q less 128 + z: a whole number, exact.  A fused multiply-add by one: the subtraction of bf16 pairs is not one instruction here.
 __host__ __device__ __forceinline__ uint32_t w4_bias(uint32_t z) { return 0xC300C300u | z * 0x00010001u; }   // - (128 + z), twice
 __device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {
@@ -60,7 +65,7 @@ struct W4VecArgs {
   const uint4* codes;
   const uint32_t* scales;     // bf16 pairs
   const uint16_t* zeros;      // byte pairs; NULL: 8
-  int K, KU, RT, group;       // reduction, units of a row tile, row tiles of an expert
+  int K, KU, RT, RTS, group;  // reduction, units of a row tile, row tiles of an expert that hold rows, that are stored
   int down;                   // 0: x -> A = w silu(gate) up; 1: A -> Y
   int n_out;                  // features of the result
   const uint16_t* in;         // x [T][in_ld] or A [rows][in_ld]
@@ -84,7 +89,7 @@ constexpr int W4_SMALL_SLOTS = 128;   // up to here the blocks order the slots t
 struct W4TileArgs {
   CUtensorMap tok[4];         // Xp or A, boxes of 16, 32, 48, 64 rows x 64 columns
   const uint8_t *codes, *scales, *zeros;   // zeros NULL: 8
-  int K, KU, RT, group;
+  int K, KU, RT, RTS, group;
   int ntn;                    // tiles of 256 weight rows
   int down, n_out;
   uint16_t* A;

@@ -12,14 +12,14 @@ namespace {
 constexpr int CODE_WARPS = 8, CODE_LD = 17;   // words of a staged row: 16 of codes, one so that rows fall into different banks
 
 struct CodeTask { int64_t unit; int m, rt, chunk, t; };   // unit of all, matrix, row tile, unit of the tile, upper or lower 16 rows
-__device__ __forceinline__ CodeTask code_task(int64_t i, int RT, int chunks) {
+__device__ __forceinline__ CodeTask code_task(int64_t i, int RTS, int chunks) {
   CodeTask t;
   t.unit = i >> 1;
   t.t = (int)(i & 1);
-  const int64_t tile = t.unit / chunks;
-  t.chunk = (int)(t.unit - tile * chunks);
-  t.m = (int)(tile / RT);
-  t.rt = (int)(tile - (int64_t)t.m * RT);
+  const int64_t four = t.unit >> 2, tiles = four / chunks;   // four units, four row tiles
+  t.chunk = (int)(four - tiles * chunks);
+  t.m = (int)(tiles / (RTS >> 2));
+  t.rt = (int)(tiles - (int64_t)t.m * (RTS >> 2)) * 4 + (int)(t.unit & 3);
   return t;
 }
 
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(32 * CODE_WARPS) w4_encode_kernel(const void* 
   __shared__ uint32_t stage[CODE_WARPS][16 * CODE_LD];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = lane >> 4, m = lane & 15;
   uint32_t* const st = stage[warp];
-  const int RT = s.row_tiles(), ng = s.unit_groups(), ng_src = (s.cols + s.group - 1) / s.group;
+  const int RT = s.stored_tiles(), ng = s.unit_groups(), ng_src = (s.cols + s.group - 1) / s.group;
   const int gl = s.group >> 3;   // lanes of a group
   const bool asym = zeros != nullptr;
   pdl_wait();
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(32 * CODE_WARPS) w4_decode_kernel(const uint4*
   __shared__ uint32_t stage[CODE_WARPS][16 * CODE_LD];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = lane >> 4, m = lane & 15;
   uint32_t* const st = stage[warp];
-  const int RT = s.row_tiles(), ng = s.unit_groups();
+  const int RT = s.stored_tiles(), ng = s.unit_groups();
   pdl_wait();
   pdl_trigger();
   for (int64_t i = (int64_t)blockIdx.x * CODE_WARPS + warp; i < tasks; i += (int64_t)gridDim.x * CODE_WARPS) {
@@ -183,20 +183,20 @@ static dim3 code_grid(int64_t tasks) {
 
 cudaError_t launch_w4_quantize(const uint16_t* W, int n, const W4Shape& s, uint32_t* codes, uint16_t* scales, uint8_t* zeros, cudaStream_t st) {
   const int chunks = s.units();
-  const int64_t tasks = (int64_t)n * s.row_tiles() * chunks * 2;
+  const int64_t tasks = (int64_t)n * s.stored_tiles() * chunks * 2;
   return launch_dependent(w4_encode_kernel<true>, code_grid(tasks), dim3(32 * CODE_WARPS), 0, st, W, nullptr, nullptr, tasks, chunks, s,
                           reinterpret_cast<uint4*>(codes), scales, zeros);
 }
 cudaError_t launch_w4_pack(const uint8_t* q, const uint16_t* qs, const uint8_t* qz, int n, const W4Shape& s, uint32_t* codes, uint16_t* scales,
                            uint8_t* zeros, cudaStream_t st) {
   const int chunks = s.units();
-  const int64_t tasks = (int64_t)n * s.row_tiles() * chunks * 2;
+  const int64_t tasks = (int64_t)n * s.stored_tiles() * chunks * 2;
   return launch_dependent(w4_encode_kernel<false>, code_grid(tasks), dim3(32 * CODE_WARPS), 0, st, q, qs, qz, tasks, chunks, s,
                           reinterpret_cast<uint4*>(codes), scales, zeros);
 }
 cudaError_t launch_w4_dequantize(const uint32_t* codes, const uint16_t* scales, const uint8_t* zeros, int n, const W4Shape& s, uint16_t* W, cudaStream_t st) {
   const int chunks = s.units();
-  const int64_t tasks = (int64_t)n * s.row_tiles() * chunks * 2;
+  const int64_t tasks = (int64_t)n * s.stored_tiles() * chunks * 2;
   return launch_dependent(w4_decode_kernel, code_grid(tasks), dim3(32 * CODE_WARPS), 0, st, reinterpret_cast<const uint4*>(codes), scales, zeros,
                           tasks, chunks, s, W);
 }

@@ -9,8 +9,9 @@
 // reduction; the epilogue warps scale it in fp32 and add it up in registers while the next group is multiplied.  So there is no
 // rounding that the formula does not have but that of the activations to bf16 between the two products.
 //
-// Roles per CTA: warp 0 loads codes, scales and zero points, warp 1 issues the products (even CTA), warp 2 loads rows of x, warps 4-7
-// widen, warps 8-15 scale and add up.
+// Roles per CTA: warp 0 loads codes, scales and zero points (a copy of each for 128 rows x 128 columns; with one for every 32 rows
+// issuing them took 1000 clocks, twice as long as the products), warp 26 the rows of x, warp 1 issues the products (even CTA), warps 2-9 widen (four for each half of a unit's 128 columns),
+// warps 10-25 scale and add up (four for each quarter of the columns).
 #include "gemm_tile.cuh"
 #include "launch_pairs.cuh"
 #include "topk.cuh"
@@ -20,12 +21,13 @@ namespace moe {
 
 namespace {
 
-constexpr int WT_THREADS = 512;
+constexpr int WT_WIDEN_WARP = 2, WT_EPI_WARP = 10, WT_EPI_SIDES = 4, WT_TOK_WARP = WT_EPI_WARP + 4 * WT_EPI_SIDES, WT_THREADS = 32 * (WT_TOK_WARP + 1);
 constexpr int WT_CODES = 4 * W4_UNIT_BYTES;   // 128 rows x 128 columns
-constexpr int WT_CODE_STAGES = 4, WT_SCALE_STAGES = 8, WT_TOK_STAGES = 6, WT_A_STAGES = 2, WT_D_BUFS = 3;
+constexpr int WT_CODE_STAGES = 6, WT_SCALE_STAGES = 8, WT_TOK_STAGES = 6, WT_A_STAGES = 4, WT_D_BUFS = 3;
 constexpr int WT_TOK_BYTES = 64 * 256;        // half of 128 rows x 128 columns bf16
-constexpr int WT_A_COLS = 64;                 // TMEM columns of 128 bf16
+constexpr int WT_A_COLS = 32;                 // TMEM columns of 64 bf16
 constexpr int WT_A_AT = WT_D_BUFS * BLOCK_M;  // behind the accumulators
+static_assert(WT_A_STAGES % 2 == 0, "a half keeps to its slots");
 static_assert(WT_A_AT + WT_A_STAGES * WT_A_COLS <= TMEM_COLS, "TMEM");
 
 struct __align__(8) WtBarriers {
@@ -48,10 +50,12 @@ __host__ __device__ constexpr size_t wt_smem(int ng, bool asym) {
 }
 static_assert(wt_smem(4, true) <= 227 * 1024, "shared memory");
 
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes),
-               "r"(smem_u32(bar))
-               : "memory");
+__device__ __forceinline__ void bulk_load_elect(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile(
+      "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n"
+      " @e cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n}" ::"r"(smem_u32(dst)),
+      "l"(src), "r"(bytes), "r"(smem_u32(bar))
+      : "memory");
 }
 // 16 lanes x 32 columns of TMEM from operand fragments: registers 2 i, 2 i + 1 are rows lane / 4 and lane / 4 + 8 of column 4 i + lane % 4
 __device__ __forceinline__ void tmem_st_frag8(uint32_t taddr, const uint32_t (&r)[16]) {
@@ -69,23 +73,59 @@ __device__ __forceinline__ void tc_mma_ts_pair(uint32_t d_tmem, uint32_t a_tmem,
       " @e tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], db, %4, p;\n}" ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// mbar_wait_warp with acquire at cluster scope: what the partner CTA wrote before its arrival is visible
-__device__ __forceinline__ bool mbar_wait_cluster_warp(uint64_t* bar, uint32_t parity, const WaitCtl& wc, int site, int tile) {
-  const bool ok = mbar_wait_cluster(bar, parity, wc, site, tile);
-  return __all_sync(0xffffffffu, ok);
+// 32 lanes x 8 or 16 columns: thread i has lane i.  The values are there behind the wait, which they depend on.
+__device__ __forceinline__ void tmem_ld16_wait(uint32_t taddr, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
+        "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(taddr)
+      : "memory");
 }
+__device__ __forceinline__ void tmem_ld8x2_wait(uint32_t taddr, uint32_t taddr2, float (&v)[16]) {   // eight columns at each
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%16];\n"
+      " tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8,%9,%10,%11,%12,%13,%14,%15}, [%17];\n tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
+        "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(taddr), "r"(taddr2)
+      : "memory");
+}
+// Groups that share an accumulator buffer of 128 columns: the epilogue's waits and signals, some 500 clocks, are per buffer.
+__host__ __device__ constexpr int wt_groups(int ntok) { return ntok == 32 ? 4 : ntok == 64 ? 2 : 1; }
 
 struct WtItem { int e, nb, row0, ntok; };   // expert, 256-row weight tile, first row, columns (a multiple of 32)
-__device__ __forceinline__ WtItem wt_item(const W4TileArgs& a, int t) {
-  WtItem it;
-  const int mb = t / a.ntn;
-  it.nb = t - mb * a.ntn;
-  it.e = a.mblk_expert[mb];
-  it.row0 = mb * BLOCK_M;
-  const int rows = a.counts[it.e] - (mb - a.mb_start[it.e]) * BLOCK_M;
-  it.ntok = min(BLOCK_M, (rows + 31) & ~31);
-  return it;
-}
+// The items of a pair, one after another.  What an item is hangs on two loads in a row: the first of them is made two items ahead, the
+// second one item ahead, and nothing waits for either before it is used.
+struct WtItems {
+  const W4TileArgs& a;
+  int t, step, total;
+  int e1 = 0, e2 = 0, cnt1 = 0, mb1 = 0;   // of item t, and the expert of item t + step
+  __device__ __forceinline__ WtItems(const W4TileArgs& args, int first, int step_, int total_) : a(args), t(first), step(step_), total(total_) {
+    if (t < total) {
+      e1 = a.mblk_expert[t / a.ntn];
+      cnt1 = a.counts[e1];
+      mb1 = a.mb_start[e1];
+    }
+    if (t + step < total) e2 = a.mblk_expert[(t + step) / a.ntn];
+  }
+  __device__ __forceinline__ bool next(WtItem& it) {
+    if (t >= total) return false;
+    const int mb = t / a.ntn;
+    it.nb = t - mb * a.ntn;
+    it.e = e1;
+    it.row0 = mb * BLOCK_M;
+    it.ntok = min(BLOCK_M, (cnt1 - (mb - mb1) * BLOCK_M + 31) & ~31);
+    t += step;
+    if (t < total) {
+      e1 = e2;
+      cnt1 = a.counts[e1];
+      mb1 = a.mb_start[e1];
+      if (t + step < total) e2 = a.mblk_expert[(t + step) / a.ntn];
+    }
+    return true;
+  }
+};
 
 // Position in a ring of N slots and the parity to wait for next in it.
 template <int N>
@@ -93,8 +133,115 @@ struct RingAt {
   int s = 0;
   uint32_t par;
   __device__ __forceinline__ explicit RingAt(uint32_t first) : par(first) {}
-  __device__ __forceinline__ void next() {
-    if (++s == N) { s = 0; par ^= 1; }
+  __device__ __forceinline__ void next(int step = 1) {
+    s += step;
+    if (s >= N) { s -= N; par ^= 1; }
+  }
+};
+
+struct WtEpilogue {   // of a warp: 32 weight rows (a lane each) x a quarter of the columns
+  const W4TileArgs& a;
+  WtBarriers* bars;
+  const uint8_t* scale_s;
+  WaitCtl wc;
+  uint32_t tmem;     // the warp's lanes
+  int rank, quad, side, lane;
+  RingAt<WT_SCALE_STAGES> sr{0};
+  RingAt<WT_D_BUFS> dr{0};
+
+  template <int NTOK, int NG>
+  __device__ __forceinline__ bool item(const WtItem& it, int t) {
+    constexpr int NC = NTOK / 4, GPB = wt_groups(NTOK), ROUNDS = NC * GPB > 16 ? 2 : 1;   // sixteen values a round
+    const int groups = a.KU * NG;
+    float2x acc[NC / 2];   // two columns side by side
+#pragma unroll
+    for (int i = 0; i < NC / 2; ++i) acc[i] = pack2(0.f, 0.f);
+    // gate and up: the routing weight of column `lane`
+    float w_col = 0.f;
+    if (!a.down && lane < NC) w_col = __ldg(a.prow_w + it.row0 + side * NC + lane);
+    const uint32_t at = quad * 64 * NG + (lane & 7) * NG * 8 + (lane >> 3) * 2;   // of the row's scales in a stage
+    int in_unit = 0;   // group of the unit
+    auto scale = [&](int g, float& s) -> bool {   // of the g-th group, in turn
+      s = 0.f;
+      if (g >= groups) return true;
+      if (in_unit == 0 && !mbar_wait_warp(&bars->scale_full[sr.s], sr.par, wc, SITE_FULL, t)) return false;
+      s = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(scale_s + sr.s * (256 * NG) + at + in_unit * 8) << 16);
+      if (++in_unit == NG) {
+        in_unit = 0;
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(&bars->scale_empty[sr.s]);
+        sr.next();
+      }
+      return true;
+    };
+#pragma unroll 1
+    for (int g0 = 0; g0 < groups; g0 += GPB) {
+      float sc[GPB];
+#pragma unroll
+      for (int i = 0; i < GPB; ++i)
+        if (!scale(g0 + i, sc[i])) return false;
+      if (!mbar_wait_warp(&bars->d_full[dr.s], dr.par, wc, SITE_TMEM_FULL, t)) return false;
+      tc_fence_after_sync();
+      const uint32_t d = tmem + dr.s * BLOCK_M + side * NC;
+#pragma unroll
+      for (int r = 0; r < ROUNDS; ++r) {
+        float v[16];
+        if constexpr (NTOK == 128) tmem_ld16_wait(d + 16 * r, v);
+        else if constexpr (NTOK == 96) { if (r == 0) tmem_ld16_wait(d, v); else tmem_ld8x2_wait(d + 16, d + 16, v); }
+        else if constexpr (NTOK == 64) tmem_ld16_wait(d + 64 * r, v);
+        else tmem_ld8x2_wait(d + 64 * r, d + 64 * r + 32, v);
+        if (r == ROUNDS - 1) {
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_leader(&bars->d_empty[dr.s]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int to = NTOK == 128 ? 8 * r + i : NTOK == 96 ? 8 * r + i : NTOK == 64 ? i : i & 3;
+          const int grp = NTOK >= 96 ? 0 : NTOK == 64 ? r : 2 * r + (i >> 2);
+          if (to >= NC / 2) continue;
+          // (a group behind the last was not written: nothing of it is added)
+          const float2x next = fma2(pack2(sc[grp], sc[grp]), pack2(v[2 * i], v[2 * i + 1]), acc[to]);
+          if (GPB == 1 || g0 + grp < groups) acc[to] = next;
+        }
+      }
+      dr.next();
+    }
+    // ---- the result
+    const int rt = it.nb * 8 + rank * 4 + quad;   // the warp's 32 rows
+    if (rt >= a.RT) return true;
+    const int rows = it.row0 + side * NC;
+    if (a.down) {
+      const int feature = rt * 32 + lane;
+      if (feature < a.n_out) {
+        float* y = a.Y + (size_t)rows * a.y_ld + feature;
+#pragma unroll
+        for (int i = 0; i < NC / 2; ++i) {
+          float lo, hi;
+          unpack2(acc[i], lo, hi);
+          y[0] = lo;
+          y[a.y_ld] = hi;
+          y += 2 * (size_t)a.y_ld;
+        }
+      }
+    } else {
+      // lanes 0-7 and 16-23 have gate rows, the others the up rows of the same features: of two columns each takes one
+      const int is_up = (lane >> 3) & 1;
+      const int feature = rt * 16 + ((lane >> 4) << 3) + (lane & 7);
+      uint16_t* out = a.A + (size_t)(rows + is_up) * a.a_ld + feature;
+#pragma unroll
+      for (int i = 0; i < NC / 2; ++i) {
+        float lo, hi;
+        unpack2(acc[i], lo, hi);
+        const float other = __shfl_xor_sync(0xffffffffu, is_up ? lo : hi, 8);
+        const float gate = is_up ? other : lo, up = is_up ? hi : other;
+        const float w = __shfl_sync(0xffffffffu, w_col, 2 * i + is_up);
+        const float act = w * (__fdividef(gate, 1.0f + __expf(-gate)) * up);
+        if (feature < a.n_out) *out = (uint16_t)(pack_bf16x2(act, 0.f) & 0xFFFFu);
+        out += 2 * (size_t)a.a_ld;
+      }
+    }
+    return true;
   }
 };
 
@@ -116,11 +263,11 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
   const WaitCtl wc{a.status, a.budget_ns};
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < WT_CODE_STAGES; ++i) { mbar_init(&bars->code_full[i], 1); mbar_init(&bars->code_empty[i], 4); }
-    for (int i = 0; i < WT_SCALE_STAGES; ++i) { mbar_init(&bars->scale_full[i], 1); mbar_init(&bars->scale_empty[i], 8); }
+    for (int i = 0; i < WT_CODE_STAGES; ++i) { mbar_init(&bars->code_full[i], 1); mbar_init(&bars->code_empty[i], 8); }
+    for (int i = 0; i < WT_SCALE_STAGES; ++i) { mbar_init(&bars->scale_full[i], 1); mbar_init(&bars->scale_empty[i], 4 * WT_EPI_SIDES); }
     for (int i = 0; i < WT_TOK_STAGES; ++i) { mbar_init(&bars->tok_full[i], 1); mbar_init(&bars->tok_empty[i], 1); }
     for (int i = 0; i < WT_A_STAGES; ++i) { mbar_init(&bars->a_full[i], 8); mbar_init(&bars->a_empty[i], 1); }
-    for (int i = 0; i < WT_D_BUFS; ++i) { mbar_init(&bars->d_full[i], 1); mbar_init(&bars->d_empty[i], 16); }
+    for (int i = 0; i < WT_D_BUFS; ++i) { mbar_init(&bars->d_full[i], 1); mbar_init(&bars->d_empty[i], 8 * WT_EPI_SIDES); }
     mbar_init(&bars->drain, 1);
     mbar_fence_init();
     fence_proxy_async();
@@ -139,41 +286,37 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
   pdl_wait();
 
   const int total = a.meta[0] * a.ntn, KU = a.KU;
-  WtItem cur{}, next{};
-  if (pair < total) cur = wt_item(a, pair);
+  WtItem cur{};
   if (warp == 0) {
-    // ---- codes, scales, zero points: lane i < 4 has the i-th 32 rows.  Row tiles behind the last are read again and not stored.
+    // ---- codes, scales, zero points of this CTA's 128 rows.  Where it has none, the last ones are read again and not stored.
     RingAt<WT_CODE_STAGES> cr(1);
     RingAt<WT_SCALE_STAGES> sr(1);
     bool ok = true;
-    for (int t = pair; t < total && ok; t += npairs, cur = next) {
-      if (t + npairs < total) next = wt_item(a, t + npairs);
-      const int rt = min(cur.nb * 8 + rank * 4 + min(lane, 3), a.RT - 1);
-      size_t unit = ((size_t)cur.e * a.RT + rt) * KU;
-      for (int ku = 0; ku < KU; ++ku, ++unit) {
-        if (!mbar_wait_warp(&bars->code_empty[cr.s], cr.par, wc, SITE_EMPTY, t, 20) ||
-            !mbar_wait_warp(&bars->scale_empty[sr.s], sr.par, wc, SITE_EMPTY, t, 20)) { ok = false; break; }
-        uint8_t *const cs = code_s + cr.s * CODE_STAGE, *const ss = scale_s + sr.s * SCALE_STAGE;
-        if (lane == 0) {
-          mbar_expect_tx(&bars->code_full[cr.s], CODE_STAGE);
-          mbar_expect_tx(&bars->scale_full[sr.s], SCALE_STAGE);
-        }
-        __syncwarp();
-        if (lane < 4) {
-          bulk_load(cs + lane * W4_UNIT_BYTES, a.codes + unit * W4_UNIT_BYTES, W4_UNIT_BYTES, &bars->code_full[cr.s]);
-          if (ASYM) bulk_load(cs + WT_CODES + lane * 32 * NG, a.zeros + unit * (32 * NG), 32 * NG, &bars->code_full[cr.s]);
-          bulk_load(ss + lane * 64 * NG, a.scales + unit * (64 * NG), 64 * NG, &bars->scale_full[sr.s]);
-        }
+    WtItems items(a, pair, npairs, total);
+    while (ok && items.next(cur)) {
+      const int t = items.t;
+      const int four = min(uniform(cur.nb) * 2 + rank, (a.RTS >> 2) - 1);
+      size_t at = ((size_t)uniform(cur.e) * (a.RTS >> 2) + four) * KU;
+      for (int ku = 0; ku < KU; ++ku, ++at) {
+        if (!mbar_wait_warp(&bars->code_empty[cr.s], cr.par, wc, SITE_EMPTY, t, 20)) { ok = false; break; }
+        uint8_t* const cs = code_s + cr.s * CODE_STAGE;
+        mbar_expect_tx_elect(&bars->code_full[cr.s], CODE_STAGE);
+        bulk_load_elect(cs, a.codes + at * WT_CODES, WT_CODES, &bars->code_full[cr.s]);
+        if (ASYM) bulk_load_elect(cs + WT_CODES, a.zeros + at * (128 * NG), 128 * NG, &bars->code_full[cr.s]);
+        if (!mbar_wait_warp(&bars->scale_empty[sr.s], sr.par, wc, SITE_EMPTY, t, 20)) { ok = false; break; }
+        mbar_expect_tx_elect(&bars->scale_full[sr.s], SCALE_STAGE);
+        bulk_load_elect(scale_s + sr.s * SCALE_STAGE, a.scales + at * SCALE_STAGE, SCALE_STAGE, &bars->scale_full[sr.s]);
         cr.next();
         sr.next();
       }
     }
-  } else if (warp == 2) {
+  } else if (warp == WT_TOK_WARP) {
     // ---- rows of x: this CTA's half, two boxes of 64 columns
     RingAt<WT_TOK_STAGES> tr(1);
     bool ok = true;
-    for (int t = pair; t < total && ok; t += npairs, cur = next) {
-      if (t + npairs < total) next = wt_item(a, t + npairs);
+    WtItems items(a, pair, npairs, total);
+    while (ok && items.next(cur)) {
+      const int t = items.t;
       const int ntok = uniform(cur.ntok), half = ntok >> 1, row = uniform(cur.row0) + rank * half;
       const CUtensorMap* tm = &a.tok[(half >> 4) - 1];
       for (int ku = 0; ku < KU; ++ku) {
@@ -192,31 +335,39 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
     RingAt<WT_D_BUFS> dr(1);
     bool ok = true;
     constexpr int STEPS = 8 / NG;   // of 16 columns in a group
-    for (int t = pair; t < total && ok; t += npairs, cur = next) {
-      if (t + npairs < total) next = wt_item(a, t + npairs);
+    WtItems items(a, pair, npairs, total);
+    while (ok && items.next(cur)) {
+      const int t = items.t;
       const int ntok = uniform(cur.ntok);
       const uint32_t idesc = make_idesc_bf16(2 * BLOCK_M, ntok, 0, 0), box = (uint32_t)(ntok >> 1) * 128 >> 4;
+      const int gpb = wt_groups(ntok), groups = KU * NG;
+      int grp = 0, in_buf = 0;   // group of the item, of the accumulator buffer
       for (int ku = 0; ku < KU && ok; ++ku) {
-        if (!mbar_wait_warp(&bars->tok_full[tr.s], tr.par, wc, SITE_FULL, t) ||
-            !mbar_wait_cluster_warp(&bars->a_full[ar.s], ar.par, wc, SITE_FULL, t)) { ok = false; break; }
+        if (!mbar_wait_warp(&bars->tok_full[tr.s], tr.par, wc, SITE_FULL, t)) { ok = false; break; }
         const uint32_t b_lo = smem_desc_lo(smem_u32(tok_s + tr.s * WT_TOK_BYTES), 16);
-        const uint32_t a_t = tmem_base + WT_A_AT + ar.s * WT_A_COLS;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          if (!mbar_wait_warp(&bars->d_empty[dr.s], dr.par, wc, SITE_TMEM_EMPTY, t)) { ok = false; break; }
-          tc_fence_after_sync();
-          const uint32_t d_t = tmem_base + dr.s * BLOCK_M;
+        for (int h = 0; h < 2; ++h) {   // halves of 64 columns: a stage of the A operand, a box of the B operand
+          if (!mbar_wait_warp(&bars->a_full[ar.s], ar.par, wc, SITE_FULL, t)) { ok = false; break; }
+          const uint32_t a_t = tmem_base + WT_A_AT + ar.s * WT_A_COLS;
 #pragma unroll
-          for (int j = 0; j < STEPS; ++j) {
-            const int k16 = g * STEPS + j;
-            tc_mma_ts_pair(d_t, a_t + 8 * k16, b_lo + (k16 >> 2) * box + 2 * (k16 & 3), smem_desc_hi(1024), idesc, j != 0);
+          for (int j = 0; j < 4; ++j) {
+            const int k16 = 4 * h + j;
+            if (k16 % STEPS == 0 && in_buf == 0 && !mbar_wait_warp(&bars->d_empty[dr.s], dr.par, wc, SITE_TMEM_EMPTY, t)) { ok = false; break; }
+            if (j == 0 || k16 % STEPS == 0) tc_fence_after_sync();
+            tc_mma_ts_pair(tmem_base + dr.s * BLOCK_M + in_buf * ntok, a_t + 8 * j, b_lo + h * box + 2 * j, smem_desc_hi(1024), idesc, k16 % STEPS != 0);
+            if (k16 % STEPS == STEPS - 1) {
+              ++grp;
+              if (++in_buf == gpb || grp == groups) {
+                tc_commit_pair(&bars->d_full[dr.s]);
+                dr.next();
+                in_buf = 0;
+              }
+            }
           }
-          tc_commit_pair(&bars->d_full[dr.s]);
-          dr.next();
+          tc_commit_pair(&bars->a_empty[ar.s]);
+          ar.next();
         }
-        tc_commit_pair(&bars->a_empty[ar.s]);
         tc_commit_pair(&bars->tok_empty[tr.s]);
-        ar.next();
         tr.next();
       }
     }
@@ -225,133 +376,64 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
       const WaitCtl shortwc{a.status, 20ull * 1000 * 1000};
       mbar_wait_warp(&bars->drain, 0, shortwc, SITE_DRAIN, 0);
     }
-  } else if (warp >= 4 && warp < 8) {
-    // ---- codes to whole numbers in TMEM: a warp has the 32 lanes of its quarter
+  } else if (warp >= WT_WIDEN_WARP && warp < WT_EPI_WARP) {
+    // ---- codes to whole numbers in TMEM: a warp has the 32 lanes of its quarter, half of the unit's columns
+    const int quad = warp & 3, h = (warp - WT_WIDEN_WARP) >> 2, g = lane >> 2;
     RingAt<WT_CODE_STAGES> cr(0);
     RingAt<WT_A_STAGES> ar(1);
-    const int quad = warp & 3, g = lane >> 2;
+    ar.s = h;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    bool ok = true;
-    for (int t = pair; t < total && ok; t += npairs) {
-      for (int ku = 0; ku < KU; ++ku) {
-        if (!mbar_wait_warp(&bars->code_full[cr.s], cr.par, wc, SITE_FULL, t)) { ok = false; break; }
-        const uint8_t* const cs = code_s + cr.s * CODE_STAGE + quad * W4_UNIT_BYTES + lane * 16;
-        uint4 q[4];
+    const int units = (pair < total ? (total - pair + npairs - 1) / npairs : 0) * KU;
+    for (int u = 0; u < units; ++u) {
+      if (!mbar_wait_warp(&bars->code_full[cr.s], cr.par, wc, SITE_FULL, u)) break;
+      const uint8_t* const cs = code_s + cr.s * CODE_STAGE + quad * W4_UNIT_BYTES + h * 1024 + lane * 16;
+      const uint4 q[2] = {*reinterpret_cast<const uint4*>(cs), *reinterpret_cast<const uint4*>(cs + 512)};
+      constexpr int HG = NG == 4 ? 2 : 1;   // groups of the half
+      uint32_t zp[HG];
+      if constexpr (ASYM) {
+        const uint32_t* z = reinterpret_cast<const uint32_t*>(code_s + cr.s * CODE_STAGE + WT_CODES + quad * 32 * NG + g * 4 * NG) + (NG == 1 ? 0 : h * HG);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const uint4*>(cs + 512 * i);
-        uint32_t zp[ASYM ? NG : 1];
-        if constexpr (ASYM) {
-          const uint32_t* z = reinterpret_cast<const uint32_t*>(code_s + cr.s * CODE_STAGE + WT_CODES + quad * 32 * NG + g * 4 * NG);
-#pragma unroll
-          for (int i = 0; i < NG; ++i) zp[i] = z[i];
-        }
-        if (!mbar_wait_warp(&bars->a_empty[ar.s], ar.par, wc, SITE_TMEM_EMPTY, t)) { ok = false; break; }
-        tc_fence_after_sync();
-        const uint32_t a_t = tmem_base + lanes + WT_A_AT + ar.s * WT_A_COLS;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {   // halves of 64 columns, sixteen rows
-            const uint4 w = q[2 * h + s];
-            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-            uint32_t v[16];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int grp = (4 * h + j) * NG / 8;
-              const uint32_t z = ASYM ? zp[ASYM ? grp : 0] >> (16 * s) : 0;
-              uint32_t f[4];
-              w4_fragment(words[j], f);
-              const uint32_t lo = ASYM ? w4_bias(z & 0xFFu) : w4_bias(8), hi = ASYM ? w4_bias((z >> 8) & 0xFFu) : w4_bias(8);
-#pragma unroll
-              for (int r = 0; r < 4; ++r) v[4 * j + r] = add_bf16x2(f[r], r & 1 ? hi : lo);
-            }
-            tmem_st_frag8(a_t + ((uint32_t)(16 * s) << 16) + 32 * h, v);
-          }
-        tmem_st_wait();
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive_cluster_addr(smem_u32(&bars->a_full[ar.s]) & PEER_BIT_MASK);
-          mbar_arrive_cta(&bars->code_empty[cr.s]);
-        }
-        cr.next();
-        ar.next();
+        for (int i = 0; i < HG; ++i) zp[i] = z[i];
       }
+      if (!mbar_wait_warp(&bars->a_empty[ar.s], ar.par, wc, SITE_TMEM_EMPTY, u)) break;
+      tc_fence_after_sync();
+      const uint32_t a_t = tmem_base + lanes + WT_A_AT + ar.s * WT_A_COLS;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {   // sixteen rows
+        const uint32_t words[4] = {q[s].x, q[s].y, q[s].z, q[s].w};
+        uint32_t v[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t z = ASYM ? zp[j * HG / 4] >> (16 * s) : 0;
+          const uint32_t lo = ASYM ? w4_bias(z & 0xFFu) : w4_bias(8), hi = ASYM ? w4_bias((z >> 8) & 0xFFu) : w4_bias(8);
+          uint32_t f[4];
+          w4_fragment(words[j], f);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[4 * j + r] = add_bf16x2(f[r], r & 1 ? hi : lo);
+        }
+        tmem_st_frag8(a_t + ((uint32_t)(16 * s) << 16), v);
+      }
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive_leader(&bars->a_full[ar.s]);   // TMEM is ordered by the tcgen05 fences: a release at cluster scope took 1800 clocks
+        mbar_arrive_cta(&bars->code_empty[cr.s]);
+      }
+      cr.next();
+      ar.next(2);
     }
-  } else if (warp >= 8) {
-    // ---- groups scaled and added up: a thread has a weight row, half of the columns
-    RingAt<WT_SCALE_STAGES> sr(0);
-    RingAt<WT_D_BUFS> dr(0);
-    const int quad = warp & 3, side = (warp - 8) >> 2;
-    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+  } else if (warp >= WT_EPI_WARP) {
+    // ---- groups scaled and added up
+    WtEpilogue ep{a, bars, scale_s, wc, tmem_base + ((uint32_t)((warp & 3) * 32) << 16), rank, warp & 3, (warp - WT_EPI_WARP) >> 2, lane};
+    WtItems items(a, pair, npairs, total);
     bool ok = true;
-    for (int t = pair; t < total && ok; t += npairs, cur = next) {
-      if (t + npairs < total) next = wt_item(a, t + npairs);
-      const int cols = uniform(cur.ntok) >> 1, c0 = side * cols;   // 16, 32, 48 or 64 columns
-      float acc[64];
-#pragma unroll
-      for (int i = 0; i < 64; ++i) acc[i] = 0.f;
-      for (int ku = 0; ku < KU && ok; ++ku) {
-        if (!mbar_wait_warp(&bars->scale_full[sr.s], sr.par, wc, SITE_FULL, t)) { ok = false; break; }
-        float sc[NG];
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-          sc[g] = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(scale_s + sr.s * SCALE_STAGE + quad * 64 * NG + ((lane & 7) * NG + g) * 8 +
-                                                                                (lane >> 3) * 2)
-                                  << 16);
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cta(&bars->scale_empty[sr.s]);
-        sr.next();
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          if (!mbar_wait_warp(&bars->d_full[dr.s], dr.par, wc, SITE_TMEM_FULL, t)) { ok = false; break; }
-          tc_fence_after_sync();
-          const uint32_t d_t = tmem_base + lanes + dr.s * BLOCK_M + c0;
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (16 * c < cols) {
-              float v[16];
-              tmem_ld16(d_t + 16 * c, v);
-              tmem_ld_wait();
-#pragma unroll
-              for (int i = 0; i < 16; ++i) acc[16 * c + i] = fmaf(sc[g], v[i], acc[16 * c + i]);
-            }
-          tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_leader(&bars->d_empty[dr.s]);
-          dr.next();
-        }
-      }
-      if (!ok) break;
-      const int rt = cur.nb * 8 + rank * 4 + quad;   // the warp's 32 rows
-      const int rows = cur.row0 + c0;
-      if (rt < a.RT) {
-        if (a.down) {
-          const int feature = rt * 32 + lane;
-          if (feature < a.n_out) {
-            float* y = a.Y + (size_t)rows * a.y_ld + feature;
-#pragma unroll
-            for (int i = 0; i < 64; ++i)
-              if (i < cols) { *y = acc[i]; y += a.y_ld; }
-          }
-        } else {
-          // lanes 0-7 and 16-23 have gate rows, the others the up rows of the same features: of two columns each takes one
-          const bool is_up = lane & 8;
-          const int feature = rt * 16 + ((lane >> 4) << 3) + (lane & 7);
-          const int row = rows + (is_up ? 1 : 0);
-          uint16_t* out = a.A + (size_t)row * a.a_ld + feature;
-          const float* w = a.prow_w + row;
-#pragma unroll
-          for (int i = 0; i < 64; i += 2)
-            if (i < cols) {
-              const float other = __shfl_xor_sync(0xffffffffu, is_up ? acc[i] : acc[i + 1], 8);
-              const float gate = is_up ? other : acc[i], up = is_up ? acc[i + 1] : other;
-              const float act = __ldg(w + i) * (gate / (1.0f + __expf(-gate)) * up);
-              if (feature < a.n_out) *out = (uint16_t)(pack_bf16x2(act, 0.f) & 0xFFFFu);
-              out += 2 * (size_t)a.a_ld;
-            }
-        }
-      }
+    while (ok && items.next(cur)) {
+      const int ntok = uniform(cur.ntok);
+      if (ntok == 128) ok = ep.item<128, NG>(cur, items.t);
+      else if (ntok == 96) ok = ep.item<96, NG>(cur, items.t);
+      else if (ntok == 64) ok = ep.item<64, NG>(cur, items.t);
+      else ok = ep.item<32, NG>(cur, items.t);
     }
   }
 

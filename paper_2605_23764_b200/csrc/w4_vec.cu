@@ -240,25 +240,25 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
     int tile = u0 / a.KU, ku = u0 - tile * a.KU;   // row tile of the segment, unit of it
     int pass = (rt0 + tile) / a.RT, rt = rt0 + tile - pass * a.RT;
 
-    // ---- the stream: from unit to unit of an expert the addresses grow by a constant
+    // ---- the stream: from unit to unit of a row tile the addresses grow by four units
     const uint8_t *f_codes = nullptr, *f_scales = nullptr, *f_zeros = nullptr;
-    int f_pass = pass, f_left = u1 - u0, f_run = 0;   // units to fetch, of them in this pass
-    auto seek = [&](size_t unit) {   // of all experts' units; lane l copies 16 bytes at 16 l
+    int f_pass = pass, f_rt = rt, f_left = u1 - u0, f_run = 0;   // units to fetch, of them in this row tile
+    auto seek = [&](int from) {   // lane l copies 16 bytes at 16 l
+      const int64_t unit = (int64_t)sg_e[f_pass] * a.RTS * a.KU + w4_unit(f_rt, from, a.KU);
       f_codes = reinterpret_cast<const uint8_t*>(a.codes) + unit * W4_UNIT_BYTES + lane * 16;
       f_scales = reinterpret_cast<const uint8_t*>(a.scales) + unit * (64 * NG) + lane * 16;
       if (ASYM) f_zeros = reinterpret_cast<const uint8_t*>(a.zeros) + unit * (32 * NG) + lane * 16;
+      f_run = min(f_left, a.KU - from);
     };
-    if (u0 < u1) {
-      const int at = rt * a.KU + ku;
-      seek((size_t)sg_e[pass] * a.RT * a.KU + at);
-      f_run = min(f_left, a.RT * a.KU - at);
-    }
+    if (u0 < u1) seek(ku);
     const uint32_t ring = smem_u32(vsm) + warp * VEC_DEPTH * SLOT, ring_end = ring + VEC_DEPTH * SLOT;
     auto fetch = [&](uint32_t slot) {
       if (f_run == 0 && f_left > 0) {
-        ++f_pass;
-        seek((size_t)sg_e[f_pass] * a.RT * a.KU);
-        f_run = min(f_left, a.RT * a.KU);
+        if (++f_rt == a.RT) {
+          f_rt = 0;
+          ++f_pass;
+        }
+        seek(0);
       }
       if (f_run > 0) {
         --f_run;
@@ -268,9 +268,9 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
         for (int h = 0; h < 4; ++h) cp_async16(to + 512 * h, f_codes + 512 * h);
         if (lane < 4 * NG) cp_async16(to + W4_UNIT_BYTES, f_scales);
         if (ASYM && lane < 2 * NG) cp_async16(to + W4_UNIT_BYTES + 64 * NG, f_zeros);
-        f_codes += W4_UNIT_BYTES;
-        f_scales += 64 * NG;
-        if (ASYM) f_zeros += 32 * NG;
+        f_codes += 4 * W4_UNIT_BYTES;
+        f_scales += 4 * 64 * NG;
+        if (ASYM) f_zeros += 4 * 32 * NG;
       }
       cp_async_commit();
     };

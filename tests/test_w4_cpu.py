@@ -11,9 +11,9 @@ def _built():
 
 
 def test_sizes():
-    assert B.moe_w4_sizes(32, 128, 64) == (2048, 64)
-    assert B.moe_w4_sizes(16, 64, 32) == (2048, 128)
-    assert B.moe_w4_sizes(33, 136, 128) == (4 * 2048, 4 * 32)        # rows to 32, columns to 128
+    assert B.moe_w4_sizes(128, 128, 64) == (8192, 256)
+    assert B.moe_w4_sizes(16, 64, 32) == (8192, 512)
+    assert B.moe_w4_sizes(129, 136, 128) == (4 * 8192, 4 * 128)      # rows to 128, columns to 128
     assert B.moe_w4_sizes(4096, 7168, 128, B.MOE_W4_GATE_UP) == (4096 * 7168 // 2, 4096 * 56)
     for bad in ((0, 64, 64, 0), (16, 0, 64, 0), (16, 60, 64, 0), (16, 64, 16, 0), (16, 64, 256, 0), (24, 64, 64, 1), (16, 64, 64, 2)):
         with pytest.raises(MoeError):
