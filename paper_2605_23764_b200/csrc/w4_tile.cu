@@ -9,9 +9,10 @@
 // reduction; the epilogue warps scale it in fp32 and add it up in registers while the next group is multiplied.  So there is no
 // rounding that the formula does not have but that of the activations to bf16 between the two products.
 //
-// Roles per CTA: warp 0 loads codes, scales and zero points (a copy of each for 128 rows x 128 columns; with one for every 32 rows
-// issuing them took 1000 clocks, twice as long as the products), warp 26 the rows of x, warp 1 issues the products (even CTA), warps 2-9 widen (four for each half of a unit's 128 columns),
-// warps 10-25 scale and add up (four for each quarter of the columns).
+// Roles per CTA: warp 0 loads codes and zero points (a copy of each for 128 rows x 128 columns; with one for every 32 rows
+// issuing them took 1000 clocks, twice as long as the products), warp 18 the rows of x, warp 1 issues the products (even CTA), warps 2-9 widen (four for each half of a unit's 128 columns),
+// warps 10-17 scale and add up (four for each half of the columns; with
+// sixteen warps their waits and signals took the issue slots that the widening warps need: a prompt of 4096 tokens 841 us).
 #include "gemm_tile.cuh"
 #include "launch_pairs.cuh"
 #include "topk.cuh"
@@ -21,22 +22,19 @@ namespace moe {
 
 namespace {
 
-constexpr int WT_WIDEN_WARP = 2, WT_EPI_WARP = 10, WT_EPI_SIDES = 4, WT_TOK_WARP = WT_EPI_WARP + 4 * WT_EPI_SIDES, WT_THREADS = 32 * (WT_TOK_WARP + 1);
+constexpr int WT_WIDEN_WARP = 2, WT_EPI_WARP = 10, WT_EPI_SIDES = 2, WT_TOK_WARP = WT_EPI_WARP + 4 * WT_EPI_SIDES, WT_THREADS = 32 * (WT_TOK_WARP + 1);
 constexpr int WT_CODES = 4 * W4_UNIT_BYTES;   // 128 rows x 128 columns
-constexpr int WT_CODE_STAGES = 6, WT_SCALE_STAGES = 8, WT_TOK_STAGES = 6, WT_A_STAGES = 4, WT_D_BUFS = 3;
+constexpr int WT_CODE_STAGES = 6, WT_TOK_STAGES = 6, WT_A_STAGES = 2, WT_D_BUFS = 3;
 constexpr int WT_TOK_BYTES = 64 * 256;        // half of 128 rows x 128 columns bf16
-constexpr int WT_A_COLS = 32;                 // TMEM columns of 64 bf16
+constexpr int WT_A_COLS = 64;                 // TMEM columns of 128 bf16
 constexpr int WT_A_AT = WT_D_BUFS * BLOCK_M;  // behind the accumulators
-static_assert(WT_A_STAGES % 2 == 0, "a half keeps to its slots");
 static_assert(WT_A_AT + WT_A_STAGES * WT_A_COLS <= TMEM_COLS, "TMEM");
 
 struct __align__(8) WtBarriers {
   uint64_t code_full[WT_CODE_STAGES], code_empty[WT_CODE_STAGES];      // in each CTA
-  uint64_t scale_full[WT_SCALE_STAGES], scale_empty[WT_SCALE_STAGES];  // in each CTA
-  uint64_t tok_full[WT_TOK_STAGES];    // even CTA: both CTAs' rows
-  uint64_t tok_empty[WT_TOK_STAGES];   // in each CTA
-  uint64_t a_full[WT_A_STAGES];        // even CTA: the widening warps of both
-  uint64_t a_empty[WT_A_STAGES];       // in each CTA
+  // of unit u, at u % WT_TOK_STAGES: one wait and one commit for both operands (each costs the issuer some 100 clocks)
+  uint64_t full[WT_TOK_STAGES];        // even CTA: both CTAs' rows of x and widened weights
+  uint64_t done[WT_TOK_STAGES];        // in each CTA: multiplied
   uint64_t d_full[WT_D_BUFS];          // in each CTA
   uint64_t d_empty[WT_D_BUFS];         // even CTA: the epilogue warps of both
   uint64_t drain;
@@ -45,8 +43,7 @@ struct __align__(8) WtBarriers {
 
 __host__ __device__ constexpr int wt_code_stage(int ng, bool asym) { return WT_CODES + (asym ? 128 * ng : 0); }
 __host__ __device__ constexpr size_t wt_smem(int ng, bool asym) {
-  return 1024 + (size_t)WT_TOK_STAGES * WT_TOK_BYTES + (size_t)WT_CODE_STAGES * wt_code_stage(ng, asym) + (size_t)WT_SCALE_STAGES * 256 * ng +
-         sizeof(WtBarriers);
+  return 1024 + (size_t)WT_TOK_STAGES * WT_TOK_BYTES + (size_t)WT_CODE_STAGES * wt_code_stage(ng, asym) + sizeof(WtBarriers);
 }
 static_assert(wt_smem(4, true) <= 227 * 1024, "shared memory");
 
@@ -65,30 +62,38 @@ __device__ __forceinline__ void tmem_st_frag8(uint32_t taddr, const uint32_t (&r
                : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// One 16-deep product with the A operand in TMEM.
+// Two or four 16-deep products with the A operand in TMEM (8 columns each).
+template <int N>
 __device__ __forceinline__ void tc_mma_ts_pair(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n .reg .pred e, p;\n .reg .b64 db;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %5, 0;\n"
-      " mov.b64 db, {%2, %3};\n"
-      " @e tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], db, %4, p;\n}" ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
-      : "memory");
+  static_assert(N == 2 || N == 4, "");
+  if constexpr (N == 4)
+    asm volatile(
+        "{\n .reg .pred e, p;\n .reg .b64 db;\n .reg .b32 ta;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %5, 0;\n"
+        " mov.b64 db, {%2, %3};\n"
+        " @e tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], db, %4, p;\n"
+        " add.u64 db, db, 2;\n add.u32 ta, %1, 8;\n"
+        " @e tcgen05.mma.cta_group::2.kind::f16 [%0], [ta], db, %4, 1;\n"
+        " add.u64 db, db, 2;\n add.u32 ta, %1, 16;\n"
+        " @e tcgen05.mma.cta_group::2.kind::f16 [%0], [ta], db, %4, 1;\n"
+        " add.u64 db, db, 2;\n add.u32 ta, %1, 24;\n"
+        " @e tcgen05.mma.cta_group::2.kind::f16 [%0], [ta], db, %4, 1;\n}" ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred e, p;\n .reg .b64 db;\n .reg .b32 ta;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %5, 0;\n"
+        " mov.b64 db, {%2, %3};\n"
+        " @e tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], db, %4, p;\n"
+        " add.u64 db, db, 2;\n add.u32 ta, %1, 8;\n"
+        " @e tcgen05.mma.cta_group::2.kind::f16 [%0], [ta], db, %4, 1;\n}" ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        : "memory");
 }
-// 32 lanes x 8 or 16 columns: thread i has lane i.  The values are there behind the wait, which they depend on.
+// 32 lanes x 16 columns: thread i has lane i.  The values are there behind the wait, which they depend on.
 __device__ __forceinline__ void tmem_ld16_wait(uint32_t taddr, float (&v)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n tcgen05.wait::ld.sync.aligned;"
       : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
         "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
       : "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_ld8x2_wait(uint32_t taddr, uint32_t taddr2, float (&v)[16]) {   // eight columns at each
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%16];\n"
-      " tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8,%9,%10,%11,%12,%13,%14,%15}, [%17];\n tcgen05.wait::ld.sync.aligned;"
-      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
-        "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-      : "r"(taddr), "r"(taddr2)
       : "memory");
 }
 // Groups that share an accumulator buffer of 128 columns: the epilogue's waits and signals, some 500 clocks, are per buffer.
@@ -133,63 +138,60 @@ struct RingAt {
   int s = 0;
   uint32_t par;
   __device__ __forceinline__ explicit RingAt(uint32_t first) : par(first) {}
-  __device__ __forceinline__ void next(int step = 1) {
-    s += step;
-    if (s >= N) { s -= N; par ^= 1; }
+  __device__ __forceinline__ void next() {
+    if (++s == N) { s = 0; par ^= 1; }
   }
 };
 
-struct WtEpilogue {   // of a warp: 32 weight rows (a lane each) x a quarter of the columns
+struct WtEpilogue {   // of a warp: 32 weight rows (a lane each) x half of the columns
   const W4TileArgs& a;
   WtBarriers* bars;
-  const uint8_t* scale_s;
   WaitCtl wc;
   uint32_t tmem;     // the warp's lanes
   int rank, quad, side, lane;
-  RingAt<WT_SCALE_STAGES> sr{0};
   RingAt<WT_D_BUFS> dr{0};
 
   template <int NTOK, int NG>
   __device__ __forceinline__ bool item(const WtItem& it, int t) {
-    constexpr int NC = NTOK / 4, GPB = wt_groups(NTOK), ROUNDS = NC * GPB > 16 ? 2 : 1;   // sixteen values a round
+    constexpr int NC = NTOK / WT_EPI_SIDES, GPB = wt_groups(NTOK), ROUNDS = NC * GPB / 16;   // sixteen values a round
     const int groups = a.KU * NG;
     float2x acc[NC / 2];   // two columns side by side
 #pragma unroll
     for (int i = 0; i < NC / 2; ++i) acc[i] = pack2(0.f, 0.f);
-    // gate and up: the routing weight of column `lane`
-    float w_col = 0.f;
-    if (!a.down && lane < NC) w_col = __ldg(a.prow_w + it.row0 + side * NC + lane);
-    const uint32_t at = quad * 64 * NG + (lane & 7) * NG * 8 + (lane >> 3) * 2;   // of the row's scales in a stage
-    int in_unit = 0;   // group of the unit
-    auto scale = [&](int g, float& s) -> bool {   // of the g-th group, in turn
-      s = 0.f;
-      if (g >= groups) return true;
-      if (in_unit == 0 && !mbar_wait_warp(&bars->scale_full[sr.s], sr.par, wc, SITE_FULL, t)) return false;
-      s = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(scale_s + sr.s * (256 * NG) + at + in_unit * 8) << 16);
-      if (++in_unit == NG) {
-        in_unit = 0;
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cta(&bars->scale_empty[sr.s]);
-        sr.next();
+    // gate and up: the routing weights of columns lane and lane + 32
+    float w_col[2] = {0.f, 0.f};
+    if (!a.down) {
+      const float* w = a.prow_w + it.row0 + side * NC + lane;
+      if (lane < NC) w_col[0] = __ldg(w);
+      if (lane + 32 < NC) w_col[1] = __ldg(w + 32);
+    }
+    // The row's scales, read a buffer ahead.  Group g of the row: group g % NG of unit g / NG.
+    const int four = min(it.nb * 2 + rank, (a.RTS >> 2) - 1);
+    const uint16_t* const scales = reinterpret_cast<const uint16_t*>(a.scales) + ((size_t)it.e * (a.RTS >> 2) + four) * a.KU * (128 * NG) + quad * 32 * NG +
+                                   (lane & 7) * 4 * NG + (lane >> 3);
+    uint16_t ahead[GPB];
+    auto fetch = [&](int g0) {
+#pragma unroll
+      for (int i = 0; i < GPB; ++i) {
+        const int g = g0 + i;
+        ahead[i] = g < groups ? __ldg(scales + (g / NG) * (128 * NG) + (g % NG) * 4) : (uint16_t)0;
       }
-      return true;
     };
+    fetch(0);
 #pragma unroll 1
     for (int g0 = 0; g0 < groups; g0 += GPB) {
       float sc[GPB];
 #pragma unroll
-      for (int i = 0; i < GPB; ++i)
-        if (!scale(g0 + i, sc[i])) return false;
+      for (int i = 0; i < GPB; ++i) sc[i] = __uint_as_float((uint32_t)ahead[i] << 16);
+      fetch(g0 + GPB);
       if (!mbar_wait_warp(&bars->d_full[dr.s], dr.par, wc, SITE_TMEM_FULL, t)) return false;
       tc_fence_after_sync();
       const uint32_t d = tmem + dr.s * BLOCK_M + side * NC;
 #pragma unroll
       for (int r = 0; r < ROUNDS; ++r) {
         float v[16];
-        if constexpr (NTOK == 128) tmem_ld16_wait(d + 16 * r, v);
-        else if constexpr (NTOK == 96) { if (r == 0) tmem_ld16_wait(d, v); else tmem_ld8x2_wait(d + 16, d + 16, v); }
-        else if constexpr (NTOK == 64) tmem_ld16_wait(d + 64 * r, v);
-        else tmem_ld8x2_wait(d + 64 * r, d + 64 * r + 32, v);
+        const int grp = 16 * r / NC, col = 16 * r % NC;
+        tmem_ld16_wait(d + grp * NTOK + col, v);
         if (r == ROUNDS - 1) {
           tc_fence_before_sync();
           __syncwarp();
@@ -197,9 +199,7 @@ struct WtEpilogue {   // of a warp: 32 weight rows (a lane each) x a quarter of 
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int to = NTOK == 128 ? 8 * r + i : NTOK == 96 ? 8 * r + i : NTOK == 64 ? i : i & 3;
-          const int grp = NTOK >= 96 ? 0 : NTOK == 64 ? r : 2 * r + (i >> 2);
-          if (to >= NC / 2) continue;
+          const int to = col / 2 + i;
           // (a group behind the last was not written: nothing of it is added)
           const float2x next = fma2(pack2(sc[grp], sc[grp]), pack2(v[2 * i], v[2 * i + 1]), acc[to]);
           if (GPB == 1 || g0 + grp < groups) acc[to] = next;
@@ -235,7 +235,7 @@ struct WtEpilogue {   // of a warp: 32 weight rows (a lane each) x a quarter of 
         unpack2(acc[i], lo, hi);
         const float other = __shfl_xor_sync(0xffffffffu, is_up ? lo : hi, 8);
         const float gate = is_up ? other : lo, up = is_up ? hi : other;
-        const float w = __shfl_sync(0xffffffffu, w_col, 2 * i + is_up);
+        const float w = __shfl_sync(0xffffffffu, w_col[i / 16], (2 * i & 31) + is_up);
         const float act = w * (__fdividef(gate, 1.0f + __expf(-gate)) * up);
         if (feature < a.n_out) *out = (uint16_t)(pack_bf16x2(act, 0.f) & 0xFFFFu);
         out += 2 * (size_t)a.a_ld;
@@ -251,11 +251,10 @@ template <bool ASYM, int NG>
 __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_constant__ W4TileArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  constexpr int CODE_STAGE = wt_code_stage(NG, ASYM), SCALE_STAGE = 256 * NG;
+  constexpr int CODE_STAGE = wt_code_stage(NG, ASYM);
   uint8_t* const tok_s = smem;
   uint8_t* const code_s = tok_s + WT_TOK_STAGES * WT_TOK_BYTES;
-  uint8_t* const scale_s = code_s + WT_CODE_STAGES * CODE_STAGE;
-  WtBarriers* const bars = reinterpret_cast<WtBarriers*>(scale_s + WT_SCALE_STAGES * SCALE_STAGE);
+  WtBarriers* const bars = reinterpret_cast<WtBarriers*>(code_s + WT_CODE_STAGES * CODE_STAGE);
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();
@@ -264,9 +263,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < WT_CODE_STAGES; ++i) { mbar_init(&bars->code_full[i], 1); mbar_init(&bars->code_empty[i], 8); }
-    for (int i = 0; i < WT_SCALE_STAGES; ++i) { mbar_init(&bars->scale_full[i], 1); mbar_init(&bars->scale_empty[i], 4 * WT_EPI_SIDES); }
-    for (int i = 0; i < WT_TOK_STAGES; ++i) { mbar_init(&bars->tok_full[i], 1); mbar_init(&bars->tok_empty[i], 1); }
-    for (int i = 0; i < WT_A_STAGES; ++i) { mbar_init(&bars->a_full[i], 8); mbar_init(&bars->a_empty[i], 1); }
+    for (int i = 0; i < WT_TOK_STAGES; ++i) { mbar_init(&bars->full[i], 1 + 16); mbar_init(&bars->done[i], 1); }
     for (int i = 0; i < WT_D_BUFS; ++i) { mbar_init(&bars->d_full[i], 1); mbar_init(&bars->d_empty[i], 8 * WT_EPI_SIDES); }
     mbar_init(&bars->drain, 1);
     mbar_fence_init();
@@ -288,9 +285,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
   const int total = a.meta[0] * a.ntn, KU = a.KU;
   WtItem cur{};
   if (warp == 0) {
-    // ---- codes, scales, zero points of this CTA's 128 rows.  Where it has none, the last ones are read again and not stored.
+    // ---- codes and zero points of this CTA's 128 rows.  Where it has none, the last ones are read again and not stored.
     RingAt<WT_CODE_STAGES> cr(1);
-    RingAt<WT_SCALE_STAGES> sr(1);
     bool ok = true;
     WtItems items(a, pair, npairs, total);
     while (ok && items.next(cur)) {
@@ -303,11 +299,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
         mbar_expect_tx_elect(&bars->code_full[cr.s], CODE_STAGE);
         bulk_load_elect(cs, a.codes + at * WT_CODES, WT_CODES, &bars->code_full[cr.s]);
         if (ASYM) bulk_load_elect(cs + WT_CODES, a.zeros + at * (128 * NG), 128 * NG, &bars->code_full[cr.s]);
-        if (!mbar_wait_warp(&bars->scale_empty[sr.s], sr.par, wc, SITE_EMPTY, t, 20)) { ok = false; break; }
-        mbar_expect_tx_elect(&bars->scale_full[sr.s], SCALE_STAGE);
-        bulk_load_elect(scale_s + sr.s * SCALE_STAGE, a.scales + at * SCALE_STAGE, SCALE_STAGE, &bars->scale_full[sr.s]);
         cr.next();
-        sr.next();
       }
     }
   } else if (warp == WT_TOK_WARP) {
@@ -320,19 +312,19 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
       const int ntok = uniform(cur.ntok), half = ntok >> 1, row = uniform(cur.row0) + rank * half;
       const CUtensorMap* tm = &a.tok[(half >> 4) - 1];
       for (int ku = 0; ku < KU; ++ku) {
-        if (!mbar_wait_warp(&bars->tok_empty[tr.s], tr.par, wc, SITE_EMPTY, t, 20)) { ok = false; break; }
+        if (!mbar_wait_warp(&bars->done[tr.s], tr.par, wc, SITE_EMPTY, t, 20)) { ok = false; break; }
         uint8_t* const ts = tok_s + tr.s * WT_TOK_BYTES;
-        if (rank == 0) mbar_expect_tx_elect(&bars->tok_full[tr.s], (uint32_t)ntok * 256);
-        tma_load_2d_pair(ts, tm, ku * W4_UNIT_K, row, &bars->tok_full[tr.s]);
-        tma_load_2d_pair(ts + half * 128, tm, ku * W4_UNIT_K + 64, row, &bars->tok_full[tr.s]);
+        if (rank == 0) mbar_expect_tx_elect(&bars->full[tr.s], (uint32_t)ntok * 256);
+        tma_load_2d_pair(ts, tm, ku * W4_UNIT_K, row, &bars->full[tr.s]);
+        tma_load_2d_pair(ts + half * 128, tm, ku * W4_UNIT_K + 64, row, &bars->full[tr.s]);
         tr.next();
       }
     }
   } else if (warp == 1 && rank == 0) {
     // ---- products
     RingAt<WT_TOK_STAGES> tr(0);
-    RingAt<WT_A_STAGES> ar(0);
     RingAt<WT_D_BUFS> dr(1);
+    uint32_t a_t = tmem_base + WT_A_AT;
     bool ok = true;
     constexpr int STEPS = 8 / NG;   // of 16 columns in a group
     WtItems items(a, pair, npairs, total);
@@ -343,32 +335,27 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
       const int gpb = wt_groups(ntok), groups = KU * NG;
       int grp = 0, in_buf = 0;   // group of the item, of the accumulator buffer
       for (int ku = 0; ku < KU && ok; ++ku) {
-        if (!mbar_wait_warp(&bars->tok_full[tr.s], tr.par, wc, SITE_FULL, t)) { ok = false; break; }
+        if (!mbar_wait_warp(&bars->full[tr.s], tr.par, wc, SITE_FULL, t)) { ok = false; break; }
         const uint32_t b_lo = smem_desc_lo(smem_u32(tok_s + tr.s * WT_TOK_BYTES), 16);
+        constexpr int RUN = STEPS < 4 ? STEPS : 4;   // products in a row: of one box and one group
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {   // halves of 64 columns: a stage of the A operand, a box of the B operand
-          if (!mbar_wait_warp(&bars->a_full[ar.s], ar.par, wc, SITE_FULL, t)) { ok = false; break; }
-          const uint32_t a_t = tmem_base + WT_A_AT + ar.s * WT_A_COLS;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int k16 = 4 * h + j;
-            if (k16 % STEPS == 0 && in_buf == 0 && !mbar_wait_warp(&bars->d_empty[dr.s], dr.par, wc, SITE_TMEM_EMPTY, t)) { ok = false; break; }
-            if (j == 0 || k16 % STEPS == 0) tc_fence_after_sync();
-            tc_mma_ts_pair(tmem_base + dr.s * BLOCK_M + in_buf * ntok, a_t + 8 * j, b_lo + h * box + 2 * j, smem_desc_hi(1024), idesc, k16 % STEPS != 0);
-            if (k16 % STEPS == STEPS - 1) {
-              ++grp;
-              if (++in_buf == gpb || grp == groups) {
-                tc_commit_pair(&bars->d_full[dr.s]);
-                dr.next();
-                in_buf = 0;
-              }
+        for (int k16 = 0; k16 < 8; k16 += RUN) {
+          if (k16 % STEPS == 0 && in_buf == 0 && !mbar_wait_warp(&bars->d_empty[dr.s], dr.par, wc, SITE_TMEM_EMPTY, t)) { ok = false; break; }
+          if (k16 % STEPS == 0) tc_fence_after_sync();
+          tc_mma_ts_pair<RUN>(tmem_base + dr.s * BLOCK_M + in_buf * ntok, a_t + 8 * k16, b_lo + (k16 >> 2) * box + 2 * (k16 & 3), smem_desc_hi(1024), idesc,
+                              k16 % STEPS != 0);
+          if ((k16 + RUN) % STEPS == 0) {
+            ++grp;
+            if (++in_buf == gpb || grp == groups) {
+              tc_commit_pair(&bars->d_full[dr.s]);
+              dr.next();
+              in_buf = 0;
             }
           }
-          tc_commit_pair(&bars->a_empty[ar.s]);
-          ar.next();
         }
-        tc_commit_pair(&bars->tok_empty[tr.s]);
+        tc_commit_pair(&bars->done[tr.s]);
         tr.next();
+        a_t ^= (tmem_base + WT_A_AT) ^ (tmem_base + WT_A_AT + WT_A_COLS);   // the other stage
       }
     }
     if (uniform(!ok || *reinterpret_cast<volatile int*>(&a.status->abort) ? 1 : 0)) {   // let what was issued end before TMEM is freed
@@ -380,9 +367,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
     // ---- codes to whole numbers in TMEM: a warp has the 32 lanes of its quarter, half of the unit's columns
     const int quad = warp & 3, h = (warp - WT_WIDEN_WARP) >> 2, g = lane >> 2;
     RingAt<WT_CODE_STAGES> cr(0);
-    RingAt<WT_A_STAGES> ar(1);
-    ar.s = h;
-    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+    RingAt<WT_TOK_STAGES> fr(0), before(0);   // the unit, and the one that had its stage of the A operand before
+    const uint32_t a_t = tmem_base + ((uint32_t)(quad * 32) << 16) + WT_A_AT + 32 * h;
     const int units = (pair < total ? (total - pair + npairs - 1) / npairs : 0) * KU;
     for (int u = 0; u < units; ++u) {
       if (!mbar_wait_warp(&bars->code_full[cr.s], cr.par, wc, SITE_FULL, u)) break;
@@ -395,13 +381,10 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
 #pragma unroll
         for (int i = 0; i < HG; ++i) zp[i] = z[i];
       }
-      if (!mbar_wait_warp(&bars->a_empty[ar.s], ar.par, wc, SITE_TMEM_EMPTY, u)) break;
-      tc_fence_after_sync();
-      const uint32_t a_t = tmem_base + lanes + WT_A_AT + ar.s * WT_A_COLS;
+      uint32_t v[2][16];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {   // sixteen rows
         const uint32_t words[4] = {q[s].x, q[s].y, q[s].z, q[s].w};
-        uint32_t v[16];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t z = ASYM ? zp[j * HG / 4] >> (16 * s) : 0;
@@ -409,23 +392,30 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
           uint32_t f[4];
           w4_fragment(words[j], f);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) v[4 * j + r] = add_bf16x2(f[r], r & 1 ? hi : lo);
+          for (int r = 0; r < 4; ++r) v[s][4 * j + r] = add_bf16x2(f[r], r & 1 ? hi : lo);
         }
-        tmem_st_frag8(a_t + ((uint32_t)(16 * s) << 16), v);
       }
+      // (widened ahead: from here on the products of this stage's last content wait for nothing but the stores)
+      if (u >= WT_A_STAGES) {
+        if (!mbar_wait_warp(&bars->done[before.s], before.par, wc, SITE_TMEM_EMPTY, u)) break;
+        before.next();
+        tc_fence_after_sync();
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) tmem_st_frag8(a_t + (u % WT_A_STAGES) * WT_A_COLS + ((uint32_t)(16 * s) << 16), v[s]);
       tmem_st_wait();
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive_leader(&bars->a_full[ar.s]);   // TMEM is ordered by the tcgen05 fences: a release at cluster scope took 1800 clocks
+        mbar_arrive_leader(&bars->full[fr.s]);   // TMEM is ordered by the tcgen05 fences: a release at cluster scope took 1800 clocks
         mbar_arrive_cta(&bars->code_empty[cr.s]);
       }
       cr.next();
-      ar.next(2);
+      fr.next();
     }
   } else if (warp >= WT_EPI_WARP) {
     // ---- groups scaled and added up
-    WtEpilogue ep{a, bars, scale_s, wc, tmem_base + ((uint32_t)((warp & 3) * 32) << 16), rank, warp & 3, (warp - WT_EPI_WARP) >> 2, lane};
+    WtEpilogue ep{a, bars, wc, tmem_base + ((uint32_t)((warp & 3) * 32) << 16), rank, warp & 3, (warp - WT_EPI_WARP) >> 2, lane};
     WtItems items(a, pair, npairs, total);
     bool ok = true;
     while (ok && items.next(cur)) {
