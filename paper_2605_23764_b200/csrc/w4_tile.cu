@@ -28,6 +28,7 @@ constexpr int WT_CODE_STAGES = 6, WT_TOK_STAGES = 6, WT_A_STAGES = 2, WT_D_BUFS 
 constexpr int WT_TOK_BYTES = 64 * 256;        // half of 128 rows x 128 columns bf16
 constexpr int WT_A_COLS = 64;                 // TMEM columns of 128 bf16
 constexpr int WT_A_AT = WT_D_BUFS * BLOCK_M;  // behind the accumulators
+static_assert(WT_CODE_STAGES % 2 == 0 && WT_TOK_STAGES % 2 == 0 && WT_A_STAGES == 2, "a set of widening warps keeps to every other slot");
 static_assert(WT_A_AT + WT_A_STAGES * WT_A_COLS <= TMEM_COLS, "TMEM");
 
 struct __align__(8) WtBarriers {
@@ -138,8 +139,9 @@ struct RingAt {
   int s = 0;
   uint32_t par;
   __device__ __forceinline__ explicit RingAt(uint32_t first) : par(first) {}
-  __device__ __forceinline__ void next() {
-    if (++s == N) { s = 0; par ^= 1; }
+  __device__ __forceinline__ void next(int step = 1) {
+    s += step;
+    if (s >= N) { s -= N; par ^= 1; }
   }
 };
 
@@ -262,8 +264,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
   const WaitCtl wc{a.status, a.budget_ns};
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < WT_CODE_STAGES; ++i) { mbar_init(&bars->code_full[i], 1); mbar_init(&bars->code_empty[i], 8); }
-    for (int i = 0; i < WT_TOK_STAGES; ++i) { mbar_init(&bars->full[i], 1 + 16); mbar_init(&bars->done[i], 1); }
+    for (int i = 0; i < WT_CODE_STAGES; ++i) { mbar_init(&bars->code_full[i], 1); mbar_init(&bars->code_empty[i], 4); }
+    for (int i = 0; i < WT_TOK_STAGES; ++i) { mbar_init(&bars->full[i], 1 + 8); mbar_init(&bars->done[i], 1); }
     for (int i = 0; i < WT_D_BUFS; ++i) { mbar_init(&bars->d_full[i], 1); mbar_init(&bars->d_empty[i], 8 * WT_EPI_SIDES); }
     mbar_init(&bars->drain, 1);
     mbar_fence_init();
@@ -324,7 +326,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
     // ---- products
     RingAt<WT_TOK_STAGES> tr(0);
     RingAt<WT_D_BUFS> dr(1);
-    uint32_t a_t = tmem_base + WT_A_AT;
+    const uint32_t a_first = tmem_base + WT_A_AT, a_end = a_first + WT_A_STAGES * WT_A_COLS;
+    uint32_t a_t = a_first;
     bool ok = true;
     constexpr int STEPS = 8 / NG;   // of 16 columns in a group
     WtItems items(a, pair, npairs, total);
@@ -355,7 +358,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
         }
         tc_commit_pair(&bars->done[tr.s]);
         tr.next();
-        a_t ^= (tmem_base + WT_A_AT) ^ (tmem_base + WT_A_AT + WT_A_COLS);   // the other stage
+        a_t = a_t + WT_A_COLS == a_end ? a_first : a_t + WT_A_COLS;
       }
     }
     if (uniform(!ok || *reinterpret_cast<volatile int*>(&a.status->abort) ? 1 : 0)) {   // let what was issued end before TMEM is freed
@@ -364,45 +367,54 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
       mbar_wait_warp(&bars->drain, 0, shortwc, SITE_DRAIN, 0);
     }
   } else if (warp >= WT_WIDEN_WARP && warp < WT_EPI_WARP) {
-    // ---- codes to whole numbers in TMEM: a warp has the 32 lanes of its quarter, half of the unit's columns
-    const int quad = warp & 3, h = (warp - WT_WIDEN_WARP) >> 2, g = lane >> 2;
+    // ---- codes to whole numbers in TMEM: a warp has the 32 lanes of its quarter, a set of four every other unit and one of the two
+    // stages of the A operand.  The first half is widened ahead: what the products wait for once a stage is free is short.
+    const int quad = warp & 3, set = (warp - WT_WIDEN_WARP) >> 2, g = lane >> 2;
     RingAt<WT_CODE_STAGES> cr(0);
-    RingAt<WT_TOK_STAGES> fr(0), before(0);   // the unit, and the one that had its stage of the A operand before
-    const uint32_t a_t = tmem_base + ((uint32_t)(quad * 32) << 16) + WT_A_AT + 32 * h;
+    RingAt<WT_TOK_STAGES> fr(0), before(0);   // the unit, and the one that had the stage before
+    cr.s = fr.s = before.s = set;
+    const uint32_t a_t = tmem_base + ((uint32_t)(quad * 32) << 16) + WT_A_AT + set * WT_A_COLS;
     const int units = (pair < total ? (total - pair + npairs - 1) / npairs : 0) * KU;
-    for (int u = 0; u < units; ++u) {
-      if (!mbar_wait_warp(&bars->code_full[cr.s], cr.par, wc, SITE_FULL, u)) break;
-      const uint8_t* const cs = code_s + cr.s * CODE_STAGE + quad * W4_UNIT_BYTES + h * 1024 + lane * 16;
-      const uint4 q[2] = {*reinterpret_cast<const uint4*>(cs), *reinterpret_cast<const uint4*>(cs + 512)};
-      constexpr int HG = NG == 4 ? 2 : 1;   // groups of the half
-      uint32_t zp[HG];
-      if constexpr (ASYM) {
-        const uint32_t* z = reinterpret_cast<const uint32_t*>(code_s + cr.s * CODE_STAGE + WT_CODES + quad * 32 * NG + g * 4 * NG) + (NG == 1 ? 0 : h * HG);
+    for (int u = set; u < units; u += 2) {
+      if (!mbar_wait_warp(&bars->code_full[cr.s], cr.par, wc, SITE_FULL, u, 50)) break;
+      const uint8_t* const cs = code_s + cr.s * CODE_STAGE + quad * W4_UNIT_BYTES + lane * 16;
+      uint4 q[4];
 #pragma unroll
-        for (int i = 0; i < HG; ++i) zp[i] = z[i];
+      for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const uint4*>(cs + 512 * i);
+      uint32_t zp[ASYM ? NG : 1];
+      if constexpr (ASYM) {
+        const uint32_t* z = reinterpret_cast<const uint32_t*>(code_s + cr.s * CODE_STAGE + WT_CODES + quad * 32 * NG + g * 4 * NG);
+#pragma unroll
+        for (int i = 0; i < NG; ++i) zp[i] = z[i];
       }
       uint32_t v[2][16];
+      auto widen = [&](int h) {   // half of 64 columns; two times sixteen rows
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {   // sixteen rows
-        const uint32_t words[4] = {q[s].x, q[s].y, q[s].z, q[s].w};
+        for (int s = 0; s < 2; ++s) {
+          const uint4 w = q[2 * h + s];
+          const uint32_t words[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t z = ASYM ? zp[j * HG / 4] >> (16 * s) : 0;
-          const uint32_t lo = ASYM ? w4_bias(z & 0xFFu) : w4_bias(8), hi = ASYM ? w4_bias((z >> 8) & 0xFFu) : w4_bias(8);
-          uint32_t f[4];
-          w4_fragment(words[j], f);
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t z = ASYM ? zp[ASYM ? (4 * h + j) * NG / 8 : 0] >> (16 * s) : 0;
+            const uint32_t lo = ASYM ? w4_bias(z & 0xFFu) : w4_bias(8), hi = ASYM ? w4_bias((z >> 8) & 0xFFu) : w4_bias(8);
+            uint32_t f[4];
+            w4_fragment(words[j], f);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) v[s][4 * j + r] = add_bf16x2(f[r], r & 1 ? hi : lo);
+            for (int r = 0; r < 4; ++r) v[s][4 * j + r] = add_bf16x2(f[r], r & 1 ? hi : lo);
+          }
         }
-      }
-      // (widened ahead: from here on the products of this stage's last content wait for nothing but the stores)
+      };
+      widen(0);
       if (u >= WT_A_STAGES) {
-        if (!mbar_wait_warp(&bars->done[before.s], before.par, wc, SITE_TMEM_EMPTY, u)) break;
-        before.next();
+        if (!mbar_wait_warp(&bars->done[before.s], before.par, wc, SITE_TMEM_EMPTY, u, 50)) break;
+        before.next(2);
         tc_fence_after_sync();
       }
 #pragma unroll
-      for (int s = 0; s < 2; ++s) tmem_st_frag8(a_t + (u % WT_A_STAGES) * WT_A_COLS + ((uint32_t)(16 * s) << 16), v[s]);
+      for (int s = 0; s < 2; ++s) tmem_st_frag8(a_t + ((uint32_t)(16 * s) << 16), v[s]);
+      widen(1);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) tmem_st_frag8(a_t + ((uint32_t)(16 * s) << 16) + 32, v[s]);
       tmem_st_wait();
       tc_fence_before_sync();
       __syncwarp();
@@ -410,8 +422,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) w4_tile_kernel(const __grid_con
         mbar_arrive_leader(&bars->full[fr.s]);   // TMEM is ordered by the tcgen05 fences: a release at cluster scope took 1800 clocks
         mbar_arrive_cta(&bars->code_empty[cr.s]);
       }
-      cr.next();
-      fr.next();
+      cr.next(2);
+      fr.next(2);
     }
   } else if (warp >= WT_EPI_WARP) {
     // ---- groups scaled and added up
