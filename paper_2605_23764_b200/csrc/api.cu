@@ -189,7 +189,7 @@ WsPlan plan_workspace(const moe_shape& s) {
   p.ctr = c.take(sizeof(int) * (size_t)p.ctr_count * (train ? 2 : 1));   // forward, backward
   p.trace_cap = (s.flags & MOE_FLAG_TRACE) ? TRACE_RECORDS : 0;
   p.trace = c.take((size_t)p.trace_cap * 32);
-  p.balance = c.take(balance_scratch_bytes(s.T_max, s.E));
+  p.balance = c.take(balance_scratch_bytes(s.E));
   p.tickets = c.take(sizeof(int) * (BAL_MAX_BLOCKS + 1));
   p.Y4 = c.take((s.flags & MOE_FLAG_W4) ? sizeof(float) * cap * s.d : 0);
   p.total = c.off;
@@ -1084,7 +1084,7 @@ int moe_balance_bwd(moe_ctx* c, const float* logits, const int32_t* topk_ids, co
   a.d_topk_w = d_topk_w;
   a.d_logits = d_logits;
   Phase ph(c, MOE_PHASE_ROUTE, st);
-  MOE_CUDA(launch_balance_bwd(a, st, &c->launches));
+  MOE_CUDA(launch_balance_bwd(a, c->num_sms, st, &c->launches));
   return MOE_OK;
 }
 

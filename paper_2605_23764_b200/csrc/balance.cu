@@ -21,37 +21,61 @@ namespace moe {
 
 namespace {
 
-constexpr int BAL_MAX_WARPS = 16;
+constexpr int BAL_MAX_WARPS = 32;   // of a forward block: one block an SM, so that few blocks' pieces are to be joined
 
 __device__ __forceinline__ float group_sum(float v, int lpt) {
   for (int off = lpt >> 1; off; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
   return v;
+}
+// N sums at a time: their shuffles overlap
+template <int LPT, int N>
+__device__ __forceinline__ void group_sums(float (&v)[N]) {
+#pragma unroll
+  for (int off = LPT >> 1; off; off >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], off);
 }
 __device__ __forceinline__ float group_max(float v, int lpt) {
   for (int off = lpt >> 1; off; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
   return v;
 }
 
-// First token of sequence s (s = n: one behind the last).  Offsets are the caller's: kept inside the batch.
-__device__ __forceinline__ int seq_begin(const int* off, int s, int T) {
-  if (!off) return s ? T : 0;
-  return min(max(__ldg(off + s), 0), T);
-}
-// Sequence of token t: -1 in front of the first one, n behind the last.  A warp's 32 probes a round, where a lane's bisection
-// would be a chain of dependent reads.
-__device__ __forceinline__ int seq_of(const int* off, int n, int T, int t, int lane) {
-  if (!off) return 0;
-  int lo = 0, len = n + 1;
-  while (len > 32) {
-    const int step = (len + 31) >> 5;
-    const int i = lane * step;
-    const int c = __popc(__ballot_sync(0xffffffffu, i < len && seq_begin(off, lo + i, T) <= t));
-    if (c == 0) return lo - 1;
-    const int at = (c - 1) * step;
-    lo += at;
-    len = min(step, len - at);
+// Sequence offsets: the caller's, kept inside the batch; staged in shared memory where they fit, since they are looked up in turn.
+struct SeqTable {
+  const int* off;    // NULL: the batch is one sequence
+  const int* staged; // NULL: not staged
+  int n, T;
+  // first token of sequence s (s = n: one behind the last)
+  __device__ __forceinline__ int begin(int s) const {
+    if (staged) return staged[s];
+    if (!off) return s ? T : 0;
+    return min(max(__ldg(off + s), 0), T);
   }
-  return lo - 1 + __popc(__ballot_sync(0xffffffffu, lane < len && seq_begin(off, lo + lane, T) <= t));
+  // Sequence of token t: -1 in front of the first one, n behind the last.  A warp's 32 probes a round, where a lane's bisection
+  // would be a chain of dependent reads.
+  __device__ __forceinline__ int of(int t, int lane) const {
+    if (!off) return 0;
+    int lo = 0, len = n + 1;
+    while (len > 32) {
+      const int step = (len + 31) >> 5;
+      const int i = lane * step;
+      const int c = __popc(__ballot_sync(0xffffffffu, i < len && begin(lo + i) <= t));
+      if (c == 0) return lo - 1;
+      const int at = (c - 1) * step;
+      lo += at;
+      len = min(step, len - at);
+    }
+    return lo - 1 + __popc(__ballot_sync(0xffffffffu, lane < len && begin(lo + lane) <= t));
+  }
+};
+constexpr int BAL_STAGED = 1024;   // offsets in shared memory, at most
+// Fills `to` by the whole block (a barrier follows in the caller).
+__device__ __forceinline__ void stage_offsets(const BalanceArgs& a, int* to) {
+  if (a.seq_offsets && a.n_seq < BAL_STAGED)
+    for (int i = threadIdx.x; i <= a.n_seq; i += blockDim.x) to[i] = min(max(__ldg(a.seq_offsets + i), 0), a.T);
+}
+__device__ __forceinline__ SeqTable seq_table(const BalanceArgs& a, const int* staged) {
+  return SeqTable{a.seq_offsets, a.seq_offsets && a.n_seq < BAL_STAGED ? staged : nullptr, a.n_seq, a.T};
 }
 
 // Value i of lane l of a group stands for expert ((i / VW) LPT + l) VW + i % VW: vectors of VW lie side by side.
@@ -73,44 +97,45 @@ __device__ __forceinline__ void load_row(const float* row, int E, int l, bool on
   }
 }
 
-// Softmax of a row and its logsumexp.  A row without a finite logit has no probabilities: zeros, and logsumexp counts as 0.
-template <int LPT, int VPL>
-__device__ __forceinline__ float softmax_row(const float (&v)[VPL], float (&p)[VPL]) {
-  float m = v[0];
-#pragma unroll
-  for (int i = 1; i < VPL; ++i) m = fmaxf(m, v[i]);
-  m = group_max(m, LPT);
-  if (m == -INFINITY) m = 0.f;
-  float den = 0.f;
-#pragma unroll
-  for (int i = 0; i < VPL; ++i) { p[i] = __expf(v[i] - m); den += p[i]; }
-  den = group_sum(den, LPT);
-  const float r = den == 0.f ? 0.f : 1.0f / den;
-#pragma unroll
-  for (int i = 0; i < VPL; ++i) p[i] *= r;
-  return den == 0.f ? 0.f : m + logf(den);
+constexpr float LOG2E = 1.4426950408889634f;
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
-// Normalised sigmoids; s: the sigmoids themselves (NULL: not wanted).  Below zero sigmoid(l) = exp(l) / (1 + exp(l)), so a row of
-// large negative logits is scaled by its largest as a softmax is, and keeps its proportions where every sigmoid underflows.
+
 template <int LPT, int VPL>
-__device__ __forceinline__ void sigmoid_row(const float (&v)[VPL], float (&p)[VPL], float* s) {
+__device__ __forceinline__ float row_max(const float (&v)[VPL]) {
   float m = v[0];
 #pragma unroll
   for (int i = 1; i < VPL; ++i) m = fmaxf(m, v[i]);
-  m = fminf(group_max(m, LPT), 0.f);
+  return group_max(m, LPT);
+}
+// Softmax terms exp(v - max) and -- SIG -- sigmoids of a row before they are normalised: ex, p, inv[0] and inv[1] = 1 / their sums, sig
+// the sigmoids themselves (NULL: not wanted); the answer is the row's logsumexp.  A row without a finite logit has no probabilities:
+// zeros, and logsumexp counts as 0.  Below zero sigmoid(l) = exp(l) / (1 + exp(l)), so sigmoids of a row of large negative logits are
+// scaled by its largest as a softmax is, and keep their proportions where every sigmoid underflows.
+template <int LPT, int VPL, bool SIG>
+__device__ __forceinline__ float row_terms(const float (&v)[VPL], float (&ex)[VPL], float (&p)[SIG ? VPL : 1], float* sig, float (&inv)[2]) {
+  float m = row_max<LPT, VPL>(v);
   const bool low = m < -16.f && m > -INFINITY;
-  float den = 0.f;
+  if (m == -INFINITY) m = 0.f;
+  float den[SIG ? 2 : 1] = {};
 #pragma unroll
   for (int i = 0; i < VPL; ++i) {
-    const float t = __expf(-fabsf(v[i])), sig = v[i] >= 0.f ? 1.0f / (1.0f + t) : t / (1.0f + t);
-    if (s) s[i] = sig;
-    p[i] = low ? __expf(v[i] - m) / (1.0f + t) : sig;
-    den += p[i];
+    ex[i] = ex2((v[i] - m) * LOG2E);
+    den[0] += ex[i];
+    if constexpr (SIG) {
+      const float t = ex2(-fabsf(v[i]) * LOG2E), r = __fdividef(1.0f, 1.0f + t), s = v[i] >= 0.f ? r : t * r;
+      if (sig) sig[i] = s;
+      p[i] = low ? ex[i] * r : s;
+      den[1] += p[i];
+    }
   }
-  den = group_sum(den, LPT);
-  const float r = den == 0.f ? 0.f : 1.0f / den;
-#pragma unroll
-  for (int i = 0; i < VPL; ++i) p[i] *= r;
+  group_sums<LPT>(den);
+  inv[0] = den[0] == 0.f ? 0.f : __fdividef(1.0f, den[0]);
+  if constexpr (SIG) inv[1] = den[1] == 0.f ? 0.f : __fdividef(1.0f, den[1]);
+  return den[0] == 0.f ? 0.f : m + __logf(den[0]);
 }
 
 }  // namespace
@@ -124,16 +149,20 @@ __device__ __forceinline__ void sigmoid_row(const float (&v)[VPL], float (&p)[VP
 // ------------------------------------------------------------------------------------------
 // A piece in global memory, two a block: of the sequence that began before the block, of the one that goes on behind it.
 // [block][2] x {float psum[E]; int count[E]}, then per block {seq of both pieces, tokens of both, loss, z, tokens}
-struct BalBlock { int seq[2], n[2]; double loss, z; long long tokens; };
+__host__ __device__ constexpr int balance_warps_most(int vpl) { return vpl <= 8 ? BAL_MAX_WARPS : vpl <= 16 ? 24 : 16; }   // registers
+struct BalBlock { int seq[2], n[2]; double loss, z, tokens; };
 
 template <int LPT, int VPL, int VW, bool SIG>
-__global__ void __launch_bounds__(32 * BAL_MAX_WARPS) balance_fwd_kernel(const BalanceArgs a) {
+__global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kernel(const BalanceArgs a) {
   constexpr int TPW = 32 / LPT;
   extern __shared__ __align__(16) int bsm[];
+  __shared__ int offsets[BAL_STAGED];
   __shared__ int w_seq[2 * BAL_MAX_WARPS], w_n[2 * BAL_MAX_WARPS];
-  __shared__ double s_loss[BAL_MAX_WARPS], s_z[BAL_MAX_WARPS];
-  __shared__ long long s_tok[BAL_MAX_WARPS];
-  __shared__ int s_last;
+  __shared__ double s_sum[3][32];
+  // stretches of the warps' pieces that are one sequence: pieces [from, to), where the sum goes (0, 1: that piece of the block; 2: final)
+  __shared__ int g_seq[2 * BAL_MAX_WARPS], g_from[2 * BAL_MAX_WARPS + 1], g_n[2 * BAL_MAX_WARPS], g_to[2 * BAL_MAX_WARPS], g_count;
+  __shared__ unsigned long long g_valid;
+  __shared__ int s_last[3], s_live, b_seq[2];
   const int E = a.E, n = a.n_seq, T = a.T;
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPT, grp = lane / LPT;
   int* const hist = bsm + warp * E;                                   // [warps][E]
@@ -141,46 +170,52 @@ __global__ void __launch_bounds__(32 * BAL_MAX_WARPS) balance_fwd_kernel(const B
   int* const w_cnt = bsm + 3 * warps * E;                             // [warps][2][E]
   for (int e = lane; e < E; e += 32) hist[e] = 0;
   if (lane < 2) w_seq[2 * warp + lane] = -1;
-  __syncwarp();
   pdl_wait();
   pdl_trigger();
 
-  const int b0 = (int)((long long)T * blockIdx.x / gridDim.x), b1 = (int)((long long)T * (blockIdx.x + 1) / gridDim.x);
-  const int wa = b0 + (int)((long long)(b1 - b0) * warp / warps), wb = b0 + (int)((long long)(b1 - b0) * (warp + 1) / warps);
+  const int b0 = blockIdx.x * a.chunk, b1 = min(b0 + a.chunk, T), per_warp = (a.chunk + warps - 1) / warps;
+  const int wa = min(b0 + warp * per_warp, b1), wb = min(wa + per_warp, b1);
+  // A token's row, mask and the lane's first id are read a round ahead, the first ones while the offsets arrive.
+  float v[VPL], next[VPL];
+  int next_id = -1, next_at = wa;
+  bool next_on = false;
+  auto fetch = [&](int t0) {
+    const int tt = t0 + grp;
+    next_at = t0;
+    load_row<LPT, VPL, VW>(a.logits + (size_t)tt * E, E, l, tt < wb, next);
+    next_on = tt < wb && (!a.token_mask || a.token_mask[tt] != 0);
+    next_id = tt < wb && l < a.k ? a.topk_ids[(size_t)tt * a.k + l] : -1;
+  };
+  fetch(wa);
+  stage_offsets(a, offsets);
+  __syncthreads();
+  const SeqTable seqs = seq_table(a, offsets);
   const float unit = (float)E / ((float)a.k * (float)n);
-  double loss = 0.0, zsum = 0.0;
-  long long tokens = 0;
-  int s = wa < wb ? seq_of(a.seq_offsets, n, T, wa, lane) : n;
+  double my_loss = 0.0, zsum = 0.0;   // of the thread; of the warp
+  int tokens = 0;
+  int s = wa < wb ? seqs.of(wa, lane) : n;
   for (int t = wa; t < wb;) {
     // the run [t, end) of sequence s
-    const int begins = s >= 0 && s < n ? seq_begin(a.seq_offsets, s, T) : 0;
-    int stop = s < n ? seq_begin(a.seq_offsets, s + 1, T) : T;
+    const bool inside = s >= 0 && s < n;
+    const int begins = inside ? seqs.begin(s) : 0;
+    int stop = s < n ? seqs.begin(s + 1) : T;
     if (stop <= t) stop = t + 1;   // (offsets that do not ascend)
     const int end = min(stop, wb);
-    if (s >= 0 && s < n) {
+    if (inside) {
       float acc[VPL];
 #pragma unroll
       for (int i = 0; i < VPL; ++i) acc[i] = 0.f;
       float z = 0.f;
       int live = 0;
-      // a token's row, mask and first id of the lane are read a round ahead
-      float v[VPL], next[VPL];
-      int next_id = -1;
-      bool next_on = false;
-      auto fetch = [&](int tt) {
-        load_row<LPT, VPL, VW>(a.logits + (size_t)tt * E, E, l, tt < end, next);
-        next_on = tt < end && (!a.token_mask || a.token_mask[tt] != 0);
-        next_id = tt < end && l < a.k ? a.topk_ids[(size_t)tt * a.k + l] : -1;
-      };
-      fetch(t + grp);
+      if (next_at != t) fetch(t);
 #pragma unroll 1
       for (int t0 = t; t0 < end; t0 += TPW) {
         const int tt = t0 + grp;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) v[i] = next[i];
-        const bool on = next_on;
+        const bool on = next_on && tt < end;
         const int id = next_id;
-        fetch(tt + TPW);
+        fetch(t0 + TPW);
         if (on) {
           if (id >= 0 && id < E) atomicAdd(&hist[id], 1);
           for (int j = l + LPT; j < a.k; j += LPT) {
@@ -188,12 +223,11 @@ __global__ void __launch_bounds__(32 * BAL_MAX_WARPS) balance_fwd_kernel(const B
             if (e >= 0 && e < E) atomicAdd(&hist[e], 1);
           }
         }
-        float p[VPL];
-        const float lse = softmax_row<LPT, VPL>(v, p);
-        if (SIG) sigmoid_row<LPT, VPL>(v, p, nullptr);
+        float ex[VPL], p[SIG ? VPL : 1], inv[2];
+        const float lse = row_terms<LPT, VPL, SIG>(v, ex, p, nullptr, inv);
         if (on) {
 #pragma unroll
-          for (int i = 0; i < VPL; ++i) acc[i] += p[i];
+          for (int i = 0; i < VPL; ++i) acc[i] = SIG ? fmaf(p[SIG ? i : 0], inv[1], acc[i]) : fmaf(ex[i], inv[0], acc[i]);
           if (l == 0) { z = fmaf(lse, lse, z); ++live; }
         }
       }
@@ -203,16 +237,14 @@ __global__ void __launch_bounds__(32 * BAL_MAX_WARPS) balance_fwd_kernel(const B
 #pragma unroll
         for (int i = 0; i < VPL; ++i) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], off);
       }
-      z = group_sum(z, 32);
       live = __reduce_add_sync(0xffffffffu, live);
-      zsum += z;
+      zsum += (double)group_sum(z, 32);
       tokens += live;
       __syncwarp();
       const bool whole = begins >= wa && stop <= wb;
       const int piece = t == wa ? 0 : 1;
       if (!whole && lane == 0) { w_seq[2 * warp + piece] = s; w_n[2 * warp + piece] = live; }
       const float inv = live ? 1.0f / (float)live : 0.f;
-      float dot = 0.f;
       if (grp == 0) {
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
@@ -223,7 +255,7 @@ __global__ void __launch_bounds__(32 * BAL_MAX_WARPS) balance_fwd_kernel(const B
             if (whole) {
               a.counts[(size_t)s * E + e] = c;
               a.prob[(size_t)s * E + e] = acc[i] * inv;
-              dot = fmaf((float)c * inv, acc[i] * inv, dot);
+              my_loss += (double)(unit * ((float)c * inv) * (acc[i] * inv));
             } else {
               w_sum[(2 * warp + piece) * E + e] = acc[i];
               w_cnt[(2 * warp + piece) * E + e] = c;
@@ -231,19 +263,15 @@ __global__ void __launch_bounds__(32 * BAL_MAX_WARPS) balance_fwd_kernel(const B
           }
         }
       }
-      if (whole) {
-        loss += (double)(unit * group_sum(dot, 32));
-        if (lane == 0) a.tokens[s] = live;
-      }
+      if (whole && lane == 0) a.tokens[s] = live;
       __syncwarp();
     }
     t = end;
-    if (t < wb) s = seq_of(a.seq_offsets, n, T, t, lane);
+    if (t < wb) s = seqs.of(t, lane);
   }
-  if (lane == 0) { s_loss[warp] = loss; s_z[warp] = zsum; s_tok[warp] = tokens; }
   // sequences without tokens belong to no warp's range
   for (int q = blockIdx.x * warps + warp; q < n; q += gridDim.x * warps)
-    if (seq_begin(a.seq_offsets, q, T) >= seq_begin(a.seq_offsets, q + 1, T)) {
+    if (seqs.begin(q) >= seqs.begin(q + 1)) {
       for (int e = lane; e < E; e += 32) {
         a.counts[(size_t)q * E + e] = 0;
         a.prob[(size_t)q * E + e] = 0.f;
@@ -252,142 +280,215 @@ __global__ void __launch_bounds__(32 * BAL_MAX_WARPS) balance_fwd_kernel(const B
     }
   __syncthreads();
 
-  // ---- the warps' pieces in order: every thread has its experts
+  // ---- the warps' pieces: which of them are one sequence ..
   const size_t slot_ints = 2 * (size_t)E;
   BalBlock* const meta = reinterpret_cast<BalBlock*>(a.scratch);
   float* const slots = reinterpret_cast<float*>(meta + gridDim.x);   // [block][2][psum | count]
-  double my_loss = 0.0;
-  if (threadIdx.x == 0) {
-    BalBlock m{{-1, -1}, {0, 0}, 0.0, 0.0, 0};
-    for (int w = 0; w < warps; ++w) { m.loss += s_loss[w]; m.z += s_z[w]; m.tokens += s_tok[w]; }
-    int q = 0;
-    while (q < 2 * warps) {
-      if (w_seq[q] < 0) { ++q; continue; }
-      const int sq = w_seq[q];
-      int live = 0;
-      while (q < 2 * warps && (w_seq[q] < 0 || w_seq[q] == sq)) { if (w_seq[q] == sq) live += w_n[q]; ++q; }
-      const int begins = seq_begin(a.seq_offsets, sq, T), stop = seq_begin(a.seq_offsets, sq + 1, T);
-      if (begins >= b0 && stop <= b1) a.tokens[sq] = live;
-      else { const int h = begins < b0 ? 0 : 1; m.seq[h] = sq; m.n[h] = live; }
+  if (warp == 0) {
+    // lane w has both of warp w
+    int sq[2], ln[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      sq[h] = lane < warps ? w_seq[2 * lane + h] : -1;
+      ln[h] = sq[h] >= 0 ? w_n[2 * lane + h] : 0;
     }
-    meta[blockIdx.x] = m;
-  }
-  for (int e = threadIdx.x; e < E; e += blockDim.x) {
-    int q = 0;
-    while (q < 2 * warps) {
-      if (w_seq[q] < 0) { ++q; continue; }
-      const int sq = w_seq[q];
-      float sum = 0.f;
-      int cnt = 0, live = 0;
-      while (q < 2 * warps && (w_seq[q] < 0 || w_seq[q] == sq)) {
-        if (w_seq[q] == sq) { sum += w_sum[q * E + e]; cnt += w_cnt[q * E + e]; live += w_n[q]; }
-        ++q;
-      }
-      const int begins = seq_begin(a.seq_offsets, sq, T), stop = seq_begin(a.seq_offsets, sq + 1, T);
-      if (begins >= b0 && stop <= b1) {
-        const float inv = live ? 1.0f / (float)live : 0.f;
-        a.counts[(size_t)sq * E + e] = cnt;
-        a.prob[(size_t)sq * E + e] = sum * inv;
-        my_loss += (double)(unit * ((float)cnt * inv) * (sum * inv));
-      } else {
-        float* at = slots + (2 * (size_t)blockIdx.x + (begins < b0 ? 0 : 1)) * slot_ints;
-        at[e] = sum;
-        reinterpret_cast<int*>(at)[E + e] = cnt;
-      }
+    const uint32_t any = __ballot_sync(0xffffffffu, sq[0] >= 0 || sq[1] >= 0), before = any & ((1u << lane) - 1u);
+    const int tail = __shfl_sync(0xffffffffu, sq[1] >= 0 ? sq[1] : sq[0], before ? 31 - __clz(before) : 0);   // of the last lane in front
+    int prev = before ? tail : -1;
+    int run = ln[0] + ln[1];
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, run, off);
+      if (lane >= off) run += o;
     }
+    const int ahead = run - ln[0] - ln[1];   // tokens of the lanes in front
+    bool starts[2];
+    uint32_t start[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      starts[h] = sq[h] >= 0 && sq[h] != prev;
+      if (sq[h] >= 0) prev = sq[h];
+      start[h] = __ballot_sync(0xffffffffu, starts[h]);
+    }
+    if (lane < 2) b_seq[lane] = -1;
+    __syncwarp();
+    const int count = __popc(start[0]) + __popc(start[1]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (starts[h]) {
+        const uint32_t below = (1u << lane) - 1u;
+        const int i = __popc(start[0] & (h ? below | (1u << lane) : below)) + __popc(start[1] & below);
+        const int begins = seqs.begin(sq[h]), stop = seqs.begin(sq[h] + 1);
+        g_seq[i] = sq[h];
+        g_from[i] = 2 * lane + h;
+        g_n[i] = ahead + (h ? ln[0] : 0);   // tokens in front of it, until all are known
+        g_to[i] = begins >= b0 && stop <= b1 ? 2 : begins < b0 ? 0 : 1;
+      }
+    const int all = __shfl_sync(0xffffffffu, run, 31);
+    if (lane == 0) { g_count = count; g_from[count] = 2 * warps; }
+    const uint32_t v0 = __ballot_sync(0xffffffffu, sq[0] >= 0), v1 = __ballot_sync(0xffffffffu, sq[1] >= 0);
+    if (lane < 2) reinterpret_cast<uint32_t*>(&g_valid)[lane] = lane ? v1 : v0;
+    __syncwarp();
+    int live[2] = {0, 0};
+    for (int i = lane, r = 0; i < count; i += 32, ++r) live[r] = (i + 1 < count ? g_n[i + 1] : all) - g_n[i];
+    __syncwarp();
+    for (int i = lane, r = 0; i < count; i += 32, ++r) {
+      g_n[i] = live[r];
+      if (g_to[i] == 2) a.tokens[g_seq[i]] = live[r];
+      else { b_seq[g_to[i]] = g_seq[i]; meta[blockIdx.x].n[g_to[i]] = live[r]; }
+    }
+    __syncwarp();
+    if (lane < 2) meta[blockIdx.x].seq[lane] = b_seq[lane];
   }
   __syncthreads();
-  auto block_sum = [&](double v) -> double {   // fixed order; the result in thread 0
-    for (int off = 16; off; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-    if (lane == 0) s_loss[warp] = v;
+  // .. and their sums in order: every thread has an expert, and a range of the pieces where threads are left
+  const int parts = max(1, min(warps / 2, (int)blockDim.x / E)), part = (int)threadIdx.x / E;
+  float* const p_sum = reinterpret_cast<float*>(bsm);   // [parts][E], in place of the histograms
+  int* const p_cnt = bsm + parts * E;
+  // sums over [from, until) of what `at` gives for a piece and an expert, handed to `put`
+  auto pieces = [&](int from, int until, auto at, auto put) {
+    if (parts == 1) {
+      for (int e = threadIdx.x; e < E; e += blockDim.x) {
+        float sum = 0.f;
+        int cnt = 0;
+#pragma unroll 8
+        for (int q = from; q < until; ++q) at(q, e, sum, cnt);
+        put(e, sum, cnt);
+      }
+      return;
+    }
+    const int e = (int)threadIdx.x - part * E, len = (until - from + parts - 1) / parts;
+    if (part < parts) {
+      float sum = 0.f;
+      int cnt = 0;
+      const int q0 = min(from + part * len, until), q1 = min(q0 + len, until);
+#pragma unroll 8
+      for (int q = q0; q < q1; ++q) at(q, e, sum, cnt);
+      p_sum[threadIdx.x] = sum;
+      p_cnt[threadIdx.x] = cnt;
+    }
     __syncthreads();
-    double r = 0.0;
-    if (threadIdx.x == 0)
-      for (int w = 0; w < warps; ++w) r += s_loss[w];
+    if (part == 0) {
+      float sum = 0.f;
+      int cnt = 0;
+      for (int q = 0; q < parts; ++q) { sum += p_sum[q * E + e]; cnt += p_cnt[q * E + e]; }
+      put(e, sum, cnt);
+    }
     __syncthreads();
-    return r;
   };
-  my_loss = block_sum(my_loss);
-  if (threadIdx.x == 0) meta[blockIdx.x].loss += my_loss;
+  for (int i = 0; i < g_count; ++i) {
+    const int sq = g_seq[i], to = g_to[i];
+    const float inv = g_n[i] ? 1.0f / (float)g_n[i] : 0.f;
+    const uint32_t v0 = (uint32_t)g_valid, v1 = (uint32_t)(g_valid >> 32);
+    float* const slot = slots + (2 * (size_t)blockIdx.x + (to & 1)) * slot_ints;
+    pieces(g_from[i], g_from[i + 1],
+           [&](int q, int e, float& sum, int& cnt) {   // (a piece that is not there holds anything)
+             const float x = w_sum[q * E + e];
+             const int c = w_cnt[q * E + e];
+             const bool there = (q & 1 ? v1 : v0) >> (q >> 1) & 1;
+             sum += there ? x : 0.f;
+             cnt += there ? c : 0;
+           },
+           [&](int e, float sum, int cnt) {
+             if (to == 2) {
+               a.counts[(size_t)sq * E + e] = cnt;
+               a.prob[(size_t)sq * E + e] = sum * inv;
+               my_loss += (double)(unit * ((float)cnt * inv) * (sum * inv));
+             } else {
+               __stcg(slot + e, sum);
+               __stcg(reinterpret_cast<int*>(slot) + E + e, cnt);
+             }
+           });
+  }
 
   // ---- a sequence over several blocks: its pieces in order, by the block whose piece arrives last.  The block that holds its
   // first token has it as second piece and its ticket, the others have it as first piece.
   const int nb = gridDim.x;
-  auto block_of = [&](int t) {   // floor(T i / nb) <= t, the largest such i
-    int i = (int)((long long)t * nb / T);
-    while (i + 1 < nb && (long long)T * (i + 1) / nb <= t) ++i;
-    return i;
+  auto block_of = [&](int t) { return t / a.chunk; };
+  auto join = [&](int sq) {   // fills the sequence's outputs and adds the threads' shares of the loss
+    const int first = block_of(seqs.begin(sq)), last = block_of(seqs.begin(sq + 1) - 1);
+    if (warp == warps - 1) {
+      int live = 0;
+      for (int q = first + lane; q <= last; q += 32) live += __ldcg(&meta[q].n[q == first ? 1 : 0]);
+      live = __reduce_add_sync(0xffffffffu, live);
+      if (lane == 0) { s_live = live; a.tokens[sq] = live; }
+    }
+    __syncthreads();
+    const float inv = s_live ? 1.0f / (float)s_live : 0.f;
+    pieces(first, last + 1,
+           [&](int q, int e, float& sum, int& cnt) {
+             const float* at = slots + (2 * (size_t)q + (q == first ? 1 : 0)) * slot_ints;
+             sum += __ldcg(at + e);
+             cnt += __ldcg(reinterpret_cast<const int*>(at) + E + e);
+           },
+           [&](int e, float sum, int cnt) {
+             a.counts[(size_t)sq * E + e] = cnt;
+             a.prob[(size_t)sq * E + e] = sum * inv;
+             my_loss += (double)(unit * ((float)cnt * inv) * (sum * inv));
+           });
   };
-  auto arrive = [&](int* ticket, int expected) -> bool {   // of the whole block; true: everybody else has been
+  // the sums of three values over the block, in thread 0; the order is fixed
+  auto block_sums = [&](double x, double y, double w, double (&r)[3]) {
+#pragma unroll
+    for (int off = 16; off; off >>= 1) {
+      x += __shfl_xor_sync(0xffffffffu, x, off);
+      y += __shfl_xor_sync(0xffffffffu, y, off);
+      w += __shfl_xor_sync(0xffffffffu, w, off);
+    }
+    __syncthreads();
+    if (lane == 0) { s_sum[0][warp] = x; s_sum[1][warp] = y; s_sum[2][warp] = w; }
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        r[i] = lane < warps ? s_sum[i][lane] : 0.0;
+#pragma unroll
+        for (int off = 16; off; off >>= 1) r[i] += __shfl_xor_sync(0xffffffffu, r[i], off);
+      }
+    }
+  };
+  if (n > 1 && nb > 1) {
     __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) s_last = atomicAdd(ticket, 1) == expected - 1;
-    __syncthreads();
-    const bool last = s_last != 0;
-    if (last) __threadfence();
-    return last;
-  };
-  const int parts = max(1, min(2 * warps, (int)blockDim.x / E));
-  auto join = [&](int sq) -> double {   // fills the sequence's outputs; its share of the loss
-    const int first = block_of(seq_begin(a.seq_offsets, sq, T)), last = block_of(seq_begin(a.seq_offsets, sq + 1, T) - 1);
-    int live = 0;
-    for (int q = first + threadIdx.x; q <= last; q += blockDim.x) live += __ldcg(&meta[q].n[q == first ? 1 : 0]);
-    live = (int)block_sum((double)live);
-    if (threadIdx.x == 0) { s_last = live; a.tokens[sq] = live; }
-    // the experts, and ranges of the blocks where threads are left
-    const int nq = last - first + 1, part = (int)threadIdx.x / E;
-    const bool split = parts > 1;
-    const int q0 = first + (split ? (int)((long long)nq * part / parts) : 0), q1 = first + (split ? (int)((long long)nq * (part + 1) / parts) : nq);
-    auto sums = [&](int e, float* sum, int* cnt) {
-      float v = 0.f;
-      int c = 0;
-#pragma unroll 8
-      for (int q = q0; q < q1; ++q) {
-        const float* at = slots + (2 * (size_t)q + (q == first ? 1 : 0)) * slot_ints;
-        v += __ldcg(at + e);
-        c += __ldcg(reinterpret_cast<const int*>(at) + E + e);
+    if (threadIdx.x < 2) {
+      const int sq = b_seq[threadIdx.x];
+      int last_one = 0;
+      if (sq >= 0) {
+        const int first = block_of(seqs.begin(sq)), last = block_of(seqs.begin(sq + 1) - 1);
+        if (last > first && (int)blockIdx.x >= first && (int)blockIdx.x <= last)   // (else offsets that do not ascend)
+          last_one = atomicAdd(a.tickets + 1 + first, 1) == last - first;
       }
-      *sum = v;
-      *cnt = c;
-    };
-    float* const p_sum = w_sum;   // [parts][E]
-    int* const p_cnt = w_cnt;
-    if (split && part < parts) sums((int)threadIdx.x % E, &p_sum[threadIdx.x], &p_cnt[threadIdx.x]);
-    __syncthreads();
-    live = s_last;
-    const float inv = live ? 1.0f / (float)live : 0.f;
-    double share = 0.0;
-    for (int e = threadIdx.x; e < E; e += blockDim.x) {
-      float sum = 0.f;
-      int cnt = 0;
-      if (split) {
-        for (int q = 0; q < parts; ++q) { sum += p_sum[q * E + e]; cnt += p_cnt[q * E + e]; }
-      } else {
-        sums(e, &sum, &cnt);
-      }
-      a.counts[(size_t)sq * E + e] = cnt;
-      a.prob[(size_t)sq * E + e] = sum * inv;
-      share += (double)(unit * ((float)cnt * inv) * (sum * inv));
+      s_last[threadIdx.x] = last_one;
     }
     __syncthreads();
-    return block_sum(share);
-  };
-  if (n > 1) {
 #pragma unroll 1
-    for (int h = 0; h < 2; ++h) {
-      __syncthreads();
-      const int sq = meta[blockIdx.x].seq[h];
-      if (sq < 0) continue;
-      const int begins = seq_begin(a.seq_offsets, sq, T), stop = seq_begin(a.seq_offsets, sq + 1, T);
-      const int first = block_of(begins), last = block_of(stop - 1);
-      if (last <= first || (int)blockIdx.x < first || (int)blockIdx.x > last) continue;   // (offsets that do not ascend)
-      if (arrive(a.tickets + 1 + first, last - first + 1)) {
-        const double share = join(sq);
-        if (threadIdx.x == 0) meta[blockIdx.x].loss += share;
+    for (int h = 0; h < 2; ++h)
+      if (s_last[h]) {
+        __threadfence();
+        join(b_seq[h]);
       }
-    }
   }
-  if (!arrive(a.tickets, nb)) return;
+  // the warps' z and tokens: lane 0 of each has them still
+  double r[3];
+  block_sums(my_loss, lane == 0 ? zsum : 0.0, lane == 0 ? (double)tokens : 0.0, r);
+  auto finish = [&]() {
+    if (threadIdx.x == 0) {
+      a.losses[0] = (float)r[0];
+      a.losses[1] = r[2] > 0.0 ? (float)(r[1] / r[2]) : 0.f;
+      a.tokens[n] = (int)r[2];
+    }
+  };
+  if (nb == 1) return finish();
+  if (threadIdx.x == 0) {
+    BalBlock& m = meta[blockIdx.x];
+    m.loss = r[0]; m.z = r[1]; m.tokens = r[2];
+  }
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) s_last[2] = atomicAdd(a.tickets, 1) == nb - 1;
+  __syncthreads();
+  if (!s_last[2]) return;
+  __threadfence();
 
   // ---- the last block of all
   for (int i = threadIdx.x; i <= nb; i += blockDim.x) a.tickets[i] = 0;   // for the next call
@@ -395,23 +496,18 @@ __global__ void __launch_bounds__(32 * BAL_MAX_WARPS) balance_fwd_kernel(const B
   for (int b = threadIdx.x; b < nb; b += blockDim.x) {
     total += __ldcg(&meta[b].loss);
     total_z += __ldcg(&meta[b].z);
-    total_tokens += (double)__ldcg(&meta[b].tokens);
+    total_tokens += __ldcg(&meta[b].tokens);
   }
-  if (n == 1 && nb > 1) {
-    const int begins = seq_begin(a.seq_offsets, 0, T), stop = seq_begin(a.seq_offsets, 1, T);
+  if (n == 1) {
+    const int begins = seqs.begin(0), stop = seqs.begin(1);
     if (begins < stop && block_of(begins) < block_of(stop - 1)) {
-      const double share = join(0);
-      if (threadIdx.x == 0) total += share;
+      my_loss = 0.0;
+      join(0);
+      total += my_loss;
     }
   }
-  total = block_sum(total);
-  total_z = block_sum(total_z);
-  total_tokens = block_sum(total_tokens);
-  if (threadIdx.x == 0) {
-    a.losses[0] = (float)total;
-    a.losses[1] = total_tokens > 0.0 ? (float)(total_z / total_tokens) : 0.f;
-    a.tokens[n] = (int)total_tokens;
-  }
+  block_sums(total, total_z, total_tokens, r);
+  finish();
 }
 
 // ------------------------------------------------------------------------------------------
@@ -424,6 +520,7 @@ template <int LPT, int VPL, int VW, bool SIG>
 __global__ void __launch_bounds__(32 * BAL_BWD_WARPS) balance_bwd_kernel(const BalanceArgs a) {
   constexpr int TPW = 32 / LPT;
   extern __shared__ __align__(16) float fsm[];
+  __shared__ int offsets[BAL_STAGED];
   const int E = a.E, n = a.n_seq, T = a.T, k = a.k;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPT, grp = lane / LPT;
   constexpr int ROW = LPT * VPL;
@@ -437,50 +534,67 @@ __global__ void __launch_bounds__(32 * BAL_BWD_WARPS) balance_bwd_kernel(const B
   const int gw = blockIdx.x * BAL_BWD_WARPS + warp, nw = gridDim.x * BAL_BWD_WARPS;
   const int wa = (int)((long long)T * gw / nw), wb = (int)((long long)T * (gw + 1) / nw);
   const bool scores = a.d_topk_w != nullptr, renorm = (a.mode & GATE_RENORM) != 0;
-  const float g_bal = a.d_losses[0];
+  // read a round ahead, the first ones while the offsets arrive
+  float v[VPL], next[VPL];
+  int next_id = -1, next_at = wa;
+  float next_g = 0.f;
+  bool next_on = false;
+  auto fetch = [&](int t0) {
+    const int tt = t0 + grp;
+    const bool in = tt < wb;
+    next_at = t0;
+    load_row<LPT, VPL, VW>(a.logits + (size_t)tt * E, E, l, in, next);
+    next_on = in && (!a.token_mask || a.token_mask[tt] != 0);
+    if (scores) {
+      next_id = in && l < k ? a.topk_ids[(size_t)tt * k + l] : -1;
+      next_g = in && l < k ? a.d_topk_w[(size_t)tt * k + l] : 0.f;
+    }
+  };
+  fetch(wa);
+  const float g_bal = a.d_losses[0], g_zl = a.d_losses[1];
   const int total = a.tokens[n];
-  const float g_z = total > 0 ? 2.0f * a.d_losses[1] / (float)total : 0.f;
-  int s = wa < wb ? seq_of(a.seq_offsets, n, T, wa, lane) : n;
+  stage_offsets(a, offsets);
+  __syncthreads();
+  const SeqTable seqs = seq_table(a, offsets);
+  const float g_z = total > 0 ? 2.0f * g_zl / (float)total : 0.f;
+  int s = wa < wb ? seqs.of(wa, lane) : n;
   for (int t = wa; t < wb;) {
-    int stop = s < n ? seq_begin(a.seq_offsets, s + 1, T) : T;
+    int stop = s < n ? seqs.begin(s + 1) : T;
     if (stop <= t) stop = t + 1;   // (offsets that do not ascend)
     const int end = min(stop, wb);
     const bool inside = s >= 0 && s < n;
     float x[VPL];
     const float ns = inside ? (float)a.tokens[s] : 0.f;
-    const float unit = ns > 0.f ? g_bal * (float)E / ((float)k * (float)n) / ns / ns : 0.f;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
       const int e = expert_at<LPT, VW>(i, l);
-      x[i] = inside && e < E ? unit * (float)a.counts[(size_t)s * E + e] : 0.f;
+      x[i] = inside && e < E ? (float)a.counts[(size_t)s * E + e] : 0.f;
     }
-    float v[VPL], next[VPL];
-    int next_id = -1;
-    float next_g = 0.f;
-    bool next_on = false;
-    auto fetch = [&](int tt) {
-      const bool in = tt < end;
-      load_row<LPT, VPL, VW>(a.logits + (size_t)tt * E, E, l, in, next);
-      next_on = inside && in && (!a.token_mask || a.token_mask[tt] != 0);
-      if (scores) {
-        next_id = in && l < k ? a.topk_ids[(size_t)tt * k + l] : -1;
-        next_g = in && l < k ? a.d_topk_w[(size_t)tt * k + l] : 0.f;
-      }
-    };
-    fetch(t + grp);
+    const float unit = ns > 0.f ? g_bal * (float)E / ((float)k * (float)n) / ns / ns : 0.f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) x[i] *= unit;
+    if (next_at != t) fetch(t);
 #pragma unroll 1
     for (int t0 = t; t0 < end; t0 += TPW) {
       const int tt = t0 + grp;
 #pragma unroll
       for (int i = 0; i < VPL; ++i) v[i] = next[i];
-      const bool on = next_on;
+      const bool on = next_on && inside;
       const int id = next_id;
       const float g = next_g;
-      fetch(tt + TPW);
-      float soft[VPL], p[SIG ? VPL : 1], sig[SIG ? VPL : 1], d[VPL];
-      const float lse = softmax_row<LPT, VPL>(v, soft);
-      if constexpr (SIG) sigmoid_row<LPT, VPL>(v, p, sig);
-      // ---- the scores' share: lane l of the group has the ids l, l + LPT, ..
+      fetch(t0 + TPW);
+      float soft[VPL], p[SIG ? VPL : 1], sig[SIG ? VPL : 1], inv[2];
+      const float lse = row_terms<LPT, VPL, SIG>(v, soft, p, sig, inv);
+      float sum[3] = {0.f, 0.f, 0.f};   // p x; of the selected experts v and g v, v = softmax or sigmoid
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        soft[i] *= inv[0];
+        if constexpr (SIG) p[i] *= inv[1];
+        const int e = expert_at<LPT, VW>(i, l);
+        if (scores && e < E) val[e] = SIG ? sig[SIG ? i : 0] : soft[i];
+        if (on) sum[0] = fmaf(SIG ? p[SIG ? i : 0] : soft[i], x[i], sum[0]);
+      }
+      // lane l of the group has the ids l, l + LPT, ..
       auto each = [&](auto body) {
         if (tt < end)
           for (int j = l; j < k; j += LPT) {
@@ -489,47 +603,30 @@ __global__ void __launch_bounds__(32 * BAL_BWD_WARPS) balance_bwd_kernel(const B
           }
       };
       if (scores) {
-        if (SIG || renorm) {
-#pragma unroll
-          for (int i = 0; i < VPL; ++i) {
-            const int e = expert_at<LPT, VW>(i, l);
-            if (e < E) val[e] = SIG ? sig[SIG ? i : 0] : soft[i];
-          }
-          __syncwarp();
-          float Z = 0.f, dot = 0.f;
-          if (renorm) {
-            each([&](int e, float) { Z += val[e]; });
-            Z = group_sum(Z, LPT);
-            const float inv = Z > 0.f ? 1.0f / Z : 0.f;
-            each([&](int e, float ge) { dot = fmaf(ge, val[e] * inv, dot); });
-            dot = group_sum(dot, LPT);
-            each([&](int e, float ge) { const float w = val[e] * inv; atomicAdd(&add[e], w * (ge - dot) * (SIG ? 1.0f - val[e] : 1.0f)); });
-          } else {
-            each([&](int e, float ge) { atomicAdd(&add[e], ge * val[e] * (1.0f - val[e])); });
-          }
-        } else {
-          each([&](int e, float ge) { atomicAdd(&add[e], ge); });   // joins x: both are gradients of the softmax
+        __syncwarp();
+        each([&](int e, float ge) { sum[1] += val[e]; sum[2] = fmaf(ge, val[e], sum[2]); });
+      }
+      group_sums<LPT>(sum);
+      float dense = sum[0];
+      if (scores) {
+        if (renorm) {   // w = v / sum v:  w (g - sum g w)
+          const float iz = sum[1] > 0.f ? __fdividef(1.0f, sum[1]) : 0.f, dot = sum[2] * iz;
+          each([&](int e, float ge) { atomicAdd(&add[e], val[e] * iz * (ge - dot) * (SIG ? 1.0f - val[e] : 1.0f)); });
+        } else if (SIG) {
+          each([&](int e, float ge) { atomicAdd(&add[e], ge * val[e] * (1.0f - val[e])); });
+        } else {        // a gradient of the same softmax as x
+          dense += sum[2];
+          each([&](int e, float ge) { atomicAdd(&add[e], ge * val[e]); });
         }
         __syncwarp();
       }
-      // ---- the whole gradient
-      float q[VPL], dot = 0.f;
-      const bool joins = scores && !SIG && !renorm;
+      const float zc = on ? g_z * lse : 0.f;
+      float d[VPL];
 #pragma unroll
       for (int i = 0; i < VPL; ++i) {
         const int e = expert_at<LPT, VW>(i, l);
-        const float more = scores && e < E ? add[e] : 0.f;
-        const float xi = (on ? x[i] : 0.f) + (joins ? more : 0.f);
-        d[i] = joins ? 0.f : more;
-        q[i] = xi;
-        dot = fmaf(SIG ? p[SIG ? i : 0] : soft[i], xi, dot);
-      }
-      dot = group_sum(dot, LPT);
-      const float zc = on ? g_z * lse : 0.f;
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) {
         const float pi = SIG ? p[SIG ? i : 0] * (1.0f - sig[SIG ? i : 0]) : soft[i];
-        d[i] = fmaf(pi, q[i] - dot, fmaf(zc, soft[i], d[i]));
+        d[i] = fmaf(pi, (on ? x[i] : 0.f) - dense, fmaf(zc, soft[i], scores && e < E ? add[e] : 0.f));
       }
       if (scores) {
         __syncwarp();
@@ -549,7 +646,7 @@ __global__ void __launch_bounds__(32 * BAL_BWD_WARPS) balance_bwd_kernel(const B
       __syncwarp();
     }
     t = end;
-    if (t < wb) s = seq_of(a.seq_offsets, n, T, t, lane);
+    if (t < wb) s = seqs.of(t, lane);
   }
 }
 
@@ -560,10 +657,10 @@ static cudaError_t with_balance_shape(int E, bool vec, F f) {
 #define MOE_BAL_CASE(LPT, VPL) return vec ? f(std::integral_constant<int, LPT>(), std::integral_constant<int, VPL>(), std::integral_constant<int, 4>()) \
                                           : f(std::integral_constant<int, LPT>(), std::integral_constant<int, VPL>(), std::integral_constant<int, 1>())
   if (E <= 8) MOE_BAL_CASE(1, 8);
-  if (E <= 32) MOE_BAL_CASE(4, 8);
-  if (E <= 64) MOE_BAL_CASE(8, 8);
-  if (E <= 128) MOE_BAL_CASE(16, 8);
-  if (E <= 256) MOE_BAL_CASE(32, 8);
+  if (E <= 32) MOE_BAL_CASE(2, 16);
+  if (E <= 64) MOE_BAL_CASE(4, 16);
+  if (E <= 128) MOE_BAL_CASE(8, 16);
+  if (E <= 256) MOE_BAL_CASE(16, 16);
   if (E <= 512) MOE_BAL_CASE(32, 16);
   MOE_BAL_CASE(32, 32);
 #undef MOE_BAL_CASE
@@ -571,27 +668,37 @@ static cudaError_t with_balance_shape(int E, bool vec, F f) {
 
 static bool rows_of_vectors(const void* p, int E) { return E % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-int balance_fwd_blocks(int T, int E) {
-  const long bytes = (long)T * E * 4;
-  long b = (bytes + BAL_BLOCK_BYTES - 1) / BAL_BLOCK_BYTES;
-  if (b > BAL_MAX_BLOCKS) b = BAL_MAX_BLOCKS;
-  if (b > T) b = T;
-  return b < 1 ? 1 : (int)b;
+static int balance_warps(int E) {
+  int warps = balance_warps_most(E <= 8 ? 8 : E <= 512 ? 16 : 32);
+  while (warps > 4 && 5 * warps * E * (int)sizeof(int) > BAL_SMEM) warps >>= 1;
+  return warps;
 }
-size_t balance_scratch_bytes(int T_max, int E) {
-  return (size_t)balance_fwd_blocks(T_max, E) * (sizeof(BalBlock) + 4 * (size_t)E * sizeof(int));
+// Tokens of a block: as many blocks as leave every warp a round of tokens, up to one an SM (few tokens are bound by the latencies of
+// a round).
+static int balance_chunk(int T, int E) {
+  int lpt = 1;
+  while (lpt < 32 && (E <= 8 ? 8 : 16) * lpt < E) lpt <<= 1;
+  const int per_block = balance_warps(E) * (32 / lpt), even = (T + BAL_MAX_BLOCKS - 1) / BAL_MAX_BLOCKS;
+  return even > per_block ? even : per_block;
+}
+static int balance_fwd_blocks(int T, int E) {
+  const int chunk = balance_chunk(T, E);
+  return T > chunk ? (T + chunk - 1) / chunk : 1;
+}
+size_t balance_scratch_bytes(int E) {
+  return (size_t)BAL_MAX_BLOCKS * (sizeof(BalBlock) + 4 * (size_t)E * sizeof(int));
 }
 
-cudaError_t launch_balance_fwd(const BalanceArgs& a, cudaStream_t s, int* launches) {
-  int warps = BAL_MAX_WARPS;
-  while (warps > 4 && 5 * warps * a.E * (int)sizeof(int) > 96 * 1024) warps >>= 1;
+cudaError_t launch_balance_fwd(BalanceArgs a, cudaStream_t s, int* launches) {
+  a.chunk = balance_chunk(a.T, a.E);
+  const int warps = balance_warps(a.E);
   const size_t smem = 5 * (size_t)warps * a.E * sizeof(int);
   const int blocks = balance_fwd_blocks(a.T, a.E);
   return with_balance_shape(a.E, rows_of_vectors(a.logits, a.E), [&](auto lpt, auto vpl, auto vw) -> cudaError_t {
     auto go = [&](auto sig) -> cudaError_t {
       constexpr auto kernel = balance_fwd_kernel<lpt(), vpl(), vw(), sig()>;
-      if (smem > 48 * 1024)
-        if (cudaError_t e = opt_in_smem<kernel>(100 * 1024)) return e;
+      if (smem > 32 * 1024)   // (static shared memory counts too)
+        if (cudaError_t e = opt_in_smem<kernel>(BAL_SMEM)) return e;
       ++*launches;
       return launch_dependent(kernel, dim3(blocks), dim3(warps * 32), smem, s, a);
     };
@@ -599,19 +706,20 @@ cudaError_t launch_balance_fwd(const BalanceArgs& a, cudaStream_t s, int* launch
   });
 }
 
-cudaError_t launch_balance_bwd(const BalanceArgs& a, cudaStream_t s, int* launches) {
+cudaError_t launch_balance_bwd(const BalanceArgs& a, int num_sms, cudaStream_t s, int* launches) {
   const bool vec = rows_of_vectors(a.logits, a.E) && rows_of_vectors(a.d_logits, a.E);
   return with_balance_shape(a.E, vec, [&](auto lpt, auto vpl, auto vw) -> cudaError_t {
     constexpr size_t smem = 2 * sizeof(float) * (size_t)BAL_BWD_WARPS * 32 * vpl();
     const int per_block = BAL_BWD_WARPS * (32 / lpt());   // tokens of a round
     int blocks = (a.T + per_block - 1) / per_block;
-    if (blocks > BAL_BWD_MAX_BLOCKS) blocks = BAL_BWD_MAX_BLOCKS;
     auto go = [&](auto sig) -> cudaError_t {
       constexpr auto kernel = balance_bwd_kernel<lpt(), vpl(), vw(), sig()>;
-      if (smem > 48 * 1024)
+      if (smem > 32 * 1024)   // (static shared memory counts too)
         if (cudaError_t e = opt_in_smem<kernel>((int)smem)) return e;
+      int resident = 0;   // one wave: a second one, a third full, cost as much as the first
+      if (cudaError_t e = blocks_per_sm<kernel>(32 * BAL_BWD_WARPS, smem, &resident)) return e;
       ++*launches;
-      return launch_dependent(kernel, dim3(blocks), dim3(32 * BAL_BWD_WARPS), smem, s, a);
+      return launch_dependent(kernel, dim3(blocks < resident * num_sms ? blocks : resident * num_sms), dim3(32 * BAL_BWD_WARPS), smem, s, a);
     };
     return (a.mode & GATE_SIGMOID) ? go(std::true_type()) : go(std::false_type());
   });

@@ -35,6 +35,24 @@ cudaError_t opt_in_smem(int bytes) {
   return e;
 }
 
+// Blocks of a kernel that an SM holds together; asked once per device.
+template <auto Kernel>
+cudaError_t blocks_per_sm(int threads, size_t smem, int* blocks) {
+  static std::atomic<int> known[MAX_DEVICES];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, Kernel, threads, smem)) != cudaSuccess) return e;
+    if (n < 1) n = 1;
+    known[dev].store(n, std::memory_order_relaxed);
+  }
+  *blocks = n;
+  return cudaSuccess;
+}
+
 template <class Kernel, class Args>
 cudaError_t launch_on_pairs(PairLaunchState& st, Kernel kernel, const Args& args, int threads, size_t smem_bytes,
                             int num_sms, cudaStream_t s, bool dependent = false) {

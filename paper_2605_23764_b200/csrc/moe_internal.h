@@ -213,15 +213,15 @@ cudaError_t launch_router_bwd(const float* logits, const int* ids, const float* 
                               float* dlogits, cudaStream_t s, int* launches);
 
 // Balance losses of the router (balance.cu)
-constexpr int BAL_BLOCK_BYTES = 64 * 1024;   // logits of a block, at least
-constexpr int BAL_MAX_BLOCKS = 2 * 148;
-constexpr int BAL_BWD_MAX_BLOCKS = 4 * 148;
+constexpr int BAL_MAX_BLOCKS = 148;
+constexpr int BAL_SMEM = 200 * 1024;
 struct BalanceArgs {
   const float* logits;         // [T][E]
   const int* topk_ids;         // [T][k]
   const int* seq_offsets;      // [n_seq + 1]; NULL: the batch is one sequence
   const uint8_t* token_mask;   // [T]; NULL: every token counts
   int T, E, k, n_seq, mode;    // mode: GATE_RENORM | GATE_SIGMOID
+  int chunk;                   // tokens of a forward block; filled by the launch
   // forward's outputs; counts and tokens are the backward's inputs
   float* losses;               // [2] balance, z
   int* counts;                 // [n_seq][E]
@@ -234,10 +234,9 @@ struct BalanceArgs {
   const float* d_topk_w;       // [T][k]; NULL: without the scores' gradient
   float* d_logits;             // [T][E]
 };
-int balance_fwd_blocks(int T, int E);
-size_t balance_scratch_bytes(int T_max, int E);
-cudaError_t launch_balance_fwd(const BalanceArgs& a, cudaStream_t s, int* launches);
-cudaError_t launch_balance_bwd(const BalanceArgs& a, cudaStream_t s, int* launches);
+size_t balance_scratch_bytes(int E);
+cudaError_t launch_balance_fwd(BalanceArgs a, cudaStream_t s, int* launches);
+cudaError_t launch_balance_bwd(const BalanceArgs& a, int num_sms, cudaStream_t s, int* launches);
 
 int vector_warps();   // vector warps per CTA of the persistent launch
 // Not a cooperative launch: that attribute holds a launch back until the one in front of it has ended (2 us each: the smallest
