@@ -148,7 +148,7 @@ __device__ __forceinline__ float row_terms(const float (&v)[VPL], float (&ex)[VP
 // Bound by the read of the logits, at few tokens by the latencies of launch, join and last block.
 // ------------------------------------------------------------------------------------------
 // A piece in global memory, two a block: of the sequence that began before the block, of the one that goes on behind it.
-// [block][2] x {float psum[E]; int count[E]}, then per block {seq of both pieces, tokens of both, loss, z, tokens}
+// Per block {seq of both pieces, tokens of both, loss, z, tokens}, then [block][2][E] {sum, count}
 __host__ __device__ constexpr int balance_warps_most(int vpl) { return vpl <= 8 ? BAL_MAX_WARPS : vpl <= 16 ? 24 : 16; }   // registers
 struct BalBlock { int seq[2], n[2]; double loss, z, tokens; };
 
@@ -281,9 +281,8 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
   __syncthreads();
 
   // ---- the warps' pieces: which of them are one sequence ..
-  const size_t slot_ints = 2 * (size_t)E;
   BalBlock* const meta = reinterpret_cast<BalBlock*>(a.scratch);
-  float* const slots = reinterpret_cast<float*>(meta + gridDim.x);   // [block][2][psum | count]
+  float2* const slots = reinterpret_cast<float2*>(meta + gridDim.x);
   if (warp == 0) {
     // lane w has both of warp w
     int sq[2], ln[2];
@@ -362,7 +361,7 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
       float sum = 0.f;
       int cnt = 0;
       const int q0 = min(from + part * len, until), q1 = min(q0 + len, until);
-#pragma unroll 8
+#pragma unroll 16
       for (int q = q0; q < q1; ++q) at(q, e, sum, cnt);
       p_sum[threadIdx.x] = sum;
       p_cnt[threadIdx.x] = cnt;
@@ -380,7 +379,7 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
     const int sq = g_seq[i], to = g_to[i];
     const float inv = g_n[i] ? 1.0f / (float)g_n[i] : 0.f;
     const uint32_t v0 = (uint32_t)g_valid, v1 = (uint32_t)(g_valid >> 32);
-    float* const slot = slots + (2 * (size_t)blockIdx.x + (to & 1)) * slot_ints;
+    float2* const slot = slots + (2 * (size_t)blockIdx.x + (to & 1)) * E;
     pieces(g_from[i], g_from[i + 1],
            [&](int q, int e, float& sum, int& cnt) {   // (a piece that is not there holds anything)
              const float x = w_sum[q * E + e];
@@ -395,8 +394,7 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
                a.prob[(size_t)sq * E + e] = sum * inv;
                my_loss += (double)(unit * ((float)cnt * inv) * (sum * inv));
              } else {
-               __stcg(slot + e, sum);
-               __stcg(reinterpret_cast<int*>(slot) + E + e, cnt);
+               __stcg(slot + e, make_float2(sum, __int_as_float(cnt)));
              }
            });
   }
@@ -407,21 +405,22 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
   auto block_of = [&](int t) { return t / a.chunk; };
   auto join = [&](int sq) {   // fills the sequence's outputs and adds the threads' shares of the loss
     const int first = block_of(seqs.begin(sq)), last = block_of(seqs.begin(sq + 1) - 1);
+    if (parts == 1) __syncthreads();   // (an earlier join's tokens have been used)
     if (warp == warps - 1) {
       int live = 0;
       for (int q = first + lane; q <= last; q += 32) live += __ldcg(&meta[q].n[q == first ? 1 : 0]);
       live = __reduce_add_sync(0xffffffffu, live);
       if (lane == 0) { s_live = live; a.tokens[sq] = live; }
     }
-    __syncthreads();
-    const float inv = s_live ? 1.0f / (float)s_live : 0.f;
+    if (parts == 1) __syncthreads();   // (else there is one between the sums and their use)
     pieces(first, last + 1,
            [&](int q, int e, float& sum, int& cnt) {
-             const float* at = slots + (2 * (size_t)q + (q == first ? 1 : 0)) * slot_ints;
-             sum += __ldcg(at + e);
-             cnt += __ldcg(reinterpret_cast<const int*>(at) + E + e);
+             const float2 x = __ldcg(slots + (2 * (size_t)q + (q == first ? 1 : 0)) * E + e);
+             sum += x.x;
+             cnt += __float_as_int(x.y);
            },
            [&](int e, float sum, int cnt) {
+             const float inv = s_live ? 1.0f / (float)s_live : 0.f;
              a.counts[(size_t)sq * E + e] = cnt;
              a.prob[(size_t)sq * E + e] = sum * inv;
              my_loss += (double)(unit * ((float)cnt * inv) * (sum * inv));
