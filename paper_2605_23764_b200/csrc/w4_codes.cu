@@ -23,22 +23,31 @@ __device__ __forceinline__ CodeTask code_task(int64_t i, int RTS, int chunks) {
   return t;
 }
 
-// natural words [16][CODE_LD] <-> the lane's words of half b of the unit
+// Staged words [16 rows][CODE_LD]: word m of a row has columns 8 m .., the even ones in its low half, the odd ones in its high half --
+// pair c of the four in bits 4 c .. and 16 + 4 c .., where the layout's lanes want them.
+// -> the lane's words of half b of the unit
 __device__ __forceinline__ uint4 gather_words(const uint32_t* st, int b, int lane) {
-  const int g = lane >> 2, c8 = (lane & 3) * 8;
+  const int g = lane >> 2, c4 = (lane & 3) * 4;
   uint32_t out[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int at = 8 * b + 2 * j;
-    const uint32_t by[4] = {st[g * CODE_LD + at] >> c8, st[(g + 8) * CODE_LD + at] >> c8, st[g * CODE_LD + at + 1] >> c8,
-                            st[(g + 8) * CODE_LD + at + 1] >> c8};
+    const uint32_t in[4] = {st[g * CODE_LD + at], st[(g + 8) * CODE_LD + at], st[g * CODE_LD + at + 1], st[(g + 8) * CODE_LD + at + 1]};
     uint32_t w = 0;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) w |= (by[r] & 15u) << (4 * r) | ((by[r] >> 4) & 15u) << (16 + 4 * r);
+    for (int r = 0; r < 4; ++r) w += ((in[r] >> c4) & 0x000F000Fu) << (4 * r);
     out[j] = w;
   }
   return make_uint4(out[0], out[1], out[2], out[3]);
 }
+// Natural codes (two to a byte, the even column in its low half) to and from such a word.
+__device__ __forceinline__ uint32_t squeeze(uint32_t x) {   // the low halves of four bytes side by side
+  x &= 0x0F0F0F0Fu;
+  x = (x | x >> 4) & 0x00FF00FFu;
+  return (x | x >> 8) & 0xFFFFu;
+}
+__device__ __forceinline__ uint32_t split_word(uint32_t natural) { return squeeze(natural) | squeeze(natural >> 4) << 16; }
+// the decoder's way back: natural words
 __device__ __forceinline__ void scatter_words(uint32_t* st, int b, int lane, uint4 v) {
   const int g = lane >> 2, c = lane & 3;
   uint8_t* by = reinterpret_cast<uint8_t*>(st);
@@ -91,43 +100,93 @@ __global__ void __launch_bounds__(32 * CODE_WARPS) w4_encode_kernel(const void* 
         else in[q].x = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(src) + at / 2));
       }
     }
+    // ---- scale and zero point of each row's group, known to its lanes
+    float scale[8], zero[8], inv[8];
+    bool plain = false;   // a scale so small that its reciprocal is none
+    if (QUANT) {
+      float lo[8], hi[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const uint32_t w[4] = {in[q].x, in[q].y, in[q].z, in[q].w};
+        lo[q] = hi[q] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          lo[q] = fminf(lo[q], fminf(bf16lo(w[e]), bf16hi(w[e])));
+          hi[q] = fmaxf(hi[q], fmaxf(bf16lo(w[e]), bf16hi(w[e])));
+        }
+        if (!asym) hi[q] = fmaxf(hi[q], -lo[q]);
+      }
+#pragma unroll
+      for (int off = 8; off; off >>= 1)
+        if (off < gl)
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            if (asym) lo[q] = fminf(lo[q], __shfl_xor_sync(0xffffffffu, lo[q], off));
+            hi[q] = fmaxf(hi[q], __shfl_xor_sync(0xffffffffu, hi[q], off));
+          }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        scale[q] = bf16_round(asym ? __fdiv_rn(hi[q] - lo[q], 15.f) : __fdiv_rn(hi[q], 7.f));
+        const float step = scale[q] > 0.f ? scale[q] : 1.f;
+        zero[q] = asym ? fminf(fmaxf(rintf(__fdiv_rn(-lo[q], step)), 0.f), 15.f) : 8.f;
+        inv[q] = __fdividef(1.0f, step);
+        plain |= step < 1e-30f;
+      }
+    } else {
+      const bool in_matrix = t.chunk * 128 + (m / gl) * s.group < s.cols;   // the group has columns
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int row = s.row_at(t.rt, 16 * t.t + 2 * q + h);
+        scale[q] = 0.f;
+        zero[q] = 8.f;
+        if (in_matrix && row >= 0) {
+          const size_t at = ((size_t)t.m * s.rows + row) * ng_src + grp;
+          scale[q] = __uint_as_float((uint32_t)qs[at] << 16);
+          if (asym) zero[q] = (float)min((int)qz[at], 15);
+        }
+      }
+    }
+    const bool exact = QUANT && __any_sync(0xffffffffu, plain);
+    // ---- codes
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       const int r = 2 * q + h, row = s.row_at(t.rt, 16 * t.t + r);
       uint32_t word;
-      float scale = 0.f, zero = 8.f;
       if (QUANT) {
-        float v[8] = {bf16lo(in[q].x), bf16hi(in[q].x), bf16lo(in[q].y), bf16hi(in[q].y), bf16lo(in[q].z), bf16hi(in[q].z), bf16lo(in[q].w), bf16hi(in[q].w)};
-        float lo = 0.f, hi = 0.f;
+        const uint32_t w[4] = {in[q].x, in[q].y, in[q].z, in[q].w};
+        if (exact) {
+          word = 0;
+          const float step = scale[q] > 0.f ? scale[q] : 1.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { lo = fminf(lo, v[e]); hi = fmaxf(hi, v[e]); }
-        for (int off = gl >> 1; off; off >>= 1) {
-          lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, off));
-          hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, off));
-        }
-        scale = bf16_round(asym ? __fdiv_rn(hi - lo, 15.f) : __fdiv_rn(fmaxf(hi, -lo), 7.f));
-        const float step = scale > 0.f ? scale : 1.f;
-        if (asym) zero = fminf(fmaxf(rintf(__fdiv_rn(-lo, step)), 0.f), 15.f);
-        word = 0;
+          for (int e = 0; e < 8; ++e) {
+            const float v = e & 1 ? bf16hi(w[e >> 1]) : bf16lo(w[e >> 1]);
+            const float code = fminf(fmaxf(rintf(__fdiv_rn(v, step)) + zero[q], 0.f), 15.f);
+            word += (uint32_t)code << (e & 1 ? 16 + 2 * (e - 1) : 2 * e);
+          }
+        } else {
+          // w / s to the nearest whole number, ties to even, without a division.  Both have 8 significant bits, so w / s is a tie or at
+          // least 2^-9 away from one, while w (1 / s) is off by no more than 2^-20: rounded to 2^-11 -- by the sum with 6144 -- it is
+          // exactly the tie, or on its side of it.  The sum with 1.5 x 2^23 then leaves the code in the lowest bits.
+          constexpr float FINE = 6144.f, WHOLE = 12582912.f;
+          uint32_t sum = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float code = fminf(fmaxf(rintf(__fdiv_rn(v[e], step)) + zero, 0.f), 15.f);
-          word |= (uint32_t)code << (4 * e);
+          for (int e = 0; e < 8; ++e) {
+            const float v = e & 1 ? bf16hi(w[e >> 1]) : bf16lo(w[e >> 1]);
+            float y = __fadd_rn(__fadd_rn(__fmaf_rn(v, inv[q], FINE), -FINE), WHOLE);   // the whole number
+            if (asym) y = fminf(fmaxf(__fadd_rn(y, zero[q]), WHOLE), WHOLE + 15.f);
+            sum += __float_as_uint(y) * (1u << (e & 1 ? 16 + 2 * (e - 1) : 2 * e));
+          }
+          // (the bits above the code, which each of the eight brought along, and the 8 of a code without zero points)
+          word = sum - (asym ? 0x4B400000u : 0x4B400000u - 8u) * 0x11111111u;
         }
       } else {
-        const bool in_matrix = row >= 0 && t.chunk * 128 + (m / gl) * s.group < s.cols;   // the group has columns
-        if (in_matrix) {
-          const size_t at = ((size_t)t.m * s.rows + row) * ng_src + grp;
-          scale = __uint_as_float((uint32_t)qs[at] << 16);
-          if (asym) zero = (float)min((int)qz[at], 15);
-        }
-        word = row >= 0 && col < s.cols ? in[q].x : (uint32_t)zero * 0x11111111u;
+        word = row >= 0 && col < s.cols ? split_word(in[q].x) : (uint32_t)zero[q] * 0x11111111u;
       }
       st[r * CODE_LD + m] = word;
       if (leads) {
         const size_t at = (((size_t)t.unit * 8 + (r & 7)) * ng + m / gl) * 4 + 2 * t.t + (r >> 3);
-        scales[at] = (uint16_t)(__float_as_uint(scale) >> 16);
-        if (asym) zeros[at] = (uint8_t)zero;
+        scales[at] = (uint16_t)(__float_as_uint(scale[q]) >> 16);
+        if (asym) zeros[at] = (uint8_t)zero[q];
       }
     }
     __syncwarp();
