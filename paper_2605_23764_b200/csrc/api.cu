@@ -798,17 +798,29 @@ W4VecArgs w4_vec_args(const moe_ctx* c, const moe_w4_weights& w, int rows, int c
   a.y_ld = s.d;
   a.ids = ids;
   a.T = T; a.k = s.k; a.kp = s.k + s.n_shared; a.E = s.E; a.Ep = s.E + s.n_shared;
-  a.rows_most = INT32_MAX;
   a.status = c->status();
-  const LayoutView lv = c->layout();
-  if ((long)T * a.kp > W4_SMALL_SLOTS) {
-    a.counts = lv.counts;
-    a.offsets = lv.offsets;
-    a.pad_off = lv.pad_off;
-    a.src_of = lv.src_of;
-  }
-  a.prow_of = lv.prow_of;
+  a.prow_of = c->layout().prow_of;
   return a;
+}
+// The vector kernel, or layout, gather and the tile kernel?  The first has fewer launches and reads an expert's weights once for the
+// rows it stages (8, fewer of long rows); the second has work for every group's scales, so that small groups cost it more.  Measured,
+// vector against tile kernel, us for the layer (E + S experts of d x F, k' slots a token):
+//   66 x 2048 x 1408, k' 8   groups of 128: 32 slots 43 / 52, 64: 69 / 67, 96: 89 / 79;  64: 128: 100 / 101, 192: 114 / 111;
+//                            32: 192: 135 / 164, 384: 166 / 184
+//   33 x 7168 x 2048, k' 9   128: 72 slots 186 / 196, 108: 201 / 201, 144: 213 / 208
+//   128 x 2048 x 768, k' 8   128: 64 slots 60 / 61, 128: 83 / 84, 192: 103 / 97
+//   8 x 1024 x 2816, k' 2    128: 32 slots 30 / 33, 64: 38 / 32;  64: 48: 35 / 36;  32: 48: 38 / 46, 80: 47 / 46
+//   9 x 16384 x 1024, k' 3   (two staged rows) 128: 6 slots 49 / 68, 12: 71 / 75, 24: 98 / 80;  32: 12: 85 / 127, 36: 152 / 138
+// So: slots by the groups of a unit, and not more than three quarters of the staged rows to an expert.
+bool w4_few(const W4VecArgs& up, const W4VecArgs& down) {
+  const int ng = W4_UNIT_K / (up.group > down.group ? up.group : down.group);
+  int rows = 8;
+  for (const W4VecArgs* a : {&up, &down}) {
+    const int staged = w4_vec_rows(a->K, a->Ep, a->group, a->zeros != nullptr);
+    rows = staged < rows ? staged : rows;
+  }
+  const long slots = (long)up.T * up.kp;
+  return slots <= W4_VEC_SLOTS_GROUP * ng && 4 * slots <= 3L * rows * up.Ep;
 }
 
 W4TileArgs w4_tile_args(const moe_ctx* c, const moe_w4_weights& w, int rows, int cols, int paired, const CUtensorMap* tok) {
@@ -855,7 +867,7 @@ int run_fwd_w4(moe_ctx* c, const uint16_t* x, const int32_t* ids, const float* w
   down.n_out = s.d;
   down.in = up.A;
   down.in_ld = up.a_ld;
-  if (up.counts) {
+  if (!w4_few(up, down)) {
     {
       Phase ph(c, MOE_PHASE_LAYOUT, st);
       MOE_CUDA(launch_layout(ids, dm, lv, false, 0, nullptr, 0, c->status(), st, &c->launches));
@@ -1189,7 +1201,6 @@ int moe_ffn_fwd_w4(moe_ctx* c, const uint16_t* x, const int32_t* topk_ids, const
                    const moe_w4_weights* W_down, uint16_t* out, int32_t T, void* stream) {
   if (!c || T < 0 || T > c->shape.T_max) return MOE_ERR_INVALID_ARG;
   if (!(c->shape.flags & MOE_FLAG_W4)) return MOE_ERR_STATE;
-  if (w4_vec_rows(c->shape.d) < 1 || w4_vec_rows(c->shape.F) < 1) return MOE_ERR_TOO_LARGE;
   c->begin_call(static_cast<cudaStream_t>(stream));
   if (T == 0) return MOE_OK;
   if (!x || !topk_ids || !topk_w || !out || !w4_ok(W_gate_up) || !w4_ok(W_down) || !aligned16(x) || !aligned16(out)) return MOE_ERR_INVALID_ARG;

@@ -77,13 +77,11 @@ struct W4VecArgs {
   const int* ids;             // [T][k]
   const float* w;             // [T][k]
   int T, k, kp, E, Ep;
-  const int *counts, *offsets, *pad_off, *src_of;   // the layout; counts NULL: few slots, each block orders them itself
-  int* prow_of;               // few slots, first product: filled here for the combine
-  int rows_most;              // experts with more rows are left to the tile kernel
+  int* prow_of;               // [T k'] row of the slot, -1: none; the first product fills it for the combine
   int rows_cap, group_rows;   // filled by the launch: staged rows, rows of a pass over an expert's weights
   DevStatus* status;
 };
-constexpr int W4_SMALL_SLOTS = 128;   // up to here the blocks order the slots themselves
+constexpr int W4_VEC_SLOTS_GROUP = 80, W4_VEC_SLOTS = 4 * W4_VEC_SLOTS_GROUP;   // T k' at most: for each group of a unit, in all
 
 // The same for a batch, on the tensor cores (w4_tile.cu): M-blocks of the padded row space, x gathered into it.
 struct W4TileArgs {
@@ -108,7 +106,7 @@ cudaError_t launch_w4_pack(const uint8_t* q, const uint16_t* qs, const uint8_t* 
                            uint8_t* zeros, cudaStream_t st);
 cudaError_t launch_w4_dequantize(const uint32_t* codes, const uint16_t* scales, const uint8_t* zeros, int n, const W4Shape& s, uint16_t* W, cudaStream_t st);
 // rows the vector kernel can stage at reduction K; 0: too long
-int w4_vec_rows(int K);
+int w4_vec_rows(int K, int Ep, int group, bool asym);
 cudaError_t launch_w4_vec(W4VecArgs a, int num_sms, cudaStream_t st, int* launches);
 // out[t] = sum_j Y[prow_of[t kp + j]], j ascending
 cudaError_t launch_w4_combine(const float* Y, int y_ld, const int* prow_of, int T, int d, int kp, uint16_t* out, cudaStream_t st, int* launches);

@@ -100,7 +100,7 @@ __device__ __forceinline__ int block_scan3(int (&v)[3], int* warp_sums) {
   for (int i = 0; i < 3; ++i) { const int x = v[i]; v[i] = at; at += x; }
   return total;
 }
-static_assert(3 * VEC_THREADS >= 1024 + 64 && VEC_THREADS >= W4_SMALL_SLOTS, "an expert for each scanned value");
+static_assert(3 * VEC_THREADS >= 1024 + 64 && VEC_THREADS >= W4_VEC_SLOTS, "an expert for each scanned value, a slot for each thread");
 
 }  // namespace
 
@@ -109,7 +109,7 @@ template <bool ASYM, int NG>
 __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs a) {
   extern __shared__ __align__(16) uint8_t vsm[];
   __shared__ int warp_sums[VEC_WARPS];
-  __shared__ int slot_at[W4_SMALL_SLOTS], slot_e[W4_SMALL_SLOTS];
+  __shared__ int slot_at[W4_VEC_SLOTS], slot_e[W4_VEC_SLOTS];
   // the segment: passes (expert, first staged row, rows), staged rows (row of A / Y, slot's weight)
   __shared__ int sg_e[VEC_SEG_GROUPS], sg_x[VEC_SEG_GROUPS], sg_n[VEC_SEG_GROUPS], seg_end, seg_rows;
   __shared__ int row_p[VEC_ROWS_MOST], row_t[VEC_ROWS_MOST];
@@ -118,55 +118,47 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
   float* const acc_s = reinterpret_cast<float*>(vsm + VEC_WARPS * VEC_DEPTH * SLOT);   // [VEC_SEG_TILES][32][8]
   float* const head_s = acc_s + VEC_SEG_TILES * PIECE;                                 // [VEC_WARPS][32][8]
   int* const cnt = reinterpret_cast<int*>(head_s + VEC_WARPS * PIECE);                     // [Ep] rows of the expert
-  int* const first = cnt + a.Ep;                                                       // [Ep] first row of the expert (few slots)
+  int* const first = cnt + a.Ep;                                                       // [Ep] first row of the expert
   int* const gstart = first + a.Ep;                                                    // [Ep + 1] first pass of the expert
   const int ld = vec_ld(a.KU);
   uint8_t* const xs = vsm + ((vec_fixed_smem(a.Ep, NG, ASYM) + 15) & ~size_t(15));               // [rows_cap][ld]
   const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x, g = lane >> 2, c = lane & 3;
-  const bool small = a.counts == nullptr;
 
-  // The first product waits for what is in front of it here; the second one's ids or layout were complete before the first started,
+  // The first product waits for what is in front of it here; the second one's ids were complete before the first started,
   // so it waits only where it reads what the first product wrote.
   if (!a.down) {
     pdl_wait();
     pdl_trigger();
   }
-  // ---- rows of each expert, passes over each expert's weights
-  if (small) {
-    const int n = a.T * a.kp;
-    for (int e = tid; e < a.Ep; e += VEC_THREADS) cnt[e] = 0;
-    __syncthreads();
-    int e = -1;
-    if (tid < n) {
-      const int t = tid / a.kp, j = tid - t * a.kp;
-      e = j < a.k ? __ldcg(a.ids + t * a.k + j) : a.E + j - a.k;
-      if (j < a.k && (e < 0 || e >= a.E)) e = -1;
-      slot_e[tid] = e;
-      if (e >= 0) atomicAdd(&cnt[e], 1);
-      else if (blockIdx.x == 0 && !a.down) note(a.status, /*MOE_ERR_BAD_EXPERT_ID*/ 1, tid);
-    }
-    __syncthreads();
-    int rank = 0;
-    if (e >= 0)
-      for (int i = 0; i < tid; ++i) rank += slot_e[i] == e;
-    int v[3];
+  // ---- the slots in order of their experts (every block for itself: fewer clocks than a launch), passes over each expert's weights
+  const int n = a.T * a.kp;
+  for (int e = tid; e < a.Ep; e += VEC_THREADS) cnt[e] = 0;
+  __syncthreads();
+  int e = -1;
+  if (tid < n) {
+    const int t = tid / a.kp, j = tid - t * a.kp;
+    e = j < a.k ? __ldcg(a.ids + t * a.k + j) : a.E + j - a.k;
+    if (j < a.k && (e < 0 || e >= a.E)) e = -1;
+    slot_e[tid] = e;
+    if (e >= 0) atomicAdd(&cnt[e], 1);
+    else if (blockIdx.x == 0 && !a.down) note(a.status, /*MOE_ERR_BAD_EXPERT_ID*/ 1, tid);
+  }
+  __syncthreads();
+  int rank = 0;
+  if (e >= 0)
+    for (int i = 0; i < tid; ++i) rank += slot_e[i] == e;
+  int v[3];
 #pragma unroll
-    for (int i = 0; i < 3; ++i) v[i] = 3 * tid + i < a.Ep ? cnt[3 * tid + i] : 0;
-    block_scan3(v, warp_sums);
+  for (int i = 0; i < 3; ++i) v[i] = 3 * tid + i < a.Ep ? cnt[3 * tid + i] : 0;
+  block_scan3(v, warp_sums);
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
-      if (3 * tid + i < a.Ep) first[3 * tid + i] = v[i];
-    __syncthreads();
-    if (tid < n) {
-      const int at = e >= 0 ? first[e] + rank : -1;
-      if (e >= 0) slot_at[at] = tid;
-      if (blockIdx.x == 0 && !a.down) a.prow_of[tid] = at;
-    }
-  } else {
-    for (int e = tid; e < a.Ep; e += VEC_THREADS) {
-      const int n = __ldcg(a.counts + e);
-      cnt[e] = n <= a.rows_most ? n : 0;
-    }
+  for (int i = 0; i < 3; ++i)
+    if (3 * tid + i < a.Ep) first[3 * tid + i] = v[i];
+  __syncthreads();
+  if (tid < n) {
+    const int at = e >= 0 ? first[e] + rank : -1;
+    if (e >= 0) slot_at[at] = tid;
+    if (blockIdx.x == 0 && !a.down) a.prow_of[tid] = at;
   }
   __syncthreads();
   int passes;
@@ -218,9 +210,7 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
         sg_x[lane] = x;
         sg_n[lane] = n;
         for (int i = 0; i < n; ++i) {
-          int slot, p_row;
-          if (small) { p_row = first[e] + i0 + i; slot = slot_at[p_row]; }
-          else { slot = __ldcg(a.src_of + __ldcg(a.offsets + e) + i0 + i); p_row = __ldcg(a.pad_off + e) + i0 + i; }
+          const int p_row = first[e] + i0 + i, slot = slot_at[p_row];
           const int t = slot / a.kp, j = slot - t * a.kp;
           row_p[x + i] = p_row;
           row_t[x + i] = a.down ? p_row : t;
@@ -441,18 +431,18 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
   }
 }
 
-static int vec_rows(int K, int Ep, int ng, bool asym) {
+int w4_vec_rows(int K, int Ep, int group, bool asym) {
+  const int ng = W4_UNIT_K / group;
   const long room = (long)VEC_SMEM - (long)((vec_fixed_smem(Ep, ng, asym) + 15) & ~size_t(15));
   const long rows = room / vec_ld((K + W4_UNIT_K - 1) / W4_UNIT_K);
-  return (int)(rows < VEC_ROWS_MOST ? rows : VEC_ROWS_MOST);
+  return (int)(rows < 0 ? 0 : rows < VEC_ROWS_MOST ? rows : VEC_ROWS_MOST);
 }
-int w4_vec_rows(int K) { return vec_rows(K, 1024 + 64, 4, true); }
 
 cudaError_t launch_w4_vec(W4VecArgs a, int num_sms, cudaStream_t st, int* launches) {
   const int ng = W4_UNIT_K / a.group;
   const bool asym = a.zeros != nullptr;
   const size_t fixed = (vec_fixed_smem(a.Ep, ng, asym) + 15) & ~size_t(15);
-  a.rows_cap = vec_rows(a.K, a.Ep, ng, asym);
+  a.rows_cap = w4_vec_rows(a.K, a.Ep, a.group, asym);
   const long slots = (long)a.T * a.kp;
   if (a.rows_cap > slots) a.rows_cap = (int)slots;
   a.group_rows = a.rows_cap < VEC_ROWS ? a.rows_cap : VEC_ROWS;

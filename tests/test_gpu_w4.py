@@ -103,6 +103,39 @@ def test_long_rows(T, d, E, k, S, F):
     _check(_run(T, d, E, k, S, F, *p, 128), *p, 128, E)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("T", [10, 11, 20, 21, 40, 41])
+def test_either_side_of_the_vector_kernels_slots(T, group):
+    """Slots from 80 to 328: what the two kernels share of a batch does not depend on its length by more than their roundings."""
+    d, E, k, S, F = 136, 90, 7, 1, 72
+    p = _problem(T, d, E, k, S, F, group, True, 5)
+    _check(_run(T, d, E, k, S, F, *p, group), *p, group, E)
+
+
+@pytest.mark.parametrize("T", [1, 3, 40])
+@pytest.mark.parametrize("groups", [(32, 128), (128, 32), (64, 32)])
+def test_groups_of_their_own_for_either_product(groups, T):
+    d, E, k, S, F = 200, 24, 2, 1, 136
+    rng = np.random.default_rng(T)
+    x, ids, w, up, _ = _problem(T, d, E, k, S, F, groups[0], False, T)
+    down = R.random_codes(rng, E + S, d, F, groups[1], True)
+    from paper_2605_23764_b200 import MoeLayer, MoeW4Weights
+    W1 = MoeW4Weights.pack(_cuda(up[0]), _cuda(up[1], BF), None, group=groups[0], gate_up=True)
+    W2 = MoeW4Weights.pack(_cuda(down[0]), _cuda(down[1], BF), _cuda(down[2]), group=groups[1])
+    layer = MoeLayer(T, d, E, k, S, F, w4=True)
+    got = layer.ffn_fwd_w4(_cuda(x, BF), _cuda(ids), _cuda(w), W1, W2).float().cpu().numpy()
+    assert layer.status() == (0, 0)
+    layer.close()
+    want, bound = R.layer(x, ids, w, R.values(*up, groups[0]), R.values(*down, groups[1]), E, rounded_weights=True)
+    assert (np.abs(got - want) <= bound).all()
+
+
+@pytest.mark.parametrize("T,d,F,group", [(1, 40000, 8, 128), (1, 8, 40000, 32), (2, 26000, 16, 32), (5, 45056, 24, 64)])
+def test_rows_longer_than_shared_memory(T, d, F, group):
+    p = _problem(T, d, 3, 2, 1, F, group, True, T + d)
+    _check(_run(T, d, 3, 2, 1, F, *p, group), *p, group, 3)
+
+
 @pytest.mark.parametrize("rows", [7, 8, 9, 16, 31, 32, 33, 100, 128, 129, 192, 193, 257])
 def test_one_expert_takes_all(rows):
     d, E, F = 136, 40, 72
