@@ -139,6 +139,26 @@ def test_masked_logits_and_rows_without_a_finite_logit():
             assert np.all(np.abs(d - rd)[keep] <= 100 * U * size[keep, None] + 1e-30)
 
 
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E", [40, 41])
+def test_padding_holds_anything(E, sigmoid):
+    """NaN and infinities in tokens that are masked or outside of the sequences, and ids that are none."""
+    T, k = 90, 4
+    logits, ids, dw = _case(T, E, k, 15)
+    mask = np.ones(T, np.uint8)
+    mask[5:17] = 0
+    off = np.array([3, 40, 80], np.int32)
+    idle = (mask == 0) | (np.arange(T) < 3) | (np.arange(T) >= 80)
+    clean = [g.copy() for g in _run(logits, ids, None, off, mask, sigmoid=sigmoid)]
+    _check(clean, logits, ids, None, off, mask, sigmoid=sigmoid)
+    for v in (np.nan, np.inf, -np.inf):
+        logits[idle], ids[idle] = v, 12345678
+        logits[7, ::2] = 1.0
+        for want, got in zip(clean, _run(logits, ids, None, off, mask, sigmoid=sigmoid)):
+            assert np.array_equal(want, got)
+    assert not clean[4][idle].any()
+
+
 def test_sigmoids_that_underflow_keep_their_proportions():
     logits, ids, dw = _case(50, 16, 2, 6)
     logits -= 200.0
