@@ -1,6 +1,7 @@
 // Weights into 4 bits, from a checkpoint's natural codes into the layout of w4.cuh, and back to the values they stand for.
 // A warp takes 16 rows x 128 columns, half a unit: lanes 16 h + m have columns 8 m .. of rows 2 i + h, and change places with the
-// layout's lanes through 1 KB of shared memory.  Bound by the bytes of the matrices.
+// layout's lanes through 1 KB of shared memory.  Measured for 64 matrices of 2816 x 2048, groups of 128: 400 us to quantize (740 MB in,
+// 190 MB out: 2.3 TB/s; bound by the instructions of a code -- largest value, product, two roundings, clamp, place), 200 us back (4.7 TB/s).
 #include "launch_pairs.cuh"
 #include "topk.cuh"
 #include "w4.cuh"

@@ -7,12 +7,17 @@
 // of the bytes of bf16), four warps of each CTA widen them to whole numbers q - z -- exact in bf16 -- and write them to TMEM in the
 // fragments that the layout of w4.cuh holds, so they never are in shared memory as bf16.  An accumulator holds one group of the
 // reduction; the epilogue warps scale it in fp32 and add it up in registers while the next group is multiplied.  So there is no
-// rounding that the formula does not have but that of the activations to bf16 between the two products.
+// rounding that the formula does not have but that of the activations to bf16 between the two products.  (Scales folded into the widened
+// weights would spare the accumulators between groups, but round every weight: twice the error of the plain formula instead of 1.4 times.)
 //
-// Roles per CTA: warp 0 loads codes and zero points (a copy of each for 128 rows x 128 columns; with one for every 32 rows
-// issuing them took 1000 clocks, twice as long as the products), warp 18 the rows of x, warp 1 issues the products (even CTA), warps 2-9 widen (four for each half of a unit's 128 columns),
-// warps 10-17 scale and add up (four for each half of the columns; with
-// sixteen warps their waits and signals took the issue slots that the widening warps need: a prompt of 4096 tokens 841 us).
+// Measured for 66 experts of 2048 x 1408, 8 rows a token, groups of 128: 64 tokens 111 us, 512 tokens 165, 4096 tokens 785 (720
+// TFLOP/s).  What bounds it: with many rows the epilogue, which takes every group's accumulator out of TMEM (800 clocks a unit beside 512
+// of products); with few the chain from codes to operand to products through two stages of A (760 clocks a unit).
+//
+// Roles per CTA: warp 0 loads codes and zero points (a copy of each for 128 rows x 128 columns; with one for every 32 rows issuing
+// them took 1000 clocks, twice as long as the products), warp 18 the rows of x, warp 1 issues the products (even CTA), warps 2-9 widen
+// (four for every other unit), warps 10-17 scale and add up (four for each half of the columns; with sixteen warps their waits and
+// signals took the issue slots that the widening warps need: a prompt of 4096 tokens 841 us).
 #include "gemm_tile.cuh"
 #include "launch_pairs.cuh"
 #include "topk.cuh"
