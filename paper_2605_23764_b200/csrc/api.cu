@@ -816,8 +816,9 @@ bool w4_few(const W4VecArgs& up, const W4VecArgs& down) {
   const int ng = W4_UNIT_K / (up.group > down.group ? up.group : down.group);
   int rows = 8;
   for (const W4VecArgs* a : {&up, &down}) {
-    const int staged = w4_vec_rows(a->K, a->Ep, a->group, a->zeros != nullptr);
+    const int staged = w4_vec_rows(a->K, a->group, a->zeros != nullptr);
     rows = staged < rows ? staged : rows;
+    if (a->RT > INT32_MAX / W4_VEC_SLOTS) return false;   // it counts row tiles of passes in 32 bits
   }
   const long slots = (long)up.T * up.kp;
   return slots <= W4_VEC_SLOTS_GROUP * ng && 4 * slots <= 3L * rows * up.Ep;

@@ -106,7 +106,7 @@ cudaError_t launch_w4_pack(const uint8_t* q, const uint16_t* qs, const uint8_t* 
                            uint8_t* zeros, cudaStream_t st);
 cudaError_t launch_w4_dequantize(const uint32_t* codes, const uint16_t* scales, const uint8_t* zeros, int n, const W4Shape& s, uint16_t* W, cudaStream_t st);
 // rows the vector kernel can stage at reduction K; 0: too long
-int w4_vec_rows(int K, int Ep, int group, bool asym);
+int w4_vec_rows(int K, int group, bool asym);
 cudaError_t launch_w4_vec(W4VecArgs a, int num_sms, cudaStream_t st, int* launches);
 // out[t] = sum_j Y[prow_of[t kp + j]], j ascending
 cudaError_t launch_w4_combine(const float* Y, int y_ld, const int* prow_of, int T, int d, int kp, uint16_t* out, cudaStream_t st, int* launches);

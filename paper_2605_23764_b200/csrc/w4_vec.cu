@@ -3,8 +3,8 @@
 //   h[i] = sum_groups s_g sum_k (q - z) x[i][k];   A = w silu(h_gate) h_up;   Y = the same over A;   out[t] = sum_j Y of its slots
 //
 // What bounds it: the weights' bytes are the floor, the instructions that widen and multiply them what it takes.  33 experts of 7168 x
-// 2048, groups of 128: 8 tokens 186 us, 3.6 TB/s of codes and scales (an instruction a code to widen them on a pipe of half rate, a product
-// of 16 x 8 x 16 for 256 codes and one more for the sums of x).  One token of eight experts of 2048 x 1408: 27 us, of which reading is 5:
+// 2048, groups of 128: 8 tokens 156 us, 4.3 TB/s of codes and scales (an instruction a code to widen them on a pipe of half rate, a product
+// of 16 x 8 x 16 for 256 codes and one more for the sums of x).  One token of eight experts of 2048 x 1408: 22 us, of which reading is 5:
 // three launches, each of the latencies of its ids, first units and rows of x.  Every warp streams its share of the units (2 KB) through a ring of its own in shared
 // memory (loads kept in registers instead did not overlap: a unit then cost a memory latency, 2.7 TB/s), widens the codes to bf16
 // 128 + q -- a mask and an exponent -- and multiplies 32 rows by up to 8 rows of x at a time (mma.m16n8k16, which a matrix-vector
@@ -32,17 +32,17 @@ namespace {
 constexpr int VEC_WARPS = 16, VEC_THREADS = 32 * VEC_WARPS;
 constexpr int VEC_ROWS = 8;          // rows of x that a pass over an expert's weights takes
 constexpr int VEC_SEG_TILES = 16;    // row tiles between two joins
-constexpr int VEC_SEG_GROUPS = 32;   // passes a segment may touch: a lane each
+static_assert(VEC_SEG_TILES <= 32, "a lane for each pass that a segment may touch");
 constexpr int VEC_DEPTH = 3;         // slots of a warp's ring: two units in flight, 50 KB an SM
-constexpr int VEC_SMEM = 222 * 1024;
+constexpr int VEC_SMEM = 221 * 1024;
 constexpr int VEC_PIECE_BYTES = W4_TILE_ROWS * VEC_ROWS * 4;   // sums of a row tile
 constexpr int VEC_ROWS_MOST = 64;    // staged rows, at most
+static_assert((1024 + 64) < 0x8000, "an expert and a bit");
 
 __host__ __device__ constexpr int vec_ld(int KU) { return KU * W4_UNIT_K * 2 + 16; }   // bytes from row to row: ldmatrix rows in different banks
 __host__ __device__ constexpr int vec_slot(int ng, bool asym) { return W4_UNIT_BYTES + 64 * ng + (asym ? 32 * ng : 0); }   // codes, scales, zero points
-__host__ __device__ constexpr size_t vec_fixed_smem(int Ep, int ng, bool asym) {
-  return (size_t)VEC_WARPS * VEC_DEPTH * vec_slot(ng, asym) +
-         (size_t)(VEC_SEG_TILES + VEC_WARPS) * VEC_PIECE_BYTES + sizeof(int) * (3 * (size_t)Ep + 4);
+__host__ __device__ constexpr size_t vec_fixed_smem(int ng, bool asym) {
+  return (size_t)VEC_WARPS * VEC_DEPTH * vec_slot(ng, asym) + (size_t)(VEC_SEG_TILES + VEC_WARPS) * VEC_PIECE_BYTES;
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
@@ -82,32 +82,7 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Exclusive scan of v over the block, n <= 3 values a thread; returns the total.
-__device__ __forceinline__ int block_scan3(int (&v)[3], int* warp_sums) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int mine = v[0] + v[1] + v[2];
-  int run = mine;
-#pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const int o = __shfl_up_sync(0xffffffffu, run, off);
-    if (lane >= off) run += o;
-  }
-  if (lane == 31) warp_sums[warp] = run;
-  __syncthreads();
-  int before = 0, total = 0;
-#pragma unroll
-  for (int w = 0; w < VEC_WARPS; ++w) {
-    const int s = warp_sums[w];
-    if (w < warp) before += s;
-    total += s;
-  }
-  __syncthreads();
-  int at = before + run - mine;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) { const int x = v[i]; v[i] = at; at += x; }
-  return total;
-}
-static_assert(3 * VEC_THREADS >= 1024 + 64 && VEC_THREADS >= W4_VEC_SLOTS, "an expert for each scanned value, a slot for each thread");
+static_assert(VEC_THREADS >= W4_VEC_SLOTS, "a slot for each thread");
 
 }  // namespace
 
@@ -115,20 +90,17 @@ static_assert(3 * VEC_THREADS >= 1024 + 64 && VEC_THREADS >= W4_VEC_SLOTS, "an e
 template <bool ASYM, int NG>
 __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs a) {
   extern __shared__ __align__(16) uint8_t vsm[];
-  __shared__ int warp_sums[VEC_WARPS];
-  __shared__ int slot_at[W4_VEC_SLOTS], slot_e[W4_VEC_SLOTS];
-  // the segment: passes (expert, first staged row, rows), staged rows (row of A / Y, slot's weight)
-  __shared__ int sg_e[VEC_SEG_GROUPS], sg_x[VEC_SEG_GROUPS], sg_n[VEC_SEG_GROUPS], seg_end, seg_rows;
-  __shared__ int row_p[VEC_ROWS_MOST], row_t[VEC_ROWS_MOST];
-  __shared__ float row_w[VEC_ROWS_MOST];
-  constexpr int SLOT = vec_slot(NG, ASYM), PIECE = VEC_PIECE_BYTES / 4;
+  __shared__ int slot_e[W4_VEC_SLOTS];
+  __shared__ float slot_w[W4_VEC_SLOTS];
+  // rows in the order of their experts: slot, token, expert (its top bit: a pass begins); passes over an expert's weights: first row, expert
+  __shared__ uint16_t row_slot[W4_VEC_SLOTS], row_t[W4_VEC_SLOTS], row_e[W4_VEC_SLOTS], pass_row[W4_VEC_SLOTS + 1], pass_e[W4_VEC_SLOTS];
+  __shared__ int pass_count;
+  __shared__ uint8_t tile_from[VEC_SEG_TILES], tile_to[VEC_SEG_TILES];   // warps that have the first and the last piece of a row tile
+  constexpr int SLOT = vec_slot(NG, ASYM), PIECE = VEC_PIECE_BYTES / 4, STARTS = 0x8000;
   float* const acc_s = reinterpret_cast<float*>(vsm + VEC_WARPS * VEC_DEPTH * SLOT);   // [VEC_SEG_TILES][32][8]
   float* const head_s = acc_s + VEC_SEG_TILES * PIECE;                                 // [VEC_WARPS][32][8]
-  int* const cnt = reinterpret_cast<int*>(head_s + VEC_WARPS * PIECE);                     // [Ep] rows of the expert
-  int* const first = cnt + a.Ep;                                                       // [Ep] first row of the expert
-  int* const gstart = first + a.Ep;                                                    // [Ep + 1] first pass of the expert
   const int ld = vec_ld(a.KU);
-  uint8_t* const xs = vsm + ((vec_fixed_smem(a.Ep, NG, ASYM) + 15) & ~size_t(15));               // [rows_cap][ld]
+  uint8_t* const xs = vsm + vec_fixed_smem(NG, ASYM);                                  // [rows_cap][ld]
   const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x, g = lane >> 2, c = lane & 3;
 
   // The first product waits for what is in front of it here; the second one's ids were complete before the first started,
@@ -137,160 +109,167 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
     pdl_wait();
     pdl_trigger();
   }
-  // ---- the slots in order of their experts (every block for itself: fewer clocks than a launch), passes over each expert's weights
+  // ---- the slots in order of their experts, by every block for itself: a slot's place is the number of slots in front of it, which
+  // 512 / n threads count.  (Scans over the experts, searches and the rows of a segment by one warp took 9000 of 28000 clocks of a call
+  // for one token.)
   const int n = a.T * a.kp;
-  for (int e = tid; e < a.Ep; e += VEC_THREADS) cnt[e] = 0;
-  __syncthreads();
-  int e = -1;
   if (tid < n) {
     const int t = tid / a.kp, j = tid - t * a.kp;
-    e = j < a.k ? __ldcg(a.ids + t * a.k + j) : a.E + j - a.k;
-    if (j < a.k && (e < 0 || e >= a.E)) e = -1;
-    slot_e[tid] = e;
-    if (e >= 0) atomicAdd(&cnt[e], 1);
-    else if (blockIdx.x == 0 && !a.down) note(a.status, /*MOE_ERR_BAD_EXPERT_ID*/ 1, tid);
-  }
-  __syncthreads();
-  int rank = 0;
-  if (e >= 0)
-    for (int i = 0; i < tid; ++i) rank += slot_e[i] == e;
-  int v[3];
-#pragma unroll
-  for (int i = 0; i < 3; ++i) v[i] = 3 * tid + i < a.Ep ? cnt[3 * tid + i] : 0;
-  block_scan3(v, warp_sums);
-#pragma unroll
-  for (int i = 0; i < 3; ++i)
-    if (3 * tid + i < a.Ep) first[3 * tid + i] = v[i];
-  __syncthreads();
-  if (tid < n) {
-    const int at = e >= 0 ? first[e] + rank : -1;
-    if (e >= 0) slot_at[at] = tid;
-    if (blockIdx.x == 0 && !a.down) a.prow_of[tid] = at;
-  }
-  __syncthreads();
-  int passes;
-  {
-    int v[3];
-#pragma unroll
-    for (int i = 0; i < 3; ++i) v[i] = 3 * tid + i < a.Ep ? (cnt[3 * tid + i] + a.group_rows - 1) / a.group_rows : 0;
-    passes = block_scan3(v, warp_sums);
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-      if (3 * tid + i < a.Ep) gstart[3 * tid + i] = v[i];
-    if (tid == 0) gstart[a.Ep] = passes;
-  }
-  __syncthreads();
-
-  const int64_t tiles = (int64_t)passes * a.RT;
-  int64_t t0 = tiles * blockIdx.x / gridDim.x;
-  const int64_t t1 = tiles * (blockIdx.x + 1) / gridDim.x;
-  bool waited = !a.down;
-  while (t0 < t1) {
-    // ---- the segment [t0, te): as many tiles as have room, rows staged once
-    const int p0 = (int)(t0 / a.RT);
-    if (warp == 0) {
-      const int p = p0 + lane;
-      const int64_t most = min(t1, t0 + VEC_SEG_TILES);
-      const bool in = p < passes && (int64_t)p * a.RT < most;
-      int e = 0, i0 = 0, n = 0;
-      if (in) {
-        int lo = 0, hi = a.Ep;   // gstart[lo] <= p < gstart[hi]
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (gstart[mid] <= p) lo = mid; else hi = mid;
-        }
-        e = lo;
-        i0 = (p - gstart[e]) * a.group_rows;
-        n = min(a.group_rows, cnt[e] - i0);
-      }
-      int run = n;
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const int o = __shfl_up_sync(0xffffffffu, run, off);
-        if (lane >= off) run += o;
-      }
-      const uint32_t fits = __ballot_sync(0xffffffffu, in && run <= a.rows_cap);
-      const int m = __popc(fits);   // the first m passes: their rows ascend
-      if (lane < m) {
-        const int x = run - n;
-        sg_e[lane] = e;
-        sg_x[lane] = x;
-        sg_n[lane] = n;
-        for (int i = 0; i < n; ++i) {
-          const int p_row = first[e] + i0 + i, slot = slot_at[p_row];
-          const int t = slot / a.kp, j = slot - t * a.kp;
-          row_p[x + i] = p_row;
-          row_t[x + i] = a.down ? p_row : t;
-          row_w[x + i] = a.down || j >= a.k ? 1.f : __ldcg(a.w + (size_t)t * a.k + j);
-        }
-        if (lane == m - 1) seg_rows = run;
-      }
-      if (lane == 0) {
-        const int64_t end = min(most, (int64_t)(p0 + m) * a.RT);
-        seg_end = (int)(end - t0);
+    int e = a.E + j - a.k;
+    float w = 1.f;
+    if (j < a.k) {
+      e = __ldcg(a.ids + t * a.k + j);
+      if (!a.down) w = __ldcg(a.w + t * a.k + j);
+      if (e < 0 || e >= a.E) {
+        e = INT_MAX;   // behind all others
+        if (blockIdx.x == 0 && !a.down) note(a.status, /*MOE_ERR_BAD_EXPERT_ID*/ 1, tid);
       }
     }
-    __syncthreads();
-    const int ntiles = seg_end, rt0 = (int)(t0 - (int64_t)p0 * a.RT);
-    const int units = ntiles * a.KU;
-    const int u0 = (int)((int64_t)units * warp / VEC_WARPS), u1 = (int)((int64_t)units * (warp + 1) / VEC_WARPS);
-    int tile = u0 / a.KU, ku = u0 - tile * a.KU;   // row tile of the segment, unit of it
-    int pass = (rt0 + tile) / a.RT, rt = rt0 + tile - pass * a.RT;
+    slot_e[tid] = e;
+    slot_w[tid] = w;
+  }
+  __syncthreads();
+  int rows;   // slots that name an expert
+  {
+    const int lg = n > 256 ? 0 : min(5, 31 - __clz(VEC_THREADS / n)), i = tid >> lg, part = tid & ((1 << lg) - 1);
+    const int e = i < n ? slot_e[i] : INT_MAX;
+    int less = 0, rank = 0;
+    if (e < INT_MAX)
+      for (int j = part; j < n; j += 1 << lg) {
+        const int o = slot_e[j];
+        less += o < e;
+        rank += o == e && j < i;
+      }
+    for (int off = 1 << lg >> 1; off; off >>= 1) {
+      less += __shfl_xor_sync(0xffffffffu, less, off);
+      rank += __shfl_xor_sync(0xffffffffu, rank, off);
+    }
+    const bool mine = i < n && part == 0, there = mine && e < INT_MAX;
+    const int at = less + rank;
+    if (there) {
+      row_slot[at] = (uint16_t)i;
+      row_t[at] = (uint16_t)(i / a.kp);
+      row_e[at] = (uint16_t)(e | (rank % a.group_rows ? 0 : STARTS));
+    }
+    if (mine && blockIdx.x == 0 && !a.down) a.prow_of[i] = there ? at : -1;
+    rows = __syncthreads_count(there);
+  }
+  if (warp * 32 < rows) {
+    int before = 0;
+    uint32_t starts = 0;
+    for (int q = 0; q <= warp; ++q) {
+      before += __popc(starts);
+      starts = __ballot_sync(0xffffffffu, q * 32 + lane < rows && (row_e[q * 32 + lane] & STARTS));
+    }
+    const int pass = before + __popc(starts & ((1u << lane) - 1u));
+    if (starts >> lane & 1) {
+      pass_row[pass] = (uint16_t)tid;
+      pass_e[pass] = row_e[tid] & (STARTS - 1);
+    }
+    if (tid == rows - 1) {
+      pass_count = before + __popc(starts);
+      pass_row[before + __popc(starts)] = (uint16_t)rows;
+    }
+  }
+  __syncthreads();
+  const int passes = rows ? pass_count : 0;
 
-    // ---- the stream: from unit to unit of a row tile the addresses grow by four units
-    const uint8_t *f_codes = nullptr, *f_scales = nullptr, *f_zeros = nullptr;
-    int f_pass = pass, f_rt = rt, f_left = u1 - u0, f_run = 0;   // units to fetch, of them in this row tile
-    auto seek = [&](int from) {   // lane l copies 16 bytes at 16 l
-      const int64_t unit = (int64_t)sg_e[f_pass] * a.RTS * a.KU + w4_unit(f_rt, from, a.KU);
-      f_codes = reinterpret_cast<const uint8_t*>(a.codes) + unit * W4_UNIT_BYTES + lane * 16;
-      f_scales = reinterpret_cast<const uint8_t*>(a.scales) + unit * (64 * NG) + lane * 16;
-      if (ASYM) f_zeros = reinterpret_cast<const uint8_t*>(a.zeros) + unit * (32 * NG) + lane * 16;
-      f_run = min(f_left, a.KU - from);
-    };
-    if (u0 < u1) seek(ku);
-    const uint32_t ring = smem_u32(vsm) + warp * VEC_DEPTH * SLOT, ring_end = ring + VEC_DEPTH * SLOT;
-    auto fetch = [&](uint32_t slot) {
-      if (f_run == 0 && f_left > 0) {
-        if (++f_rt == a.RT) {
-          f_rt = 0;
-          ++f_pass;
-        }
-        seek(0);
+  const int tiles = passes * a.RT, share = tiles / (int)gridDim.x, extra = tiles - share * (int)gridDim.x;
+  const int t1 = share * ((int)blockIdx.x + 1) + min((int)blockIdx.x + 1, extra);
+  // The segment that begins at tile `from`: as many tiles as have room, rows staged once.  Every warp works it out.
+  struct Segment { int from, tiles, pass0, rt0, row0, rows; };
+  auto plan = [&](int from) {
+    Segment sg{from, 0, 0, 0, 0, 0};
+    if (from >= t1) return sg;
+    sg.pass0 = from / a.RT;
+    sg.rt0 = from - sg.pass0 * a.RT;
+    sg.row0 = pass_row[sg.pass0];
+    const int most = min(t1, from + VEC_SEG_TILES), p = sg.pass0 + lane;
+    const bool in = p < passes && p * a.RT < most;
+    const int m = __popc(__ballot_sync(0xffffffffu, in && pass_row[in ? p + 1 : 0] - sg.row0 <= a.rows_cap));   // the first m passes
+    sg.tiles = min(most, (sg.pass0 + m) * a.RT) - from;
+    sg.rows = pass_row[sg.pass0 + m] - sg.row0;
+    return sg;
+  };
+
+  // ---- a warp's units of a segment
+  int units = 0, u0 = 0, u1 = 0, tile = 0, ku = 0, pass = 0, rt = 0;   // of the segment; row tile of it, unit of that; pass, row tile of the expert
+  // The stream: from unit to unit of a row tile the addresses grow by four units.
+  const uint8_t *f_codes = nullptr, *f_scales = nullptr, *f_zeros = nullptr;
+  int f_pass = 0, f_rt = 0, f_left = 0, f_run = 0;   // units to fetch, of them in this row tile
+  auto seek = [&](int from) {   // lane l copies 16 bytes at 16 l
+    const int64_t unit = (int64_t)pass_e[f_pass] * a.RTS * a.KU + w4_unit(f_rt, from, a.KU);
+    f_codes = reinterpret_cast<const uint8_t*>(a.codes) + unit * W4_UNIT_BYTES + lane * 16;
+    f_scales = reinterpret_cast<const uint8_t*>(a.scales) + unit * (64 * NG) + lane * 16;
+    if (ASYM) f_zeros = reinterpret_cast<const uint8_t*>(a.zeros) + unit * (32 * NG) + lane * 16;
+    f_run = min(f_left, a.KU - from);
+  };
+  const uint32_t ring = smem_u32(vsm) + warp * VEC_DEPTH * SLOT, ring_end = ring + VEC_DEPTH * SLOT;
+  auto fetch = [&](uint32_t slot) {
+    if (f_run == 0 && f_left > 0) {
+      if (++f_rt == a.RT) {
+        f_rt = 0;
+        ++f_pass;
       }
-      if (f_run > 0) {
-        --f_run;
-        --f_left;
-        const uint32_t to = slot + lane * 16;
+      seek(0);
+    }
+    if (f_run > 0) {
+      --f_run;
+      --f_left;
+      const uint32_t to = slot + lane * 16;
 #pragma unroll
-        for (int h = 0; h < 4; ++h) cp_async16(to + 512 * h, f_codes + 512 * h);
-        if (lane < 4 * NG) cp_async16(to + W4_UNIT_BYTES, f_scales);
-        if (ASYM && lane < 2 * NG) cp_async16(to + W4_UNIT_BYTES + 64 * NG, f_zeros);
-        f_codes += 4 * W4_UNIT_BYTES;
-        f_scales += 4 * 64 * NG;
-        if (ASYM) f_zeros += 4 * 32 * NG;
-      }
-      cp_async_commit();
-    };
+      for (int h = 0; h < 4; ++h) cp_async16(to + 512 * h, f_codes + 512 * h);
+      if (lane < 4 * NG) cp_async16(to + W4_UNIT_BYTES, f_scales);
+      if (ASYM && lane < 2 * NG) cp_async16(to + W4_UNIT_BYTES + 64 * NG, f_zeros);
+      f_codes += 4 * W4_UNIT_BYTES;
+      f_scales += 4 * 64 * NG;
+      if (ASYM) f_zeros += 4 * 32 * NG;
+    }
+    cp_async_commit();
+  };
+  auto begin = [&](const Segment& sg) {
+    units = sg.tiles * a.KU;
+    u0 = units * warp / VEC_WARPS;
+    u1 = units * (warp + 1) / VEC_WARPS;
+    tile = u0 / a.KU;
+    ku = u0 - tile * a.KU;
+    const int over = (sg.rt0 + tile) / a.RT;
+    pass = sg.pass0 + over;
+    rt = sg.rt0 + tile - over * a.RT;
+    f_pass = pass;
+    f_rt = rt;
+    f_left = u1 - u0;
+    f_run = 0;
+    if (u0 < u1) seek(ku);
 #pragma unroll
     for (int i = 0; i < VEC_DEPTH - 1; ++i) fetch(ring + i * SLOT);
+  };
+  // Rows of x, zeros behind K.
+  auto stage = [&](const Segment& sg) {
+    const int pieces = a.KU * (W4_UNIT_K / 8), full = a.K >> 3;
+    const int row_step = VEC_THREADS / pieces, step = VEC_THREADS - row_step * pieces;
+    int row = tid / pieces, v = tid - row * pieces;
+    while (row < sg.rows) {
+      const int at = sg.row0 + row;
+      uint8_t* dst = xs + (size_t)row * ld + v * 16;
+      if (v < full) cp_async16(smem_u32(dst), a.in + (size_t)(a.down ? at : row_t[at]) * a.in_ld + v * 8);
+      else *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
+      row += row_step;
+      v += step;
+      if (v >= pieces) { v -= pieces; ++row; }
+    }
+    cp_async_commit();
+  };
 
-    // ---- the rows of x, zeros behind K
-    if (!waited) {
-      pdl_wait();
-      pdl_trigger();
-      waited = true;
-    }
-    {
-      const int pieces = a.KU * (W4_UNIT_K / 8), full = a.K >> 3, rows = seg_rows;
-      for (int i = tid; i < rows * pieces; i += VEC_THREADS) {
-        const int r = i / pieces, v = i - r * pieces;
-        uint8_t* dst = xs + (size_t)r * ld + v * 16;
-        if (v < full) cp_async16(smem_u32(dst), a.in + (size_t)row_t[r] * a.in_ld + v * 8);
-        else *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
-      }
-      cp_async_commit();
-      cp_async_wait<0>();   // (the first units as well)
-    }
+  Segment sg = plan(share * (int)blockIdx.x + min((int)blockIdx.x, extra));
+  if (sg.tiles > 0) begin(sg);
+  if (a.down) {
+    pdl_wait();
+    pdl_trigger();
+  }
+  if (sg.tiles > 0) stage(sg);
+  while (sg.tiles > 0) {
+    cp_async_wait<0>();   // (the first units as well)
     __syncthreads();
 
     // ---- the products
@@ -298,8 +277,8 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
     bool began = ku == 0;   // this warp has the tile from its first unit on
     uint32_t x_row = 0;
     auto enter_pass = [&]() {   // operand rows: lane l gives row l % 8 of matrix l / 8; rows that are not there are computed and dropped
-      const int r = min(lane & 7, sg_n[pass] - 1);
-      x_row = smem_u32(xs + (size_t)(sg_x[pass] + r) * ld) + (lane >> 3) * 16;
+      const int first = pass_row[pass], r = min(lane & 7, pass_row[pass + 1] - first - 1);
+      x_row = smem_u32(xs + (size_t)(first - sg.row0 + r) * ld) + (lane >> 3) * 16;
     };
     if (u0 < u1) enter_pass();
     uint32_t rd = ring, wr = ring + (VEC_DEPTH - 1) * SLOT;
@@ -381,6 +360,7 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
       }
       u += n;
       ku += n;
+      if (began && lane == 0) tile_from[tile] = (uint8_t)warp;
       float* const to = began ? acc_s + tile * PIECE : head_s + warp * PIECE;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -390,6 +370,7 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
         for (int i = 0; i < 4; ++i) acc[t][i] = 0.f;
       }
       if (ku == a.KU) {
+        if (lane == 0) tile_to[tile] = (uint8_t)warp;
         began = true;
         ku = 0;
         ++tile;
@@ -400,47 +381,44 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
         }
       }
     }
-    cp_async_wait<0>();
+    // The next segment's first units and rows of x are read while this one is put together.
+    const Segment done = sg;
+    const int done_units = units;
+    sg = plan(done.from + done.tiles);
+    if (sg.tiles > 0) begin(sg);
     __syncthreads();
+    if (sg.tiles > 0) stage(sg);
 
     // ---- pieces of a tile in the warps' order, then the result.  Threads: features fastest, 16 (gate and up) or 32 to a tile
     auto total = [&](int tl, int r, int col) {
       float v = acc_s[tl * PIECE + r * 8 + col];
-      const int lo = tl * a.KU, hi = lo + a.KU;   // units of the tile
-      for (int w = (int)((int64_t)lo * VEC_WARPS / units); w < VEC_WARPS; ++w) {
-        const int b0 = (int)((int64_t)units * w / VEC_WARPS), b1 = (int)((int64_t)units * (w + 1) / VEC_WARPS);
-        if (b0 >= hi) break;
-        if (b0 > lo && b1 > b0) v += head_s[w * PIECE + r * 8 + col];
-      }
+      const int last = tile_to[tl];
+      for (int w = tile_from[tl] + 1; w <= last; ++w)
+        if (done_units * w / VEC_WARPS < done_units * (w + 1) / VEC_WARPS) v += head_s[w * PIECE + r * 8 + col];
       return v;
     };
-    const int per = a.down ? 32 : 16;
-    for (int i = tid; i < ntiles * per * VEC_ROWS; i += VEC_THREADS) {
-      const int f = i % per, rest = i / per, tl = rest % ntiles, col = rest / ntiles;
-      const int at = rt0 + tl, ps = at / a.RT, feature = (at - ps * a.RT) * per + f;
-      if (col >= sg_n[ps] || feature >= a.n_out) continue;
-      const int xr = sg_x[ps] + col;
+    const int lg = a.down ? 5 : 4;
+    for (int i = tid; i < done.tiles * VEC_ROWS << lg; i += VEC_THREADS) {
+      const int f = i & ((1 << lg) - 1), rest = i >> lg, col = rest / done.tiles, tl = rest - col * done.tiles;
+      const int over = (done.rt0 + tl) / a.RT, ps = done.pass0 + over, feature = (done.rt0 + tl - over * a.RT << lg) + f;
+      const int at = pass_row[ps] + col;
+      if (at >= pass_row[ps + 1] || feature >= a.n_out) continue;
       if (a.down) {
-        a.Y[(size_t)row_p[xr] * a.y_ld + feature] = total(tl, f, col);
+        a.Y[(size_t)at * a.y_ld + feature] = total(tl, f, col);
       } else {
         const int r = (f & 8) * 2 + (f & 7);   // of the two sixteens of rows
         const float gate = total(tl, r, col), up = total(tl, r + 8, col);
-        const float act = row_w[xr] * (gate / (1.0f + __expf(-gate)) * up);
-        a.A[(size_t)row_p[xr] * a.a_ld + feature] = (uint16_t)(pack_bf16x2(act, 0.f) & 0xFFFFu);
+        const float act = slot_w[row_slot[at]] * (gate / (1.0f + __expf(-gate)) * up);
+        a.A[(size_t)at * a.a_ld + feature] = (uint16_t)(pack_bf16x2(act, 0.f) & 0xFFFFu);
       }
     }
-    __syncthreads();
-    t0 += ntiles;
   }
-  if (!waited) {
-    pdl_wait();
-    pdl_trigger();
-  }
+  cp_async_wait<0>();
 }
 
-int w4_vec_rows(int K, int Ep, int group, bool asym) {
+int w4_vec_rows(int K, int group, bool asym) {
   const int ng = W4_UNIT_K / group;
-  const long room = (long)VEC_SMEM - (long)((vec_fixed_smem(Ep, ng, asym) + 15) & ~size_t(15));
+  const long room = (long)VEC_SMEM - (long)vec_fixed_smem(ng, asym);
   const long rows = room / vec_ld((K + W4_UNIT_K - 1) / W4_UNIT_K);
   return (int)(rows < 0 ? 0 : rows < VEC_ROWS_MOST ? rows : VEC_ROWS_MOST);
 }
@@ -448,12 +426,11 @@ int w4_vec_rows(int K, int Ep, int group, bool asym) {
 cudaError_t launch_w4_vec(W4VecArgs a, int num_sms, cudaStream_t st, int* launches) {
   const int ng = W4_UNIT_K / a.group;
   const bool asym = a.zeros != nullptr;
-  const size_t fixed = (vec_fixed_smem(a.Ep, ng, asym) + 15) & ~size_t(15);
-  a.rows_cap = w4_vec_rows(a.K, a.Ep, a.group, asym);
+  a.rows_cap = w4_vec_rows(a.K, a.group, asym);
   const long slots = (long)a.T * a.kp;
   if (a.rows_cap > slots) a.rows_cap = (int)slots;
   a.group_rows = a.rows_cap < VEC_ROWS ? a.rows_cap : VEC_ROWS;
-  const size_t smem = fixed + (size_t)a.rows_cap * vec_ld(a.KU);
+  const size_t smem = vec_fixed_smem(ng, asym) + (size_t)a.rows_cap * vec_ld(a.KU);
   ++*launches;
 #define MOE_W4_VEC(ASYM, NG)                                                                  \
   do {                                                                                        \
