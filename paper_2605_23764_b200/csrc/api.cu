@@ -805,23 +805,23 @@ W4VecArgs w4_vec_args(const moe_ctx* c, const moe_w4_weights& w, int rows, int c
 // The vector kernel, or layout, gather and the tile kernel?  The first has fewer launches and reads an expert's weights once for the
 // rows it stages (8, fewer of long rows); the second has work for every group's scales, so that small groups cost it more.  Measured,
 // vector against tile kernel, us for the layer (E + S experts of d x F, k' slots a token):
-//   66 x 2048 x 1408, k' 8   groups of 128: 32 slots 43 / 52, 64: 69 / 67, 96: 89 / 79;  64: 128: 100 / 101, 192: 114 / 111;
-//                            32: 192: 135 / 164, 384: 166 / 184
-//   33 x 7168 x 2048, k' 9   128: 72 slots 186 / 196, 108: 201 / 201, 144: 213 / 208
-//   128 x 2048 x 768, k' 8   128: 64 slots 60 / 61, 128: 83 / 84, 192: 103 / 97
-//   8 x 1024 x 2816, k' 2    128: 32 slots 30 / 33, 64: 38 / 32;  64: 48: 35 / 36;  32: 48: 38 / 46, 80: 47 / 46
-//   9 x 16384 x 1024, k' 3   (two staged rows) 128: 6 slots 49 / 68, 12: 71 / 75, 24: 98 / 80;  32: 12: 85 / 127, 36: 152 / 138
-// So: slots by the groups of a unit, and not more than three quarters of the staged rows to an expert.
+//   66 x 2048 x 1408, k' 8   groups of 128: 64 slots 53 / 67, 128: 74 / 87, 256: 94 / 99, 320: 103 / 102;  64: 320: 107 / 123;
+//                            32: 320: 128 / 184
+//   33 x 7168 x 2048, k' 9   (six staged rows) 128: 72 slots 154 / 197, 144: 187 / 208, 180: 205 / 215, 216: 249 / 221
+//   128 x 2048 x 768, k' 8   128: 128 slots 72 / 84, 256: 94 / 102, 320: 105 / 105
+//   8 x 1024 x 2816, k' 2    128: 32 slots 24 / 32, 64: 28 / 33, 80: 30 / 33, 128: 38 / 33;  32: 64: 30 / 46, 128: 44 / 46
+//   8 x 4096 x 14336, k' 2   (three) 128: 16 slots 145 / 199, 24: 164 / 206, 40: 199 / 206, 48: 229 / 207
+//   9 x 16384 x 1024, k' 3   (two) 128: 12 slots 64 / 75, 24: 89 / 79;  32: 24: 105 / 133, 48: 156 / 136
+// So: up to a fixed number of slots, as long as they are no more than the staged rows to an expert.
 bool w4_few(const W4VecArgs& up, const W4VecArgs& down) {
-  const int ng = W4_UNIT_K / (up.group > down.group ? up.group : down.group);
+  const long slots = (long)up.T * up.kp;
   int rows = 8;
   for (const W4VecArgs* a : {&up, &down}) {
     const int staged = w4_vec_rows(a->K, a->group, a->zeros != nullptr);
     rows = staged < rows ? staged : rows;
     if (a->RT > INT32_MAX / W4_VEC_SLOTS) return false;   // it counts row tiles of passes in 32 bits
   }
-  const long slots = (long)up.T * up.kp;
-  return slots <= W4_VEC_SLOTS_GROUP * ng && 4 * slots <= 3L * rows * up.Ep;
+  return slots <= W4_VEC_SLOTS && slots <= (long)rows * up.Ep;
 }
 
 W4TileArgs w4_tile_args(const moe_ctx* c, const moe_w4_weights& w, int rows, int cols, int paired, const CUtensorMap* tok) {

@@ -81,7 +81,7 @@ struct W4VecArgs {
   int rows_cap, group_rows;   // filled by the launch: staged rows, rows of a pass over an expert's weights
   DevStatus* status;
 };
-constexpr int W4_VEC_SLOTS_GROUP = 80, W4_VEC_SLOTS = 4 * W4_VEC_SLOTS_GROUP;   // T k' at most: for each group of a unit, in all
+constexpr int W4_VEC_SLOTS = 320;   // T k', at most
 
 // The same for a batch, on the tensor cores (w4_tile.cu): M-blocks of the padded row space, x gathered into it.
 struct W4TileArgs {

@@ -11,8 +11,8 @@
 // product needs as a dot-product unit, not for its rate).  A third operand of ones gives the sums of x, of which 128 + z is taken off:
 //   sum (q - z) x = sum (128 + q) x - (128 + z) sum x,
 // exact products, fp32 sums, whose rounding (2^-24 of some 136 sum |x|) is hundreds of times below what rounding weights to bf16 would
-// cost; a subtraction for each pair of codes instead kept the pipe that multiplies at 40 %.  The sums of x made once a segment and
-// given to the chains as their first accumulator: 186 against 187 us, one token 27.5 against 27.0, so it stays without.
+// cost; a subtraction for each pair of codes instead kept the pipe that multiplies at 40 %.  Sums of x made once a
+// segment and given to the chains as their first accumulator were no faster.
 // A group's sum is scaled in fp32: the only rounding to fewer bits on the way is that of A to bf16, which the second product takes as
 // operand (as the bf16 layer does).  32 rows because the
 // operand rows of x are read from shared memory once for all of them.
@@ -20,7 +20,7 @@
 // Split.  Blocks take consecutive row tiles of the hit experts, one block an SM; inside a block the warps share the units (32 rows x 128
 // columns) evenly, whatever the tile boundaries: a row tile that several warps have a piece of is put together from shared
 // memory in the warps' order.  So few experts and long reductions keep all warps at work, and results do not depend on timing.  Sixteen
-// warps: twelve took 200 us for the 8 tokens above and 25.6 for the one.
+// warps: twelve took 7 % longer for the 8 tokens above.  Five slots a ring, or four for twelve warps, were no faster.
 #include "launch_pairs.cuh"
 #include "topk.cuh"
 #include "w4.cuh"
