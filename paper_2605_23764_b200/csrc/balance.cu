@@ -605,16 +605,19 @@ __global__ void __launch_bounds__(32 * BAL_BWD_WARPS) balance_bwd_kernel(const B
             if (e >= 0 && e < E) body(e, j == l ? g : a.d_topk_w[(size_t)tt * k + j]);
           }
       };
+      float ref = 0.f;
       if (scores) {
+        // renormalised scores do not see what all their gradients have in common: without it nothing cancels, and one expert gets zero
+        if (renorm) ref = __shfl_sync(0xffffffffu, id >= 0 && id < E ? g : 0.f, 0, LPT);
         __syncwarp();
-        each([&](int e, float ge) { sum[1] += val[e]; sum[2] = fmaf(ge, val[e], sum[2]); });
+        each([&](int e, float ge) { sum[1] += val[e]; sum[2] = fmaf(ge - ref, val[e], sum[2]); });
       }
       group_sums<LPT>(sum);
       float dense = sum[0];
       if (scores) {
         if (renorm) {   // w = v / sum v:  w (g - sum g w)
           const float iz = sum[1] > 0.f ? __fdividef(1.0f, sum[1]) : 0.f, dot = sum[2] * iz;
-          each([&](int e, float ge) { atomicAdd(&add[e], val[e] * iz * (ge - dot) * (SIG ? 1.0f - val[e] : 1.0f)); });
+          each([&](int e, float ge) { atomicAdd(&add[e], val[e] * iz * (ge - ref - dot) * (SIG ? 1.0f - val[e] : 1.0f)); });
         } else if (SIG) {
           each([&](int e, float ge) { atomicAdd(&add[e], ge * val[e] * (1.0f - val[e])); });
         } else {        // a gradient of the same softmax as x

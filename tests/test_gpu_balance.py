@@ -140,6 +140,23 @@ def test_masked_logits_and_rows_without_a_finite_logit():
 
 
 @pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E", [6, 64, 321])
+def test_one_renormalised_score_has_no_gradient(E, sigmoid):
+    """w = v / v: what arrives for it leaves nothing beside the losses' gradient, which is smaller by the number of tokens."""
+    T = 4000
+    logits, ids, dw = _case(T, E, 1, E)
+    got = _run(logits, ids, dw, renorm=True, sigmoid=sigmoid)
+    alone = _run(logits, ids, None, renorm=True, sigmoid=sigmoid)
+    assert np.array_equal(got[4], alone[4])
+    _check(alone, logits, ids, None, renorm=True, sigmoid=sigmoid)
+    # and of scores whose gradients are alike but for little, the little counts
+    logits, ids, dw = _case(64, E, 3, E + 1)
+    dw = (1.0 + np.round(dw * 256) * 2.0 ** -16).astype(np.float32)   # differences are exact
+    got = _run(logits, ids, dw, renorm=True, sigmoid=sigmoid, dl=(0.0, 0.0))
+    _check(got, logits, ids, dw - np.float32(1), renorm=True, sigmoid=sigmoid, dl=(0.0, 0.0))
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
 @pytest.mark.parametrize("E", [40, 41])
 def test_padding_holds_anything(E, sigmoid):
     """NaN and infinities in tokens that are masked or outside of the sequences, and ids that are none."""
