@@ -5,17 +5,18 @@
 // What bounds it: the weights' bytes are the floor, the instructions that widen and multiply them what it takes.  33 experts of 7168 x
 // 2048, groups of 128: 8 tokens 156 us, 4.3 TB/s of codes and scales (an instruction a code to widen them on a pipe of half rate, a product
 // of 16 x 8 x 16 for 256 codes and one more for the sums of x).  One token of eight experts of 2048 x 1408: 22 us, of which reading is 5:
-// three launches, each of the latencies of its ids, first units and rows of x.  Every warp streams its share of the units (2 KB) through a ring of its own in shared
-// memory (loads kept in registers instead did not overlap: a unit then cost a memory latency, 2.7 TB/s), widens the codes to bf16
-// 128 + q -- a mask and an exponent -- and multiplies 32 rows by up to 8 rows of x at a time (mma.m16n8k16, which a matrix-vector
-// product needs as a dot-product unit, not for its rate).  A third operand of ones gives the sums of x, of which 128 + z is taken off:
+// three launches, each of the latencies of its ids, first units and rows of x.
+//
+// Every warp streams its share of the units (2 KB) through a ring of its own in shared memory (loads kept in registers instead did not
+// overlap: a unit then cost a memory latency, 2.7 TB/s), widens the codes to bf16 128 + q -- a mask and an exponent -- and multiplies 32
+// rows by up to 8 rows of x at a time (mma.m16n8k16, which a matrix-vector product needs as a dot-product unit, not for its rate; 32
+// rows because the operand rows of x are read from shared memory once for all of them).  A third operand of ones gives the sums of x, of
+// which 128 + z is taken off:
 //   sum (q - z) x = sum (128 + q) x - (128 + z) sum x,
 // exact products, fp32 sums, whose rounding (2^-24 of some 136 sum |x|) is hundreds of times below what rounding weights to bf16 would
-// cost; a subtraction for each pair of codes instead kept the pipe that multiplies at 40 %.  Sums of x made once a
-// segment and given to the chains as their first accumulator were no faster.
-// A group's sum is scaled in fp32: the only rounding to fewer bits on the way is that of A to bf16, which the second product takes as
-// operand (as the bf16 layer does).  32 rows because the
-// operand rows of x are read from shared memory once for all of them.
+// cost; a subtraction for each pair of codes instead kept the pipe that multiplies at 40 %.  Sums of x made once a segment and given to
+// the chains as their first accumulator were no faster.  A group's sum is scaled in fp32: the only rounding to fewer bits on the way is
+// that of A to bf16, which the second product takes as operand (as the bf16 layer does).
 //
 // Split.  Blocks take consecutive row tiles of the hit experts, one block an SM; inside a block the warps share the units (32 rows x 128
 // columns) evenly, whatever the tile boundaries: a row tile that several warps have a piece of is put together from shared
