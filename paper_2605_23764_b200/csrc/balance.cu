@@ -150,9 +150,9 @@ __device__ __forceinline__ float row_terms(const float (&v)[VPL], float (&ex)[VP
 // 8192 x 256 16 us, in 8 sequences 20; 65536 x 256 25 us (2.7 TB/s), sigmoid scores in 97 sequences 35.
 // ------------------------------------------------------------------------------------------
 // A piece in global memory, two a block: of the sequence that began before the block, of the one that goes on behind it.
-// Per block {seq of both pieces, tokens of both, loss, z, tokens}, then [block][2][E] {sum, count}
+// Per block {seq of both pieces, tokens of both, sums of the block}, then [block][2][E] {sum, count}
 __host__ __device__ constexpr int balance_warps_most(int vpl) { return vpl <= 8 ? BAL_MAX_WARPS : vpl <= 16 ? 24 : 16; }   // registers
-struct BalBlock { int seq[2], n[2]; double loss, z, tokens; };
+struct BalBlock { int seq[2], n[2]; double loss, joined, z, tokens; };   // joined: share of the sequence that goes on behind it
 
 template <int LPT, int VPL, int VW, bool SIG>
 __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kernel(const BalanceArgs a) {
@@ -340,6 +340,7 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
     }
     __syncwarp();
     if (lane < 2) meta[blockIdx.x].seq[lane] = b_seq[lane];
+    if (lane == 0) meta[blockIdx.x].joined = 0.0;
   }
   __syncthreads();
   // .. and their sums in order: every thread has an expert, and a range of the pieces where threads are left
@@ -405,7 +406,7 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
   // first token has it as second piece and its ticket, the others have it as first piece.
   const int nb = gridDim.x;
   auto block_of = [&](int t) { return t / a.chunk; };
-  auto join = [&](int sq) {   // fills the sequence's outputs and adds the threads' shares of the loss
+  auto join = [&](int sq, double& loss) {   // fills the sequence's outputs and adds the threads' shares of its loss
     const int first = block_of(seqs.begin(sq)), last = block_of(seqs.begin(sq + 1) - 1);
     if (parts == 1) __syncthreads();   // (an earlier join's tokens have been used)
     if (warp == warps - 1) {
@@ -425,26 +426,28 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
              const float inv = s_live ? 1.0f / (float)s_live : 0.f;
              a.counts[(size_t)sq * E + e] = cnt;
              a.prob[(size_t)sq * E + e] = sum * inv;
-             my_loss += (double)(unit * ((float)cnt * inv) * (sum * inv));
+             loss += (double)(unit * ((float)cnt * inv) * (sum * inv));
            });
   };
-  // the sums of three values over the block, in thread 0; the order is fixed
-  auto block_sums = [&](double x, double y, double w, double (&r)[3]) {
+  // sums over the block, in thread 0; the order is fixed
+  auto block_sums = [&](auto& v) {
+    constexpr int N = sizeof(v) / sizeof(double);
 #pragma unroll
-    for (int off = 16; off; off >>= 1) {
-      x += __shfl_xor_sync(0xffffffffu, x, off);
-      y += __shfl_xor_sync(0xffffffffu, y, off);
-      w += __shfl_xor_sync(0xffffffffu, w, off);
-    }
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int off = 16; off; off >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], off);
     __syncthreads();
-    if (lane == 0) { s_sum[0][warp] = x; s_sum[1][warp] = y; s_sum[2][warp] = w; }
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s_sum[i][warp] = v[i];
+    }
     __syncthreads();
     if (warp == 0) {
 #pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        r[i] = lane < warps ? s_sum[i][lane] : 0.0;
+      for (int i = 0; i < N; ++i) {
+        v[i] = lane < warps ? s_sum[i][lane] : 0.0;
 #pragma unroll
-        for (int off = 16; off; off >>= 1) r[i] += __shfl_xor_sync(0xffffffffu, r[i], off);
+        for (int off = 16; off; off >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], off);
       }
     }
   };
@@ -462,16 +465,20 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
       s_last[threadIdx.x] = last_one;
     }
     __syncthreads();
+    // Which block joins depends on timing, so a sequence's share does not count as this block's: it goes to the sequence's first one.
 #pragma unroll 1
     for (int h = 0; h < 2; ++h)
       if (s_last[h]) {
         __threadfence();
-        join(b_seq[h]);
+        double loss[1] = {0.0};
+        join(b_seq[h], loss[0]);
+        block_sums(loss);
+        if (threadIdx.x == 0) meta[block_of(seqs.begin(b_seq[h]))].joined = loss[0];
       }
   }
   // the warps' z and tokens: lane 0 of each has them still
-  double r[3];
-  block_sums(my_loss, lane == 0 ? zsum : 0.0, lane == 0 ? (double)tokens : 0.0, r);
+  double r[3] = {my_loss, lane == 0 ? zsum : 0.0, lane == 0 ? (double)tokens : 0.0};
+  block_sums(r);
   auto finish = [&]() {
     if (threadIdx.x == 0) {
       a.losses[0] = (float)r[0];
@@ -493,21 +500,17 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
 
   // ---- the last block of all
   for (int i = threadIdx.x; i <= nb; i += blockDim.x) a.tickets[i] = 0;   // for the next call
-  double total = 0.0, total_z = 0.0, total_tokens = 0.0;
+  for (int i = 0; i < 3; ++i) r[i] = 0.0;
   for (int b = threadIdx.x; b < nb; b += blockDim.x) {
-    total += __ldcg(&meta[b].loss);
-    total_z += __ldcg(&meta[b].z);
-    total_tokens += __ldcg(&meta[b].tokens);
+    r[0] += __ldcg(&meta[b].loss) + __ldcg(&meta[b].joined);
+    r[1] += __ldcg(&meta[b].z);
+    r[2] += __ldcg(&meta[b].tokens);
   }
   if (n == 1) {
     const int begins = seqs.begin(0), stop = seqs.begin(1);
-    if (begins < stop && block_of(begins) < block_of(stop - 1)) {
-      my_loss = 0.0;
-      join(0);
-      total += my_loss;
-    }
+    if (begins < stop && block_of(begins) < block_of(stop - 1)) join(0, r[0]);
   }
-  block_sums(total, total_z, total_tokens, r);
+  block_sums(r);
   finish();
 }
 
