@@ -1374,6 +1374,8 @@ int moe_debug_layout_blocks(int32_t T, int32_t kp, int32_t Ep, int32_t fits8, in
   return layout_blocks(T, kp, Ep, fits8 != 0, fits16 != 0);
 }
 
+int moe_debug_balance_blocks(int32_t T, int32_t E) { return T < 0 || E < 1 || E > 1024 ? 0 : balance_fwd_blocks(T, E); }
+
 int moe_debug_buffer(moe_ctx* c, int which, void** ptr, size_t* elems) {
   if (!c || !ptr || !elems) return MOE_ERR_INVALID_ARG;
   const moe_shape& s = c->shape;

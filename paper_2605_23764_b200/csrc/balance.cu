@@ -663,36 +663,38 @@ __global__ void __launch_bounds__(32 * BAL_BWD_WARPS) balance_bwd_kernel(const B
 
 // ------------------------------------------------------------------------------------------
 // Lanes a token and values a lane by the number of experts; vectors of four where rows are whole 16-byte pieces.
-template <class F>
+struct BalShape { int most, lpt, vpl; };   // experts, at most
+constexpr BalShape BAL_SHAPES[] = {{8, 1, 8}, {32, 2, 16}, {64, 4, 16}, {128, 8, 16}, {256, 16, 16}, {512, 32, 16}, {1024, 32, 32}};
+constexpr int BAL_NUM_SHAPES = sizeof(BAL_SHAPES) / sizeof(BAL_SHAPES[0]);
+static BalShape balance_shape(int E) {
+  int i = 0;
+  while (i + 1 < BAL_NUM_SHAPES && E > BAL_SHAPES[i].most) ++i;
+  return BAL_SHAPES[i];
+}
+template <int I = 0, class F>
 static cudaError_t with_balance_shape(int E, bool vec, F f) {
-#define MOE_BAL_CASE(LPT, VPL) return vec ? f(std::integral_constant<int, LPT>(), std::integral_constant<int, VPL>(), std::integral_constant<int, 4>()) \
-                                          : f(std::integral_constant<int, LPT>(), std::integral_constant<int, VPL>(), std::integral_constant<int, 1>())
-  if (E <= 8) MOE_BAL_CASE(1, 8);
-  if (E <= 32) MOE_BAL_CASE(2, 16);
-  if (E <= 64) MOE_BAL_CASE(4, 16);
-  if (E <= 128) MOE_BAL_CASE(8, 16);
-  if (E <= 256) MOE_BAL_CASE(16, 16);
-  if (E <= 512) MOE_BAL_CASE(32, 16);
-  MOE_BAL_CASE(32, 32);
-#undef MOE_BAL_CASE
+  constexpr BalShape s = BAL_SHAPES[I];
+  if constexpr (I + 1 < BAL_NUM_SHAPES)
+    if (E > s.most) return with_balance_shape<I + 1>(E, vec, f);
+  constexpr std::integral_constant<int, s.lpt> lpt{};
+  constexpr std::integral_constant<int, s.vpl> vpl{};
+  return vec ? f(lpt, vpl, std::integral_constant<int, 4>()) : f(lpt, vpl, std::integral_constant<int, 1>());
 }
 
 static bool rows_of_vectors(const void* p, int E) { return E % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 static int balance_warps(int E) {
-  int warps = balance_warps_most(E <= 8 ? 8 : E <= 512 ? 16 : 32);
+  int warps = balance_warps_most(balance_shape(E).vpl);
   while (warps > 4 && 5 * warps * E * (int)sizeof(int) > BAL_SMEM) warps >>= 1;
   return warps;
 }
 // Tokens of a block: as many blocks as leave every warp a round of tokens, up to one an SM (few tokens are bound by the latencies of
 // a round).
 static int balance_chunk(int T, int E) {
-  int lpt = 1;
-  while (lpt < 32 && (E <= 8 ? 8 : 16) * lpt < E) lpt <<= 1;
-  const int per_block = balance_warps(E) * (32 / lpt), even = (T + BAL_MAX_BLOCKS - 1) / BAL_MAX_BLOCKS;
-  return even > per_block ? even : per_block;
+  const int round = balance_warps(E) * (32 / balance_shape(E).lpt), even = (T + BAL_MAX_BLOCKS - 1) / BAL_MAX_BLOCKS;
+  return even > round ? even : round;
 }
-static int balance_fwd_blocks(int T, int E) {
+int balance_fwd_blocks(int T, int E) {
   const int chunk = balance_chunk(T, E);
   return T > chunk ? (T + chunk - 1) / chunk : 1;
 }

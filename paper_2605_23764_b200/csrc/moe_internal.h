@@ -235,6 +235,7 @@ struct BalanceArgs {
   float* d_logits;             // [T][E]
 };
 size_t balance_scratch_bytes(int E);
+int balance_fwd_blocks(int T, int E);
 cudaError_t launch_balance_fwd(BalanceArgs a, cudaStream_t s, int* launches);
 cudaError_t launch_balance_bwd(const BalanceArgs& a, int num_sms, cudaStream_t s, int* launches);
 
