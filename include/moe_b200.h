@@ -259,7 +259,8 @@ int moe_router_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, c
  * moe_balance_bwd: d_logits[T][E] fp32 (overwritten; may be the logits themselves) = d_losses[0] * d losses[0] / d logits +
  * d_losses[1] * d losses[1] / d logits (the counts pass no gradient) + what moe_router_bwd gives for d_topk_w[T][k] (NULL: without;
  * then topk_ids may be NULL too).  An expert that a token names twice gets both gradients.  counts and tokens as the forward left them,
- * d_losses[2] on the device.  Tokens that take no part get the scores' gradient alone.
+ * d_losses[2] on the device.  Tokens that take no part get the scores' gradient alone, and zeros, whatever their logits hold, where
+ * none arrives: without d_topk_w, or where a token's are all 0.
  * Offsets that do not ascend give unspecified values.  Both calls are asynchronous on `stream`. */
 int moe_balance_fwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, int32_t T, const int32_t* seq_offsets, int32_t n_seq,
                     const uint8_t* token_mask, float* losses, int32_t* counts, float* prob, int32_t* tokens, void* stream);

@@ -609,12 +609,15 @@ __global__ void __launch_bounds__(32 * BAL_BWD_WARPS) balance_bwd_kernel(const B
           }
       };
       float ref = 0.f;
+      bool mine = false;   // a score's gradient that is not zero
       if (scores) {
         // renormalised scores do not see what all their gradients have in common: without it nothing cancels, and one expert gets zero
         if (renorm) ref = __shfl_sync(0xffffffffu, id >= 0 && id < E ? g : 0.f, 0, LPT);
         __syncwarp();
-        each([&](int e, float ge) { sum[1] += val[e]; sum[2] = fmaf(ge - ref, val[e], sum[2]); });
+        each([&](int e, float ge) { sum[1] += val[e]; sum[2] = fmaf(ge - ref, val[e], sum[2]); mine |= ge != 0.f; });
       }
+      const uint32_t arrives = __ballot_sync(0xffffffffu, mine) >> (grp * LPT) & (0xffffffffu >> (32 - LPT));   // for the group's token
+      const bool idle = !on && !arrives;
       group_sums<LPT>(sum);
       float dense = sum[0];
       if (scores) {
@@ -642,7 +645,7 @@ __global__ void __launch_bounds__(32 * BAL_BWD_WARPS) balance_bwd_kernel(const B
         each([&](int e, float) { add[e] = 0.f; });
       }
       float* const out = a.d_logits + (size_t)tt * E;
-      if (tt < end && !on && !scores) {   // a token that takes no part, whatever its logits hold
+      if (tt < end && idle) {   // whatever its logits hold
         for (int e = l; e < E; e += LPT) out[e] = 0.f;
       } else if (tt < end) {
 #pragma unroll
