@@ -591,13 +591,16 @@ __global__ void __launch_bounds__(32 * BAL_BWD_WARPS) balance_bwd_kernel(const B
       fetch(t0 + TPW);
       float soft[VPL], p[SIG ? VPL : 1], sig[SIG ? VPL : 1], inv[2];
       const float lse = row_terms<LPT, VPL, SIG>(v, soft, p, sig, inv);
-      float sum[3] = {0.f, 0.f, 0.f};   // p x; of the selected experts v and g v, v = softmax or sigmoid
+      // p x; of the selected experts v and g v, v = sigmoid or softmax -- the softmax's terms as they are for renormalised scores, which are
+      // the same and whose sum has a reciprocal
+      float sum[3] = {0.f, 0.f, 0.f};
+      const float v_scale = renorm ? 1.0f : inv[0];
 #pragma unroll
       for (int i = 0; i < VPL; ++i) {
+        const int e = expert_at<LPT, VW>(i, l);
+        if (scores && e < E) val[e] = SIG ? sig[SIG ? i : 0] : soft[i] * v_scale;
         soft[i] *= inv[0];
         if constexpr (SIG) p[i] *= inv[1];
-        const int e = expert_at<LPT, VW>(i, l);
-        if (scores && e < E) val[e] = SIG ? sig[SIG ? i : 0] : soft[i];
         if (on) sum[0] = fmaf(SIG ? p[SIG ? i : 0] : soft[i], x[i], sum[0]);
       }
       // lane l of the group has the ids l, l + LPT, ..
