@@ -270,7 +270,7 @@ int moe_balance_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, 
 
 /* ---- Experts with 4-bit weights ---------------------------------------------------------------------------
  * A weight is w = s (q - z): codes q in 0..15, a bf16 scale s and, in matrices with zero points, z in 0..15 for every `group` (32, 64
- * or 128) consecutive columns of a row; without zero points z = 8.  cols need not be a multiple of the group.
+ * or 128) consecutive columns of a row; without zero points z = 8.  cols need not be a multiple of the group.  rows, cols < 2^31 - 128.
  *
  * Weights are laid out once for the kernels: n matrices [rows][cols] (cols % 8 == 0) become codes (n * code_bytes), scales (n *
  * group_elems bf16) and zeros (n * group_elems bytes; NULL: no zero points), all 16-byte aligned, the sizes from moe_w4_sizes.  The

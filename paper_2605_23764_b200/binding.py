@@ -296,6 +296,14 @@ except AttributeError:
         return torch.cuda.current_stream().cuda_stream
 
 
+def _i32(v, name):
+    """ctypes would pass the lowest 32 bits of a larger number."""
+    v = int(v)
+    if not -2**31 <= v < 2**31:
+        raise MoeError(f"{name}: {v} is not a 32-bit number")
+    return v
+
+
 _BF, _I32, _F32 = torch.bfloat16, torch.int32, torch.float32
 
 
@@ -438,6 +446,7 @@ def _here(t, dtype, name, n=0):
 @_sizes_first
 def moe_balance_fwd(ctx, logits, topk_ids, T, seq_offsets, n_seq, token_mask, losses, counts, prob, tokens):
     _, _, E, k, _, _, _ = _shape_of(ctx)
+    T, n_seq = _i32(T, "T"), _i32(n_seq, "n_seq")
     _check(load_library().moe_balance_fwd(ctx, _here(logits, _F32, "logits", T * E), _here(topk_ids, _I32, "topk_ids", T * k), T,
                                           _here(seq_offsets, _I32, "seq_offsets", n_seq + 1), n_seq,
                                           _here(token_mask, torch.uint8, "token_mask", T), _here(losses, _F32, "losses", 2),
@@ -448,6 +457,7 @@ def moe_balance_fwd(ctx, logits, topk_ids, T, seq_offsets, n_seq, token_mask, lo
 @_sizes_first
 def moe_balance_bwd(ctx, logits, topk_ids, counts, tokens, d_losses, d_topk_w, T, seq_offsets, n_seq, token_mask, d_logits):
     _, _, E, k, _, _, _ = _shape_of(ctx)
+    T, n_seq = _i32(T, "T"), _i32(n_seq, "n_seq")
     _check(load_library().moe_balance_bwd(ctx, _here(logits, _F32, "logits", T * E), _here(topk_ids, _I32, "topk_ids", T * k),
                                           _here(counts, _I32, "counts", n_seq * E), _here(tokens, _I32, "tokens", n_seq + 1),
                                           _here(d_losses, _F32, "d_losses", 2), _here(d_topk_w, _F32, "d_topk_w", T * k), T,
@@ -459,7 +469,7 @@ def moe_balance_bwd(ctx, logits, topk_ids, counts, tokens, d_losses, d_topk_w, T
 def moe_w4_sizes(rows, cols, group, flags=0):
     """(bytes of codes, elements of scales and of zero points) of one matrix."""
     code_bytes, elems = ctypes.c_size_t(), ctypes.c_size_t()
-    _check(load_library().moe_w4_sizes(int(rows), int(cols), int(group), int(flags), ctypes.byref(code_bytes), ctypes.byref(elems)),
+    _check(load_library().moe_w4_sizes(_i32(rows, "rows"), _i32(cols, "cols"), _i32(group, "group"), int(flags), ctypes.byref(code_bytes), ctypes.byref(elems)),
            "moe_w4_sizes")
     return code_bytes.value, elems.value
 
@@ -467,6 +477,7 @@ def moe_w4_sizes(rows, cols, group, flags=0):
 @_sizes_first
 def moe_w4_quantize(W, n, rows, cols, group, flags, codes, scales, zeros):
     nb, ne = moe_w4_sizes(rows, cols, group, flags)
+    n = _i32(n, "n")
     _check(load_library().moe_w4_quantize(_here(W, _BF, "W", n * rows * cols), n, rows, cols, group, flags,
                                           _here(codes, _I32, "codes", n * nb // 4), _here(scales, _BF, "scales", n * ne),
                                           _here(zeros, torch.uint8, "zeros", n * ne), _stream()), "moe_w4_quantize")
@@ -475,6 +486,7 @@ def moe_w4_quantize(W, n, rows, cols, group, flags, codes, scales, zeros):
 @_sizes_first
 def moe_w4_pack(q, q_scales, q_zeros, n, rows, cols, group, flags, codes, scales, zeros):
     nb, ne = moe_w4_sizes(rows, cols, group, flags)
+    n = _i32(n, "n")
     nq = n * rows * -(-cols // group)
     _check(load_library().moe_w4_pack(_here(q, torch.uint8, "q", n * rows * cols // 2), _here(q_scales, _BF, "q_scales", nq),
                                       _here(q_zeros, torch.uint8, "q_zeros", nq), n, rows, cols, group, flags,
@@ -485,6 +497,7 @@ def moe_w4_pack(q, q_scales, q_zeros, n, rows, cols, group, flags, codes, scales
 @_sizes_first
 def moe_w4_dequantize(codes, scales, zeros, group, n, rows, cols, flags, W):
     nb, ne = moe_w4_sizes(rows, cols, group, flags)
+    n = _i32(n, "n")
     w = _W4(_here(codes, _I32, "codes", n * nb // 4), _here(scales, _BF, "scales", n * ne), _here(zeros, torch.uint8, "zeros", n * ne), group)
     _check(load_library().moe_w4_dequantize(ctypes.byref(w), n, rows, cols, flags, _here(W, _BF, "W", n * rows * cols), _stream()),
            "moe_w4_dequantize")
@@ -499,6 +512,7 @@ def _w4_of_shape(W, n, rows, cols, gate_up, name):
 def moe_ffn_fwd_w4(ctx, x, topk_ids, topk_w, W_gate_up, W_down, out, T):
     """W_gate_up, W_down: MoeW4Weights."""
     _, d, E, k, S, F, _ = _shape_of(ctx)
+    T = _i32(T, "T")
     _w4_of_shape(W_gate_up, E + S, 2 * F, d, True, "W_gate_up")
     _w4_of_shape(W_down, E + S, d, F, False, "W_down")
     ws = []

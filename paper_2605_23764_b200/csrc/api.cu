@@ -1161,7 +1161,8 @@ int moe_ffn_fwd(moe_ctx* c, const uint16_t* x, const int32_t* topk_ids, const fl
 
 int moe_w4_sizes(int32_t rows, int32_t cols, int32_t group, uint32_t flags, size_t* code_bytes, size_t* group_elems) {
   const int paired = (flags & MOE_W4_GATE_UP) ? 1 : 0;
-  if (rows < 1 || cols < 8 || cols % 8 || !w4_group_ok(group) || (flags & ~MOE_W4_GATE_UP) || (paired && rows % 16)) return MOE_ERR_INVALID_ARG;
+  constexpr int MOST = INT32_MAX - 128;   // sizes are rounded up to 128
+  if (rows < 1 || rows > MOST || cols < 8 || cols > MOST || cols % 8 || !w4_group_ok(group) || (flags & ~MOE_W4_GATE_UP) || (paired && rows % 16)) return MOE_ERR_INVALID_ARG;
   const W4Shape s{rows, cols, group, paired};
   if (code_bytes) *code_bytes = (size_t)s.stored_tiles() * s.units() * W4_UNIT_BYTES;
   if (group_elems) *group_elems = (size_t)s.stored_tiles() * s.units() * s.unit_groups() * W4_TILE_ROWS;

@@ -251,6 +251,10 @@ T* here(PyObject* o, at::ScalarType type, int64_t n) {
 }
 template <class T>
 T* here_or_null(PyObject* o, at::ScalarType type, int64_t n) { return o == Py_None ? nullptr : here<T>(o, type, n); }
+int64_t rows_of(const at::Tensor& t) {   // a token count: the slower path refuses what is none
+  if (t.dim() != 2 || t.size(0) > INT32_MAX) throw Slow();
+  return t.size(0);
+}
 int64_t sequences(PyObject* o) {   // of an offsets tensor
   if (o == Py_None) return 1;
   const int64_t n = tensor(o).numel() - 1;
@@ -263,8 +267,7 @@ PyObject* balance_fwd_new(PyObject*, PyObject* const* a, Py_ssize_t n) {   // ct
     moe_ctx* c = static_cast<moe_ctx*>(handle(a[0]));
     const Shape& s = shape_of(c);
     const at::Tensor& l = tensor(a[1]);
-    if (l.dim() != 2) throw Slow();
-    const int64_t T = l.size(0), ns = sequences(a[3]);
+    const int64_t T = rows_of(l), ns = sequences(a[3]);
     const float* logits = here<float>(a[1], F32, T * s.E);
     const int32_t *ids = here<int32_t>(a[2], I32, T * s.k), *off = here_or_null<int32_t>(a[3], I32, ns + 1);
     const uint8_t* mask = here_or_null<uint8_t>(a[4], at::kByte, T);
@@ -283,8 +286,7 @@ PyObject* balance_bwd_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
     moe_ctx* c = static_cast<moe_ctx*>(handle(a[0]));
     const Shape& s = shape_of(c);
     const at::Tensor& l = tensor(a[1]);
-    if (l.dim() != 2) throw Slow();
-    const int64_t T = l.size(0), ns = sequences(a[7]);
+    const int64_t T = rows_of(l), ns = sequences(a[7]);
     const float* logits = here<float>(a[1], F32, T * s.E);
     const float* dw = here_or_null<float>(a[6], F32, T * s.k);
     const int32_t *ids = dw ? here<int32_t>(a[2], I32, T * s.k) : nullptr, *counts = here<int32_t>(a[3], I32, ns * s.E),
@@ -305,8 +307,7 @@ PyObject* ffn_fwd_w4_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
     moe_ctx* c = static_cast<moe_ctx*>(handle(a[0]));
     const Shape& s = shape_of(c);
     const at::Tensor& xt = tensor(a[1]);
-    if (xt.dim() != 2) throw Slow();
-    const int64_t T = xt.size(0);
+    const int64_t T = rows_of(xt);
     const uint16_t* x = here<uint16_t>(a[1], BF, T * s.d);
     const int32_t* ids = here<int32_t>(a[2], I32, T * s.k);
     const float* w = here<float>(a[3], F32, T * s.k);
