@@ -127,7 +127,8 @@ __global__ void __launch_bounds__(32 * CODE_WARPS) w4_encode_kernel(const void* 
           }
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        scale[q] = bf16_round(asym ? __fdiv_rn(hi[q] - lo[q], 15.f) : __fdiv_rn(hi[q], 7.f));
+        // (hi - lo) / 15 of halves, which are exact: the difference may be beyond fp32
+        scale[q] = bf16_round(asym ? __fdiv_rn(__fmaf_rn(0.5f, hi[q], -0.5f * lo[q]), 7.5f) : __fdiv_rn(hi[q], 7.f));
         const float step = scale[q] > 0.f ? scale[q] : 1.f;
         zero[q] = asym ? fminf(fmaxf(rintf(__fdiv_rn(-lo[q], step)), 0.f), 15.f) : 8.f;
         inv[q] = __fdividef(1.0f, step);
