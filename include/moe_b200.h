@@ -68,7 +68,7 @@ enum {
                                     next on the stream (e.g. the backward) instead of in front of it; out_host is complete
                                     once a LATER call on the context -- moe_ffn_bwd_host, the next moe_ffn_fwd_host,
                                     moe_get_status -- has completed, not yet when this call's stream work has */
-  MOE_FLAG_W4 = 64u,           /* room in the workspace for moe_ffn_fwd_w4: T_max * (k + n_shared) + 127 (E + n_shared) fp32 rows of d */
+  MOE_FLAG_W4 = 64u,           /* room in the workspace for moe_ffn_fwd_w4: n + 127 min(n, E + n_shared) fp32 rows of d, n = T_max * (k + n_shared) */
   MOE_FLAG_TRACE = 8u,         /* the persistent launches record a per-tile trace (role, phase, item,
                                   start and end time) into the workspace; read it with
                                   moe_debug_trace (moe_b200_debug.h).  Costs 8 MB of workspace and one

@@ -191,7 +191,9 @@ WsPlan plan_workspace(const moe_shape& s) {
   p.trace = c.take((size_t)p.trace_cap * 32);
   p.balance = c.take(balance_scratch_bytes(s.E));
   p.tickets = c.take(sizeof(int) * (BAL_MAX_BLOCKS + 1));
-  p.Y4 = c.take((s.flags & MOE_FLAG_W4) ? sizeof(float) * cap * s.d : 0);
+  // an expert without a row has no padding either, and no more experts have rows than there are slots
+  const size_t w4_rows = slots + (slots < (size_t)Ep ? slots : Ep) * (BLOCK_M - 1);
+  p.Y4 = c.take((s.flags & MOE_FLAG_W4) ? sizeof(float) * w4_rows * s.d : 0);
   p.total = c.off;
   return p;
 }

@@ -60,3 +60,14 @@ def test_numbers_that_are_no_32_bit_numbers():
     with pytest.raises(MoeError, match="n: "):
         B.moe_w4_pack(wide(torch.zeros(1, 1, 1, dtype=u8), many, 16, 4), wide(torch.zeros(1, 1, 1, dtype=bf), many, 16, 1), None, many, 16, 8, 32, 0, codes,
                       scales, None)
+
+
+def test_the_workspace_has_room_for_the_rows_that_there_can_be():
+    """One token of a layer of 257 experts hits nine of them."""
+    def room(T, d, E, k, S, F):
+        return B.moe_workspace_bytes(T, d, E, k, S, F, B.MOE_FLAG_W4) - B.moe_workspace_bytes(T, d, E, k, S, F)
+
+    for T, d, E, k, S, F in ((1, 7168, 256, 8, 1, 2048), (8, 7168, 256, 8, 1, 2048), (64, 2048, 64, 6, 2, 1408), (4096, 2048, 64, 6, 2, 1408), (0, 64, 4, 2, 0, 32)):
+        slots = T * (k + S)
+        need = (slots + 127 * min(slots, E + S)) * d * 4
+        assert need <= room(T, d, E, k, S, F) <= need + 512, (T, E)
