@@ -285,8 +285,8 @@ int moe_balance_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, 
  * moe_ffn_fwd_w4: moe_ffn_fwd's layer over such weights (W_gate_up: E + S matrices [2F][d], W_down: E + S matrices [d][F]), any T up to
  * T_max, on a context with MOE_FLAG_W4 (MOE_ERR_STATE otherwise).  bf16 x and out, fp32 sums, scales applied in fp32; the activations
  * between the two products are bf16.  It uses the context's layout: a forward saved for moe_ffn_bwd is given up.
- * Finite x and activations below 2^119 (about 6e35): a sum is taken over 128 + q and corrected.  The two matrices' groups, and whether
- * they have zero points, are each one's own. */
+ * x and activations below 2^115 (about 4e34): for few tokens a group's sum is taken over 16 + q, and 16 + z times the sum of x off it.
+ * The two matrices' groups, and whether they have zero points, are each one's own. */
 #define MOE_W4_GATE_UP 1u
 typedef struct {
   const uint32_t* codes;

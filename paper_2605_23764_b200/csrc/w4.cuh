@@ -8,9 +8,11 @@
 // given of a 16 x 16 bf16 operand of a matrix instruction -- the pairs of columns {2 c, 2 c + 1} and {2 c + 8, 2 c + 9} of rows g
 // and g + 8:
 //   pair r (0: row g, first pair; 1: row g + 8, first; 2: row g, second; 3: row g + 8, second)
-//   has its even column in bits 4 r .. 4 r + 3 and its odd column in bits 16 + 4 r ..
-// so that (word >> 4 r) & 0x000F000F is a pair in the place of two bf16 mantissas.  The same fragment is what a warp writes to
-// TMEM for 16 lanes x 8 columns (two bf16 each), so matrix-vector and tensor-core kernels read one layout.
+//   has its even column in bits 4 r + 3 .. 4 r + 6 and its odd column in bits 4 r + 19 .., counted round the word's end,
+// so that (word rotated right by 4 r) & 0x00780078 is a pair in the place of the highest mantissa bits of two bf16 numbers: with the
+// exponent of 16 they are 16 + q.  (In the lowest bits they would be 128 + q: what is taken off again would be five times as much.)
+// The same fragment is what a warp writes to TMEM for 16 lanes x 8 columns (two bf16 each), so matrix-vector and tensor-core kernels
+// read one layout.
 // Scales [unit][8][groups of a unit][4] bf16 and zero points [..] bytes: lanes 4 g + c need rows {g, g + 8, g + 16, g + 24} of the unit's
 // 1, 2 or 4 groups, side by side, in the same order of units.
 // Rows of W_gate_up: of 16 rows, 0 .. 7 are gate rows, 8 .. 15 the up rows of the same features (SwiGLU needs no exchange).
@@ -37,28 +39,28 @@ struct W4Shape {
   }
 };
 
-// The four registers of a 16 x 16 bf16 operand from a word of codes: 128 + q, the codes being the low mantissa bits.
-constexpr uint32_t W4_MAGIC = 0x43004300u;
+// The four registers of a 16 x 16 bf16 operand from a word of codes: 16 + q, the codes being the high mantissa bits.
+constexpr uint32_t W4_MAGIC = 0x41804180u;
 __device__ __forceinline__ uint32_t w4_pair(uint32_t word) {
   uint32_t r;
-  asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(r) : "r"(word), "r"(W4_MAGIC));   // (word & mask) | magic
+  asm("lop3.b32 %0, %1, 0x00780078, %2, 0xEA;" : "=r"(r) : "r"(word), "r"(W4_MAGIC));   // (word & mask) | magic
   return r;
 }
 __device__ __forceinline__ void w4_fragment(uint32_t word, uint32_t (&a)[4]) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) a[r] = w4_pair(word >> (4 * r));
+  for (int r = 0; r < 4; ++r) a[r] = w4_pair(r < 3 ? word >> (4 * r) : __funnelshift_r(word, word, 12));
 }
 // Unit ku of row tile rt of a matrix of KU units a row tile.
 __host__ __device__ __forceinline__ int64_t w4_unit(int rt, int ku, int KU) { return ((int64_t)(rt >> 2) * KU + ku) * 4 + (rt & 3); }
 
-// 128 + q less 128 + z: a whole number, exact.  A fused multiply-add by one: the subtraction of bf16 pairs is not one instruction here.
-__host__ __device__ __forceinline__ uint32_t w4_bias(uint32_t z) { return 0xC300C300u | z * 0x00010001u; }   // - (128 + z), twice
+// 16 + q less 16 + z: a whole number, exact.  A fused multiply-add by one: the subtraction of bf16 pairs is not one instruction here.
+__host__ __device__ __forceinline__ uint32_t w4_bias(uint32_t z) { return 0xC180C180u | z * 0x00080008u; }   // - (16 + z), twice
 __device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(0x3F803F80u), "r"(b));
   return r;
 }
-__device__ __forceinline__ float w4_offset(uint32_t z) { return __uint_as_float(0x43000000u | (z & 0xFFu) << 16); }   // 128 + z, z < 128
+__device__ __forceinline__ float w4_offset(uint32_t z) { return __uint_as_float(0x41800000u | (z & 0xFu) << 19); }   // 16 + z
 
 // One expert product of the layer over experts with few rows (w4_vec.cu).
 struct W4VecArgs {

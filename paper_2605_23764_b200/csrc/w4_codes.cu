@@ -37,7 +37,7 @@ __device__ __forceinline__ uint4 gather_words(const uint32_t* st, int b, int lan
     uint32_t w = 0;
 #pragma unroll
     for (int r = 0; r < 4; ++r) w += ((in[r] >> c4) & 0x000F000Fu) << (4 * r);
-    out[j] = w;
+    out[j] = __funnelshift_l(w, w, 3);
   }
   return make_uint4(out[0], out[1], out[2], out[3]);
 }
@@ -52,7 +52,9 @@ __device__ __forceinline__ uint32_t split_word(uint32_t natural) { return squeez
 __device__ __forceinline__ void scatter_words(uint32_t* st, int b, int lane, uint4 v) {
   const int g = lane >> 2, c = lane & 3;
   uint8_t* by = reinterpret_cast<uint8_t*>(st);
-  const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+  uint32_t in[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) in[j] = __funnelshift_r(in[j], in[j], 3);
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll

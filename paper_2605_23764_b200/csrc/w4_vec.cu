@@ -8,15 +8,16 @@
 // three launches, each of the latencies of its ids, first units and rows of x.
 //
 // Every warp streams its share of the units (2 KB) through a ring of its own in shared memory (loads kept in registers instead did not
-// overlap: a unit then cost a memory latency, 2.7 TB/s), widens the codes to bf16 128 + q -- a mask and an exponent -- and multiplies 32
+// overlap: a unit then cost a memory latency, 2.7 TB/s), widens the codes to bf16 16 + q -- a mask and an exponent -- and multiplies 32
 // rows by up to 8 rows of x at a time (mma.m16n8k16, which a matrix-vector product needs as a dot-product unit, not for its rate; 32
 // rows because the operand rows of x are read from shared memory once for all of them).  A third operand of ones gives the sums of x, of
-// which 128 + z is taken off:
-//   sum (q - z) x = sum (128 + q) x - (128 + z) sum x,
-// exact products, fp32 sums, whose rounding (2^-24 of some 136 sum |x|) is hundreds of times below what rounding weights to bf16 would
-// cost; a subtraction for each pair of codes instead kept the pipe that multiplies at 40 %.  Sums of x made once a segment and given to
-// the chains as their first accumulator were no faster.  A group's sum is scaled in fp32: the only rounding to fewer bits on the way is
-// that of A to bf16, which the second product takes as operand (as the bf16 layer does).
+// which 16 + z is taken off:
+//   sum (q - z) x = sum (16 + q) x - (16 + z) sum x,
+// exact products, fp32 sums, whose rounding is 2^-23 of some 24 sum |x| a step.  (Of 128 + q it was of 136 sum |x|, and showed in the
+// result where x has much in common and most codes are zero points: an error of 3.3e-3 in the norm instead of 2.4e-3.)  A subtraction for
+// each pair of codes instead kept the pipe that multiplies at 40 %.  Sums of x made once a segment and given to the chains as their
+// first accumulator were no faster.  A group's sum is scaled in fp32: the only rounding to fewer bits on the way is that of A to bf16,
+// which the second product takes as operand (as the bf16 layer does).
 //
 // Split.  Blocks take consecutive row tiles of the hit experts, one block an SM; inside a block the warps share the units (32 rows x 128
 // columns) evenly, whatever the tile boundaries: a row tile that several warps have a piece of is put together from shared
@@ -345,8 +346,8 @@ __global__ void __launch_bounds__(VEC_THREADS, 1) w4_vec_kernel(const W4VecArgs 
             if (at % STEPS == STEPS - 1)
 #pragma unroll
               for (int t = 0; t < 2; ++t) {
-                const float zlo = ASYM ? w4_offset(zp[ASYM ? grp : 0] >> (16 * t)) : 136.f;
-                const float zhi = ASYM ? w4_offset(zp[ASYM ? grp : 0] >> (16 * t + 8)) : 136.f;
+                const float zlo = ASYM ? w4_offset(zp[ASYM ? grp : 0] >> (16 * t)) : 24.f;
+                const float zhi = ASYM ? w4_offset(zp[ASYM ? grp : 0] >> (16 * t + 8)) : 24.f;
                 const float slo = bf16lo(sc[t][grp]), shi = bf16hi(sc[t][grp]);
                 acc[t][0] = fmaf(slo, fmaf(-zlo, sums[0], part[t][0]), acc[t][0]);
                 acc[t][1] = fmaf(slo, fmaf(-zlo, sums[1], part[t][1]), acc[t][1]);
