@@ -19,7 +19,7 @@ extern "C" {
  * The pointer is into the workspace -- except for an expert-ordered tensor whose row is not a multiple of
  * 64 elements: its rows lie farther apart there, and *ptr is a compact copy made by this call on the context's last stream
  * (it waits for that stream).  Each tensor has a copy of its own, allocated outside the workspace when it is
- * first asked for and freed with the context. */
+ * first asked for and freed with the context.  moe_ffn_fwd_w4 is no such forward: what it leaves in these tensors is its own. */
 enum {
   MOE_BUF_COUNTS = 0,    /* int32 [E+S] */
   MOE_BUF_OFFSETS = 1,   /* int32 [E+S+1] */

@@ -1,7 +1,7 @@
 // C ABI of libmoe_b200: context, workspace carving, tensor-map encoding and the launch
 // sequences of the forward and backward layer.  Argument marshalling and planning only; every
 // step of the layer runs in the kernels of route_layout.cu, permute.cu, gemm_tc3.cu, gemm_wgrad.cu and fused.cu; over 4-bit
-// weights in those of w4_vec.cu.
+// weights in those of w4_vec.cu for few tokens, else of route_layout.cu, permute.cu and w4_tile.cu.
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
@@ -814,7 +814,8 @@ W4VecArgs w4_vec_args(const moe_ctx* c, const moe_w4_weights& w, int rows, int c
 //   8 x 1024 x 2816, k' 2    128: 32 slots 24 / 32, 64: 28 / 33, 80: 30 / 33, 128: 38 / 33;  32: 64: 30 / 46, 128: 44 / 46
 //   8 x 4096 x 14336, k' 2   (three) 128: 16 slots 145 / 199, 24: 164 / 206, 40: 199 / 206, 48: 229 / 207
 //   9 x 16384 x 1024, k' 3   (two) 128: 12 slots 64 / 75, 24: 89 / 79;  32: 24: 105 / 133, 48: 156 / 136
-// So: up to a fixed number of slots, as long as they are no more than the staged rows to an expert.
+// So: up to a fixed number of slots, as long as they are no more than the staged rows to an expert.  (The number is what the vector
+// kernel has room for, and where the two meet at groups of 128; at groups of 32 it is still the faster one there.)
 bool w4_few(const W4VecArgs& up, const W4VecArgs& down) {
   const long slots = (long)up.T * up.kp;
   int rows = 8;

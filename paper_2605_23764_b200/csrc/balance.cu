@@ -145,9 +145,11 @@ __device__ __forceinline__ float row_terms(const float (&v)[VPL], float (&ex)[VP
 // warps' pieces of a block are joined in order in shared memory, the blocks' in order by the block that arrives last.  Sums
 // are therefore the same from call to call.
 //
-// Bound by the read of the logits, at few tokens by the chain of latencies: a round of tokens, the join of the warps, of the blocks and
-// the last block are some 7000 clocks one after another.  One block an SM: two and four left more pieces to join.  Measured:
-// 8192 x 256 16 us, in 8 sequences 20; 65536 x 256 25 us (2.7 TB/s), sigmoid scores in 97 sequences 35.
+// Bound by the chain of latencies behind the read of the logits.  Clocks of the block that ends last, one sequence of 8192 x 256 (16 us):
+// first loads 1400, rounds of tokens 8400, the warps' pieces sorted and joined 4900, sums over the block 3000 in all, ticket 3000, the
+// blocks' pieces joined by the last one 10700; of 31700.  In 8 sequences (20-22 us) a block that joins two of them spends 19500 of 43100
+// there.  65536 x 256 (24.5 us, 2.7 TB/s): rounds 25000 of 49000; sigmoid scores in 97 sequences (35 us) 38000 of 70000.  One block an
+// SM: two and four left more pieces to join.  The registers that so many warps leave (64 to 128 a thread) spill 7 to 29 words.
 // ------------------------------------------------------------------------------------------
 // A piece in global memory, two a block: of the sequence that began before the block, of the one that goes on behind it.
 // Per block {seq of both pieces, tokens of both, sums of the block}, then [block][2][E] {sum, count}
@@ -517,8 +519,9 @@ __global__ void __launch_bounds__(32 * balance_warps_most(VPL)) balance_fwd_kern
 // ------------------------------------------------------------------------------------------
 // Backward: one read of the logits, one write of the gradient.  The coefficients x of a run stay in registers; what the
 // k selected experts get is scattered into a row of shared memory that is zero in between, so an id that a token names twice adds up.
-// Measured: 8192 x 256 7 us; 65536 x 256 34 us (4 TB/s), sigmoid scores in 97 sequences 43: exponentials and the chain
-// of reductions a round beside the two streams of memory.
+// Measured: 8192 x 256 7.3 us; 65536 x 256 34 us (4 TB/s), sigmoid scores in 97 sequences 43: issue slots two thirds full
+// (exponentials, reductions), and a quarter of the shared memory's cycles are conflicts over the rows of `val` and `add`, whose lanes
+// lie four apart.
 // ------------------------------------------------------------------------------------------
 constexpr int BAL_BWD_WARPS = 8;
 

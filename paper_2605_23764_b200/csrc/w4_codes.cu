@@ -1,7 +1,9 @@
 // Weights into 4 bits, from a checkpoint's natural codes into the layout of w4.cuh, and back to the values they stand for.
 // A warp takes 16 rows x 128 columns, half a unit: lanes 16 h + m have columns 8 m .. of rows 2 i + h, and change places with the
-// layout's lanes through 1 KB of shared memory.  Measured for 64 matrices of 2816 x 2048, groups of 128: 400 us to quantize (740 MB in,
-// 190 MB out: 2.3 TB/s; bound by the instructions of a code -- largest value, product, two roundings, clamp, place), 200 us back (4.7 TB/s).
+// layout's lanes through 1 KB of shared memory.  Measured for 64 matrices of 2816 x 2048, groups of 128: 395 us to quantize (740 MB in,
+// 190 MB out: 2.4 TB/s; the instructions of a code -- largest value, product, two roundings, clamp, place -- fill 64 % of the issue slots,
+// with four warps a scheduler), 450 with zero points of groups of 64; 218 us to pack, 267 with those (1.7 TB/s); 194 us back
+// (4.8 TB/s; three quarters of the issue slots).
 #include "launch_pairs.cuh"
 #include "topk.cuh"
 #include "w4.cuh"
@@ -169,8 +171,8 @@ __global__ void __launch_bounds__(32 * CODE_WARPS) w4_encode_kernel(const void* 
           }
         } else {
           // w / s to the nearest whole number, ties to even, without a division.  Both have 8 significant bits, so w / s is a tie or at
-          // least 2^-9 away from one, while w (1 / s) is off by no more than 2^-20: rounded to 2^-11 -- by the sum with 6144 -- it is
-          // exactly the tie, or on its side of it.  The sum with 1.5 x 2^23 then leaves the code in the lowest bits.
+          // least 2^-9 away from one, while w (1 / s) is off by less than 2^-18 (15.1 times the two units of
+          // 2^-23 that the reciprocal may be off by): rounded to 2^-11 -- by the sum with 6144 -- it is exactly the tie, or on its side of it.  The sum with 1.5 x 2^23 then leaves the code in the lowest bits.
           constexpr float FINE = 6144.f, WHOLE = 12582912.f;
           uint32_t sum = 0;
 #pragma unroll

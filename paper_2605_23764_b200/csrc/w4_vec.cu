@@ -3,9 +3,10 @@
 //   h[i] = sum_groups s_g sum_k (q - z) x[i][k];   A = w silu(h_gate) h_up;   Y = the same over A;   out[t] = sum_j Y of its slots
 //
 // What bounds it: the weights' bytes are the floor, the instructions that widen and multiply them what it takes.  33 experts of 7168 x
-// 2048, groups of 128: 8 tokens 156 us, 4.3 TB/s of codes and scales (an instruction a code to widen them on a pipe of half rate, a product
-// of 16 x 8 x 16 for 256 codes and one more for the sums of x).  One token of eight experts of 2048 x 1408: 22 us, of which reading is 5:
-// three launches, each of the latencies of its ids, first units and rows of x.
+// 2048, groups of 128: 8 tokens that hit 30 of them 155 to 160 us a call, calls back to back, 4.3 TB/s of codes and scales (an instruction
+// a code to widen them on a pipe of half rate, 61 % busy, a product of 16 x 8 x 16 for 256 codes and one more for the sums of x).  One
+// token of eight experts of 2048 x 1408: 21 to 23 us, of which reading is 5: three launches, each of the latencies of its ids, first units
+// and rows of x.
 //
 // Every warp streams its share of the units (2 KB) through a ring of its own in shared memory (loads kept in registers instead did not
 // overlap: a unit then cost a memory latency, 2.7 TB/s), widens the codes to bf16 16 + q -- a mask and an exponent -- and multiplies 32
@@ -35,7 +36,7 @@ constexpr int VEC_WARPS = 16, VEC_THREADS = 32 * VEC_WARPS;
 constexpr int VEC_ROWS = 8;          // rows of x that a pass over an expert's weights takes
 constexpr int VEC_SEG_TILES = 16;    // row tiles between two joins
 static_assert(VEC_SEG_TILES <= 32, "a lane for each pass that a segment may touch");
-constexpr int VEC_DEPTH = 3;         // slots of a warp's ring: two units in flight, 50 KB an SM
+constexpr int VEC_DEPTH = 3;         // slots of a warp's ring: two units in flight, 66 KB an SM or more
 constexpr int VEC_SMEM = 221 * 1024;
 constexpr int VEC_PIECE_BYTES = W4_TILE_ROWS * VEC_ROWS * 4;   // sums of a row tile
 constexpr int VEC_ROWS_MOST = 64;    // staged rows, at most
