@@ -251,8 +251,8 @@ int moe_router_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, c
  *   prob[s][e] = mean of p[t][e] over the sequence's tokens (0 for a sequence without tokens)
  *   losses[0] = 1/n_seq * sum_s E / (k tokens[s]) * sum_e counts[s][e] prob[s][e]      (1 where everything is even)
  *   losses[1] = mean over all sequences' tokens of logsumexp(logits[t])^2              (the z loss)
- * Sequence s is the tokens [seq_offsets[s], seq_offsets[s + 1]) (device int32[n_seq + 1], ascending, within [0, T]; NULL with
- * n_seq = 1: the whole batch); tokens outside of all sequences take no part, nor do tokens whose token_mask (device uint8[T], may be
+ * Sequence s is the tokens [seq_offsets[s], seq_offsets[s + 1]) (device int32[n_seq + 1], ascending, within [0, T], n_seq up to
+ * 2^30; NULL with n_seq = 1: the whole batch); tokens outside of all sequences take no part, nor do tokens whose token_mask (device uint8[T], may be
  * NULL) is 0.  Ids out of range are not counted.  Logits are finite or -infinity; a
  * token whose logits are all -infinity has p = 0 and a z loss of 0.
  * losses[2] fp32, counts[n_seq][E] int32, prob[n_seq][E] fp32, tokens[n_seq + 1] int32: overwritten.  The sums' order is fixed.

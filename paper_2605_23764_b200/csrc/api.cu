@@ -1063,7 +1063,7 @@ int moe_router_bwd(moe_ctx* c, const float* logits, const int32_t* topk_ids, con
 
 int moe_balance_fwd(moe_ctx* c, const float* logits, const int32_t* topk_ids, int32_t T, const int32_t* seq_offsets, int32_t n_seq,
                     const uint8_t* token_mask, float* losses, int32_t* counts, float* prob, int32_t* tokens, void* stream) {
-  if (!c || T < 0 || T > c->shape.T_max || n_seq < 1 || (n_seq > 1 && !seq_offsets) || !losses || !counts || !prob || !tokens)
+  if (!c || T < 0 || T > c->shape.T_max || n_seq < 1 || n_seq > BAL_MAX_SEQS || (n_seq > 1 && !seq_offsets) || !losses || !counts || !prob || !tokens)
     return MOE_ERR_INVALID_ARG;
   if (T > 0 && (!logits || !topk_ids)) return MOE_ERR_INVALID_ARG;
   if (!on_its_device(c)) return MOE_ERR_INVALID_ARG;
@@ -1087,7 +1087,7 @@ int moe_balance_fwd(moe_ctx* c, const float* logits, const int32_t* topk_ids, in
 int moe_balance_bwd(moe_ctx* c, const float* logits, const int32_t* topk_ids, const int32_t* counts, const int32_t* tokens, const float* d_losses,
                     const float* d_topk_w, int32_t T, const int32_t* seq_offsets, int32_t n_seq, const uint8_t* token_mask, float* d_logits,
                     void* stream) {
-  if (!c || T < 0 || T > c->shape.T_max || n_seq < 1 || (n_seq > 1 && !seq_offsets)) return MOE_ERR_INVALID_ARG;
+  if (!c || T < 0 || T > c->shape.T_max || n_seq < 1 || n_seq > BAL_MAX_SEQS || (n_seq > 1 && !seq_offsets)) return MOE_ERR_INVALID_ARG;
   if (T > 0 && (!logits || !counts || !tokens || !d_losses || !d_logits || (d_topk_w && !topk_ids))) return MOE_ERR_INVALID_ARG;
   if (!on_its_device(c)) return MOE_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -214,6 +214,7 @@ cudaError_t launch_router_bwd(const float* logits, const int* ids, const float* 
 
 // Balance losses of the router (balance.cu)
 constexpr int BAL_MAX_BLOCKS = 148;
+constexpr int BAL_MAX_SEQS = 1 << 30;   // the warps of all blocks step over sequences in 32 bits
 constexpr int BAL_SMEM = 200 * 1024;
 struct BalanceArgs {
   const float* logits;         // [T][E]
