@@ -252,9 +252,9 @@ int moe_router_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, c
  *   losses[0] = 1/n_seq * sum_s E / (k tokens[s]) * sum_e counts[s][e] prob[s][e]      (1 where everything is even)
  *   losses[1] = mean over all sequences' tokens of logsumexp(logits[t])^2              (the z loss)
  * Sequence s is the tokens [seq_offsets[s], seq_offsets[s + 1]) (device int32[n_seq + 1], ascending, within [0, T], n_seq up to
- * 2^30; NULL with n_seq = 1: the whole batch); tokens outside of all sequences take no part, nor do tokens whose token_mask (device uint8[T], may be
- * NULL) is 0.  Ids out of range are not counted.  Logits are finite or -infinity; a
- * token whose logits are all -infinity has p = 0 and a z loss of 0.
+ * 2^30; NULL with n_seq = 1: the whole batch); tokens outside of all sequences take no part, nor do tokens whose token_mask (device
+ * uint8[T], may be NULL) is 0.  Ids out of range are not counted.  Logits are finite or -infinity; a token whose logits are all
+ * -infinity has p = 0 and a z loss of 0.
  * losses[2] fp32, counts[n_seq][E] int32, prob[n_seq][E] fp32, tokens[n_seq + 1] int32: overwritten.  The sums' order is fixed.
  *
  * moe_balance_bwd: d_logits[T][E] fp32 (overwritten; may be the logits themselves) = d_losses[0] * d losses[0] / d logits +
@@ -288,8 +288,8 @@ int moe_balance_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, 
  * between the two products are bf16.  It uses the context's layout: a forward saved for moe_ffn_bwd is given up.
  * x and activations below 2^115 (about 4e34): for few tokens a group's sum is taken over 16 + q, and 16 + z times the sum of x off it.
  * The two matrices' groups, and whether they have zero points, are each one's own.
- * It is made for token generation: from some 80 rows a routed expert on moe_ffn_fwd over bf16 weights is the faster one (66 experts of 2048 x
- * 1408: 512 tokens 164 us here and 212 there, 1024 265 and 241, 4096 806 and 565). */
+ * It is made for token generation: from some 80 rows a routed expert on moe_ffn_fwd over bf16 weights is the faster one (66 experts of
+ * 2048 x 1408: 512 tokens 164 us here and 212 there, 1024 265 and 241, 4096 806 and 565). */
 #define MOE_W4_GATE_UP 1u
 typedef struct {
   const uint32_t* codes;

@@ -171,8 +171,9 @@ __global__ void __launch_bounds__(32 * CODE_WARPS) w4_encode_kernel(const void* 
           }
         } else {
           // w / s to the nearest whole number, ties to even, without a division.  Both have 8 significant bits, so w / s is a tie or at
-          // least 2^-9 away from one, while w (1 / s) is off by less than 2^-18 (15.1 times the two units of
-          // 2^-23 that the reciprocal may be off by): rounded to 2^-11 -- by the sum with 6144 -- it is exactly the tie, or on its side of it.  The sum with 1.5 x 2^23 then leaves the code in the lowest bits.
+          // least 2^-9 away from one, while w (1 / s) is off by less than 2^-18 (15.1 times the two units of 2^-23 that the reciprocal
+          // may be off by): rounded to 2^-11 -- by the sum with 6144 -- it is exactly the tie, or on its side of it.  The sum with
+          // 1.5 x 2^23 then leaves the code in the lowest bits.
           constexpr float FINE = 6144.f, WHOLE = 12582912.f;
           uint32_t sum = 0;
 #pragma unroll

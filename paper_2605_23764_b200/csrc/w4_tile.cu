@@ -11,8 +11,9 @@
 // weights would spare the accumulators between groups, but round every weight: twice the error of the plain formula instead of 1.4 times.)
 //
 // Measured for 66 experts of 2048 x 1408, 8 rows a token, groups of 128: 64 tokens 104 us, 512 tokens 164, 4096 tokens 806 (703
-// TFLOP/s; the bf16 layer takes 190, 212 and 565: it is the faster one from some 850 tokens on, about 80 rows a routed expert).  What bounds it: with many rows the epilogue, which takes every group's accumulator out of TMEM (800 clocks a unit beside 512
-// of products); with few the chain from codes to operand to products through two stages of A (760 clocks a unit).
+// TFLOP/s; the bf16 layer takes 190, 212 and 565: it is the faster one from some 850 tokens on, about 80 rows a routed expert).  What
+// bounds it: with many rows the epilogue, which takes every group's accumulator out of TMEM (800 clocks a unit beside 512 of products);
+// with few the chain from codes to operand to products through two stages of A (760 clocks a unit).
 //
 // Roles per CTA: warp 0 loads codes and zero points (a copy of each for 128 rows x 128 columns; with one for every 32 rows issuing
 // them took 1000 clocks, twice as long as the products), warp 18 the rows of x, warp 1 issues the products (even CTA), warps 2-9 widen
