@@ -269,6 +269,35 @@ int moe_balance_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, 
                     const float* d_topk_w, int32_t T, const int32_t* seq_offsets, int32_t n_seq, const uint8_t* token_mask, float* d_logits,
                     void* stream);
 
+/* ---- Routing by groups, with a bias for balance -----------------------------------------------------------
+ * Experts stand in n_groups groups of E / n_groups neighbours.  With s = softmax(logits) or, with MOE_FLAG_SIGMOID_GATE, the sigmoids:
+ *   c[t][e] = s[t][e] + bias[e] (bias fp32 [E], NULL: none)         what decides; -infinity where the logit is
+ *   a group's score is the sum of its group_top (1 or 2) largest c; the top_groups groups of the largest scores stay
+ *   topk_ids[t]: the k experts of the largest c in them, in descending order
+ *   topk_w[t]: their scores s, without the bias -- over their sum with MOE_FLAG_RENORM_TOPK (0 where that is 0) -- times scale
+ * Values are compared as they are in 64 bits, equal ones go to the lower group or expert, so which experts come out does not hang on
+ * an fp32 rounding (without a bias the experts' order is that of the logits).  n_groups = top_groups = 1: all experts.
+ * counts[E] (may be NULL): slots of each expert.  Logits are finite or -infinity; NaN gives ids in range and unspecified weights.
+ * Requirements: E % n_groups == 0, n_groups <= 32, 1 <= top_groups <= n_groups, group_top <= E / n_groups where groups are left
+ * out, k <= top_groups * E / n_groups.
+ *
+ * moe_route_grouped_bwd: d_logits[T][E] fp32 from d_topk_w[T][k] with the ids and the scale of the forward; groups and bias pass no
+ * gradient.  Overwritten, or added to with accumulate != 0 (behind moe_balance_bwd without a score gradient, for one).  An expert that a
+ * token names twice gets both gradients, ids out of range none; a token whose d_topk_w is all 0 gets zeros, whatever its logits hold.
+ *
+ * moe_bias_update: bias_out[e] = bias[e] + rate * sign(mean count - count[e]), counts[n_seq][E] summed over n_seq (those of
+ * moe_route_grouped: n_seq = 1; those of moe_balance_fwd leave padding out).  bias_out may be bias.
+ * All three are asynchronous on `stream`. */
+typedef struct {
+  int32_t n_groups, top_groups, group_top;
+  float scale;
+} moe_route_groups;
+int moe_route_grouped(moe_ctx* ctx, const float* logits, const float* bias, int32_t T, const moe_route_groups* groups, int32_t* topk_ids, float* topk_w,
+                      int32_t* counts, void* stream);
+int moe_route_grouped_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, const float* d_topk_w, int32_t T, float scale, int32_t accumulate,
+                          float* d_logits, void* stream);
+int moe_bias_update(moe_ctx* ctx, const float* bias, const int32_t* counts, int32_t n_seq, float rate, float* bias_out, void* stream);
+
 /* ---- Experts with 4-bit weights ---------------------------------------------------------------------------
  * A weight is w = s (q - z): codes q in 0..15, a bf16 scale s and, in matrices with zero points, z in 0..15 for every `group` (32, 64
  * or 128) consecutive columns of a row; without zero points z = 8.  cols need not be a multiple of the group.  rows, cols < 2^31 - 128.
@@ -305,6 +334,43 @@ int moe_w4_pack(const uint8_t* q, const uint16_t* q_scales, const uint8_t* q_zer
 int moe_w4_dequantize(const moe_w4_weights* w, int32_t n, int32_t rows, int32_t cols, uint32_t flags, uint16_t* W, void* stream);
 int moe_ffn_fwd_w4(moe_ctx* ctx, const uint16_t* x, const int32_t* topk_ids, const float* topk_w, const moe_w4_weights* W_gate_up,
                    const moe_w4_weights* W_down, uint16_t* out, int32_t T, void* stream);
+
+/* ---- Orthogonalised momentum for weight matrices ----------------------------------------------------------
+ * An update whose singular values all are about 1, for n matrices [rows][cols] at a time (W_gate_up of a layer: 2 (E + S) matrices
+ * [F][d], the gate and the up projection each by itself; W_down: E + S matrices [d][F]):
+ *   X = u / (|u| + eps), |u| the root of the sum of squares;   for each step:  X <- a X + (b A + c A A) X,  A = X X^T
+ * with (a, b, c) = coefficients[step].  (3.4445, -4.7750, 2.0315) five times takes singular values above a hundredth of |u| to 0.7 .. 1.2.
+ * The polynomials must keep singular values of at most 1 within 2.  A matrix of zeros (an expert without tokens) stays zero.
+ *   moe_muon_orthogonalize   u = G (bf16 or fp32, MOE_MUON_*) -> out bf16
+ *   moe_muon_step            M_out = momentum M + dW;  u = dW + momentum M_out with nesterov, else M_out;
+ *                            W_out = (1 - lr weight_decay) W - lr scale X;  W, dW, W_out bf16, M, M_out fp32; M_out may be M, W_out may be W
+ * Products take fp16 operands (X to 11 significant bits) and sum in fp32; the linear term takes X to 22 bits.  For five such steps X is
+ * 1e-3 off in the norm before it is rounded to bf16 (itself 1.7e-3).  A matrix with NaN or infinite elements gives NaN, the others are not affected.
+ *
+ * moe_muon_create: like moe_create; the workspace (moe_muon_workspace_bytes, 0 for an invalid shape; 256-byte aligned device memory, or
+ * NULL) holds a batch of the matrices, about 1 GB at most unless a single one needs more.  Tensors need their type's alignment only;
+ * 16-byte aligned ones with cols % 8 == 0 are read and written in vectors.  1 <= n, rows, cols <= MOE_MUON_MAX_SIZE,
+ * 1 <= steps <= MOE_MUON_MAX_STEPS, eps >= 0.  Calls are asynchronous on `stream`; like a moe_ctx, a moe_muon serves one call at a
+ * time, and two captured graphs that use one must not run at the same time. */
+#define MOE_MUON_MAX_STEPS 16
+#define MOE_MUON_MAX_SIZE 65536
+#define MOE_MUON_BF16 0
+#define MOE_MUON_FP32 1
+typedef struct moe_muon moe_muon;
+typedef struct {
+  int32_t n, rows, cols, steps;
+  float coefficients[MOE_MUON_MAX_STEPS][3];
+  float eps;
+} moe_muon_shape;
+size_t moe_muon_workspace_bytes(const moe_muon_shape* shape);
+int moe_muon_create(moe_muon** out, const moe_muon_shape* shape, void* workspace, size_t workspace_bytes);
+int moe_muon_destroy(moe_muon* m);
+int moe_muon_orthogonalize(moe_muon* m, const void* G, int32_t g_type, uint16_t* out, void* stream);
+int moe_muon_step(moe_muon* m, const uint16_t* W, const float* M, const uint16_t* dW, float momentum, int32_t nesterov, float lr, float weight_decay,
+                  float scale, uint16_t* W_out, float* M_out, void* stream);
+/* as moe_get_status, moe_last_launch_count */
+int moe_muon_get_status(moe_muon* m, int32_t* code, int32_t* detail);
+int moe_muon_last_launch_count(const moe_muon* m);
 
 /* ---- Scheduling microbenchmark: SwiGLU + Add operator pair (Section 6.1, Section 6.2) -------------
  * The two element-wise operators the paper uses to study scheduling in isolation, on

@@ -33,7 +33,9 @@ EXPORTS = ["moe_workspace_bytes", "moe_create", "moe_destroy", "moe_route", "moe
            "moe_sched_study_workspace_bytes", "moe_sched_study", "moe_sched_study_stats", "moe_router_fwd",
            "moe_router_bwd", "moe_taskflow_compile", "moe_taskflow_workspace_bytes", "moe_taskflow_run",
            "moe_taskflow_status", "moe_ep_plan", "moe_ep_dispatch", "moe_ep_combine", "moe_balance_fwd", "moe_balance_bwd",
-           "moe_w4_sizes", "moe_w4_quantize", "moe_w4_pack", "moe_w4_dequantize", "moe_ffn_fwd_w4"]
+           "moe_w4_sizes", "moe_w4_quantize", "moe_w4_pack", "moe_w4_dequantize", "moe_ffn_fwd_w4",
+           "moe_route_grouped", "moe_route_grouped_bwd", "moe_bias_update", "moe_muon_workspace_bytes", "moe_muon_create", "moe_muon_destroy",
+           "moe_muon_orthogonalize", "moe_muon_step", "moe_muon_get_status", "moe_muon_last_launch_count"]
 PHASES = ["route", "layout", "gather", "gemm_gate_up", "gemm_down", "combine", "bwd_gather", "act_grad",
           "dw_reduce", "wgrad_down", "gate_grad", "wgrad_gate_up", "bwd_combine", "fused_fwd", "fused_bwd"]
 
@@ -74,6 +76,18 @@ class MoeEpLocalCombine(ctypes.Structure):
 
 class _W4(ctypes.Structure):   # moe_w4_weights
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p), ("group", ctypes.c_int32)]
+
+
+class MoeRouteGroups(ctypes.Structure):   # moe_route_groups
+    _fields_ = [("n_groups", ctypes.c_int32), ("top_groups", ctypes.c_int32), ("group_top", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+MOE_MUON_MAX_STEPS, MOE_MUON_BF16, MOE_MUON_FP32 = 16, 0, 1
+
+
+class MoeMuonShape(ctypes.Structure):   # moe_muon_shape
+    _fields_ = [("n", ctypes.c_int32), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("steps", ctypes.c_int32),
+                ("coefficients", (ctypes.c_float * 3) * MOE_MUON_MAX_STEPS), ("eps", ctypes.c_float)]
 
 
 class MoeTfTensor(ctypes.Structure):
@@ -186,6 +200,18 @@ def load_library() -> ctypes.CDLL:
     lib.moe_ep_combine.argtypes = [ctypes.POINTER(MoeEpPeer), ctypes.POINTER(MoeEpLocalCombine), i32, i32, i32, i32, vp, vp]
     lib.moe_balance_fwd.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp]
     lib.moe_balance_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp]
+    f32 = ctypes.c_float
+    lib.moe_route_grouped.argtypes = [vp, vp, vp, i32, ctypes.POINTER(MoeRouteGroups), vp, vp, vp, vp]
+    lib.moe_route_grouped_bwd.argtypes = [vp, vp, vp, vp, i32, f32, i32, vp, vp]
+    lib.moe_bias_update.argtypes = [vp, vp, vp, i32, f32, vp, vp]
+    lib.moe_muon_workspace_bytes.restype = sz
+    lib.moe_muon_workspace_bytes.argtypes = [ctypes.POINTER(MoeMuonShape)]
+    lib.moe_muon_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(MoeMuonShape), vp, sz]
+    lib.moe_muon_destroy.argtypes = [vp]
+    lib.moe_muon_orthogonalize.argtypes = [vp, vp, i32, vp, vp]
+    lib.moe_muon_step.argtypes = [vp, vp, vp, vp, f32, i32, f32, f32, f32, vp, vp, vp]
+    lib.moe_muon_get_status.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i32)]
+    lib.moe_muon_last_launch_count.argtypes = [vp]
     lib.moe_w4_sizes.argtypes = [i32, i32, i32, ctypes.c_uint32, ctypes.POINTER(sz), ctypes.POINTER(sz)]
     lib.moe_w4_quantize.argtypes = [vp, i32, i32, i32, i32, ctypes.c_uint32, vp, vp, vp, vp]
     lib.moe_w4_pack.argtypes = [vp, vp, vp, i32, i32, i32, i32, ctypes.c_uint32, vp, vp, vp, vp]
@@ -464,6 +490,107 @@ def moe_balance_bwd(ctx, logits, topk_ids, counts, tokens, d_losses, d_topk_w, T
                                           _here(seq_offsets, _I32, "seq_offsets", n_seq + 1), n_seq,
                                           _here(token_mask, torch.uint8, "token_mask", T), _here(d_logits, _F32, "d_logits", T * E),
                                           _stream()), "moe_balance_bwd")
+
+
+def moe_route_groups(n_groups=1, top_groups=1, group_top=1, scale=1.0):
+    return MoeRouteGroups(_i32(n_groups, "n_groups"), _i32(top_groups, "top_groups"), _i32(group_top, "group_top"), float(scale))
+
+
+@_sizes_first
+def moe_route_grouped(ctx, logits, bias, T, groups, topk_ids, topk_w, counts=None):
+    """groups: of moe_route_groups"""
+    _, _, E, k, _, _, _ = _shape_of(ctx)
+    T = _i32(T, "T")
+    _check(load_library().moe_route_grouped(ctx, _here(logits, _F32, "logits", T * E), _here(bias, _F32, "bias", E), T, ctypes.byref(groups),
+                                            _here(topk_ids, _I32, "topk_ids", T * k), _here(topk_w, _F32, "topk_w", T * k),
+                                            _here(counts, _I32, "counts", E), _stream()), "moe_route_grouped")
+
+
+@_sizes_first
+def moe_route_grouped_bwd(ctx, logits, topk_ids, d_topk_w, T, scale, accumulate, d_logits):
+    _, _, E, k, _, _, _ = _shape_of(ctx)
+    T = _i32(T, "T")
+    _check(load_library().moe_route_grouped_bwd(ctx, _here(logits, _F32, "logits", T * E), _here(topk_ids, _I32, "topk_ids", T * k),
+                                                _here(d_topk_w, _F32, "d_topk_w", T * k), T, float(scale), int(bool(accumulate)),
+                                                _here(d_logits, _F32, "d_logits", T * E), _stream()), "moe_route_grouped_bwd")
+
+
+@_sizes_first
+def moe_bias_update(ctx, bias, counts, n_seq, rate, bias_out):
+    _, _, E, _, _, _, _ = _shape_of(ctx)
+    n_seq = _i32(n_seq, "n_seq")
+    _check(load_library().moe_bias_update(ctx, _here(bias, _F32, "bias", E), _here(counts, _I32, "counts", n_seq * E), n_seq, float(rate),
+                                          _here(bias_out, _F32, "bias_out", E), _stream()), "moe_bias_update")
+
+
+def moe_muon_shape(n, rows, cols, coefficients, steps, eps):
+    """coefficients: (a, b, c) for all steps, or one triple for each"""
+    s = MoeMuonShape(_i32(n, "n"), _i32(rows, "rows"), _i32(cols, "cols"), _i32(steps, "steps"))
+    s.eps = float(eps)
+    if not 1 <= s.steps <= MOE_MUON_MAX_STEPS:
+        raise MoeError(f"steps: {s.steps}, expected 1 to {MOE_MUON_MAX_STEPS}")
+    triples = list(coefficients)
+    if len(triples) == 3 and all(isinstance(v, (int, float)) for v in triples):
+        triples = [triples] * s.steps
+    if len(triples) != s.steps or any(len(t) != 3 for t in triples):
+        raise MoeError(f"coefficients: expected (a, b, c), or {s.steps} of them")
+    for i, t in enumerate(triples):
+        s.coefficients[i][:] = [float(v) for v in t]
+    return s
+
+
+def moe_muon_workspace_bytes(shape) -> int:
+    return int(load_library().moe_muon_workspace_bytes(ctypes.byref(shape)))
+
+
+_MUON_ELEMS = {}   # muon handle -> elements of its matrices
+
+
+def moe_muon_create(shape, workspace=None):
+    """-> opaque handle.  `workspace`: CUDA uint8 tensor (kept alive by the caller) or None."""
+    h = ctypes.c_void_p()
+    _check(load_library().moe_muon_create(ctypes.byref(h), ctypes.byref(shape), ctypes.c_void_p(workspace.data_ptr()) if workspace is not None else None,
+                                          workspace.numel() if workspace is not None else 0), "moe_muon_create")
+    _MUON_ELEMS[h.value] = shape.n * shape.rows * shape.cols
+    return h
+
+
+def moe_muon_destroy(muon):
+    _check(load_library().moe_muon_destroy(muon), "moe_muon_destroy")
+    _MUON_ELEMS.pop(getattr(muon, "value", None), None)
+
+
+def _elems_of(muon):
+    try:
+        return _MUON_ELEMS[muon.value]
+    except (KeyError, AttributeError):
+        raise MoeError("unknown muon handle (not created by moe_muon_create, or already destroyed)") from None
+
+
+@_sizes_first
+def moe_muon_orthogonalize(muon, G, out):
+    n = _elems_of(muon)
+    fp32 = G.dtype is _F32
+    _check(load_library().moe_muon_orthogonalize(muon, _here(G, _F32 if fp32 else _BF, "G", n), MOE_MUON_FP32 if fp32 else MOE_MUON_BF16,
+                                                 _here(out, _BF, "out", n), _stream()), "moe_muon_orthogonalize")
+
+
+@_sizes_first
+def moe_muon_step(muon, W, M, dW, momentum, nesterov, lr, weight_decay, scale, W_out, M_out):
+    n = _elems_of(muon)
+    _check(load_library().moe_muon_step(muon, _here(W, _BF, "W", n), _here(M, _F32, "M", n), _here(dW, _BF, "dW", n), float(momentum),
+                                        int(bool(nesterov)), float(lr), float(weight_decay), float(scale), _here(W_out, _BF, "W_out", n),
+                                        _here(M_out, _F32, "M_out", n), _stream()), "moe_muon_step")
+
+
+def moe_muon_get_status(muon):
+    code, detail = ctypes.c_int32(), ctypes.c_int32()
+    _check(load_library().moe_muon_get_status(muon, ctypes.byref(code), ctypes.byref(detail)), "moe_muon_get_status")
+    return code.value, detail.value
+
+
+def moe_muon_last_launch_count(muon) -> int:
+    return int(load_library().moe_muon_last_launch_count(muon))
 
 
 def moe_w4_sizes(rows, cols, group, flags=0):
@@ -866,6 +993,61 @@ class MoeW4Weights:
         return out
 
 
+class MoeMuon:
+    """Orthogonalised momentum for n weight matrices [rows][cols]; owns the workspace, the caller weights and momentum."""
+
+    def __init__(self, n, rows, cols, momentum=0.95, nesterov=True, coefficients=(3.4445, -4.7750, 2.0315), steps=5, eps=1e-7):
+        self.n, self.rows, self.cols, self.momentum, self.nesterov = int(n), int(rows), int(cols), float(momentum), bool(nesterov)
+        self.handle = None
+        shape = moe_muon_shape(n, rows, cols, coefficients, steps, eps)
+        nbytes = moe_muon_workspace_bytes(shape)
+        if nbytes == 0:
+            raise MoeError("invalid shape")
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        self.handle = moe_muon_create(shape, self.workspace)
+
+    @classmethod
+    def for_gate_up(cls, layer, **options):
+        """For a MoeLayer's W_gate_up: the gate and the up projection of every expert by itself."""
+        return cls(2 * (layer.E + layer.S), layer.F, layer.d, **options)
+
+    @classmethod
+    def for_down(cls, layer, **options):
+        """For a MoeLayer's W_down."""
+        return cls(layer.E + layer.S, layer.d, layer.F, **options)
+
+    def close(self):
+        if self.handle is not None:
+            torch.cuda.synchronize()
+            moe_muon_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def orthogonalize(self, G, out=None):
+        """bf16 or fp32 G -> bf16, of G's shape"""
+        if out is None:
+            out = torch.empty(G.shape, dtype=_BF, device=G.device)
+        moe_muon_orthogonalize(self.handle, G, out)
+        return out
+
+    def step(self, W, M, dW, lr, weight_decay=0.0, scale=1.0, W_out=None, M_out=None):
+        """One step of weights W (bf16) and momentum M (fp32), in place unless W_out, M_out are given -> W_out, M_out"""
+        W_out, M_out = W if W_out is None else W_out, M if M_out is None else M_out
+        moe_muon_step(self.handle, W, M, dW, self.momentum, self.nesterov, lr, weight_decay, scale, W_out, M_out)
+        return W_out, M_out
+
+    def status(self):
+        return moe_muon_get_status(self.handle)
+
+    def launches(self):
+        return moe_muon_last_launch_count(self.handle)
+
+
 class MoeLayer:
     """Owns a context and its workspace (a torch allocation); allocates outputs; same calls as the C ABI."""
 
@@ -970,6 +1152,29 @@ class MoeLayer:
             d_logits = torch.empty(T, self.E, dtype=_F32, device=logits.device)
         moe_balance_bwd(self.ctx, logits, topk_ids, counts, tokens, d_losses, d_topk_w, T, seq_offsets, n, token_mask, d_logits)
         return d_logits
+
+    def route_grouped(self, logits, bias=None, n_groups=1, top_groups=1, group_top=1, scale=1.0, with_counts=False):
+        """-> ids, weights (and counts [E]): the best experts of the best groups by score + bias, weighted by their scores"""
+        T, dev = logits.shape[0], logits.device
+        ids, w = torch.empty(T, self.k, dtype=_I32, device=dev), torch.empty(T, self.k, dtype=_F32, device=dev)
+        counts = torch.empty(self.E, dtype=_I32, device=dev) if with_counts else None
+        moe_route_grouped(self.ctx, logits, bias, T, moe_route_groups(n_groups, top_groups, group_top, scale), ids, w, counts)
+        return (ids, w, counts) if with_counts else (ids, w)
+
+    def route_grouped_bwd(self, logits, topk_ids, d_topk_w, scale=1.0, d_logits=None, accumulate=False):
+        """Gradient of route_grouped's weights; added to d_logits with accumulate."""
+        if d_logits is None:
+            if accumulate:
+                raise MoeError("d_logits: accumulate needs a tensor to add to")
+            d_logits = torch.empty(logits.shape[0], self.E, dtype=_F32, device=logits.device)
+        moe_route_grouped_bwd(self.ctx, logits, topk_ids, d_topk_w, logits.shape[0], scale, accumulate, d_logits)
+        return d_logits
+
+    def bias_update(self, bias, counts, rate, out=None):
+        """bias + rate * sign(mean count - count), in place unless `out` is given; counts [E] or [n_seq][E]"""
+        out = bias if out is None else out
+        moe_bias_update(self.ctx, bias, counts, counts.shape[0] if counts.dim() > 1 else 1, rate, out)
+        return out
 
     def ffn_fwd_w4(self, x, topk_ids, topk_w, W_gate_up, W_down, out=None):
         """ffn_fwd over MoeW4Weights (the layer made with w4=True)."""

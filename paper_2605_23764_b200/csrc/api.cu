@@ -7,12 +7,15 @@
 #include <string.h>
 
 #include <algorithm>
+#include <cmath>
+#include <new>
 #include <string>
 #include <vector>
 
 #include "../../include/moe_b200.h"
 #include "../../include/moe_b200_debug.h"
 #include "moe_internal.h"
+#include "muon.cuh"
 #include "w4.cuh"
 
 using namespace moe;
@@ -64,10 +67,10 @@ EncodeTiledFn get_encode_fn() {
   return fn;
 }
 
-// bf16 tensor of `rank` dimensions (dims[0] innermost, strides in bytes for dims 1..), 128-byte
-// swizzle, zero fill outside the tensor on loads, clipping on stores.
+// bf16 (or fp16) tensor of `rank` dimensions (dims[0] innermost, strides in bytes for dims 1..), 128-byte
+// swizzle unless stated, zero fill outside the tensor on loads, clipping on stores.
 int encode_tiled(CUtensorMap* tm, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
-                 const uint32_t* box) {
+                 const uint32_t* box, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) {
     g_cuda_error = "cuTensorMapEncodeTiled entry point not available";
@@ -78,7 +81,7 @@ int encode_tiled(CUtensorMap* tm, const void* base, int rank, const uint64_t* di
   for (int i = 0; i < rank; ++i) { gdim[i] = dims[i]; bx[i] = box[i]; }
   for (int i = 0; i + 1 < rank; ++i) gstr[i] = strides[i];
   CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), gdim, gstr, bx, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
@@ -919,6 +922,188 @@ BalanceArgs balance_args(const moe_ctx* c, const float* logits, const int32_t* t
   return a;
 }
 
+// ---------------------------------------------------------------- orthogonalised momentum (muon.cuh)
+// Batches of matrices go through the workspace one after the other: enough of them that the products' last turn over the SMs is
+// a small part, few enough that the workspace stays a fraction of the weights' optimiser state.
+constexpr size_t MUON_BATCH_BYTES = size_t(1) << 30;
+
+struct MuonPlan {
+  int m, l, ld, ldm;          // smaller and larger dimension; elements from row to row of X, of A and B
+  int batch;                  // matrices of a turn
+  size_t part, hi[2], lo[2], A, B, total;
+};
+
+bool muon_shape_ok(const moe_muon_shape* s) {
+  if (!s || s->n < 1 || s->n > MOE_MUON_MAX_SIZE || s->rows < 1 || s->cols < 1 || s->rows > MOE_MUON_MAX_SIZE || s->cols > MOE_MUON_MAX_SIZE) return false;
+  if (s->steps < 1 || s->steps > MOE_MUON_MAX_STEPS || !(s->eps >= 0.f) || std::isinf(s->eps)) return false;
+  for (int i = 0; i < s->steps; ++i)
+    for (int j = 0; j < 3; ++j)
+      if (!std::isfinite(s->coefficients[i][j])) return false;
+  return true;
+}
+
+MuonPlan plan_muon(const moe_muon_shape& s) {
+  MuonPlan p;
+  p.m = std::min(s.rows, s.cols);
+  p.l = std::max(s.rows, s.cols);
+  p.ld = row_ld(s.cols);
+  p.ldm = row_ld(p.m);
+  const size_t x = sizeof(uint16_t) * (size_t)s.rows * p.ld, a = sizeof(uint16_t) * (size_t)p.m * p.ldm;
+  const long parts = muon_parts((long)s.rows * s.cols);
+  const size_t each = 4 * x + 2 * a;
+  const size_t most = std::max<size_t>(1, MUON_BATCH_BYTES / each);
+  const size_t turns = ((size_t)s.n + most - 1) / most;
+  p.batch = (int)(((size_t)s.n + turns - 1) / turns);
+  Carve c;
+  c.take(sizeof(DevStatus));
+  p.part = c.take(sizeof(double) * p.batch * parts);
+  for (int i = 0; i < 2; ++i) {
+    p.hi[i] = c.take(x * p.batch);
+    p.lo[i] = c.take(x * p.batch);
+  }
+  p.A = c.take(a * p.batch);
+  p.B = c.take(a * p.batch);
+  p.total = c.off;
+  return p;
+}
+
+}  // namespace
+
+struct moe_muon {
+  moe_muon_shape shape;
+  MuonPlan plan;
+  uint8_t* ws = nullptr;
+  bool owns_ws = false;
+  int device = 0, num_sms = 0;
+  int nt_m = 0, nt_l = 0;   // tile columns of products m and l columns wide
+  uint64_t budget_ns = 2000ull * 1000 * 1000;
+  cudaStream_t last_stream = nullptr;
+  int launches = 0;
+  // X, by buffer: 128 rows, nt_m / 2 rows, 64 x 64, epilogue boxes of hi and lo; A and B: 128 rows, nt_m / 2 rows, epilogue boxes, mirrored ones
+  CUtensorMap x128[2], xhalf[2], x64[2], xhi[2], xlo[2];
+  CUtensorMap a128, ahalf, abox, amir, b128, bhalf, bbox, bmir;
+  DevStatus* status() const { return reinterpret_cast<DevStatus*>(ws); }
+  template <class T>
+  T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
+};
+
+namespace {
+
+int encode_batch(CUtensorMap* tm, const void* base, uint64_t n, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows, uint32_t box_cols,
+                 CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
+  const uint64_t dims[3] = {cols, rows, n}, strides[2] = {ld * 2, rows * ld * 2};
+  const uint32_t box[3] = {box_cols, box_rows, 1};
+  return encode_tiled(tm, base, 3, dims, strides, box, swizzle);
+}
+
+int encode_muon(moe_muon* u) {
+  const MuonPlan& p = u->plan;
+  const uint64_t n = p.batch, rows = u->shape.rows, cols = u->shape.cols;
+  int rc = MOE_OK;
+  for (int i = 0; i < 2 && !rc; ++i) {
+    const void *hi = u->ws + p.hi[i], *lo = u->ws + p.lo[i];
+    if (!rc) rc = encode_batch(&u->x128[i], hi, n, rows, cols, p.ld, 128, 64);
+    if (!rc) rc = encode_batch(&u->xhalf[i], hi, n, rows, cols, p.ld, u->nt_m / 2, 64);
+    if (!rc) rc = encode_batch(&u->x64[i], hi, n, rows, cols, p.ld, 64, 64);
+    if (!rc) rc = encode_batch(&u->xhi[i], hi, n, rows, cols, p.ld, 32, 64);
+    if (!rc) rc = encode_batch(&u->xlo[i], lo, n, rows, cols, p.ld, 32, 64);
+  }
+  for (int i = 0; i < 2 && !rc; ++i) {
+    const void* b = u->ws + (i ? p.B : p.A);
+    rc = encode_batch(i ? &u->b128 : &u->a128, b, n, p.m, p.m, p.ldm, 128, 64);
+    if (!rc) rc = encode_batch(i ? &u->bhalf : &u->ahalf, b, n, p.m, p.m, p.ldm, u->nt_m / 2, 64);
+    if (!rc) rc = encode_batch(i ? &u->bbox : &u->abox, b, n, p.m, p.m, p.ldm, 32, 64);
+    if (!rc) rc = encode_batch(i ? &u->bmir : &u->amir, b, n, p.m, p.m, p.ldm, 64, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
+  }
+  return rc;
+}
+
+// Tile columns: the fewest padded columns, narrower tiles charged for the operand bytes that they bring in for a product.
+int muon_tile_cols(int N) {
+  static const int width[3] = {256, 192, 128}, charge[3] = {100, 105, 115};
+  int best = 256;
+  long least = -1;
+  for (int i = 0; i < 3; ++i) {
+    const long c = (long)((N + width[i] - 1) / width[i]) * width[i] * charge[i];
+    if (least < 0 || c < least) { least = c; best = width[i]; }
+  }
+  return best;
+}
+
+// u = G or the momentum's update -> X of the last step in fin's tensors, a batch at a time
+int run_muon(moe_muon* u, MuonElemArgs e, MuonFinish fin, cudaStream_t st) {
+  const moe_muon_shape& s = u->shape;
+  const MuonPlan& p = u->plan;
+  const bool wide = s.rows <= s.cols;
+  const size_t elems = (size_t)s.rows * s.cols;
+  e.elems = (long)elems; e.rows = s.rows; e.cols = s.cols; e.ld = p.ld; e.eps = s.eps;
+  e.parts = (int)muon_parts(e.elems);
+  e.part = u->at<double>(p.part);
+  e.hi = u->at<uint16_t>(p.hi[0]); e.lo = u->at<uint16_t>(p.lo[0]);
+  MuonProductArgs a;
+  memset(&a, 0, sizeof a);
+  a.status = u->status();
+  a.budget_ns = u->budget_ns;
+  for (int done = 0; done < s.n; done += p.batch) {
+    const int n = std::min(p.batch, s.n - done);
+    e.n = a.n = n;
+    MOE_CUDA(launch_muon_momentum(e, st));
+    MOE_CUDA(launch_muon_normalize(e, st));
+    u->launches += 2;
+    int cur = 0;
+    for (int k = 0; k < s.steps; ++k) {
+      const float ca = s.coefficients[k][0], cb = s.coefficients[k][1], cc = s.coefficients[k][2];
+      const float shift = k >= MUON_SHIFT_FROM && cb + cc < 0.f ? -0.75f * (cb + cc) : 0.f;
+      a.M = a.N = p.m; a.nt = u->nt_m; a.ld = p.ldm;
+      a.K = p.l;
+      a.tmA = wide ? u->x128[cur] : u->x64[cur];
+      a.tmB = wide ? u->xhalf[cur] : u->x64[cur];
+      a.tmOut0 = u->abox; a.tmOut1 = u->amir;
+      a.out = u->at<uint16_t>(p.A);
+      a.k_acc = MUON_SA / (MUON_SX * MUON_SX);
+      MOE_CUDA(launch_muon_product(MUON_GRAM, !wide, !wide, a, u->num_sms, st));
+      a.K = p.m;
+      a.tmA = u->a128; a.tmB = u->ahalf; a.tmIn0 = u->abox;
+      a.tmOut0 = u->bbox; a.tmOut1 = u->bmir;
+      a.out = u->at<uint16_t>(p.B);
+      a.k_acc = cc * (MUON_SB / (MUON_SA * MUON_SA));
+      a.k_in = cb * (MUON_SB / MUON_SA);
+      a.k_diag = shift * MUON_SB;
+      MOE_CUDA(launch_muon_product(MUON_POLY, false, false, a, u->num_sms, st));
+      const bool last = k + 1 == s.steps;
+      a.M = s.rows; a.N = s.cols; a.nt = wide ? u->nt_l : u->nt_m;
+      a.tmA = wide ? u->b128 : u->x128[cur];
+      a.tmB = wide ? u->x64[cur] : u->bhalf;
+      a.tmIn0 = u->xhi[cur]; a.tmIn1 = u->xlo[cur];
+      a.tmOut0 = u->xhi[cur ^ 1]; a.tmOut1 = u->xlo[cur ^ 1];
+      const float scale = last ? 1.f / MUON_SX : 1.f;   // of the result
+      a.k_acc = scale / MUON_SB;
+      a.k_in = (ca - shift) * scale;
+      a.fin = fin;
+      MOE_CUDA(launch_muon_product(last ? MUON_LAST : MUON_APPLY, false, wide, a, u->num_sms, st));
+      u->launches += 3;
+      cur ^= 1;
+    }
+    e.G = static_cast<const uint8_t*>(e.G) + (size_t)n * elems * (e.g_fp32 ? 4 : 2);
+    if (e.M) { e.M += (size_t)n * elems; e.M_out += (size_t)n * elems; }
+    fin.out += (size_t)n * elems;
+    if (fin.W) fin.W += (size_t)n * elems;
+  }
+  return MOE_OK;
+}
+
+bool route_groups_ok(const moe_ctx* c, const moe_route_groups* g) {
+  const moe_shape& s = c->shape;
+  return g && g->n_groups >= 1 && g->n_groups <= ROUTE_MAX_GROUPS && s.E % g->n_groups == 0 && g->top_groups >= 1 && g->top_groups <= g->n_groups &&
+         (g->group_top == 1 || g->group_top == 2) && (g->top_groups == g->n_groups || s.E / g->n_groups >= g->group_top) &&
+         (long)g->top_groups * (s.E / g->n_groups) >= s.k && std::isfinite(g->scale);
+}
+
+bool on_its_device(const moe_muon* u) {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == u->device;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1058,6 +1243,49 @@ int moe_router_bwd(moe_ctx* c, const float* logits, const int32_t* topk_ids, con
   c->begin_call(static_cast<cudaStream_t>(stream));
   MOE_CUDA(launch_router_bwd(logits, topk_ids, d_topk_w, T, s.E, s.k, gate_mode(c), d_logits,
                              c->last_stream, &c->launches));
+  return MOE_OK;
+}
+
+int moe_route_grouped(moe_ctx* c, const float* logits, const float* bias, int32_t T, const moe_route_groups* groups, int32_t* topk_ids, float* topk_w,
+                      int32_t* counts, void* stream) {
+  if (!c || T < 0 || T > c->shape.T_max || !route_groups_ok(c, groups) || (T > 0 && (!logits || !topk_ids || !topk_w))) return MOE_ERR_INVALID_ARG;
+  if (!on_its_device(c)) return MOE_ERR_INVALID_ARG;
+  c->begin_call(static_cast<cudaStream_t>(stream));
+  RouteGroupsArgs a;
+  memset(&a, 0, sizeof a);
+  a.logits = logits; a.bias = bias;
+  a.T = T; a.E = c->shape.E; a.k = c->shape.k; a.mode = gate_mode(c);
+  a.n_groups = groups->n_groups; a.top_groups = groups->top_groups; a.group_top = groups->group_top; a.scale = groups->scale;
+  a.topk_ids = topk_ids; a.topk_w = topk_w; a.counts = counts;
+  Phase ph(c, MOE_PHASE_ROUTE, c->last_stream);
+  MOE_CUDA(launch_route_groups(a, c->num_sms, c->last_stream, &c->launches));
+  return MOE_OK;
+}
+
+int moe_route_grouped_bwd(moe_ctx* c, const float* logits, const int32_t* topk_ids, const float* d_topk_w, int32_t T, float scale, int32_t accumulate,
+                          float* d_logits, void* stream) {
+  if (!c || T < 0 || T > c->shape.T_max || !std::isfinite(scale) || (T > 0 && (!logits || !topk_ids || !d_topk_w || !d_logits))) return MOE_ERR_INVALID_ARG;
+  if (!on_its_device(c)) return MOE_ERR_INVALID_ARG;
+  c->begin_call(static_cast<cudaStream_t>(stream));
+  RouteGroupsBwdArgs a;
+  memset(&a, 0, sizeof a);
+  a.logits = logits; a.topk_ids = topk_ids; a.d_topk_w = d_topk_w;
+  a.T = T; a.E = c->shape.E; a.k = c->shape.k; a.mode = gate_mode(c);
+  a.scale = scale;
+  a.accumulate = accumulate != 0;
+  a.vec = c->shape.E % 4 == 0 && aligned16(d_logits);
+  a.d_logits = d_logits;
+  Phase ph(c, MOE_PHASE_ROUTE, c->last_stream);
+  MOE_CUDA(launch_route_groups_bwd(a, c->last_stream, &c->launches));
+  return MOE_OK;
+}
+
+int moe_bias_update(moe_ctx* c, const float* bias, const int32_t* counts, int32_t n_seq, float rate, float* bias_out, void* stream) {
+  if (!c || !bias || !counts || !bias_out || n_seq < 1 || n_seq > BAL_MAX_SEQS || !std::isfinite(rate)) return MOE_ERR_INVALID_ARG;
+  if (!on_its_device(c)) return MOE_ERR_INVALID_ARG;
+  c->begin_call(static_cast<cudaStream_t>(stream));
+  Phase ph(c, MOE_PHASE_ROUTE, c->last_stream);
+  MOE_CUDA(launch_bias_update(bias, counts, n_seq, c->shape.E, rate, bias_out, c->last_stream, &c->launches));
   return MOE_OK;
 }
 
@@ -1212,6 +1440,115 @@ int moe_ffn_fwd_w4(moe_ctx* c, const uint16_t* x, const int32_t* topk_ids, const
   if (!on_its_device(c)) return MOE_ERR_INVALID_ARG;
   return run_fwd_w4(c, x, topk_ids, topk_w, *W_gate_up, *W_down, out, T, c->last_stream);
 }
+
+size_t moe_muon_workspace_bytes(const moe_muon_shape* shape) { return muon_shape_ok(shape) ? plan_muon(*shape).total : 0; }
+
+int moe_muon_create(moe_muon** out, const moe_muon_shape* shape, void* workspace, size_t workspace_bytes) {
+  if (!out || !muon_shape_ok(shape)) return MOE_ERR_INVALID_ARG;
+  *out = nullptr;
+  int dev = 0, major = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    cudaGetLastError();
+    return MOE_ERR_NO_DEVICE;
+  }
+  MOE_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
+  MOE_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  if (major != 10) return MOE_ERR_NO_DEVICE;
+  const MuonPlan plan = plan_muon(*shape);
+  if (workspace && (workspace_bytes < plan.total || (reinterpret_cast<uintptr_t>(workspace) & 255))) return MOE_ERR_WORKSPACE;
+  moe_muon* u = new (std::nothrow) moe_muon();
+  if (!u) return MOE_ERR_WORKSPACE;
+  u->shape = *shape;
+  u->plan = plan;
+  u->device = dev;
+  u->num_sms = sms;
+  u->nt_m = muon_tile_cols(plan.m);
+  u->nt_l = muon_tile_cols(shape->cols);
+  u->ws = static_cast<uint8_t*>(workspace);
+  int rc = MOE_OK;
+  if (!workspace) {
+    cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&u->ws), plan.total);
+    if (e != cudaSuccess) rc = cuda_fail(e, "cudaMalloc(workspace)");
+    else u->owns_ws = true;
+  }
+  if (!rc) {
+    cudaError_t e = cudaMemset(u->ws, 0, sizeof(DevStatus));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);   // the first call may be on any stream
+    rc = e == cudaSuccess ? encode_muon(u) : cuda_fail(e, "cudaMemset(workspace)");
+  }
+  if (rc) {
+    if (u->owns_ws) cudaFree(u->ws);
+    delete u;
+    return rc;
+  }
+  *out = u;
+  return MOE_OK;
+}
+
+int moe_muon_destroy(moe_muon* u) {
+  if (!u) return MOE_OK;
+  if (u->owns_ws) cudaFree(u->ws);
+  delete u;
+  return MOE_OK;
+}
+
+int moe_muon_orthogonalize(moe_muon* u, const void* G, int32_t g_type, uint16_t* out, void* stream) {
+  if (!u || !G || !out || (g_type != MOE_MUON_BF16 && g_type != MOE_MUON_FP32)) return MOE_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(G) & (g_type == MOE_MUON_FP32 ? 3 : 1)) || (reinterpret_cast<uintptr_t>(out) & 1)) return MOE_ERR_INVALID_ARG;
+  if (!on_its_device(u)) return MOE_ERR_INVALID_ARG;
+  u->last_stream = static_cast<cudaStream_t>(stream);
+  u->launches = 0;
+  MuonElemArgs e;
+  memset(&e, 0, sizeof e);
+  e.G = G;
+  e.g_fp32 = g_type == MOE_MUON_FP32;
+  e.vec = u->shape.cols % 8 == 0 && aligned16(G);
+  MuonFinish f;
+  memset(&f, 0, sizeof f);
+  f.out = out;
+  f.vec = u->shape.cols % 8 == 0 && aligned16(out);
+  return run_muon(u, e, f, u->last_stream);
+}
+
+int moe_muon_step(moe_muon* u, const uint16_t* W, const float* M, const uint16_t* dW, float momentum, int32_t nesterov, float lr, float weight_decay,
+                  float scale, uint16_t* W_out, float* M_out, void* stream) {
+  if (!u || !W || !M || !dW || !W_out || !M_out) return MOE_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(W) | reinterpret_cast<uintptr_t>(dW) | reinterpret_cast<uintptr_t>(W_out)) & 1) return MOE_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(M) | reinterpret_cast<uintptr_t>(M_out)) & 3) return MOE_ERR_INVALID_ARG;
+  if (!on_its_device(u)) return MOE_ERR_INVALID_ARG;
+  u->last_stream = static_cast<cudaStream_t>(stream);
+  u->launches = 0;
+  MuonElemArgs e;
+  memset(&e, 0, sizeof e);
+  e.G = dW;
+  e.M = M;
+  e.M_out = M_out;
+  e.mu = momentum;
+  e.nesterov = nesterov != 0;
+  const bool rows8 = u->shape.cols % 8 == 0;
+  e.vec = rows8 && aligned16(dW) && aligned16(M) && aligned16(M_out);
+  MuonFinish f;
+  memset(&f, 0, sizeof f);
+  f.out = W_out;
+  f.W = W;
+  f.keep = (float)(1.0 - (double)lr * (double)weight_decay);
+  f.rate = lr * scale;
+  f.vec = rows8 && aligned16(W) && aligned16(W_out);
+  return run_muon(u, e, f, u->last_stream);
+}
+
+int moe_muon_get_status(moe_muon* u, int32_t* code, int32_t* detail) {
+  if (!u) return MOE_ERR_INVALID_ARG;
+  MOE_CUDA(cudaStreamSynchronize(u->last_stream));
+  DevStatus h;
+  MOE_CUDA(cudaMemcpy(&h, u->status(), sizeof h, cudaMemcpyDeviceToHost));
+  if (code) *code = h.code;
+  if (detail) *detail = h.detail;
+  if (h.code || h.abort) MOE_CUDA(cudaMemset(u->status(), 0, sizeof h));
+  return MOE_OK;
+}
+
+int moe_muon_last_launch_count(const moe_muon* u) { return u ? u->launches : 0; }
 
 int moe_ffn_bwd(moe_ctx* c, const uint16_t* dout, const uint16_t* x, const int32_t* topk_ids, const float* topk_w,
                 const uint16_t* W_gate_up, const uint16_t* W_down, uint16_t* dx, uint16_t* dW_gate_up,

@@ -240,6 +240,32 @@ int balance_fwd_blocks(int T, int E);
 cudaError_t launch_balance_fwd(BalanceArgs a, cudaStream_t s, int* launches);
 cudaError_t launch_balance_bwd(const BalanceArgs& a, int num_sms, cudaStream_t s, int* launches);
 
+// Routing by groups with a bias (route_groups.cu)
+constexpr int ROUTE_MAX_GROUPS = 32;   // a lane a group
+struct RouteGroupsArgs {
+  const float* logits;      // [T][E]
+  const float* bias;        // [E]; NULL: none
+  int T, E, k, mode;        // mode: GATE_RENORM | GATE_SIGMOID
+  int n_groups, top_groups, group_top;
+  float scale;
+  int* topk_ids;            // [T][k]
+  float* topk_w;            // [T][k]
+  int* counts;              // [E]; may be NULL
+};
+cudaError_t launch_route_groups(const RouteGroupsArgs& a, int num_sms, cudaStream_t s, int* launches);
+struct RouteGroupsBwdArgs {
+  const float* logits;
+  const int* topk_ids;
+  const float* d_topk_w;
+  int T, E, k, mode;
+  float scale;
+  int accumulate;           // added to d_logits
+  int vec;                  // d_logits' rows are whole 16-byte vectors
+  float* d_logits;
+};
+cudaError_t launch_route_groups_bwd(const RouteGroupsBwdArgs& a, cudaStream_t s, int* launches);
+cudaError_t launch_bias_update(const float* bias, const int* counts, int n_seq, int E, float rate, float* out, cudaStream_t s, int* launches);
+
 int vector_warps();   // vector warps per CTA of the persistent launch
 // Not a cooperative launch: that attribute holds a launch back until the one in front of it has ended (2 us each: the smallest
 // training step 57 -> 52 us), and co-residency is not needed (schedule.h).  The grid is sized to what can be resident.
