@@ -68,9 +68,9 @@ EncodeTiledFn get_encode_fn() {
 }
 
 // bf16 (or fp16) tensor of `rank` dimensions (dims[0] innermost, strides in bytes for dims 1..), 128-byte
-// swizzle unless stated, zero fill outside the tensor on loads, clipping on stores.
+// swizzle, zero fill outside the tensor on loads, clipping on stores.
 int encode_tiled(CUtensorMap* tm, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
-                 const uint32_t* box, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
+                 const uint32_t* box) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) {
     g_cuda_error = "cuTensorMapEncodeTiled entry point not available";
@@ -81,7 +81,7 @@ int encode_tiled(CUtensorMap* tm, const void* base, int rank, const uint64_t* di
   for (int i = 0; i < rank; ++i) { gdim[i] = dims[i]; bx[i] = box[i]; }
   for (int i = 0; i + 1 < rank; ++i) gstr[i] = strides[i];
   CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), gdim, gstr, bx, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
@@ -930,7 +930,7 @@ constexpr size_t MUON_BATCH_BYTES = size_t(1) << 30;
 struct MuonPlan {
   int m, l, ld, ldm;          // smaller and larger dimension; elements from row to row of X, of A and B
   int batch;                  // matrices of a turn
-  size_t part, hi[2], lo[2], A, B, total;
+  size_t ctr, part, hi[2], lo[2], A, B, total;
 };
 
 bool muon_shape_ok(const moe_muon_shape* s) {
@@ -956,6 +956,7 @@ MuonPlan plan_muon(const moe_muon_shape& s) {
   p.batch = (int)(((size_t)s.n + turns - 1) / turns);
   Carve c;
   c.take(sizeof(DevStatus));
+  p.ctr = c.take(sizeof(int) * (p.batch + 1));
   p.part = c.take(sizeof(double) * p.batch * parts);
   for (int i = 0; i < 2; ++i) {
     p.hi[i] = c.take(x * p.batch);
@@ -975,13 +976,10 @@ struct moe_muon {
   uint8_t* ws = nullptr;
   bool owns_ws = false;
   int device = 0, num_sms = 0;
-  int nt_m = 0, nt_l = 0;   // tile columns of products m and l columns wide
   uint64_t budget_ns = 2000ull * 1000 * 1000;
   cudaStream_t last_stream = nullptr;
   int launches = 0;
-  // X, by buffer: 128 rows, nt_m / 2 rows, 64 x 64, epilogue boxes of hi and lo; A and B: 128 rows, nt_m / 2 rows, epilogue boxes, mirrored ones
-  CUtensorMap x128[2], xhalf[2], x64[2], xhi[2], xlo[2];
-  CUtensorMap a128, ahalf, abox, amir, b128, bhalf, bbox, bmir;
+  MuonArgs args;   // tensor maps of the workspace, factors, sizes: fixed; the rest is filled by each call
   DevStatus* status() const { return reinterpret_cast<DevStatus*>(ws); }
   template <class T>
   T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
@@ -989,105 +987,108 @@ struct moe_muon {
 
 namespace {
 
-int encode_batch(CUtensorMap* tm, const void* base, uint64_t n, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows, uint32_t box_cols,
-                 CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
+// [n][rows][cols] in 16 bits, rows ld elements apart
+int encode_batch(CUtensorMap* tm, const void* base, uint64_t n, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows) {
   const uint64_t dims[3] = {cols, rows, n}, strides[2] = {ld * 2, rows * ld * 2};
-  const uint32_t box[3] = {box_cols, box_rows, 1};
-  return encode_tiled(tm, base, 3, dims, strides, box, swizzle);
+  const uint32_t box[3] = {64, box_rows, 1};
+  return encode_tiled(tm, base, 3, dims, strides, box);
 }
 
-int encode_muon(moe_muon* u) {
-  const MuonPlan& p = u->plan;
-  const uint64_t n = p.batch, rows = u->shape.rows, cols = u->shape.cols;
-  int rc = MOE_OK;
-  for (int i = 0; i < 2 && !rc; ++i) {
-    const void *hi = u->ws + p.hi[i], *lo = u->ws + p.lo[i];
-    if (!rc) rc = encode_batch(&u->x128[i], hi, n, rows, cols, p.ld, 128, 64);
-    if (!rc) rc = encode_batch(&u->xhalf[i], hi, n, rows, cols, p.ld, u->nt_m / 2, 64);
-    if (!rc) rc = encode_batch(&u->x64[i], hi, n, rows, cols, p.ld, 64, 64);
-    if (!rc) rc = encode_batch(&u->xhi[i], hi, n, rows, cols, p.ld, 32, 64);
-    if (!rc) rc = encode_batch(&u->xlo[i], lo, n, rows, cols, p.ld, 32, 64);
-  }
-  for (int i = 0; i < 2 && !rc; ++i) {
-    const void* b = u->ws + (i ? p.B : p.A);
-    rc = encode_batch(i ? &u->b128 : &u->a128, b, n, p.m, p.m, p.ldm, 128, 64);
-    if (!rc) rc = encode_batch(i ? &u->bhalf : &u->ahalf, b, n, p.m, p.m, p.ldm, u->nt_m / 2, 64);
-    if (!rc) rc = encode_batch(i ? &u->bbox : &u->abox, b, n, p.m, p.m, p.ldm, 32, 64);
-    if (!rc) rc = encode_batch(i ? &u->bmir : &u->amir, b, n, p.m, p.m, p.ldm, 64, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
-  }
-  return rc;
-}
-
-// Tile columns: the fewest padded columns, narrower tiles charged for the operand bytes that they bring in for a product.
-int muon_tile_cols(int N) {
+// Columns of an APPLY tile: the fewest padded columns, narrower tiles charged for the operand bytes that they bring in for a product;
+// X B of tall matrices takes B by its blocks.
+int muon_tile_cols(const moe_muon_shape& s) {
   static const int width[3] = {256, 192, 128}, charge[3] = {100, 105, 115};
-  int best = 256;
+  int best = MUON_BLOCK;
   long least = -1;
-  for (int i = 0; i < 3; ++i) {
-    const long c = (long)((N + width[i] - 1) / width[i]) * width[i] * charge[i];
+  for (int i = 0; i < 3 && s.rows <= s.cols; ++i) {
+    const long c = (long)((s.cols + width[i] - 1) / width[i]) * width[i] * charge[i];
     if (least < 0 || c < least) { least = c; best = width[i]; }
   }
   return best;
 }
 
-// u = G or the momentum's update -> X of the last step in fin's tensors, a batch at a time
-int run_muon(moe_muon* u, MuonElemArgs e, MuonFinish fin, cudaStream_t st) {
+// Matrices whose phases follow one another: four turns of symmetric tiles over the pairs, so that a phase's first tiles do not wait for
+// the last ones of the phase before; groups of equal size.
+int muon_group(int m, int n, int num_sms) {
+  const long nb = (m + MUON_BLOCK - 1) / MUON_BLOCK, tri = nb * (nb + 1) / 2;
+  const long want = (4l * (num_sms / 2) + tri - 1) / tri;
+  const long groups = std::max(1l, n / want);
+  return (int)((n + groups - 1) / groups);
+}
+
+int plan_muon_args(moe_muon* u) {
+  const MuonPlan& p = u->plan;
+  const moe_muon_shape& s = u->shape;
+  MuonArgs& a = u->args;
+  memset(&a, 0, sizeof a);
+  const uint64_t n = p.batch, rows = s.rows, cols = s.cols;
+  int rc = MOE_OK;
+  for (int i = 0; i < 2 && !rc; ++i) {
+    const void *hi = u->ws + p.hi[i], *lo = u->ws + p.lo[i];
+    rc = encode_batch(&a.x128[i], hi, n, rows, cols, p.ld, 128);
+    if (!rc) rc = encode_batch(&a.x64[i], hi, n, rows, cols, p.ld, 64);
+    if (!rc) rc = encode_batch(&a.xhi[i], hi, n, rows, cols, p.ld, 32);
+    if (!rc) rc = encode_batch(&a.xlo[i], lo, n, rows, cols, p.ld, 32);
+  }
+  const void *A = u->ws + p.A, *B = u->ws + p.B;
+  if (!rc) rc = encode_batch(&a.a128, A, n, p.m, p.m, p.ldm, 128);
+  if (!rc) rc = encode_batch(&a.a64, A, n, p.m, p.m, p.ldm, 64);
+  if (!rc) rc = encode_batch(&a.abox, A, n, p.m, p.m, p.ldm, 32);
+  if (!rc) rc = encode_batch(&a.b128, B, n, p.m, p.m, p.ldm, 128);
+  if (!rc) rc = encode_batch(&a.b64, B, n, p.m, p.m, p.ldm, 64);
+  if (!rc) rc = encode_batch(&a.bbox, B, n, p.m, p.m, p.ldm, 32);
+  if (rc) return rc;
+  a.rows = s.rows; a.cols = s.cols; a.steps = s.steps;
+  a.nt = muon_tile_cols(s);
+  a.status = u->status();
+  a.budget_ns = u->budget_ns;
+  a.ctr = u->at<int>(p.ctr);
+  for (int k = 0; k < s.steps; ++k) {
+    const float ca = s.coefficients[k][0], cb = s.coefficients[k][1], cc = s.coefficients[k][2];
+    const float shift = k >= MUON_LATE && cb + cc < 0.f ? -0.75f * (cb + cc) : 0.f;
+    const float scale = k + 1 == s.steps ? 1.f / MUON_SX : 1.f;   // of the result
+    MuonArgs::Step& t = a.step[k];
+    t.gram_acc = MUON_SA / (MUON_SX * MUON_SX);
+    t.poly_acc = cc * (MUON_SB / (MUON_SA * MUON_SA));
+    t.poly_in = cb * (MUON_SB / MUON_SA);
+    t.poly_diag = shift * MUON_SB;
+    t.app_acc = scale / MUON_SB;
+    t.app_in = (ca - shift) * scale;
+  }
+  return MOE_OK;
+}
+
+// u = G or the momentum's update -> X of the last step, or W - rate X, in `out`, a batch at a time
+int run_muon(moe_muon* u, MuonElemArgs e, const uint16_t* W, uint16_t* out, float keep, float rate, cudaStream_t st) {
   const moe_muon_shape& s = u->shape;
   const MuonPlan& p = u->plan;
-  const bool wide = s.rows <= s.cols;
   const size_t elems = (size_t)s.rows * s.cols;
   e.elems = (long)elems; e.rows = s.rows; e.cols = s.cols; e.ld = p.ld; e.eps = s.eps;
   e.parts = (int)muon_parts(e.elems);
   e.part = u->at<double>(p.part);
   e.hi = u->at<uint16_t>(p.hi[0]); e.lo = u->at<uint16_t>(p.lo[0]);
-  MuonProductArgs a;
-  memset(&a, 0, sizeof a);
-  a.status = u->status();
-  a.budget_ns = u->budget_ns;
+  e.ctr = u->at<int>(p.ctr);
+  MuonArgs& a = u->args;
+  a.vec = s.cols % 8 == 0 && aligned16(out) && aligned16(W);
+  a.keep = keep; a.rate = rate;
+  if (a.vec) {
+    int rc = encode_batch(&a.out, out, s.n, s.rows, s.cols, s.cols, 32);
+    if (!rc && W) rc = encode_batch(&a.w, W, s.n, s.rows, s.cols, s.cols, 32);
+    if (rc) return rc;
+  }
   for (int done = 0; done < s.n; done += p.batch) {
     const int n = std::min(p.batch, s.n - done);
     e.n = a.n = n;
+    a.z0 = done;
+    a.sub = muon_group(p.m, n, u->num_sms);
+    a.out_ptr = out + (size_t)done * elems;
+    a.w_ptr = W ? W + (size_t)done * elems : nullptr;
     MOE_CUDA(launch_muon_momentum(e, st));
     MOE_CUDA(launch_muon_normalize(e, st));
-    u->launches += 2;
-    int cur = 0;
-    for (int k = 0; k < s.steps; ++k) {
-      const float ca = s.coefficients[k][0], cb = s.coefficients[k][1], cc = s.coefficients[k][2];
-      const float shift = k >= MUON_SHIFT_FROM && cb + cc < 0.f ? -0.75f * (cb + cc) : 0.f;
-      a.M = a.N = p.m; a.nt = u->nt_m; a.ld = p.ldm;
-      a.K = p.l;
-      a.tmA = wide ? u->x128[cur] : u->x64[cur];
-      a.tmB = wide ? u->xhalf[cur] : u->x64[cur];
-      a.tmOut0 = u->abox; a.tmOut1 = u->amir;
-      a.out = u->at<uint16_t>(p.A);
-      a.k_acc = MUON_SA / (MUON_SX * MUON_SX);
-      MOE_CUDA(launch_muon_product(MUON_GRAM, !wide, !wide, a, u->num_sms, st));
-      a.K = p.m;
-      a.tmA = u->a128; a.tmB = u->ahalf; a.tmIn0 = u->abox;
-      a.tmOut0 = u->bbox; a.tmOut1 = u->bmir;
-      a.out = u->at<uint16_t>(p.B);
-      a.k_acc = cc * (MUON_SB / (MUON_SA * MUON_SA));
-      a.k_in = cb * (MUON_SB / MUON_SA);
-      a.k_diag = shift * MUON_SB;
-      MOE_CUDA(launch_muon_product(MUON_POLY, false, false, a, u->num_sms, st));
-      const bool last = k + 1 == s.steps;
-      a.M = s.rows; a.N = s.cols; a.nt = wide ? u->nt_l : u->nt_m;
-      a.tmA = wide ? u->b128 : u->x128[cur];
-      a.tmB = wide ? u->x64[cur] : u->bhalf;
-      a.tmIn0 = u->xhi[cur]; a.tmIn1 = u->xlo[cur];
-      a.tmOut0 = u->xhi[cur ^ 1]; a.tmOut1 = u->xlo[cur ^ 1];
-      const float scale = last ? 1.f / MUON_SX : 1.f;   // of the result
-      a.k_acc = scale / MUON_SB;
-      a.k_in = (ca - shift) * scale;
-      a.fin = fin;
-      MOE_CUDA(launch_muon_product(last ? MUON_LAST : MUON_APPLY, false, wide, a, u->num_sms, st));
-      u->launches += 3;
-      cur ^= 1;
-    }
+    MOE_CUDA(launch_muon_products(s.rows <= s.cols, a, u->num_sms, st));
+    u->launches += 3;
     e.G = static_cast<const uint8_t*>(e.G) + (size_t)n * elems * (e.g_fp32 ? 4 : 2);
     if (e.M) { e.M += (size_t)n * elems; e.M_out += (size_t)n * elems; }
-    fin.out += (size_t)n * elems;
-    if (fin.W) fin.W += (size_t)n * elems;
   }
   return MOE_OK;
 }
@@ -1462,8 +1463,6 @@ int moe_muon_create(moe_muon** out, const moe_muon_shape* shape, void* workspace
   u->plan = plan;
   u->device = dev;
   u->num_sms = sms;
-  u->nt_m = muon_tile_cols(plan.m);
-  u->nt_l = muon_tile_cols(shape->cols);
   u->ws = static_cast<uint8_t*>(workspace);
   int rc = MOE_OK;
   if (!workspace) {
@@ -1474,7 +1473,7 @@ int moe_muon_create(moe_muon** out, const moe_muon_shape* shape, void* workspace
   if (!rc) {
     cudaError_t e = cudaMemset(u->ws, 0, sizeof(DevStatus));
     if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);   // the first call may be on any stream
-    rc = e == cudaSuccess ? encode_muon(u) : cuda_fail(e, "cudaMemset(workspace)");
+    rc = e == cudaSuccess ? plan_muon_args(u) : cuda_fail(e, "cudaMemset(workspace)");
   }
   if (rc) {
     if (u->owns_ws) cudaFree(u->ws);
@@ -1503,11 +1502,7 @@ int moe_muon_orthogonalize(moe_muon* u, const void* G, int32_t g_type, uint16_t*
   e.G = G;
   e.g_fp32 = g_type == MOE_MUON_FP32;
   e.vec = u->shape.cols % 8 == 0 && aligned16(G);
-  MuonFinish f;
-  memset(&f, 0, sizeof f);
-  f.out = out;
-  f.vec = u->shape.cols % 8 == 0 && aligned16(out);
-  return run_muon(u, e, f, u->last_stream);
+  return run_muon(u, e, nullptr, out, 0.f, 0.f, u->last_stream);
 }
 
 int moe_muon_step(moe_muon* u, const uint16_t* W, const float* M, const uint16_t* dW, float momentum, int32_t nesterov, float lr, float weight_decay,
@@ -1527,14 +1522,7 @@ int moe_muon_step(moe_muon* u, const uint16_t* W, const float* M, const uint16_t
   e.nesterov = nesterov != 0;
   const bool rows8 = u->shape.cols % 8 == 0;
   e.vec = rows8 && aligned16(dW) && aligned16(M) && aligned16(M_out);
-  MuonFinish f;
-  memset(&f, 0, sizeof f);
-  f.out = W_out;
-  f.W = W;
-  f.keep = (float)(1.0 - (double)lr * (double)weight_decay);
-  f.rate = lr * scale;
-  f.vec = rows8 && aligned16(W) && aligned16(W_out);
-  return run_muon(u, e, f, u->last_stream);
+  return run_muon(u, e, W, W_out, (float)(1.0 - (double)lr * (double)weight_decay), lr * scale, u->last_stream);
 }
 
 int moe_muon_get_status(moe_muon* u, int32_t* code, int32_t* detail) {

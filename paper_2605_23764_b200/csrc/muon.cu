@@ -52,6 +52,8 @@ __global__ void __launch_bounds__(MU_ELEM_THREADS) muon_momentum_kernel(const Mu
   const int mat = blockIdx.x / a.parts, part = blockIdx.x - mat * a.parts;
   const long e0 = part * MUON_PART, e1 = min(a.elems, e0 + MUON_PART);
   const size_t base = (size_t)mat * a.elems;
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i <= a.n; i += MU_ELEM_THREADS) a.ctr[i] = 0;
   double sum = 0.0;
   for (long i = e0 + threadIdx.x * N; i < e1; i += MU_ELEM_THREADS * N) {
     float u[N];

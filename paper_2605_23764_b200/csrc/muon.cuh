@@ -8,9 +8,10 @@
 // 2^-12 of the largest entries adds to a small singular value grows with it: matrices of rank 256 + rounding, 512 x 768, were 6.8e-3
 // off in the norm after five steps, with both 1.3e-3 (bf16 operands and X: 5.4e-2).
 //
-// Once the singular values have come near 1 (from the fourth step on), B's diagonal is near b + c, which a X mostly cancels: there
-// three quarters of it move from B to the linear term, X <- (a - s) X + (B + s I) X with s = -3/4 (b + c).  Errors halve: 1.6e-3 ->
-// 0.9e-3 on normally distributed matrices.
+// Three steps on (MUON_LATE) the singular values have come near 1.  There X's lo part no longer counts and is left out (0.9e-3 instead of
+// 0.8e-3, 1.8e-3 instead of 1.3e-3 for the rank of 256).  B's diagonal is near b + c there, which a X mostly cancels: three quarters of it
+// move from B to the linear term, X <- (a - s) X + (B + s I) X with s = -3/4 (b + c).  Errors halve: 1.6e-3 -> 0.9e-3 on normally
+// distributed matrices.
 #pragma once
 
 #include "moe_internal.h"
@@ -18,38 +19,40 @@
 namespace moe {
 
 constexpr float MUON_SX = 4096.f, MUON_SA = 4096.f, MUON_SB = 1024.f, MUON_SLO = 2048.f;
-constexpr int MUON_SHIFT_FROM = 3;   // first step (from 0) with the shifted diagonal
+constexpr int MUON_STEPS_MAX = 16;
+constexpr int MUON_LATE = 3;   // first step (from 0) with the shifted diagonal and X in one part
 
-enum MuonProduct : int {
+enum MuonPhase : int {
   MUON_GRAM = 0,    // A = X X^T or X^T X
   MUON_POLY = 1,    // B = b A + c A A + s I
-  MUON_APPLY = 2,   // X' = (a - s) X + B X or X B
-  MUON_LAST = 3,    // the same of the last step: into the caller's tensors
+  MUON_APPLY = 2,   // X' = (a - s) X + B X or X B; of the last step: into the caller's tensors
 };
 
-// What is done with the last step's X'
-struct MuonFinish {
-  uint16_t* out;         // bf16 [n][rows][cols], W' or X' itself
-  const uint16_t* W;     // W' = keep W - rate X'; NULL: out = X'
+// A symmetric matrix is stored by blocks of 256 x 256, those on and below the diagonal.
+constexpr int MUON_BLOCK = 256;
+
+struct MuonArgs {
+  // X, by buffer: K-major operand (128 rows x 64), MN-major operand (64 x 64), epilogue boxes (32 rows x 64) of hi and lo
+  CUtensorMap x128[2], x64[2], xhi[2], xlo[2];
+  CUtensorMap a128, a64, abox, b128, b64, bbox;   // A and B
+  CUtensorMap out, w;          // the caller's tensors by epilogue boxes (vec)
+  int n, rows, cols;           // matrices of the batch
+  int steps;
+  int nt;                      // columns of an APPLY tile: 128, 192 or 256
+  int sub;                     // matrices whose phases follow one another
+  int z0;                      // the batch's first matrix in the caller's tensors
+  struct Step { float gram_acc, poly_acc, poly_in, poly_diag, app_acc, app_in; } step[MUON_STEPS_MAX];   // factors in the stored scalings
+  // the last step's X': out = X', or with W: out = keep W - rate X'
+  uint16_t* out_ptr;           // bf16 [rows][cols] of the batch's first matrix
+  const uint16_t* w_ptr;       // NULL: none
   float keep, rate;
-  int vec;               // rows of out (and W) are whole 16-byte vectors
-};
-
-struct MuonProductArgs {
-  CUtensorMap tmA, tmB;        // operands: boxes of 64 k x 128 rows (K-major) or 64 columns x 64 k (MN-major)
-  CUtensorMap tmIn0, tmIn1;    // epilogue: boxes of 32 rows x 64 columns of A (POLY) or X hi, X lo (APPLY)
-  CUtensorMap tmOut0, tmOut1;  // GRAM, POLY: the product, and mirrored (boxes of 64 x 32, not swizzled); APPLY: X' hi, X' lo
-  int n, M, N, K;              // matrices; sizes of the product
-  int nt;                      // columns of a tile: 128, 192 or 256
-  int ld;                      // GRAM, POLY: elements from row to row of the product
-  uint16_t* out;               // GRAM, POLY: the product
-  float k_acc, k_in, k_diag;   // factors of the accumulator, of what the epilogue reads, on the diagonal; in the product's scaling
-  MuonFinish fin;              // LAST
+  int vec;                     // rows of both are whole 16-byte vectors
+  int* ctr;                    // [n] finished warps' parts of tiles of each matrix, [n]: next item; zero before the launch
   DevStatus* status;
   uint64_t budget_ns;
 };
-// a_mn, b_mn: the operand's rows are the reduction
-cudaError_t launch_muon_product(MuonProduct what, bool a_mn, bool b_mn, const MuonProductArgs& a, int num_sms, cudaStream_t s);
+// One persistent launch for all products of a batch; wide: rows <= cols
+cudaError_t launch_muon_products(bool wide, const MuonArgs& a, int num_sms, cudaStream_t s);
 
 struct MuonElemArgs {
   const void* G;        // [n][rows][cols], bf16 or fp32
@@ -65,6 +68,7 @@ struct MuonElemArgs {
   int parts;
   float eps;
   uint16_t *hi, *lo;    // X [n][rows][ld]
+  int* ctr;             // [n + 1] cleared on the way
 };
 constexpr long MUON_PART = 32768;   // elements of a part
 inline long muon_parts(long elems) { return (elems + MUON_PART - 1) / MUON_PART; }

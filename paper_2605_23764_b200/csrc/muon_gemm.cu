@@ -1,15 +1,21 @@
-// The products of an orthogonalising step (muon.cuh) on the tensor cores: fp16 operands, fp32 accumulators, CTA pairs, persistent.
+// The products of an orthogonalisation (muon.cuh) on the tensor cores: one persistent launch for all steps of a batch of matrices.
 //
-// A tile is 256 rows x nt columns of one matrix's product, its accumulator one of two in TMEM, so that a tile's products run beside
-// the epilogue of the one before.  Operands come in as they lie: K-major where the reduction is contiguous, MN-major where it is the
-// rows (X as the second operand of B X, both of X^T X), so nothing is ever transposed in memory.
+// Items are tiles of 256 rows x 256 (or nt) columns of one matrix's product.  The phases of a matrix follow one another; an item
+// waits until all tiles of its matrix's phase before have been stored (a counter a matrix), which other matrices' tiles cover.
+// CTA pairs take items from a ticket in that order, so whichever pairs are resident make progress.  The accumulator is one of two in
+// TMEM: a tile's products run beside the epilogue of the one before.
 //
-// GRAM and POLY are symmetric: only tiles that touch the lower triangle are computed (21 of 36 for 1408), and boxes of 32 rows x 64
-// columns below the diagonal are stored twice, as they are and mirrored, from a box transposed in shared memory.  Boxes on the
-// diagonal are stored element by element, each written once.
+// Operands come in as they lie: K-major where the reduction is contiguous, MN-major where it is the rows (X as the second operand of
+// B X, both of X^T X), so nothing is ever transposed in memory.  A and B are symmetric: tiles above the diagonal are neither computed
+// nor stored, and an operand's k-blocks that would lie there are read from their mirror image, MN-major -- the instruction descriptor
+// changes from k-block to k-block.  (Stored twice, as they are and mirrored, they cost the epilogue 2.3 times the shared-memory accesses.)
 //
-// Roles per CTA: warp 0 TMA producer, warp 1 MMA issuer (even CTA) and TMEM owner, warps 2-9 epilogue.
+// What bounds it: shared memory.  A k-block brings 32 KB into an SM and the products read 32 KB, 512 clocks' worth at 128 bytes a clock,
+// which is what the products take; the epilogue's boxes come on top.
+//
+// Roles per CTA: warp 0 TMA producer, warp 1 MMA issuer (even CTA) and TMEM owner, warps 2-9 epilogue, warp 10 tickets (even CTA).
 #include <cuda_fp16.h>
+#include <limits.h>
 
 #include "gemm_tile.cuh"
 #include "launch_pairs.cuh"
@@ -20,186 +26,232 @@ namespace moe {
 
 constexpr int MU_STAGES = 5;
 constexpr int MU_STAGE_BYTES = A_STAGE_BYTES + HALF_B_BYTES;   // 128 rows of A, up to 128 of the tile's columns
-constexpr int MU_EPI_WARPS = 8, MU_THREADS = 32 * (2 + MU_EPI_WARPS);
+constexpr int MU_EPI_WARPS = 8, MU_THREADS = 32 * (3 + MU_EPI_WARPS);
 constexpr int MU_BOX = 32 * 64 * 2;
+constexpr int MU_SLOTS = 3;          // tickets taken ahead
+constexpr int MU_READERS = 19;       // warps of the pair that read a ticket: two loaders, the issuer, sixteen of the epilogues
+constexpr int MU_PARTS = 2 * MU_EPI_WARPS;   // signals of a tile
 
 struct MuonBarriers {
   uint64_t full[MU_STAGES], empty[MU_STAGES];
   uint64_t tmem_full[2], tmem_empty[2];
   uint64_t in_full[MU_EPI_WARPS];
+  uint64_t item_full[MU_SLOTS], item_empty[MU_SLOTS];
   uint64_t drain;
   uint32_t tmem_base;
+  int item[MU_SLOTS];
 };
 constexpr size_t MU_SMEM = 1024 + MU_STAGES * MU_STAGE_BYTES + MU_EPI_WARPS * 2 * MU_BOX + sizeof(MuonBarriers);
 static_assert(MU_SMEM <= 227 * 1024, "shared memory budget");
 
-struct MuonTile { int mat, m0, n0; };
+struct MuonItem {
+  int phase, step, mat, m0, n0, nt;
+  int need;   // the matrix's counter when the phase before is complete
+};
 
-template <bool TRI>
-__host__ __device__ __forceinline__ int muon_row_tiles(const MuonProductArgs& a, int i) {
-  const int cols = TRI ? min(256 * (i + 1), a.N) : a.N;
-  return (cols + a.nt - 1) / a.nt;
-}
-template <bool TRI>
-__host__ __device__ __forceinline__ int muon_tiles(const MuonProductArgs& a) {   // of one matrix
-  const int rows = (a.M + 255) / 256;
-  if (!TRI) return rows * muon_row_tiles<TRI>(a, 0);
-  int n = 0;
-  for (int i = 0; i < rows; ++i) n += muon_row_tiles<TRI>(a, i);
-  return n;
-}
-template <bool TRI>
-__device__ __forceinline__ MuonTile muon_decode(const MuonProductArgs& a, int per, int t) {
-  MuonTile r;
-  r.mat = t / per;
-  int q = t - r.mat * per, i = 0;
-  if (TRI) {
-    for (int c; q >= (c = muon_row_tiles<TRI>(a, i)); ++i) q -= c;
-  } else {
-    const int c = muon_row_tiles<TRI>(a, 0);
-    i = q / c;
-    q -= i * c;
+// Tiles of a matrix's phases and how items go through them: `sub` matrices at a time, step by step, phase by phase, matrix by matrix.
+struct MuonOrder {
+  int tri, app, app_cols, per_step;
+  __host__ __device__ explicit MuonOrder(const MuonArgs& a) {
+    const int m = a.rows < a.cols ? a.rows : a.cols, nb = (m + MUON_BLOCK - 1) / MUON_BLOCK;
+    tri = nb * (nb + 1) / 2;
+    app_cols = (a.cols + a.nt - 1) / a.nt;
+    app = (a.rows + 255) / 256 * app_cols;
+    per_step = 2 * tri + app;
   }
-  r.m0 = i * 256;
-  r.n0 = q * a.nt;
-  return r;
-}
+  __host__ __device__ long total(const MuonArgs& a) const { return (long)a.n * a.steps * per_step; }
+  __device__ __forceinline__ MuonItem decode(const MuonArgs& a, int t) const {
+    MuonItem r;
+    const int full = a.sub * a.steps * per_step, g = t / full;
+    t -= g * full;
+    const int s = min(a.sub, a.n - g * a.sub);   // matrices of this group
+    r.step = t / (s * per_step);
+    t -= r.step * s * per_step;
+    r.need = r.step * per_step;
+    int tiles = tri;
+    r.phase = MUON_GRAM;
+    if (t >= s * tri) {
+      t -= s * tri;
+      r.need += tri;
+      r.phase = MUON_POLY;
+      if (t >= s * tri) {
+        t -= s * tri;
+        r.need += tri;
+        r.phase = MUON_APPLY;
+        tiles = app;
+      }
+    }
+    r.need *= MU_PARTS;
+    const int q = t / tiles;
+    t -= q * tiles;
+    r.mat = g * a.sub + q;
+    int i = 0;
+    if (r.phase == MUON_APPLY) {
+      i = t / app_cols;
+      t -= i * app_cols;
+      r.nt = a.nt;
+    } else {
+      while (t > i) t -= ++i;
+      r.nt = MUON_BLOCK;
+    }
+    r.m0 = i * 256;
+    r.n0 = t * r.nt;
+    return r;
+  }
+};
 
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ float2 unpack_h2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+__device__ __forceinline__ uint4* box_chunk(uint8_t* box, int lane, int j) { return reinterpret_cast<uint4*>(box + lane * 128 + ((j ^ (lane & 7)) << 4)); }
 
-// One box of 32 rows x 64 columns of the accumulator, first row r0 of the matrix (this lane's: r0 + lane), first column c0.
-template <int WHAT>
-__device__ __forceinline__ void muon_epilogue_box(const MuonProductArgs& a, uint32_t tcol, uint8_t* box0, uint8_t* box1, int mat, int r0, int c0, int lane) {
-  float v[64];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) tmem_ld16(tcol + 16 * q, v + 16 * q);
-  tmem_ld_wait();
-  const int r = r0 + lane;
-  uint8_t* row0 = box0 + lane * 128;
-  uint8_t* row1 = box1 + lane * 128;
-  if constexpr (WHAT == MUON_GRAM || WHAT == MUON_POLY) {
-    uint32_t h[32];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      uint4 in = make_uint4(0, 0, 0, 0);
-      if (WHAT == MUON_POLY) in = *reinterpret_cast<uint4*>(row0 + ((j ^ (lane & 7)) << 4));
-      const uint32_t w[4] = {in.x, in.y, in.z, in.w};
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        float2 x = make_float2(v[8 * j + 2 * p] * a.k_acc, v[8 * j + 2 * p + 1] * a.k_acc);
-        if (WHAT == MUON_POLY) {
-          const float2 y = unpack_h2(w[p]);
-          x.x = fmaf(y.x, a.k_in, x.x);
-          x.y = fmaf(y.y, a.k_in, x.y);
-          const int c = c0 + 8 * j + 2 * p;
-          if (c == r) x.x += a.k_diag;
-          if (c + 1 == r) x.y += a.k_diag;
-        }
-        h[4 * j + p] = pack_h2(x.x, x.y);
-      }
-    }
-    if (c0 + 63 < r0) {   // below the diagonal: as it is and mirrored
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        *reinterpret_cast<uint4*>(row0 + ((j ^ (lane & 7)) << 4)) = make_uint4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
-      uint16_t* t = reinterpret_cast<uint16_t*>(box1) + lane;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        t[(2 * i) * 32] = (uint16_t)h[i];
-        t[(2 * i + 1) * 32] = (uint16_t)(h[i] >> 16);
-      }
-      staging_release();
-      if (lane == 0) {
-        tma_store_3d(&a.tmOut0, c0, r0, mat, box0);
-        tma_store_3d(&a.tmOut1, r0, c0, mat, box1);
-        tma_store_commit();
-      }
-    } else if (r < a.M) {
-      uint16_t* A = a.out + (size_t)mat * a.M * a.ld;
-#pragma unroll
-      for (int i = 0; i < 64; ++i) {
-        const int c = c0 + i;
-        const uint16_t x = (uint16_t)(h[i >> 1] >> (16 * (i & 1)));
-        if (c <= r) A[(size_t)r * a.ld + c] = x;
-        if (c < r) A[(size_t)c * a.ld + r] = x;
-      }
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      uint4* ph = reinterpret_cast<uint4*>(row0 + ((j ^ (lane & 7)) << 4));
-      uint4* pl = reinterpret_cast<uint4*>(row1 + ((j ^ (lane & 7)) << 4));
-      const uint4 xh = *ph, xl = *pl;
-      const uint32_t wh[4] = {xh.x, xh.y, xh.z, xh.w}, wl[4] = {xl.x, xl.y, xl.z, xl.w};
-      uint32_t oh[4], ol[4];
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const float2 yh = unpack_h2(wh[p]), yl = unpack_h2(wl[p]);
-        const float x0 = fmaf(fmaf(yl.x, 1.f / MUON_SLO, yh.x), a.k_in, v[8 * j + 2 * p] * a.k_acc);
-        const float x1 = fmaf(fmaf(yl.y, 1.f / MUON_SLO, yh.y), a.k_in, v[8 * j + 2 * p + 1] * a.k_acc);
-        v[8 * j + 2 * p] = x0;
-        v[8 * j + 2 * p + 1] = x1;
-        if (WHAT == MUON_APPLY) {
-          oh[p] = pack_h2(x0, x1);
-          const float2 z = unpack_h2(oh[p]);
-          ol[p] = pack_h2((x0 - z.x) * MUON_SLO, (x1 - z.y) * MUON_SLO);
-        }
-      }
-      if (WHAT == MUON_APPLY) {
-        *ph = make_uint4(oh[0], oh[1], oh[2], oh[3]);
-        *pl = make_uint4(ol[0], ol[1], ol[2], ol[3]);
-      }
-    }
-    if (WHAT == MUON_APPLY) {
-      staging_release();
-      if (lane == 0) {
-        tma_store_3d(&a.tmOut0, c0, r0, mat, box0);
-        tma_store_3d(&a.tmOut1, c0, r0, mat, box1);
-        tma_store_commit();
-      }
-    } else {
-      staging_release();   // what was read here is overwritten by the next box's loads
-      if (r < a.M) {
-        const size_t at = ((size_t)mat * a.M + r) * a.N + c0;
-        const MuonFinish& f = a.fin;
-        if (f.vec) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (c0 + 8 * j < a.N) {
-              float* x = v + 8 * j;
-              if (f.W) {
-                const uint4 w = *reinterpret_cast<const uint4*>(f.W + at + 8 * j);
-                const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                  x[2 * p] = fmaf(f.keep, bf16lo(ww[p]), -f.rate * x[2 * p]);
-                  x[2 * p + 1] = fmaf(f.keep, bf16hi(ww[p]), -f.rate * x[2 * p + 1]);
-                }
-              }
-              *reinterpret_cast<uint4*>(f.out + at + 8 * j) =
-                  make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-            }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (c0 + i < a.N) {
-              float x = v[i];
-              if (f.W) x = fmaf(f.keep, __uint_as_float((uint32_t)f.W[at + i] << 16), -f.rate * x);
-              f.out[at + i] = (uint16_t)pack_bf16x2(x, 0.f);
-            }
-        }
-      }
-    }
-  }
+// Four 16-deep MMAs of a k-block; the operands' steps (16-byte units) follow how each lies.
+__device__ __forceinline__ void tc_mma4_pair_steps(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate,
+                                                   uint32_t a_step, uint32_t b_step) {
+  asm volatile(
+      "{\n .reg .pred e, p;\n .reg .b64 da, db;\n .reg .b32 a, b;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %5, 0;\n"
+      " mov.b64 da, {%1, %3};\n mov.b64 db, {%2, %3};\n"
+      " @e tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, p;\n"
+      " add.u32 a, %1, %6;\n add.u32 b, %2, %7;\n mov.b64 da, {a, %3};\n mov.b64 db, {b, %3};\n"
+      " @e tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, 1;\n"
+      " add.u32 a, a, %6;\n add.u32 b, b, %7;\n mov.b64 da, {a, %3};\n mov.b64 db, {b, %3};\n"
+      " @e tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, 1;\n"
+      " add.u32 a, a, %6;\n add.u32 b, b, %7;\n mov.b64 da, {a, %3};\n mov.b64 db, {b, %3};\n"
+      " @e tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, 1;\n}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(a_step), "r"(b_step)
+      : "memory");
 }
 
-template <int WHAT, bool A_MN, bool B_MN>
-__global__ void __launch_bounds__(MU_THREADS, 1) muon_product_kernel(const __grid_constant__ MuonProductArgs a) {
-  constexpr bool TRI = WHAT == MUON_GRAM || WHAT == MUON_POLY;
+// Whether the operands' k-block kb lies MN-major: X by its place in the product, a symmetric matrix beyond its stored blocks.
+template <bool WIDE>
+struct MuonMajors {
+  int a_from, b_from;   // first k-block that does
+  __device__ explicit MuonMajors(const MuonItem& it) {
+    constexpr int NEVER = INT_MAX, BKS = MUON_BLOCK / BK;
+    const int a_sym = it.m0 / BK + BKS, b_sym = it.n0 / BK + BKS;
+    if (it.phase == MUON_GRAM) {
+      a_from = b_from = WIDE ? NEVER : 0;
+    } else if (it.phase == MUON_POLY) {
+      a_from = a_sym;
+      b_from = b_sym;
+    } else {
+      a_from = WIDE ? a_sym : NEVER;
+      b_from = WIDE ? 0 : b_sym;
+    }
+  }
+};
+
+// Half a box of 32 rows x 64 columns of the accumulator: v, 32 columns of the lane's row; j0: its first chunk of eight.
+__device__ __forceinline__ void muon_box_gram(const MuonArgs::Step& k, float* v, uint8_t* box, int lane, int j0) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float* x = v + 8 * j;
+    *box_chunk(box, lane, j0 + j) = make_uint4(pack_h2(x[0] * k.gram_acc, x[1] * k.gram_acc), pack_h2(x[2] * k.gram_acc, x[3] * k.gram_acc),
+                                          pack_h2(x[4] * k.gram_acc, x[5] * k.gram_acc), pack_h2(x[6] * k.gram_acc, x[7] * k.gram_acc));
+  }
+}
+// diag: the column of v on the lane's diagonal, or none of 0 .. 31
+__device__ __forceinline__ void muon_box_poly(const MuonArgs::Step& k, float* v, uint8_t* box, int lane, int j0, int diag) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint4* p = box_chunk(box, lane, j0 + j);
+    const uint4 in = *p;
+    const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+    uint32_t o[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float2 y = unpack_h2(w[q]);
+      float x0 = fmaf(y.x, k.poly_in, v[8 * j + 2 * q] * k.poly_acc), x1 = fmaf(y.y, k.poly_in, v[8 * j + 2 * q + 1] * k.poly_acc);
+      if (diag == 8 * j + 2 * q) x0 += k.poly_diag;
+      if (diag == 8 * j + 2 * q + 1) x1 += k.poly_diag;
+      o[q] = pack_h2(x0, x1);
+    }
+    *p = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+}
+// X' (in v too) from X hi in box0 and, with LO, lo in box1; written back as hi and, with KEEP, lo
+template <bool LO, bool HI_OUT, bool LO_OUT>
+__device__ __forceinline__ void muon_box_apply(const MuonArgs::Step& k, float* v, uint8_t* box0, uint8_t* box1, int lane, int j0) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint4 *ph = box_chunk(box0, lane, j0 + j), *pl = box_chunk(box1, lane, j0 + j);
+    const uint4 xh = *ph;
+    const uint4 xl = LO ? *pl : make_uint4(0, 0, 0, 0);
+    const uint32_t wh[4] = {xh.x, xh.y, xh.z, xh.w}, wl[4] = {xl.x, xl.y, xl.z, xl.w};
+    uint32_t oh[4], ol[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float2 y = unpack_h2(wh[q]);
+      if (LO) {
+        const float2 yl = unpack_h2(wl[q]);
+        y.x = fmaf(yl.x, 1.f / MUON_SLO, y.x);
+        y.y = fmaf(yl.y, 1.f / MUON_SLO, y.y);
+      }
+      const float x0 = fmaf(y.x, k.app_in, v[8 * j + 2 * q] * k.app_acc), x1 = fmaf(y.y, k.app_in, v[8 * j + 2 * q + 1] * k.app_acc);
+      v[8 * j + 2 * q] = x0;
+      v[8 * j + 2 * q + 1] = x1;
+      if (HI_OUT) oh[q] = pack_h2(x0, x1);
+      if (LO_OUT) {
+        const float2 z = unpack_h2(oh[q]);
+        ol[q] = pack_h2((x0 - z.x) * MUON_SLO, (x1 - z.y) * MUON_SLO);
+      }
+    }
+    if (HI_OUT) *ph = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+    if (LO_OUT) *pl = make_uint4(ol[0], ol[1], ol[2], ol[3]);
+  }
+}
+// The last step's X' in v: bf16, or the weights' update, into box0; W is in box1, or with `lo` (runs of up to three steps) still in memory
+__device__ __forceinline__ void muon_box_out(const MuonArgs& a, float* v, uint8_t* box0, uint8_t* box1, int lane, int j0, bool lo, int mat, int r, int c0) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float* x = v + 8 * j;
+    if (a.w_ptr) {
+      uint4 w = make_uint4(0, 0, 0, 0);
+      const int c = c0 + 8 * (j0 + j);
+      if (!lo) w = *box_chunk(box1, lane, j0 + j);
+      else if (r < a.rows && c < a.cols) w = *reinterpret_cast<const uint4*>(a.w_ptr + ((size_t)mat * a.rows + r) * a.cols + c);
+      const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        x[2 * q] = fmaf(a.keep, bf16lo(ww[q]), -a.rate * x[2 * q]);
+        x[2 * q + 1] = fmaf(a.keep, bf16hi(ww[q]), -a.rate * x[2 * q + 1]);
+      }
+    }
+    *box_chunk(box0, lane, j0 + j) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+  }
+}
+// The same for rows that are no whole vectors, element by element
+__device__ __forceinline__ void muon_row_out(const MuonArgs& a, const float* v, int mat, int r, int c0) {
+  if (r >= a.rows) return;
+  const size_t at = ((size_t)mat * a.rows + r) * a.cols + c0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (c0 + i < a.cols) {
+      float x = v[i];
+      if (a.w_ptr) x = fmaf(a.keep, __uint_as_float((uint32_t)a.w_ptr[at + i] << 16), -a.rate * x);
+      a.out_ptr[at + i] = (uint16_t)pack_bf16x2(x, 0.f);
+    }
+}
+
+// A role's place in the ring of tickets
+struct MuonTickets {
+  uint32_t slot = 0, par = 0;
+  // all lanes: the next item; -1 after a failed wait
+  __device__ __forceinline__ int next(MuonBarriers* bars, const WaitCtl& wc, uint32_t sleep_ns) {
+    int t = -1;
+    if ((threadIdx.x & 31) == 0) {
+      if (mbar_wait_cluster(&bars->item_full[slot], par, wc, SITE_DEP, 0, sleep_ns)) t = *reinterpret_cast<volatile int*>(&bars->item[slot]);
+      mbar_arrive_cluster_addr(map_to_rank(smem_u32(&bars->item_empty[slot]), 0));
+    }
+    if (++slot == MU_SLOTS) { slot = 0; par ^= 1; }
+    return uniform(t);
+  }
+};
+
+template <bool WIDE>
+__global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __grid_constant__ MuonArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* boxes = smem + MU_STAGES * MU_STAGE_BYTES;
@@ -207,7 +259,6 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_product_kernel(const __gri
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();
-  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const WaitCtl wc{a.status, a.budget_ns};
 
   if (threadIdx.x == 0) {
@@ -217,14 +268,16 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_product_kernel(const __gri
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&bars->tmem_full[s], 1);
-      mbar_init(&bars->tmem_empty[s], 2 * MU_EPI_WARPS);
+      mbar_init(&bars->tmem_empty[s], MU_PARTS);
     }
     for (int w = 0; w < MU_EPI_WARPS; ++w) mbar_init(&bars->in_full[w], 1);
+    for (int s = 0; s < MU_SLOTS; ++s) {
+      mbar_init(&bars->item_full[s], 1);
+      mbar_init(&bars->item_empty[s], MU_READERS);
+    }
     mbar_init(&bars->drain, 1);
     mbar_fence_init();
     fence_proxy_async();
-    tma_prefetch_desc(&a.tmA);
-    tma_prefetch_desc(&a.tmB);
   }
   if (warp == 1) {
     tmem_alloc_pair(&bars->tmem_base, TMEM_COLS);
@@ -238,32 +291,67 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_product_kernel(const __gri
   pdl_trigger();
   pdl_wait();
 
-  const int per = muon_tiles<TRI>(a), total = a.n * per, nkb = (a.K + BK - 1) / BK;
-  const int half = a.nt / 2;   // columns of a tile that one CTA brings in
-  if (warp == 0) {
-    const int b_boxes = (half + 63) / 64;
-    const int bytes = 2 * (A_STAGE_BYTES + (B_MN ? b_boxes * MN_BOX_BYTES : half * BK * 2));
+  const MuonOrder order(a);
+  const int total = (int)order.total(a);
+  if (warp == 10) {
+    if (rank == 0 && lane == 0) {
+      uint32_t slot = 0, par = 1;
+      for (int t = 0; t < total;) {
+        if (!mbar_wait_cluster(&bars->item_empty[slot], par, wc, SITE_EMPTY, t, 50)) break;
+        t = atomicAdd(a.ctr + a.n, 1);
+        const uint32_t at = smem_u32(&bars->item[slot]), full = smem_u32(&bars->item_full[slot]);
+#pragma unroll
+        for (uint32_t r = 0; r < 2; ++r) {
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(at, r)), "r"(t) : "memory");
+          mbar_arrive_cluster_addr(map_to_rank(full, r));
+        }
+        if (++slot == MU_SLOTS) { slot = 0; par ^= 1; }
+      }
+    }
+  } else if (warp == 0) {
+    MuonTickets tk;
     uint32_t s = 0, par = (1u << MU_STAGES) - 1;
-    bool ok = true;
-    for (int t = pair; t < total && ok; t += npairs) {
-      const MuonTile tl = muon_decode<TRI>(a, per, t);
-      const int m0 = uniform(tl.m0 + rank * 128), n0 = uniform(tl.n0 + rank * half), mat = uniform(tl.mat);
+    for (bool ok = true; ok;) {
+      const int t = tk.next(bars, wc, 20);
+      if (t < 0 || t >= total) break;
+      const MuonItem it = order.decode(a, t);
+      const MuonMajors<WIDE> mj(it);
+      const int half = it.nt / 2, mat = uniform(it.mat), cur = it.step & 1;
+      const int m0 = uniform(it.m0 + rank * 128), n0 = uniform(it.n0 + rank * half);
+      const int K = it.phase == MUON_GRAM ? max(a.rows, a.cols) : min(a.rows, a.cols), nkb = uniform((K + BK - 1) / BK);
+      // K-major and MN-major maps of both operands
+      const CUtensorMap *a_k = &a.a128, *a_mn = &a.a64, *b_k = &a.a128, *b_mn = &a.a64;
+      if (it.phase == MUON_GRAM) {
+        a_k = b_k = &a.x128[cur];
+        a_mn = b_mn = &a.x64[cur];
+      } else if (it.phase == MUON_APPLY) {
+        a_k = WIDE ? &a.b128 : &a.x128[cur];
+        a_mn = &a.b64;
+        b_k = &a.b128;
+        b_mn = WIDE ? &a.x64[cur] : &a.b64;
+      }
+      int up = 1;
+      if (it.need && lane == 0) up = counter_wait(a.ctr + mat, it.need, wc, t, 256) ? 1 : 0;
+      if (!uniform(up)) break;
+      fence_proxy_async_global();   // what the counter announces was written by other CTAs' stores
+      const int b_boxes = (half + 63) / 64;
       for (int kb = 0; kb < nkb; ++kb) {
         if (!mbar_wait_warp(&bars->empty[s], (par >> s) & 1, wc, SITE_EMPTY, t, 20)) { ok = false; break; }
         uint8_t* st = smem + s * MU_STAGE_BYTES;
-        if (rank == 0) mbar_expect_tx_elect(&bars->full[s], bytes);
-        if (A_MN) {
-          tma_load_3d_pair(st, &a.tmA, m0, kb * BK, mat, &bars->full[s]);
-          tma_load_3d_pair(st + MN_BOX_BYTES, &a.tmA, m0 + 64, kb * BK, mat, &bars->full[s]);
+        const bool amn = kb >= mj.a_from, bmn = kb >= mj.b_from;
+        if (rank == 0) mbar_expect_tx_elect(&bars->full[s], 2 * (A_STAGE_BYTES + (bmn ? b_boxes * MN_BOX_BYTES : HALF_B_BYTES)));
+        if (amn) {
+          tma_load_3d_pair(st, a_mn, m0, kb * BK, mat, &bars->full[s]);
+          tma_load_3d_pair(st + MN_BOX_BYTES, a_mn, m0 + 64, kb * BK, mat, &bars->full[s]);
         } else {
-          tma_load_3d_pair(st, &a.tmA, kb * BK, m0, mat, &bars->full[s]);
+          tma_load_3d_pair(st, a_k, kb * BK, m0, mat, &bars->full[s]);
         }
         uint8_t* sb = st + A_STAGE_BYTES;
-        if (B_MN) {
-          tma_load_3d_pair(sb, &a.tmB, n0, kb * BK, mat, &bars->full[s]);
-          if (b_boxes > 1) tma_load_3d_pair(sb + MN_BOX_BYTES, &a.tmB, n0 + 64, kb * BK, mat, &bars->full[s]);
+        if (bmn) {
+          tma_load_3d_pair(sb, b_mn, n0, kb * BK, mat, &bars->full[s]);
+          if (b_boxes > 1) tma_load_3d_pair(sb + MN_BOX_BYTES, b_mn, n0 + 64, kb * BK, mat, &bars->full[s]);
         } else {
-          tma_load_3d_pair(sb, &a.tmB, kb * BK, n0, mat, &bars->full[s]);
+          tma_load_3d_pair(sb, b_k, kb * BK, n0, mat, &bars->full[s]);
         }
         par ^= 1u << s;
         if (++s == MU_STAGES) s = 0;
@@ -271,13 +359,20 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_product_kernel(const __gri
     }
   } else if (warp == 1) {
     if (rank == 0) {
-      const uint32_t idesc = make_idesc_f16(256, a.nt, A_MN, B_MN);
-      constexpr int ASTEP = A_MN ? 2048 >> 4 : 2, BSTEP = B_MN ? 2048 >> 4 : 2;
-      const uint32_t a_lo0 = smem_desc_lo(smem_u32(smem), A_MN ? MN_BOX_BYTES : 16);
-      const uint32_t b_lo0 = smem_desc_lo(smem_u32(smem + A_STAGE_BYTES), B_MN ? MN_BOX_BYTES : 16);
+      MuonTickets tk;
+      const uint32_t at0 = smem_u32(smem), bt0 = smem_u32(smem + A_STAGE_BYTES);
+      const uint32_t a_lo0[2] = {smem_desc_lo(at0, 16), smem_desc_lo(at0, MN_BOX_BYTES)}, b_lo0[2] = {smem_desc_lo(bt0, 16), smem_desc_lo(bt0, MN_BOX_BYTES)};
       uint32_t s = 0, par = 0, acc = 0, acc_par = 3;
       bool ok = true;
-      for (int t = pair; t < total && ok; t += npairs) {
+      for (;;) {
+        const int t = tk.next(bars, wc, 0);
+        if (t < 0) ok = false;
+        if (t < 0 || t >= total) break;
+        const MuonItem it = order.decode(a, t);
+        const MuonMajors<WIDE> mj(it);
+        const int K = it.phase == MUON_GRAM ? max(a.rows, a.cols) : min(a.rows, a.cols), nkb = uniform((K + BK - 1) / BK);
+        const uint32_t idesc = uniform(make_idesc_f16(256, it.nt, 0, 0));
+        const int a_from = uniform(mj.a_from), b_from = uniform(mj.b_from);
         if (!mbar_wait_warp(&bars->tmem_empty[acc], (acc_par >> acc) & 1, wc, SITE_TMEM_EMPTY, t)) { ok = false; break; }
         acc_par ^= 1u << acc;
         tc_fence_after_sync();
@@ -286,8 +381,9 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_product_kernel(const __gri
           if (!mbar_wait_warp(&bars->full[s], (par >> s) & 1, wc, SITE_FULL, t)) { ok = false; break; }
           par ^= 1u << s;
           tc_fence_after_sync();
-          const uint32_t at = s * (MU_STAGE_BYTES >> 4);
-          tc_mma4_bf16_pair<ASTEP, BSTEP>(d_tmem, a_lo0 + at, b_lo0 + at, smem_desc_hi(1024), idesc, kb != 0);
+          const uint32_t at = s * (MU_STAGE_BYTES >> 4), amn = kb >= a_from, bmn = kb >= b_from;
+          tc_mma4_pair_steps(d_tmem, (amn ? a_lo0[1] : a_lo0[0]) + at, (bmn ? b_lo0[1] : b_lo0[0]) + at, smem_desc_hi(1024),
+                             idesc | amn << 15 | bmn << 16, kb != 0, amn ? 2048 >> 4 : 2, bmn ? 2048 >> 4 : 2);
           tc_commit_pair(&bars->empty[s]);
           if (++s == MU_STAGES) s = 0;
         }
@@ -302,44 +398,98 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_product_kernel(const __gri
       }
     }
   } else {
+    MuonTickets tk;
     const int ew = warp - 2, quad = warp & 3;
     uint8_t* box0 = boxes + ew * 2 * MU_BOX;
     uint8_t* box1 = box0 + MU_BOX;
+    uint64_t* in_full = &bars->in_full[ew];
     uint32_t acc = 0, full_par = 0, in_par = 0;
-    bool ok = true;
-    for (int t = pair; t < total && ok; t += npairs) {
-      const MuonTile tl = muon_decode<TRI>(a, per, t);
-      const int r0 = tl.m0 + rank * 128 + quad * 32;
+    for (bool ok = true; ok;) {
+      const int t = tk.next(bars, wc, 100);
+      if (t < 0 || t >= total) break;
+      const MuonItem it = order.decode(a, t);
+      const MuonArgs::Step& k = a.step[it.step];
+      const int m = min(a.rows, a.cols), cur = it.step & 1;
+      const int M = it.phase == MUON_APPLY ? a.rows : m, N = it.phase == MUON_APPLY ? a.cols : m;
+      const bool last = it.phase == MUON_APPLY && it.step + 1 == a.steps;
+      const bool lo = it.phase == MUON_APPLY && it.step < MUON_LATE, lo_out = it.phase == MUON_APPLY && !last && it.step + 1 < MUON_LATE;
+      const bool upd = last && !lo && a.vec && a.w_ptr;   // W comes with X
+      const int r0 = it.m0 + rank * 128 + quad * 32;
       bool up = false;   // the accumulator has been seen complete
-      for (int b = (ew >> 2) * 64; b < a.nt && ok; b += 128) {
-        const int c0 = tl.n0 + b;
-        if (r0 >= a.M || c0 >= a.N || (TRI && c0 > r0 + 31)) break;
+      for (int b = (ew >> 2) * 64; b < it.nt; b += 128) {
+        const int c0 = it.n0 + b;
+        if (r0 >= M || c0 >= N) break;
         __syncwarp();   // every lane has read the boxes
-        if (lane == 0) {
-          tma_store_wait_read();
-          if (WHAT != MUON_GRAM) {
-            mbar_expect_tx(&bars->in_full[ew], WHAT == MUON_POLY ? MU_BOX : 2 * MU_BOX);
-            tma_load_3d_thread(box0, &a.tmIn0, c0, r0, tl.mat, &bars->in_full[ew]);
-            if (WHAT != MUON_POLY) tma_load_3d_thread(box1, &a.tmIn1, c0, r0, tl.mat, &bars->in_full[ew]);
+        if (it.phase != MUON_GRAM) {
+          int there = 1;
+          if (lane == 0) {
+            if (!up) there = counter_wait(a.ctr + it.mat, it.need, wc, t, 256) ? 1 : 0;
+            tma_store_wait_read();
+            if (there) {
+              fence_proxy_async_global();
+              mbar_expect_tx(in_full, lo || upd ? 2 * MU_BOX : MU_BOX);
+              tma_load_3d_thread(box0, it.phase == MUON_POLY ? &a.abox : &a.xhi[cur], c0, r0, it.mat, in_full);
+              if (lo) tma_load_3d_thread(box1, &a.xlo[cur], c0, r0, it.mat, in_full);
+              else if (upd) tma_load_3d_thread(box1, &a.w, c0, r0, a.z0 + it.mat, in_full);
+            }
           }
+          if (!uniform(there)) { ok = false; break; }
+        } else {
+          if (lane == 0) tma_store_wait_read();
+          __syncwarp();
         }
-        __syncwarp();
         if (!up) {
-          ok = mbar_wait_warp(&bars->tmem_full[acc], (full_par >> acc) & 1, wc, SITE_TMEM_FULL, t, 100);
+          if (!mbar_wait_warp(&bars->tmem_full[acc], (full_par >> acc) & 1, wc, SITE_TMEM_FULL, t, 100)) ok = false;
           tc_fence_after_sync();
           up = true;
         }
-        if (WHAT != MUON_GRAM) {
-          ok = mbar_wait_warp(&bars->in_full[ew], in_par, wc, SITE_DEP, t) && ok;
+        if (it.phase != MUON_GRAM) {
+          if (!mbar_wait_warp(in_full, in_par, wc, SITE_FULL, t)) ok = false;
           in_par ^= 1;
         }
         if (!ok) break;
-        muon_epilogue_box<WHAT>(a, tmem_base + acc * 256 + b + (static_cast<uint32_t>(quad * 32) << 16), box0, box1, tl.mat, r0, c0, lane);
+        const uint32_t tcol = tmem_base + acc * 256 + b + (static_cast<uint32_t>(quad * 32) << 16);
+#pragma unroll 1
+        for (int j0 = 0; j0 < 8; j0 += 4) {
+          float v[32];
+          tmem_ld16(tcol + 8 * j0, v);
+          tmem_ld16(tcol + 8 * j0 + 16, v + 16);
+          tmem_ld_wait();
+          if (it.phase == MUON_GRAM) {
+            muon_box_gram(k, v, box0, lane, j0);
+          } else if (it.phase == MUON_POLY) {
+            muon_box_poly(k, v, box0, lane, j0, r0 + lane - c0 - 8 * j0);
+          } else if (!last) {
+            if (lo_out) muon_box_apply<true, true, true>(k, v, box0, box1, lane, j0);
+            else if (lo) muon_box_apply<true, true, false>(k, v, box0, box1, lane, j0);
+            else muon_box_apply<false, true, false>(k, v, box0, box1, lane, j0);
+          } else {
+            if (lo) muon_box_apply<true, false, false>(k, v, box0, box1, lane, j0);
+            else muon_box_apply<false, false, false>(k, v, box0, box1, lane, j0);
+            if (a.vec) muon_box_out(a, v, box0, box1, lane, j0, lo, it.mat, r0 + lane, c0);
+            else muon_row_out(a, v, it.mat, r0 + lane, c0 + 8 * j0);
+          }
+        }
+        if (last && !a.vec) continue;
+        staging_release();
+        if (lane == 0) {
+          const CUtensorMap* o = it.phase == MUON_GRAM ? &a.abox : it.phase == MUON_POLY ? &a.bbox : last ? &a.out : &a.xhi[cur ^ 1];
+          tma_store_3d(o, c0, r0, last ? a.z0 + it.mat : it.mat, box0);
+          if (lo_out) tma_store_3d(&a.xlo[cur ^ 1], c0, r0, it.mat, box1);
+          tma_store_commit();
+        }
       }
-      if (!up && ok) ok = mbar_wait_warp(&bars->tmem_full[acc], (full_par >> acc) & 1, wc, SITE_TMEM_FULL, t, 100);
+      if (!up && ok && !mbar_wait_warp(&bars->tmem_full[acc], (full_par >> acc) & 1, wc, SITE_TMEM_FULL, t, 100)) ok = false;
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive_leader(&bars->tmem_empty[acc]);
+      if (lane == 0) {
+        mbar_arrive_leader(&bars->tmem_empty[acc]);
+        if (!last && ok) {   // this warp's part of the tile is stored
+          tma_store_wait_all();
+          fence_proxy_async_global();
+          counter_signal(a.ctr + it.mat, 1);
+        }
+      }
       full_par ^= 1u << acc;
       acc ^= 1;
     }
@@ -357,22 +507,12 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_product_kernel(const __gri
   }
 }
 
-template <int WHAT, bool A_MN, bool B_MN>
-static cudaError_t launch_one(const MuonProductArgs& a, int num_sms, cudaStream_t s) {
-  static PairLaunchState st;
-  const int tiles = a.n * muon_tiles<WHAT == MUON_GRAM || WHAT == MUON_POLY>(a);
-  const int sms = 2 * tiles < num_sms ? 2 * tiles : num_sms;
-  return launch_on_pairs(st, muon_product_kernel<WHAT, A_MN, B_MN>, a, MU_THREADS, MU_SMEM, sms, s, true);
-}
-
-cudaError_t launch_muon_product(MuonProduct what, bool a_mn, bool b_mn, const MuonProductArgs& a, int num_sms, cudaStream_t s) {
-  switch (what) {
-    case MUON_GRAM: return a_mn ? launch_one<MUON_GRAM, true, true>(a, num_sms, s) : launch_one<MUON_GRAM, false, false>(a, num_sms, s);
-    case MUON_POLY: return launch_one<MUON_POLY, false, false>(a, num_sms, s);
-    case MUON_APPLY: return b_mn ? launch_one<MUON_APPLY, false, true>(a, num_sms, s) : launch_one<MUON_APPLY, false, false>(a, num_sms, s);
-    case MUON_LAST: return b_mn ? launch_one<MUON_LAST, false, true>(a, num_sms, s) : launch_one<MUON_LAST, false, false>(a, num_sms, s);
-  }
-  return cudaErrorInvalidValue;
+cudaError_t launch_muon_products(bool wide, const MuonArgs& a, int num_sms, cudaStream_t s) {
+  static PairLaunchState st[2];
+  const long tiles = MuonOrder(a).total(a);
+  const int sms = (int)(2 * tiles < num_sms ? 2 * tiles : num_sms);
+  return wide ? launch_on_pairs(st[1], muon_products_kernel<true>, a, MU_THREADS, MU_SMEM, sms, s, true)
+              : launch_on_pairs(st[0], muon_products_kernel<false>, a, MU_THREADS, MU_SMEM, sms, s, true);
 }
 
 }  // namespace moe

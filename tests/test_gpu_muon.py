@@ -187,7 +187,7 @@ def test_more_matrices_than_the_workspace_holds():
     room = torch.full((n * rows * cols + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
     out = room[:n * rows * cols].view(n, rows, cols)
     muon.orthogonalize(G, out=out)
-    assert muon.launches() > 17 and bool((room[-64:] == 7).all())
+    assert muon.launches() > 3 and bool((room[-64:] == 7).all())
     one = MoeMuon(1, rows, cols)
     for i in (0, 33, 34, 46, 47, 69):
         assert torch.equal(_bits(out[i]), _bits(one.orthogonalize(G[i:i + 1])[0])), i
