@@ -228,7 +228,8 @@ def load_library() -> ctypes.CDLL:
     if _fast is not None:
         _fast.setup(*(ctypes.cast(getattr(lib, f), vp).value for f in (
             "moe_route", "moe_router_fwd", "moe_router_bwd", "moe_layout_noalloc", "moe_ffn_fwd", "moe_ffn_bwd",
-            "moe_balance_fwd", "moe_balance_bwd", "moe_ffn_fwd_w4")))
+            "moe_balance_fwd", "moe_balance_bwd", "moe_ffn_fwd_w4", "moe_route_grouped", "moe_route_grouped_bwd", "moe_bias_update",
+            "moe_muon_orthogonalize", "moe_muon_step")))
     _lib = lib
     return lib
 
@@ -552,11 +553,15 @@ def moe_muon_create(shape, workspace=None):
     _check(load_library().moe_muon_create(ctypes.byref(h), ctypes.byref(shape), ctypes.c_void_p(workspace.data_ptr()) if workspace is not None else None,
                                           workspace.numel() if workspace is not None else 0), "moe_muon_create")
     _MUON_ELEMS[h.value] = shape.n * shape.rows * shape.cols
+    if _fast is not None:
+        _fast.add_muon(h, _MUON_ELEMS[h.value])
     return h
 
 
 def moe_muon_destroy(muon):
     _check(load_library().moe_muon_destroy(muon), "moe_muon_destroy")
+    if _fast is not None:
+        _fast.drop_muon(muon)
     _MUON_ELEMS.pop(getattr(muon, "value", None), None)
 
 
@@ -567,16 +572,32 @@ def _elems_of(muon):
         raise MoeError("unknown muon handle (not created by moe_muon_create, or already destroyed)") from None
 
 
-@_sizes_first
 def moe_muon_orthogonalize(muon, G, out):
+    rc = _fast.muon_orthogonalize(muon, G, out) if _fast is not None else None
+    if rc is None:
+        _moe_muon_orthogonalize(muon, G, out)
+    elif rc:
+        _check(rc, "moe_muon_orthogonalize")
+
+
+@_sizes_first
+def _moe_muon_orthogonalize(muon, G, out):
     n = _elems_of(muon)
     fp32 = G.dtype is _F32
     _check(load_library().moe_muon_orthogonalize(muon, _here(G, _F32 if fp32 else _BF, "G", n), MOE_MUON_FP32 if fp32 else MOE_MUON_BF16,
                                                  _here(out, _BF, "out", n), _stream()), "moe_muon_orthogonalize")
 
 
-@_sizes_first
 def moe_muon_step(muon, W, M, dW, momentum, nesterov, lr, weight_decay, scale, W_out, M_out):
+    rc = _fast.muon_step(muon, W, M, dW, momentum, nesterov, lr, weight_decay, scale, W_out, M_out) if _fast is not None else None
+    if rc is None:
+        _moe_muon_step(muon, W, M, dW, momentum, nesterov, lr, weight_decay, scale, W_out, M_out)
+    elif rc:
+        _check(rc, "moe_muon_step")
+
+
+@_sizes_first
+def _moe_muon_step(muon, W, M, dW, momentum, nesterov, lr, weight_decay, scale, W_out, M_out):
     n = _elems_of(muon)
     _check(load_library().moe_muon_step(muon, _here(W, _BF, "W", n), _here(M, _F32, "M", n), _here(dW, _BF, "dW", n), float(momentum),
                                         int(bool(nesterov)), float(lr), float(weight_decay), float(scale), _here(W_out, _BF, "W_out", n),
@@ -1155,6 +1176,12 @@ class MoeLayer:
 
     def route_grouped(self, logits, bias=None, n_groups=1, top_groups=1, group_top=1, scale=1.0, with_counts=False):
         """-> ids, weights (and counts [E]): the best experts of the best groups by score + bias, weighted by their scores"""
+        if _fast is not None:
+            r = _fast.route_grouped_new(self.ctx, logits, bias, n_groups, top_groups, group_top, scale, with_counts)
+            if r is not None:
+                if r[0]:
+                    _check(r[0], "moe_route_grouped")
+                return r[1:]
         T, dev = logits.shape[0], logits.device
         ids, w = torch.empty(T, self.k, dtype=_I32, device=dev), torch.empty(T, self.k, dtype=_F32, device=dev)
         counts = torch.empty(self.E, dtype=_I32, device=dev) if with_counts else None
@@ -1163,6 +1190,12 @@ class MoeLayer:
 
     def route_grouped_bwd(self, logits, topk_ids, d_topk_w, scale=1.0, d_logits=None, accumulate=False):
         """Gradient of route_grouped's weights; added to d_logits with accumulate."""
+        if d_logits is None and not accumulate and _fast is not None:
+            r = _fast.route_grouped_bwd_new(self.ctx, logits, topk_ids, d_topk_w, scale)
+            if r is not None:
+                if r[0]:
+                    _check(r[0], "moe_route_grouped_bwd")
+                return r[1]
         if d_logits is None:
             if accumulate:
                 raise MoeError("d_logits: accumulate needs a tensor to add to")
@@ -1173,6 +1206,11 @@ class MoeLayer:
     def bias_update(self, bias, counts, rate, out=None):
         """bias + rate * sign(mean count - count), in place unless `out` is given; counts [E] or [n_seq][E]"""
         out = bias if out is None else out
+        rc = _fast.bias_update(self.ctx, bias, counts, rate, out) if _fast is not None else None
+        if rc is not None:
+            if rc:
+                _check(rc, "moe_bias_update")
+            return out
         moe_bias_update(self.ctx, bias, counts, counts.shape[0] if counts.dim() > 1 else 1, rate, out)
         return out
 

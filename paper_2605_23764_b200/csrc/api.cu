@@ -1257,6 +1257,7 @@ int moe_route_grouped(moe_ctx* c, const float* logits, const float* bias, int32_
   a.logits = logits; a.bias = bias;
   a.T = T; a.E = c->shape.E; a.k = c->shape.k; a.mode = gate_mode(c);
   a.n_groups = groups->n_groups; a.top_groups = groups->top_groups; a.group_top = groups->group_top; a.scale = groups->scale;
+  a.vec = c->shape.E % 4 == 0 && aligned16(logits);
   a.topk_ids = topk_ids; a.topk_w = topk_w; a.counts = counts;
   Phase ph(c, MOE_PHASE_ROUTE, c->last_stream);
   MOE_CUDA(launch_route_groups(a, c->num_sms, c->last_stream, &c->launches));

@@ -36,6 +36,12 @@ int (*f_ffn_bwd)(P, const P, const P, const P, const P, const P, const P, P, P, 
 decltype(&moe_balance_fwd) f_balance_fwd;
 decltype(&moe_balance_bwd) f_balance_bwd;
 decltype(&moe_ffn_fwd_w4) f_ffn_fwd_w4;
+decltype(&moe_route_grouped) f_route_grouped;
+decltype(&moe_route_grouped_bwd) f_route_grouped_bwd;
+decltype(&moe_bias_update) f_bias_update;
+decltype(&moe_muon_orthogonalize) f_muon_orthogonalize;
+decltype(&moe_muon_step) f_muon_step;
+std::unordered_map<void*, int64_t> g_muons;   // elements of a handle's matrices; under the GIL
 
 struct Slow {};   // not for this path
 
@@ -49,6 +55,16 @@ void* check(const at::Tensor& t, at::ScalarType type, int64_t n) {
 }
 void* dev(PyObject* o, at::ScalarType type, int64_t n) { return check(tensor(o), type, n); }
 void* dev_or_null(PyObject* o, at::ScalarType type, int64_t n) { return o == Py_None ? nullptr : dev(o, type, n); }
+float real(PyObject* o) {
+  if (PyFloat_CheckExact(o)) return (float)PyFloat_AS_DOUBLE(o);
+  if (!PyLong_CheckExact(o)) throw Slow();
+  const double v = PyLong_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) {
+    PyErr_Clear();
+    throw Slow();
+  }
+  return (float)v;
+}
 int64_t integer(PyObject* o) {
   if (!PyLong_CheckExact(o)) throw Slow();
   int over = 0;
@@ -102,9 +118,9 @@ PyObject* guarded(F body) {
 void want(Py_ssize_t n, Py_ssize_t need) { if (n != need) throw Slow(); }
 
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 9) { PyErr_SetString(PyExc_TypeError, "setup: nine addresses"); return nullptr; }
-  void* p[9];
-  for (int i = 0; i < 9; ++i) {
+  if (n != 14) { PyErr_SetString(PyExc_TypeError, "setup: fourteen addresses"); return nullptr; }
+  void* p[14];
+  for (int i = 0; i < 14; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "setup: null address");
@@ -120,6 +136,11 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
   f_balance_fwd = reinterpret_cast<decltype(f_balance_fwd)>(p[6]);
   f_balance_bwd = reinterpret_cast<decltype(f_balance_bwd)>(p[7]);
   f_ffn_fwd_w4 = reinterpret_cast<decltype(f_ffn_fwd_w4)>(p[8]);
+  f_route_grouped = reinterpret_cast<decltype(f_route_grouped)>(p[9]);
+  f_route_grouped_bwd = reinterpret_cast<decltype(f_route_grouped_bwd)>(p[10]);
+  f_bias_update = reinterpret_cast<decltype(f_bias_update)>(p[11]);
+  f_muon_orthogonalize = reinterpret_cast<decltype(f_muon_orthogonalize)>(p[12]);
+  f_muon_step = reinterpret_cast<decltype(f_muon_step)>(p[13]);
   Py_RETURN_NONE;
 }
 PyObject* add(PyObject*, PyObject* const* a, Py_ssize_t n) {   // handle, T_max, d, E, k, S, F
@@ -328,10 +349,115 @@ PyObject* ffn_fwd_w4_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ctx, logits, bias, n_groups, top_groups, group_top, scale, with counts -> (code, ids, w) or (code, ids, w, counts)
+PyObject* route_grouped_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    want(n, 8);
+    moe_ctx* c = static_cast<moe_ctx*>(handle(a[0]));
+    const Shape& s = shape_of(c);
+    const at::Tensor& l = tensor(a[1]);
+    const int64_t T = rows_of(l);
+    const float *logits = here<float>(a[1], F32, T * s.E), *bias = here_or_null<float>(a[2], F32, s.E);
+    const moe_route_groups g{(int32_t)integer(a[3]), (int32_t)integer(a[4]), (int32_t)integer(a[5]), real(a[6])};
+    const bool with_counts = a[7] == Py_True;
+    at::Tensor ids = empty({T, s.k}, I32, l), w = empty({T, s.k}, F32, l), counts;
+    if (with_counts) counts = empty({s.E}, I32, l);
+    int32_t *pi = ids.data_ptr<int32_t>(), *pc = with_counts ? counts.data_ptr<int32_t>() : nullptr;
+    float* pw = w.data_ptr<float>();
+    void* st = stream();
+    const int rc = unlocked([&] { return f_route_grouped(c, logits, bias, (int32_t)T, &g, pi, pw, pc, st); });
+    if (with_counts) return Py_BuildValue("(iNNN)", rc, THPVariable_Wrap(ids), THPVariable_Wrap(w), THPVariable_Wrap(counts));
+    return Py_BuildValue("(iNN)", rc, THPVariable_Wrap(ids), THPVariable_Wrap(w));
+  });
+}
+PyObject* route_grouped_bwd_new(PyObject*, PyObject* const* a, Py_ssize_t n) {   // ctx, logits, ids, d_w, scale -> (code, d_logits)
+  return guarded([&]() -> PyObject* {
+    want(n, 5);
+    moe_ctx* c = static_cast<moe_ctx*>(handle(a[0]));
+    const Shape& s = shape_of(c);
+    const at::Tensor& l = tensor(a[1]);
+    const int64_t T = rows_of(l);
+    const float *logits = here<float>(a[1], F32, T * s.E), *dw = here<float>(a[3], F32, T * s.k), scale = real(a[4]);
+    const int32_t* ids = here<int32_t>(a[2], I32, T * s.k);
+    at::Tensor out = empty({T, s.E}, F32, l);
+    float* po = out.data_ptr<float>();
+    void* st = stream();
+    const int rc = unlocked([&] { return f_route_grouped_bwd(c, logits, ids, dw, (int32_t)T, scale, 0, po, st); });
+    return Py_BuildValue("(iN)", rc, THPVariable_Wrap(out));
+  });
+}
+PyObject* bias_update(PyObject*, PyObject* const* a, Py_ssize_t n) {   // ctx, bias, counts, rate, out
+  return guarded([&]() -> PyObject* {
+    want(n, 5);
+    moe_ctx* c = static_cast<moe_ctx*>(handle(a[0]));
+    const Shape& s = shape_of(c);
+    const at::Tensor& ct = tensor(a[2]);
+    const int64_t ns = ct.dim() > 1 ? ct.size(0) : 1;
+    if (ns < 1 || ns > INT32_MAX) throw Slow();
+    const float *bias = here<float>(a[1], F32, s.E), rate = real(a[3]);
+    const int32_t* counts = here<int32_t>(a[2], I32, ns * s.E);
+    float* out = here<float>(a[4], F32, s.E);
+    void* st = stream();
+    return PyLong_FromLong(unlocked([&] { return f_bias_update(c, bias, counts, (int32_t)ns, rate, out, st); }));
+  });
+}
+PyObject* add_muon(PyObject*, PyObject* const* a, Py_ssize_t n) {   // handle, elements
+  return guarded([&]() -> PyObject* {
+    want(n, 2);
+    const long long elems = PyLong_AsLongLong(a[1]);
+    if (elems < 0) {
+      PyErr_Clear();
+      throw Slow();
+    }
+    g_muons[handle(a[0])] = elems;
+    Py_RETURN_NONE;
+  });
+}
+PyObject* drop_muon(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    want(n, 1);
+    g_muons.erase(handle(a[0]));
+    Py_RETURN_NONE;
+  });
+}
+int64_t elems_of(void* h) {
+  const auto it = g_muons.find(h);
+  if (it == g_muons.end()) throw Slow();
+  return it->second;
+}
+PyObject* muon_orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t n) {   // handle, G, out
+  return guarded([&]() -> PyObject* {
+    want(n, 3);
+    moe_muon* m = static_cast<moe_muon*>(handle(a[0]));
+    const int64_t ne = elems_of(m);
+    const bool fp32 = tensor(a[1]).scalar_type() == F32;
+    const void* G = fp32 ? static_cast<const void*>(here<float>(a[1], F32, ne)) : here<uint16_t>(a[1], BF, ne);
+    uint16_t* out = here<uint16_t>(a[2], BF, ne);
+    void* st = stream();
+    return PyLong_FromLong(unlocked([&] { return f_muon_orthogonalize(m, G, fp32 ? MOE_MUON_FP32 : MOE_MUON_BF16, out, st); }));
+  });
+}
+// handle, W, M, dW, momentum, nesterov, lr, weight_decay, scale, W_out, M_out
+PyObject* muon_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    want(n, 11);
+    moe_muon* m = static_cast<moe_muon*>(handle(a[0]));
+    const int64_t ne = elems_of(m);
+    const uint16_t *W = here<uint16_t>(a[1], BF, ne), *dW = here<uint16_t>(a[3], BF, ne);
+    const float *M = here<float>(a[2], F32, ne), mu = real(a[4]), lr = real(a[6]), wd = real(a[7]), scale = real(a[8]);
+    const bool nesterov = a[5] == Py_True;
+    uint16_t* Wo = here<uint16_t>(a[9], BF, ne);
+    float* Mo = here<float>(a[10], F32, ne);
+    void* st = stream();
+    return PyLong_FromLong(unlocked([&] { return f_muon_step(m, W, M, dW, mu, nesterov, lr, wd, scale, Wo, Mo, st); }));
+  });
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(setup), FAST(add), FAST(drop), FAST(route), FAST(route_new), FAST(router_fwd), FAST(router_bwd),
                          FAST(layout_noalloc), FAST(ffn_fwd), FAST(ffn_fwd_new), FAST(ffn_bwd), FAST(balance_fwd_new),
-                         FAST(balance_bwd_new), FAST(ffn_fwd_w4_new), {nullptr, nullptr, 0, nullptr}};
+                         FAST(balance_bwd_new), FAST(ffn_fwd_w4_new), FAST(route_grouped_new), FAST(route_grouped_bwd_new),
+                         FAST(bias_update), FAST(add_muon), FAST(drop_muon), FAST(muon_orthogonalize), FAST(muon_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

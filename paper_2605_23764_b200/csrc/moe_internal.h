@@ -248,6 +248,7 @@ struct RouteGroupsArgs {
   int T, E, k, mode;        // mode: GATE_RENORM | GATE_SIGMOID
   int n_groups, top_groups, group_top;
   float scale;
+  int vec;                  // the logits' rows are whole 16-byte vectors
   int* topk_ids;            // [T][k]
   float* topk_w;            // [T][k]
   int* counts;              // [E]; may be NULL
