@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libmoe_b200.so")
 OBJ = os.path.join(PKG, "_build")
 SOURCES = ["api.cu", "route_layout.cu", "permute.cu", "gemm_tc3.cu", "gemm_wgrad.cu", "fused.cu", "study.cu", "router.cu", "taskflow.cu", "ep.cu", "balance.cu",
-           "w4_codes.cu", "w4_vec.cu", "w4_tile.cu", "route_groups.cu", "muon.cu", "muon_gemm.cu"]
+           "w4_codes.cu", "w4_vec.cu", "w4_tile.cu", "route_groups.cu", "muon.cu", "muon_gemm.cu", "muon_small.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

@@ -944,18 +944,24 @@ bool muon_shape_ok(const moe_muon_shape* s) {
 
 MuonPlan plan_muon(const moe_muon_shape& s) {
   MuonPlan p;
+  memset(&p, 0, sizeof p);
   p.m = std::min(s.rows, s.cols);
   p.l = std::max(s.rows, s.cols);
   p.ld = row_ld(s.cols);
   p.ldm = row_ld(p.m);
   const size_t x = sizeof(uint16_t) * (size_t)s.rows * p.ld, a = sizeof(uint16_t) * (size_t)p.m * p.ldm;
-  const long parts = muon_parts((long)s.rows * s.cols);
+  const long parts = muon_parts((long)s.rows * s.cols, false);
   const size_t each = 4 * x + 2 * a;
   const size_t most = std::max<size_t>(1, MUON_BATCH_BYTES / each);
   const size_t turns = ((size_t)s.n + most - 1) / most;
   p.batch = (int)(((size_t)s.n + turns - 1) / turns);
   Carve c;
   c.take(sizeof(DevStatus));
+  if (muon_is_small(s.rows, s.cols)) {
+    p.batch = s.n;
+    p.total = c.off;
+    return p;
+  }
   p.ctr = c.take(sizeof(int) * (p.batch + 1));
   p.part = c.take(sizeof(double) * p.batch * parts);
   for (int i = 0; i < 2; ++i) {
@@ -994,17 +1000,31 @@ int encode_batch(CUtensorMap* tm, const void* base, uint64_t n, uint64_t rows, u
   return encode_tiled(tm, base, 3, dims, strides, box);
 }
 
-// Columns of an APPLY tile: the fewest padded columns, narrower tiles charged for the operand bytes that they bring in for a product;
-// X B of tall matrices takes B by its blocks.
-int muon_tile_cols(const moe_muon_shape& s) {
-  static const int width[3] = {256, 192, 128}, charge[3] = {100, 105, 115};
-  int best = MUON_BLOCK;
-  long least = -1;
-  for (int i = 0; i < 3 && s.rows <= s.cols; ++i) {
-    const long c = (long)((s.cols + width[i] - 1) / width[i]) * width[i] * charge[i];
-    if (least < 0 || c < least) { least = c; best = width[i]; }
+// Tile columns: the width whose turns over the pairs of SMs are over first.  A k-block takes what its operands' bytes take at 56 a clock (32 KB
+// with 256 columns, 20 KB with 64), a turn the epilogue's boxes on top.  So a batch with many tiles has wide ones, a single matrix
+// narrow ones as long as every pair has one: 256 x 7168 290 -> 232 us, 1408 x 2048 267 us, 392 with the narrowest, TODO with 128.
+// Wide matrices' APPLY may have 192; X B of tall ones takes B by its blocks.
+void muon_tile_cols(const moe_muon_shape& s, int batch, int num_sms, MuonArgs& a) {
+  const int m = std::min(s.rows, s.cols), l = std::max(s.rows, s.cols);
+  const double pairs = num_sms / 2;
+  auto cost = [&](double tiles, int nt, int K) {
+    const double turns = tiles <= 8 * pairs ? std::ceil(tiles / pairs) : tiles / pairs;
+    return turns * (((K + 63) / 64) * (128 + nt / 2) * 128 / 56.0 + 2200.0 * ((nt + 127) / 128));
+  };
+  static const int widths[4] = {256, 192, 128, 64};
+  double least_tri = 0, least_app = 0;
+  for (int nt : widths) {
+    if (nt != 192) {
+      double tiles = 0;
+      for (int r = 0; r < m; r += MUON_BLOCK) tiles += (std::min(m, r + MUON_BLOCK) + nt - 1) / nt;
+      const double c = cost(batch * tiles, nt, l) + cost(batch * tiles, nt, m);
+      if (nt == 256 || c < least_tri) { least_tri = c; a.nt_tri = nt; }
+    }
+    if (nt != 192 || s.rows <= s.cols) {
+      const double c = cost((double)batch * ((s.rows + 255) / 256) * ((s.cols + nt - 1) / nt), nt, m);
+      if (nt == 256 || c < least_app) { least_app = c; a.nt_app = nt; }
+    }
   }
-  return best;
 }
 
 // Matrices whose phases follow one another: four turns of symmetric tiles over the pairs, so that a phase's first tiles do not wait for
@@ -1019,34 +1039,13 @@ int muon_group(int m, int n, int num_sms) {
 int plan_muon_args(moe_muon* u) {
   const MuonPlan& p = u->plan;
   const moe_muon_shape& s = u->shape;
+  const bool small = muon_is_small(s.rows, s.cols);
   MuonArgs& a = u->args;
   memset(&a, 0, sizeof a);
-  const uint64_t n = p.batch, rows = s.rows, cols = s.cols;
-  int rc = MOE_OK;
-  for (int i = 0; i < 2 && !rc; ++i) {
-    const void *hi = u->ws + p.hi[i], *lo = u->ws + p.lo[i];
-    rc = encode_batch(&a.x128[i], hi, n, rows, cols, p.ld, 128);
-    if (!rc) rc = encode_batch(&a.x64[i], hi, n, rows, cols, p.ld, 64);
-    if (!rc) rc = encode_batch(&a.xhi[i], hi, n, rows, cols, p.ld, 32);
-    if (!rc) rc = encode_batch(&a.xlo[i], lo, n, rows, cols, p.ld, 32);
-  }
-  const void *A = u->ws + p.A, *B = u->ws + p.B;
-  if (!rc) rc = encode_batch(&a.a128, A, n, p.m, p.m, p.ldm, 128);
-  if (!rc) rc = encode_batch(&a.a64, A, n, p.m, p.m, p.ldm, 64);
-  if (!rc) rc = encode_batch(&a.abox, A, n, p.m, p.m, p.ldm, 32);
-  if (!rc) rc = encode_batch(&a.b128, B, n, p.m, p.m, p.ldm, 128);
-  if (!rc) rc = encode_batch(&a.b64, B, n, p.m, p.m, p.ldm, 64);
-  if (!rc) rc = encode_batch(&a.bbox, B, n, p.m, p.m, p.ldm, 32);
-  if (rc) return rc;
-  a.rows = s.rows; a.cols = s.cols; a.steps = s.steps;
-  a.nt = muon_tile_cols(s);
-  a.status = u->status();
-  a.budget_ns = u->budget_ns;
-  a.ctr = u->at<int>(p.ctr);
   for (int k = 0; k < s.steps; ++k) {
     const float ca = s.coefficients[k][0], cb = s.coefficients[k][1], cc = s.coefficients[k][2];
     const float shift = k >= MUON_LATE && cb + cc < 0.f ? -0.75f * (cb + cc) : 0.f;
-    const float scale = k + 1 == s.steps ? 1.f / MUON_SX : 1.f;   // of the result
+    const float scale = !small && k + 1 == s.steps ? 1.f / MUON_SX : 1.f;   // of the result
     MuonArgs::Step& t = a.step[k];
     t.gram_acc = MUON_SA / (MUON_SX * MUON_SX);
     t.poly_acc = cc * (MUON_SB / (MUON_SA * MUON_SA));
@@ -1055,6 +1054,32 @@ int plan_muon_args(moe_muon* u) {
     t.app_acc = scale / MUON_SB;
     t.app_in = (ca - shift) * scale;
   }
+  if (small) return MOE_OK;
+  muon_tile_cols(s, p.batch, u->num_sms, a);
+  const uint64_t n = p.batch, rows = s.rows, cols = s.cols;
+  int rc = MOE_OK;
+  for (int i = 0; i < 2 && !rc; ++i) {
+    const void *hi = u->ws + p.hi[i], *lo = u->ws + p.lo[i];
+    rc = encode_batch(&a.x128[i], hi, n, rows, cols, p.ld, 128);
+    if (!rc) rc = encode_batch(&a.x_part[i], hi, n, rows, cols, p.ld, a.nt_tri / 2);
+    if (!rc) rc = encode_batch(&a.x64[i], hi, n, rows, cols, p.ld, 64);
+    if (!rc) rc = encode_batch(&a.xhi[i], hi, n, rows, cols, p.ld, 32);
+    if (!rc) rc = encode_batch(&a.xlo[i], lo, n, rows, cols, p.ld, 32);
+  }
+  const void *A = u->ws + p.A, *B = u->ws + p.B;
+  if (!rc) rc = encode_batch(&a.a128, A, n, p.m, p.m, p.ldm, 128);
+  if (!rc) rc = encode_batch(&a.a_part, A, n, p.m, p.m, p.ldm, a.nt_tri / 2);
+  if (!rc) rc = encode_batch(&a.a64, A, n, p.m, p.m, p.ldm, 64);
+  if (!rc) rc = encode_batch(&a.abox, A, n, p.m, p.m, p.ldm, 32);
+  if (!rc) rc = encode_batch(&a.b128, B, n, p.m, p.m, p.ldm, 128);
+  if (!rc) rc = encode_batch(&a.b_part, B, n, p.m, p.m, p.ldm, a.nt_app / 2);
+  if (!rc) rc = encode_batch(&a.b64, B, n, p.m, p.m, p.ldm, 64);
+  if (!rc) rc = encode_batch(&a.bbox, B, n, p.m, p.m, p.ldm, 32);
+  if (rc) return rc;
+  a.rows = s.rows; a.cols = s.cols; a.steps = s.steps;
+  a.status = u->status();
+  a.budget_ns = u->budget_ns;
+  a.ctr = u->at<int>(p.ctr);
   return MOE_OK;
 }
 
@@ -1064,7 +1089,22 @@ int run_muon(moe_muon* u, MuonElemArgs e, const uint16_t* W, uint16_t* out, floa
   const MuonPlan& p = u->plan;
   const size_t elems = (size_t)s.rows * s.cols;
   e.elems = (long)elems; e.rows = s.rows; e.cols = s.cols; e.ld = p.ld; e.eps = s.eps;
-  e.parts = (int)muon_parts(e.elems);
+  if (muon_is_small(s.rows, s.cols)) {
+    MuonSmallArgs b;
+    memset(&b, 0, sizeof b);
+    b.e = e;
+    b.e.n = s.n;
+    b.steps = s.steps;
+    memcpy(b.step, u->args.step, sizeof b.step);
+    b.out = out; b.W = W; b.keep = keep; b.rate = rate;
+    b.vec = e.vec && aligned16(out) && aligned16(W);
+    b.status = u->status();
+    b.budget_ns = u->budget_ns;
+    MOE_CUDA(launch_muon_small(b, st));
+    u->launches = 1;
+    return MOE_OK;
+  }
+  e.parts = (int)muon_parts(e.elems, e.vec);
   e.part = u->at<double>(p.part);
   e.hi = u->at<uint16_t>(p.hi[0]); e.lo = u->at<uint16_t>(p.lo[0]);
   e.ctr = u->at<int>(p.ctr);

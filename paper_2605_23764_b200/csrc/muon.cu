@@ -50,11 +50,13 @@ __global__ void __launch_bounds__(MU_ELEM_THREADS) muon_momentum_kernel(const Mu
   pdl_trigger();
   pdl_wait();
   const int mat = blockIdx.x / a.parts, part = blockIdx.x - mat * a.parts;
-  const long e0 = part * MUON_PART, e1 = min(a.elems, e0 + MUON_PART);
+  constexpr long PART = VEC ? MUON_PART_VEC : MUON_PART_ONE;
+  const long e0 = part * PART, e1 = min(a.elems, e0 + PART);
   const size_t base = (size_t)mat * a.elems;
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i <= a.n; i += MU_ELEM_THREADS) a.ctr[i] = 0;
   double sum = 0.0;
+#pragma unroll 4
   for (long i = e0 + threadIdx.x * N; i < e1; i += MU_ELEM_THREADS * N) {
     float u[N];
     muon_load_g<VEC>(a, base + i, u);
@@ -112,6 +114,7 @@ __global__ void __launch_bounds__(MU_ELEM_THREADS) muon_normalize_kernel(const M
   const float f0 = factor[0], f1 = factor[1];
   const int r0 = blk * rows_per, nrows = min(a.rows - r0, rows_per);
   const int per_row = (a.cols + N - 1) / N, count = nrows * per_row;
+#pragma unroll 4
   for (int i = threadIdx.x; i < count; i += MU_ELEM_THREADS) {
     const int row = i / per_row, col = (i - row * per_row) * N;
     const size_t at = (size_t)mat * a.elems + (size_t)(r0 + row) * a.cols + col;
@@ -150,7 +153,7 @@ cudaError_t launch_muon_momentum(const MuonElemArgs& a, cudaStream_t s) {
                : launch_dependent(muon_momentum_kernel<false>, grid, dim3(MU_ELEM_THREADS), 0, s, a);
 }
 cudaError_t launch_muon_normalize(const MuonElemArgs& a, cudaStream_t s) {
-  int rows_per = (int)(MUON_PART / a.cols);
+  int rows_per = (int)((a.vec ? MUON_PART_VEC : MUON_PART_ONE) / a.cols);
   if (rows_per < 1) rows_per = 1;
   const int blocks_per = (a.rows + rows_per - 1) / rows_per;
   const dim3 grid((unsigned)(a.n * (long)blocks_per));

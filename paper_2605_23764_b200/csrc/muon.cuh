@@ -32,13 +32,14 @@ enum MuonPhase : int {
 constexpr int MUON_BLOCK = 256;
 
 struct MuonArgs {
-  // X, by buffer: K-major operand (128 rows x 64), MN-major operand (64 x 64), epilogue boxes (32 rows x 64) of hi and lo
-  CUtensorMap x128[2], x64[2], xhi[2], xlo[2];
-  CUtensorMap a128, a64, abox, b128, b64, bbox;   // A and B
+  // X, by buffer: K-major operands (128 rows x 64; half a tile's columns x 64), MN-major operand (64 x 64), epilogue boxes (32 rows x 64)
+  // of hi and lo; A and B likewise
+  CUtensorMap x128[2], x_part[2], x64[2], xhi[2], xlo[2];
+  CUtensorMap a128, a_part, a64, abox, b128, b_part, b64, bbox;
   CUtensorMap out, w;          // the caller's tensors by epilogue boxes (vec)
   int n, rows, cols;           // matrices of the batch
   int steps;
-  int nt;                      // columns of an APPLY tile: 128, 192 or 256
+  int nt_tri, nt_app;          // columns of a tile: 64, 128 or 256; APPLY's also 192 in wide matrices
   int sub;                     // matrices whose phases follow one another
   int z0;                      // the batch's first matrix in the caller's tensors
   struct Step { float gram_acc, poly_acc, poly_in, poly_diag, app_acc, app_in; } step[MUON_STEPS_MAX];   // factors in the stored scalings
@@ -70,11 +71,30 @@ struct MuonElemArgs {
   uint16_t *hi, *lo;    // X [n][rows][ld]
   int* ctr;             // [n + 1] cleared on the way
 };
-constexpr long MUON_PART = 32768;   // elements of a part
-inline long muon_parts(long elems) { return (elems + MUON_PART - 1) / MUON_PART; }
+// Elements of a part, of vectors and of single ones: a few turns of a block's threads (with 32768, 16 matrices 128 x 256 took 10 us longer)
+constexpr long MUON_PART_VEC = 8192, MUON_PART_ONE = 2048;
+inline long muon_parts(long elems, bool vec) { return (elems + (vec ? MUON_PART_VEC : MUON_PART_ONE) - 1) / (vec ? MUON_PART_VEC : MUON_PART_ONE); }
 // M_out = mu M + G, u = G + mu M_out (nesterov) or M_out; sums of u's squares
 cudaError_t launch_muon_momentum(const MuonElemArgs& a, cudaStream_t s);
 // X = u / (norm + eps)
 cudaError_t launch_muon_normalize(const MuonElemArgs& a, cudaStream_t s);
+
+// Small matrices: everything of one in one block (muon_small.cu), no workspace but the status
+constexpr int MUON_SMALL_M = 128, MUON_SMALL_L = 384;
+inline bool muon_is_small(int rows, int cols) {
+  return (rows < cols ? rows : cols) <= MUON_SMALL_M && (rows < cols ? cols : rows) <= MUON_SMALL_L;
+}
+struct MuonSmallArgs {
+  MuonElemArgs e;
+  int steps;
+  MuonArgs::Step step[MUON_STEPS_MAX];   // app_in: a - s
+  uint16_t* out;
+  const uint16_t* W;    // NULL: out = X'
+  float keep, rate;
+  int vec;              // rows of everything are whole vectors of eight elements
+  DevStatus* status;
+  uint64_t budget_ns;
+};
+cudaError_t launch_muon_small(const MuonSmallArgs& a, cudaStream_t s);
 
 }  // namespace moe

@@ -1,6 +1,6 @@
 // The products of an orthogonalisation (muon.cuh) on the tensor cores: one persistent launch for all steps of a batch of matrices.
 //
-// Items are tiles of 256 rows x 256 (or nt) columns of one matrix's product.  The phases of a matrix follow one another; an item
+// Items are tiles of 256 rows x 256 columns (fewer where there are not enough of them) of one matrix's product.  The phases of a matrix follow one another; an item
 // waits until all tiles of its matrix's phase before have been stored (a counter a matrix), which other matrices' tiles cover.
 // CTA pairs take items from a ticket in that order, so whichever pairs are resident make progress.  The accumulator is one of two in
 // TMEM: a tile's products run beside the epilogue of the one before.
@@ -29,6 +29,7 @@ constexpr int MU_STAGE_BYTES = A_STAGE_BYTES + HALF_B_BYTES;   // 128 rows of A,
 constexpr int MU_EPI_WARPS = 8, MU_THREADS = 32 * (3 + MU_EPI_WARPS);
 constexpr int MU_BOX = 32 * 64 * 2;
 constexpr int MU_SLOTS = 3;          // tickets taken ahead
+constexpr int MU_DEPS = MU_SLOTS + 1; // items that the loader can be ahead of the epilogue, and one
 constexpr int MU_READERS = 19;       // warps of the pair that read a ticket: two loaders, the issuer, sixteen of the epilogues
 constexpr int MU_PARTS = 2 * MU_EPI_WARPS;   // signals of a tile
 
@@ -37,6 +38,7 @@ struct MuonBarriers {
   uint64_t tmem_full[2], tmem_empty[2];
   uint64_t in_full[MU_EPI_WARPS];
   uint64_t item_full[MU_SLOTS], item_empty[MU_SLOTS];
+  uint64_t dep[MU_DEPS];            // the loader has seen what the item depends on complete
   uint64_t drain;
   uint32_t tmem_base;
   int item[MU_SLOTS];
@@ -51,11 +53,13 @@ struct MuonItem {
 
 // Tiles of a matrix's phases and how items go through them: `sub` matrices at a time, step by step, phase by phase, matrix by matrix.
 struct MuonOrder {
-  int tri, app, app_cols, per_step;
+  int blocks, per_block, tri, app, app_cols, per_step;   // rows of 256 of a symmetric matrix, tiles across one of its blocks; tiles
   __host__ __device__ explicit MuonOrder(const MuonArgs& a) {
-    const int m = a.rows < a.cols ? a.rows : a.cols, nb = (m + MUON_BLOCK - 1) / MUON_BLOCK;
-    tri = nb * (nb + 1) / 2;
-    app_cols = (a.cols + a.nt - 1) / a.nt;
+    const int m = a.rows < a.cols ? a.rows : a.cols;
+    blocks = (m + MUON_BLOCK - 1) / MUON_BLOCK;
+    per_block = MUON_BLOCK / a.nt_tri;
+    tri = per_block * (blocks * (blocks + 1) / 2 - 1) + (m - (blocks - 1) * MUON_BLOCK + a.nt_tri - 1) / a.nt_tri;
+    app_cols = (a.cols + a.nt_app - 1) / a.nt_app;
     app = (a.rows + 255) / 256 * app_cols;
     per_step = 2 * tri + app;
   }
@@ -89,10 +93,10 @@ struct MuonOrder {
     if (r.phase == MUON_APPLY) {
       i = t / app_cols;
       t -= i * app_cols;
-      r.nt = a.nt;
+      r.nt = a.nt_app;
     } else {
-      while (t > i) t -= ++i;
-      r.nt = MUON_BLOCK;
+      for (int c = per_block; i + 1 < blocks && t >= c; c += per_block, ++i) t -= c;   // row i: (i + 1) blocks; the last one's end at m
+      r.nt = a.nt_tri;
     }
     r.m0 = i * 256;
     r.n0 = t * r.nt;
@@ -130,7 +134,7 @@ struct MuonMajors {
   int a_from, b_from;   // first k-block that does
   __device__ explicit MuonMajors(const MuonItem& it) {
     constexpr int NEVER = INT_MAX, BKS = MUON_BLOCK / BK;
-    const int a_sym = it.m0 / BK + BKS, b_sym = it.n0 / BK + BKS;
+    const int a_sym = it.m0 / BK + BKS, b_sym = it.n0 / MUON_BLOCK * BKS + BKS;
     if (it.phase == MUON_GRAM) {
       a_from = b_from = WIDE ? NEVER : 0;
     } else if (it.phase == MUON_POLY) {
@@ -144,7 +148,7 @@ struct MuonMajors {
 };
 
 // Half a box of 32 rows x 64 columns of the accumulator: v, 32 columns of the lane's row; j0: its first chunk of eight.
-__device__ __forceinline__ void muon_box_gram(const MuonArgs::Step& k, float* v, uint8_t* box, int lane, int j0) {
+__device__ __forceinline__ void muon_box_gram(const MuonArgs::Step k, float* v, uint8_t* box, int lane, int j0) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float* x = v + 8 * j;
@@ -152,13 +156,15 @@ __device__ __forceinline__ void muon_box_gram(const MuonArgs::Step& k, float* v,
                                           pack_h2(x[4] * k.gram_acc, x[5] * k.gram_acc), pack_h2(x[6] * k.gram_acc, x[7] * k.gram_acc));
   }
 }
+// (All chunks are read before the first is written: the compiler keeps reads behind writes that might meet them, a latency a chunk.)
 // diag: the column of v on the lane's diagonal, or none of 0 .. 31
-__device__ __forceinline__ void muon_box_poly(const MuonArgs::Step& k, float* v, uint8_t* box, int lane, int j0, int diag) {
+__device__ __forceinline__ void muon_box_poly(const MuonArgs::Step k, float* v, uint8_t* box, int lane, int j0, int diag) {
+  uint4 in[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) in[j] = *box_chunk(box, lane, j0 + j);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    uint4* p = box_chunk(box, lane, j0 + j);
-    const uint4 in = *p;
-    const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+    const uint32_t w[4] = {in[j].x, in[j].y, in[j].z, in[j].w};
     uint32_t o[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -168,18 +174,21 @@ __device__ __forceinline__ void muon_box_poly(const MuonArgs::Step& k, float* v,
       if (diag == 8 * j + 2 * q + 1) x1 += k.poly_diag;
       o[q] = pack_h2(x0, x1);
     }
-    *p = make_uint4(o[0], o[1], o[2], o[3]);
+    *box_chunk(box, lane, j0 + j) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
 // X' (in v too) from X hi in box0 and, with LO, lo in box1; written back as hi and, with KEEP, lo
 template <bool LO, bool HI_OUT, bool LO_OUT>
-__device__ __forceinline__ void muon_box_apply(const MuonArgs::Step& k, float* v, uint8_t* box0, uint8_t* box1, int lane, int j0) {
+__device__ __forceinline__ void muon_box_apply(const MuonArgs::Step k, float* v, uint8_t* box0, uint8_t* box1, int lane, int j0) {
+  uint4 xh[4], xl[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    uint4 *ph = box_chunk(box0, lane, j0 + j), *pl = box_chunk(box1, lane, j0 + j);
-    const uint4 xh = *ph;
-    const uint4 xl = LO ? *pl : make_uint4(0, 0, 0, 0);
-    const uint32_t wh[4] = {xh.x, xh.y, xh.z, xh.w}, wl[4] = {xl.x, xl.y, xl.z, xl.w};
+    xh[j] = *box_chunk(box0, lane, j0 + j);
+    if (LO) xl[j] = *box_chunk(box1, lane, j0 + j);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t wh[4] = {xh[j].x, xh[j].y, xh[j].z, xh[j].w}, wl[4] = {xl[j].x, xl[j].y, xl[j].z, xl[j].w};
     uint32_t oh[4], ol[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -198,8 +207,8 @@ __device__ __forceinline__ void muon_box_apply(const MuonArgs::Step& k, float* v
         ol[q] = pack_h2((x0 - z.x) * MUON_SLO, (x1 - z.y) * MUON_SLO);
       }
     }
-    if (HI_OUT) *ph = make_uint4(oh[0], oh[1], oh[2], oh[3]);
-    if (LO_OUT) *pl = make_uint4(ol[0], ol[1], ol[2], ol[3]);
+    if (HI_OUT) *box_chunk(box0, lane, j0 + j) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+    if (LO_OUT) *box_chunk(box1, lane, j0 + j) = make_uint4(ol[0], ol[1], ol[2], ol[3]);
   }
 }
 // The last step's X' in v: bf16, or the weights' update, into box0; W is in box1, or with `lo` (runs of up to three steps) still in memory
@@ -222,17 +231,24 @@ __device__ __forceinline__ void muon_box_out(const MuonArgs& a, float* v, uint8_
     *box_chunk(box0, lane, j0 + j) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
   }
 }
-// The same for rows that are no whole vectors, element by element
-__device__ __forceinline__ void muon_row_out(const MuonArgs& a, const float* v, int mat, int r, int c0) {
-  if (r >= a.rows) return;
-  const size_t at = ((size_t)mat * a.rows + r) * a.cols + c0;
+// The same for rows that are no whole vectors: X' in fp32 through both boxes, so that a row's elements are next to one another when they
+// are written (a lane a row, 7 matrices 333 x 1171: 30 us more)
+__device__ __forceinline__ void muon_rows_out(const MuonArgs& a, const float* v, uint8_t* boxes, int lane, int mat, int r0, int c0) {
+  __syncwarp();   // X has been read from the boxes
 #pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (c0 + i < a.cols) {
-      float x = v[i];
-      if (a.w_ptr) x = fmaf(a.keep, __uint_as_float((uint32_t)a.w_ptr[at + i] << 16), -a.rate * x);
-      a.out_ptr[at + i] = (uint16_t)pack_bf16x2(x, 0.f);
+  for (int j = 0; j < 16; ++j)
+    *reinterpret_cast<float4*>(boxes + lane * 256 + ((j ^ (lane & 7)) << 4)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+  __syncwarp();
+#pragma unroll 4
+  for (int i = 0; i < 64; ++i) {   // row i / 2, half a row at a time
+    const int r = i >> 1, c = (i & 1) * 32 + lane;
+    if (r0 + r < a.rows && c0 + c < a.cols) {
+      float x = *reinterpret_cast<const float*>(boxes + r * 256 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4);
+      const size_t at = ((size_t)mat * a.rows + r0 + r) * a.cols + c0 + c;
+      if (a.w_ptr) x = fmaf(a.keep, __uint_as_float((uint32_t)a.w_ptr[at] << 16), -a.rate * x);
+      a.out_ptr[at] = (uint16_t)pack_bf16x2(x, 0.f);
     }
+  }
 }
 
 // A role's place in the ring of tickets
@@ -275,6 +291,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       mbar_init(&bars->item_full[s], 1);
       mbar_init(&bars->item_empty[s], MU_READERS);
     }
+    for (int s = 0; s < MU_DEPS; ++s) mbar_init(&bars->dep[s], 1);
     mbar_init(&bars->drain, 1);
     mbar_fence_init();
     fence_proxy_async();
@@ -310,7 +327,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
     }
   } else if (warp == 0) {
     MuonTickets tk;
-    uint32_t s = 0, par = (1u << MU_STAGES) - 1;
+    uint32_t s = 0, par = (1u << MU_STAGES) - 1, dep = 0;
     for (bool ok = true; ok;) {
       const int t = tk.next(bars, wc, 20);
       if (t < 0 || t >= total) break;
@@ -320,26 +337,29 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       const int m0 = uniform(it.m0 + rank * 128), n0 = uniform(it.n0 + rank * half);
       const int K = it.phase == MUON_GRAM ? max(a.rows, a.cols) : min(a.rows, a.cols), nkb = uniform((K + BK - 1) / BK);
       // K-major and MN-major maps of both operands
-      const CUtensorMap *a_k = &a.a128, *a_mn = &a.a64, *b_k = &a.a128, *b_mn = &a.a64;
+      const CUtensorMap *a_k = &a.a128, *a_mn = &a.a64, *b_k = &a.a_part, *b_mn = &a.a64;
       if (it.phase == MUON_GRAM) {
-        a_k = b_k = &a.x128[cur];
+        a_k = &a.x128[cur];
+        b_k = &a.x_part[cur];
         a_mn = b_mn = &a.x64[cur];
       } else if (it.phase == MUON_APPLY) {
         a_k = WIDE ? &a.b128 : &a.x128[cur];
         a_mn = &a.b64;
-        b_k = &a.b128;
+        b_k = &a.b_part;
         b_mn = WIDE ? &a.x64[cur] : &a.b64;
       }
       int up = 1;
       if (it.need && lane == 0) up = counter_wait(a.ctr + mat, it.need, wc, t, 256) ? 1 : 0;
       if (!uniform(up)) break;
       fence_proxy_async_global();   // what the counter announces was written by other CTAs' stores
+      if (lane == 0) mbar_arrive_cta(&bars->dep[dep]);
+      if (++dep == MU_DEPS) dep = 0;
       const int b_boxes = (half + 63) / 64;
       for (int kb = 0; kb < nkb; ++kb) {
         if (!mbar_wait_warp(&bars->empty[s], (par >> s) & 1, wc, SITE_EMPTY, t, 20)) { ok = false; break; }
         uint8_t* st = smem + s * MU_STAGE_BYTES;
         const bool amn = kb >= mj.a_from, bmn = kb >= mj.b_from;
-        if (rank == 0) mbar_expect_tx_elect(&bars->full[s], 2 * (A_STAGE_BYTES + (bmn ? b_boxes * MN_BOX_BYTES : HALF_B_BYTES)));
+        if (rank == 0) mbar_expect_tx_elect(&bars->full[s], 2 * (A_STAGE_BYTES + (bmn ? b_boxes * MN_BOX_BYTES : half * BK * 2)));
         if (amn) {
           tma_load_3d_pair(st, a_mn, m0, kb * BK, mat, &bars->full[s]);
           tma_load_3d_pair(st + MN_BOX_BYTES, a_mn, m0 + 64, kb * BK, mat, &bars->full[s]);
@@ -403,37 +423,36 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
     uint8_t* box0 = boxes + ew * 2 * MU_BOX;
     uint8_t* box1 = box0 + MU_BOX;
     uint64_t* in_full = &bars->in_full[ew];
-    uint32_t acc = 0, full_par = 0, in_par = 0;
+    uint32_t acc = 0, full_par = 0, in_par = 0, dep = 0, dep_par = 0;
     for (bool ok = true; ok;) {
       const int t = tk.next(bars, wc, 100);
       if (t < 0 || t >= total) break;
       const MuonItem it = order.decode(a, t);
-      const MuonArgs::Step& k = a.step[it.step];
+      const MuonArgs::Step k = a.step[it.step];   // (a copy: by reference the factors were read again for every chunk, 1.4 us a box)
       const int m = min(a.rows, a.cols), cur = it.step & 1;
       const int M = it.phase == MUON_APPLY ? a.rows : m, N = it.phase == MUON_APPLY ? a.cols : m;
       const bool last = it.phase == MUON_APPLY && it.step + 1 == a.steps;
       const bool lo = it.phase == MUON_APPLY && it.step < MUON_LATE, lo_out = it.phase == MUON_APPLY && !last && it.step + 1 < MUON_LATE;
       const bool upd = last && !lo && a.vec && a.w_ptr;   // W comes with X
       const int r0 = it.m0 + rank * 128 + quad * 32;
+      // the loader polls the counter for the CTA: with its eight epilogue warps polling too, 7 matrices 336 x 1176 took TODO us longer
+      if (!mbar_wait_warp(&bars->dep[dep], dep_par, wc, SITE_DEP, t, 50)) break;
+      if (++dep == MU_DEPS) { dep = 0; dep_par ^= 1; }
       bool up = false;   // the accumulator has been seen complete
       for (int b = (ew >> 2) * 64; b < it.nt; b += 128) {
         const int c0 = it.n0 + b;
         if (r0 >= M || c0 >= N) break;
         __syncwarp();   // every lane has read the boxes
         if (it.phase != MUON_GRAM) {
-          int there = 1;
           if (lane == 0) {
-            if (!up) there = counter_wait(a.ctr + it.mat, it.need, wc, t, 256) ? 1 : 0;
             tma_store_wait_read();
-            if (there) {
-              fence_proxy_async_global();
-              mbar_expect_tx(in_full, lo || upd ? 2 * MU_BOX : MU_BOX);
-              tma_load_3d_thread(box0, it.phase == MUON_POLY ? &a.abox : &a.xhi[cur], c0, r0, it.mat, in_full);
-              if (lo) tma_load_3d_thread(box1, &a.xlo[cur], c0, r0, it.mat, in_full);
-              else if (upd) tma_load_3d_thread(box1, &a.w, c0, r0, a.z0 + it.mat, in_full);
-            }
+            fence_proxy_async_global();
+            mbar_expect_tx(in_full, lo || upd ? 2 * MU_BOX : MU_BOX);
+            tma_load_3d_thread(box0, it.phase == MUON_POLY ? &a.abox : &a.xhi[cur], c0, r0, it.mat, in_full);
+            if (lo) tma_load_3d_thread(box1, &a.xlo[cur], c0, r0, it.mat, in_full);
+            else if (upd) tma_load_3d_thread(box1, &a.w, c0, r0, a.z0 + it.mat, in_full);
           }
-          if (!uniform(there)) { ok = false; break; }
+          __syncwarp();
         } else {
           if (lane == 0) tma_store_wait_read();
           __syncwarp();
@@ -449,6 +468,21 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
         }
         if (!ok) break;
         const uint32_t tcol = tmem_base + acc * 256 + b + (static_cast<uint32_t>(quad * 32) << 16);
+        if (last && !a.vec) {
+          float v[64];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) tmem_ld16(tcol + 16 * q, v + 16 * q);
+          tmem_ld_wait();
+          if (lo) {
+            muon_box_apply<true, false, false>(k, v, box0, box1, lane, 0);
+            muon_box_apply<true, false, false>(k, v + 32, box0, box1, lane, 4);
+          } else {
+            muon_box_apply<false, false, false>(k, v, box0, box1, lane, 0);
+            muon_box_apply<false, false, false>(k, v + 32, box0, box1, lane, 4);
+          }
+          muon_rows_out(a, v, box0, lane, it.mat, r0, c0);
+          continue;
+        }
 #pragma unroll 1
         for (int j0 = 0; j0 < 8; j0 += 4) {
           float v[32];
@@ -466,11 +500,9 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
           } else {
             if (lo) muon_box_apply<true, false, false>(k, v, box0, box1, lane, j0);
             else muon_box_apply<false, false, false>(k, v, box0, box1, lane, j0);
-            if (a.vec) muon_box_out(a, v, box0, box1, lane, j0, lo, it.mat, r0 + lane, c0);
-            else muon_row_out(a, v, it.mat, r0 + lane, c0 + 8 * j0);
+            muon_box_out(a, v, box0, box1, lane, j0, lo, it.mat, r0 + lane, c0);
           }
         }
-        if (last && !a.vec) continue;
         staging_release();
         if (lane == 0) {
           const CUtensorMap* o = it.phase == MUON_GRAM ? &a.abox : it.phase == MUON_POLY ? &a.bbox : last ? &a.out : &a.xhi[cur ^ 1];

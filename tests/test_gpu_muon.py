@@ -285,7 +285,7 @@ def test_refusals():
         muon.orthogonalize(G)
     shape = binding.moe_muon_shape(2, 16, 24, COEF, 5, 1e-7)
     with pytest.raises(MoeError):   # too small a workspace
-        binding.moe_muon_create(shape, torch.empty(256, dtype=torch.uint8, device="cuda"))
+        binding.moe_muon_create(shape, torch.empty(binding.moe_muon_workspace_bytes(shape) - 1, dtype=torch.uint8, device="cuda"))
     h = binding.moe_muon_create(shape)   # one of its own
     out = torch.empty_like(G)
     binding.moe_muon_orthogonalize(h, G, out)
