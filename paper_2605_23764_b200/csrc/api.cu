@@ -67,10 +67,10 @@ EncodeTiledFn get_encode_fn() {
   return fn;
 }
 
-// bf16 (or fp16) tensor of `rank` dimensions (dims[0] innermost, strides in bytes for dims 1..), 128-byte
+// bf16 (fp16, or another type's) tensor of `rank` dimensions (dims[0] innermost, strides in bytes for dims 1..), 128-byte
 // swizzle, zero fill outside the tensor on loads, clipping on stores.
 int encode_tiled(CUtensorMap* tm, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
-                 const uint32_t* box) {
+                 const uint32_t* box, CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) {
     g_cuda_error = "cuTensorMapEncodeTiled entry point not available";
@@ -80,7 +80,7 @@ int encode_tiled(CUtensorMap* tm, const void* base, int rank, const uint64_t* di
   cuuint32_t bx[5], estr[5] = {1, 1, 1, 1, 1};
   for (int i = 0; i < rank; ++i) { gdim[i] = dims[i]; bx[i] = box[i]; }
   for (int i = 0; i + 1 < rank; ++i) gstr[i] = strides[i];
-  CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), gdim, gstr, bx, estr,
+  CUresult r = fn(tm, type, rank, const_cast<void*>(base), gdim, gstr, bx, estr,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -930,7 +930,8 @@ constexpr size_t MUON_BATCH_BYTES = size_t(1) << 30;
 struct MuonPlan {
   int m, l, ld, ldm;          // smaller and larger dimension; elements from row to row of X, of A and B
   int batch;                  // matrices of a turn
-  size_t ctr, part, hi[2], lo[2], A, B, total;
+  size_t ctr, part, hi[2], lo[2], A, B, sums, total;
+  int nt_tri, nt_app, split;  // tile columns, parts of the reduction of A = X X^T
 };
 
 bool muon_shape_ok(const moe_muon_shape* s) {
@@ -940,6 +941,46 @@ bool muon_shape_ok(const moe_muon_shape* s) {
     for (int j = 0; j < 3; ++j)
       if (!std::isfinite(s->coefficients[i][j])) return false;
   return true;
+}
+
+// Tile columns: the width whose turns over the pairs of SMs are over first.  A k-block takes what its operands' bytes take at 56 a clock (32 KB
+// with 256 columns, 20 KB with 64), a turn the epilogue's boxes on top.  So a batch with many tiles has wide ones, a single matrix narrow
+// ones as long as every pair has one (1408 x 2048: 267 us with 256, 392 with 64, 214 with 128).  Where even so pairs are left, the
+// reduction of A = X X^T is split among them, for a phase that joins the parts (some 9000 clocks).
+// Wide matrices' APPLY may have 192 columns; X B of tall ones takes B by its blocks.
+void muon_tile_cols(const moe_muon_shape& s, MuonPlan& p) {
+  const int m = p.m, l = p.l, nkb = (l + 63) / 64;
+  constexpr double pairs = 74;   // of a B200: the workspace's size is asked for without a device
+  auto turn = [](int nt, double blocks) { return blocks * (128 + nt / 2) * 128 / 56.0 + 2200.0 * ((nt + 127) / 128); };
+  auto cost = [&](double tiles, int nt, int K) {
+    return (tiles <= 8 * pairs ? std::ceil(tiles / pairs) : tiles / pairs) * turn(nt, (K + 63) / 64);
+  };
+  static const int widths[4] = {256, 192, 128, 64};
+  double least_tri = 0, least_app = 0;
+  for (int nt : widths) {
+    if (nt != 192) {
+      double tiles = 0;
+      for (int r = 0; r < m; r += MUON_BLOCK) tiles += (std::min(m, r + MUON_BLOCK) + nt - 1) / nt;
+      tiles *= p.batch;
+      double gram = cost(tiles, nt, l);
+      int split = 1;
+      for (int i = 2; i <= nkb / 2 && i * tiles <= pairs; ++i) {
+        const double c = turn(nt, (nkb + i - 1) / i) + 9000 + 100 * i;
+        if (c < gram) { gram = c; split = i; }
+      }
+      const double c = gram + cost(tiles, nt, m);
+      if (nt == 256 || c < least_tri) { least_tri = c; p.nt_tri = nt; p.split = split; }
+    }
+    if (nt != 192 || s.rows <= s.cols) {
+      const double c = cost((double)p.batch * ((s.rows + 255) / 256) * ((s.cols + nt - 1) / nt), nt, m);
+      if (nt == 256 || c < least_app) { least_app = c; p.nt_app = nt; }
+    }
+  }
+}
+long muon_tri_tiles(const MuonPlan& p) {
+  long tiles = 0;
+  for (int r = 0; r < p.m; r += MUON_BLOCK) tiles += (std::min(p.m, r + MUON_BLOCK) + p.nt_tri - 1) / p.nt_tri;
+  return tiles;
 }
 
 MuonPlan plan_muon(const moe_muon_shape& s) {
@@ -970,6 +1011,8 @@ MuonPlan plan_muon(const moe_muon_shape& s) {
   }
   p.A = c.take(a * p.batch);
   p.B = c.take(a * p.batch);
+  muon_tile_cols(s, p);
+  if (p.split > 1) p.sums = c.take(sizeof(float) * p.batch * muon_tri_tiles(p) * p.split * 256 * p.nt_tri);
   p.total = c.off;
   return p;
 }
@@ -1000,33 +1043,6 @@ int encode_batch(CUtensorMap* tm, const void* base, uint64_t n, uint64_t rows, u
   return encode_tiled(tm, base, 3, dims, strides, box);
 }
 
-// Tile columns: the width whose turns over the pairs of SMs are over first.  A k-block takes what its operands' bytes take at 56 a clock (32 KB
-// with 256 columns, 20 KB with 64), a turn the epilogue's boxes on top.  So a batch with many tiles has wide ones, a single matrix
-// narrow ones as long as every pair has one: 256 x 7168 290 -> 232 us, 1408 x 2048 267 us, 392 with the narrowest, TODO with 128.
-// Wide matrices' APPLY may have 192; X B of tall ones takes B by its blocks.
-void muon_tile_cols(const moe_muon_shape& s, int batch, int num_sms, MuonArgs& a) {
-  const int m = std::min(s.rows, s.cols), l = std::max(s.rows, s.cols);
-  const double pairs = num_sms / 2;
-  auto cost = [&](double tiles, int nt, int K) {
-    const double turns = tiles <= 8 * pairs ? std::ceil(tiles / pairs) : tiles / pairs;
-    return turns * (((K + 63) / 64) * (128 + nt / 2) * 128 / 56.0 + 2200.0 * ((nt + 127) / 128));
-  };
-  static const int widths[4] = {256, 192, 128, 64};
-  double least_tri = 0, least_app = 0;
-  for (int nt : widths) {
-    if (nt != 192) {
-      double tiles = 0;
-      for (int r = 0; r < m; r += MUON_BLOCK) tiles += (std::min(m, r + MUON_BLOCK) + nt - 1) / nt;
-      const double c = cost(batch * tiles, nt, l) + cost(batch * tiles, nt, m);
-      if (nt == 256 || c < least_tri) { least_tri = c; a.nt_tri = nt; }
-    }
-    if (nt != 192 || s.rows <= s.cols) {
-      const double c = cost((double)batch * ((s.rows + 255) / 256) * ((s.cols + nt - 1) / nt), nt, m);
-      if (nt == 256 || c < least_app) { least_app = c; a.nt_app = nt; }
-    }
-  }
-}
-
 // Matrices whose phases follow one another: four turns of symmetric tiles over the pairs, so that a phase's first tiles do not wait for
 // the last ones of the phase before; groups of equal size.
 int muon_group(int m, int n, int num_sms) {
@@ -1055,7 +1071,9 @@ int plan_muon_args(moe_muon* u) {
     t.app_in = (ca - shift) * scale;
   }
   if (small) return MOE_OK;
-  muon_tile_cols(s, p.batch, u->num_sms, a);
+  a.nt_tri = p.nt_tri; a.nt_app = p.nt_app; a.split = p.split;
+  a.strips = 1;   // about an item a pair
+  while (a.strips < 32 && 2 * a.strips * p.batch * muon_tri_tiles(p) <= 74) a.strips *= 2;
   const uint64_t n = p.batch, rows = s.rows, cols = s.cols;
   int rc = MOE_OK;
   for (int i = 0; i < 2 && !rc; ++i) {
@@ -1075,7 +1093,15 @@ int plan_muon_args(moe_muon* u) {
   if (!rc) rc = encode_batch(&a.b_part, B, n, p.m, p.m, p.ldm, a.nt_app / 2);
   if (!rc) rc = encode_batch(&a.b64, B, n, p.m, p.m, p.ldm, 64);
   if (!rc) rc = encode_batch(&a.bbox, B, n, p.m, p.m, p.ldm, 32);
+  if (!rc && p.split > 1) {
+    const uint64_t dims[2] = {(uint64_t)p.nt_tri, (uint64_t)p.batch * muon_tri_tiles(p) * p.split * 256}, strides[1] = {(uint64_t)p.nt_tri * 4};
+    const uint32_t box[2] = {32, 32};
+    rc = encode_tiled(&a.part, u->ws + p.sums, 2, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
+    a.part_ptr = u->at<float>(p.sums);
+  }
   if (rc) return rc;
+  a.a_ptr = u->at<uint16_t>(p.A);
+  a.lda = p.ldm;
   a.rows = s.rows; a.cols = s.cols; a.steps = s.steps;
   a.status = u->status();
   a.budget_ns = u->budget_ns;

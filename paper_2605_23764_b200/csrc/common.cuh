@@ -173,6 +173,10 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* m, int x, int y,
                ::"l"(m), "r"(x), "r"(y), "r"(z), "r"(smem_u32(smem_src))
                : "memory");
 }
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, int x, int y, const void* smem_src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(m), "r"(x), "r"(y), "r"(smem_u32(smem_src))
+               : "memory");
+}
 __device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // Wait until the committed stores of this thread have finished READING shared memory.
 __device__ __forceinline__ void tma_store_wait_read() {

@@ -23,9 +23,10 @@ constexpr int MUON_STEPS_MAX = 16;
 constexpr int MUON_LATE = 3;   // first step (from 0) with the shifted diagonal and X in one part
 
 enum MuonPhase : int {
-  MUON_GRAM = 0,    // A = X X^T or X^T X
-  MUON_POLY = 1,    // B = b A + c A A + s I
-  MUON_APPLY = 2,   // X' = (a - s) X + B X or X B; of the last step: into the caller's tensors
+  MUON_GRAM = 0,    // A = X X^T or X^T X, or sums over parts of the reduction
+  MUON_JOIN = 1,    // A from those
+  MUON_POLY = 2,    // B = b A + c A A + s I
+  MUON_APPLY = 3,   // X' = (a - s) X + B X or X B; of the last step: into the caller's tensors
 };
 
 // A symmetric matrix is stored by blocks of 256 x 256, those on and below the diagonal.
@@ -37,9 +38,14 @@ struct MuonArgs {
   CUtensorMap x128[2], x_part[2], x64[2], xhi[2], xlo[2];
   CUtensorMap a128, a_part, a64, abox, b128, b_part, b64, bbox;
   CUtensorMap out, w;          // the caller's tensors by epilogue boxes (vec)
+  CUtensorMap part;            // GRAM's sums over parts [tile of a matrix][part][256][nt_tri] in fp32, boxes of 32 x 32
   int n, rows, cols;           // matrices of the batch
   int steps;
   int nt_tri, nt_app;          // columns of a tile: 64, 128 or 256; APPLY's also 192 in wide matrices
+  int split, strips;           // parts of GRAM's reduction (1: no JOIN); strips of a tile's rows that JOIN's items are
+  const float* part_ptr;
+  uint16_t* a_ptr;             // A, rows lda apart
+  int lda;
   int sub;                     // matrices whose phases follow one another
   int z0;                      // the batch's first matrix in the caller's tensors
   struct Step { float gram_acc, poly_acc, poly_in, poly_diag, app_acc, app_in; } step[MUON_STEPS_MAX];   // factors in the stored scalings

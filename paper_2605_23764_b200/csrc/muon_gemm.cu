@@ -1,5 +1,6 @@
 // The products of an orthogonalisation (muon.cuh) on the tensor cores: one persistent launch for all steps of a batch of matrices.
 //
+// Where there are few tiles and a long reduction, GRAM sums parts of it and a phase more joins them (one matrix of 256 x 7168: 210 -> TODO us).
 // Items are tiles of 256 rows x 256 columns (fewer where there are not enough of them) of one matrix's product.  The phases of a matrix follow one another; an item
 // waits until all tiles of its matrix's phase before have been stored (a counter a matrix), which other matrices' tiles cover.
 // CTA pairs take items from a ticket in that order, so whichever pairs are resident make progress.  The accumulator is one of two in
@@ -13,7 +14,7 @@
 // What bounds it: shared memory.  A k-block brings 32 KB into an SM and the products read 32 KB, 512 clocks' worth at 128 bytes a clock,
 // which is what the products take; the epilogue's boxes come on top.
 //
-// Roles per CTA: warp 0 TMA producer, warp 1 MMA issuer (even CTA) and TMEM owner, warps 2-9 epilogue, warp 10 tickets (even CTA).
+// Roles per CTA: warp 0 TMA producer, warp 1 MMA issuer (even CTA) or tickets (odd CTA) and TMEM owner, warps 2-9 epilogue.
 #include <cuda_fp16.h>
 #include <limits.h>
 
@@ -26,7 +27,7 @@ namespace moe {
 
 constexpr int MU_STAGES = 5;
 constexpr int MU_STAGE_BYTES = A_STAGE_BYTES + HALF_B_BYTES;   // 128 rows of A, up to 128 of the tile's columns
-constexpr int MU_EPI_WARPS = 8, MU_THREADS = 32 * (3 + MU_EPI_WARPS);
+constexpr int MU_EPI_WARPS = 8, MU_THREADS = 32 * (2 + MU_EPI_WARPS);
 constexpr int MU_BOX = 32 * 64 * 2;
 constexpr int MU_SLOTS = 3;          // tickets taken ahead
 constexpr int MU_DEPS = MU_SLOTS + 1; // items that the loader can be ahead of the epilogue, and one
@@ -48,12 +49,14 @@ static_assert(MU_SMEM <= 227 * 1024, "shared memory budget");
 
 struct MuonItem {
   int phase, step, mat, m0, n0, nt;
+  int tile, part;   // GRAM, JOIN: of the matrix's symmetric tiles; part of the reduction, strip of the tile
   int need;   // the matrix's counter when the phase before is complete
 };
 
 // Tiles of a matrix's phases and how items go through them: `sub` matrices at a time, step by step, phase by phase, matrix by matrix.
 struct MuonOrder {
-  int blocks, per_block, tri, app, app_cols, per_step;   // rows of 256 of a symmetric matrix, tiles across one of its blocks; tiles
+  int blocks, per_block, tri, app, app_cols;   // rows of 256 of a symmetric matrix, tiles across one of its blocks; tiles
+  int gram, join, per_step;                    // items
   __host__ __device__ explicit MuonOrder(const MuonArgs& a) {
     const int m = a.rows < a.cols ? a.rows : a.cols;
     blocks = (m + MUON_BLOCK - 1) / MUON_BLOCK;
@@ -61,7 +64,9 @@ struct MuonOrder {
     tri = per_block * (blocks * (blocks + 1) / 2 - 1) + (m - (blocks - 1) * MUON_BLOCK + a.nt_tri - 1) / a.nt_tri;
     app_cols = (a.cols + a.nt_app - 1) / a.nt_app;
     app = (a.rows + 255) / 256 * app_cols;
-    per_step = 2 * tri + app;
+    gram = tri * a.split;
+    join = a.split > 1 ? tri * a.strips : 0;
+    per_step = gram + join + tri + app;
   }
   __host__ __device__ long total(const MuonArgs& a) const { return (long)a.n * a.steps * per_step; }
   __device__ __forceinline__ MuonItem decode(const MuonArgs& a, int t) const {
@@ -72,29 +77,31 @@ struct MuonOrder {
     r.step = t / (s * per_step);
     t -= r.step * s * per_step;
     r.need = r.step * per_step;
-    int tiles = tri;
+    int items = gram;   // of a matrix's phase
     r.phase = MUON_GRAM;
-    if (t >= s * tri) {
-      t -= s * tri;
-      r.need += tri;
-      r.phase = MUON_POLY;
-      if (t >= s * tri) {
-        t -= s * tri;
-        r.need += tri;
-        r.phase = MUON_APPLY;
-        tiles = app;
-      }
+    while (t >= s * items) {
+      t -= s * items;
+      r.need += items;
+      ++r.phase;
+      items = r.phase == MUON_JOIN ? join : r.phase == MUON_POLY ? tri : app;
     }
     r.need *= MU_PARTS;
-    const int q = t / tiles;
-    t -= q * tiles;
+    const int q = t / items;
+    t -= q * items;
     r.mat = g * a.sub + q;
+    r.part = 0;
     int i = 0;
     if (r.phase == MUON_APPLY) {
       i = t / app_cols;
       t -= i * app_cols;
       r.nt = a.nt_app;
     } else {
+      if (r.phase != MUON_POLY) {
+        const int parts = r.phase == MUON_GRAM ? a.split : a.strips;
+        r.part = t % parts;
+        t /= parts;
+      }
+      r.tile = t;
       for (int c = per_block; i + 1 < blocks && t >= c; c += per_block, ++i) t -= c;   // row i: (i + 1) blocks; the last one's end at m
       r.nt = a.nt_tri;
     }
@@ -126,6 +133,13 @@ __device__ __forceinline__ void tc_mma4_pair_steps(uint32_t d_tmem, uint32_t a_l
       " @e tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, 1;\n}"
       ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(a_step), "r"(b_step)
       : "memory");
+}
+
+// k-blocks [first, end) of an item's products
+__device__ __forceinline__ int2 muon_blocks(const MuonArgs& a, const MuonItem& it) {
+  const int K = it.phase == MUON_GRAM ? max(a.rows, a.cols) : min(a.rows, a.cols), all = (K + BK - 1) / BK;
+  if (it.phase != MUON_GRAM) return make_int2(0, all);
+  return make_int2((int)((long)all * it.part / a.split), (int)((long)all * (it.part + 1) / a.split));
 }
 
 // Whether the operands' k-block kb lies MN-major: X by its place in the product, a symmetric matrix beyond its stored blocks.
@@ -233,7 +247,18 @@ __device__ __forceinline__ void muon_box_out(const MuonArgs& a, float* v, uint8_
 }
 // The same for rows that are no whole vectors: X' in fp32 through both boxes, so that a row's elements are next to one another when they
 // are written (a lane a row, 7 matrices 333 x 1171: 30 us more)
-__device__ __forceinline__ void muon_rows_out(const MuonArgs& a, const float* v, uint8_t* boxes, int lane, int mat, int r0, int c0) {
+__device__ __forceinline__ void muon_rows_out(const MuonArgs& a, const MuonArgs::Step& k, uint32_t tcol, uint8_t* boxes, bool lo, int lane, int mat, int r0, int c0) {
+  float v[64];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) tmem_ld16(tcol + 16 * q, v + 16 * q);
+  tmem_ld_wait();
+  if (lo) {
+    muon_box_apply<true, false, false>(k, v, boxes, boxes + MU_BOX, lane, 0);
+    muon_box_apply<true, false, false>(k, v + 32, boxes, boxes + MU_BOX, lane, 4);
+  } else {
+    muon_box_apply<false, false, false>(k, v, boxes, boxes + MU_BOX, lane, 0);
+    muon_box_apply<false, false, false>(k, v + 32, boxes, boxes + MU_BOX, lane, 4);
+  }
   __syncwarp();   // X has been read from the boxes
 #pragma unroll
   for (int j = 0; j < 16; ++j)
@@ -251,22 +276,49 @@ __device__ __forceinline__ void muon_rows_out(const MuonArgs& a, const float* v,
   }
 }
 
-// A role's place in the ring of tickets
+// JOIN: a strip of a tile's rows from the tile's parts, in their order; w: the warp of the pair.  Read past L1, which may hold an earlier
+// step's.
+__device__ __forceinline__ void muon_join(const MuonArgs& a, const MuonItem& it, int tri, int w, int lane) {
+  const int m = min(a.rows, a.cols), rows = 256 / a.strips, quads = it.nt / 4, row0 = it.part * rows;
+  const float scale = a.step[0].gram_acc;
+  const size_t step = (size_t)256 * it.nt / 4;
+  for (int u = w * 32 + lane; u < rows * quads; u += MU_PARTS * 32) {
+    const int row = row0 + u / quads, c = u % quads * 4, r = it.m0 + row;
+    if (r >= m) break;
+    const float4* p = reinterpret_cast<const float4*>(a.part_ptr + (((size_t)it.mat * tri + it.tile) * a.split * 256 + row) * it.nt + c);
+    float4 s = __ldcg(p);
+#pragma unroll 8
+    for (int i = 1; i < a.split; ++i) {
+      const float4 x = __ldcg(p + i * step);
+      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+    }
+    if (it.n0 + c < a.lda)   // columns behind m are room
+      *reinterpret_cast<uint2*>(a.a_ptr + ((size_t)it.mat * m + r) * a.lda + it.n0 + c) =
+          make_uint2(pack_h2(s.x * scale, s.y * scale), pack_h2(s.z * scale, s.w * scale));
+  }
+}
+
+// A role's place in the ring of tickets.  The slot of an item is free for another once all have read it -- where a phase has few items
+// (SPLIT), once the epilogue is done with it: a pair that took its next item early would keep it from an idle one.
 struct MuonTickets {
   uint32_t slot = 0, par = 0;
   // all lanes: the next item; -1 after a failed wait
-  __device__ __forceinline__ int next(MuonBarriers* bars, const WaitCtl& wc, uint32_t sleep_ns) {
+  __device__ __forceinline__ int next(MuonBarriers* bars, int slots, const WaitCtl& wc, uint32_t sleep_ns, bool keep = false) {
     int t = -1;
     if ((threadIdx.x & 31) == 0) {
       if (mbar_wait_cluster(&bars->item_full[slot], par, wc, SITE_DEP, 0, sleep_ns)) t = *reinterpret_cast<volatile int*>(&bars->item[slot]);
-      mbar_arrive_cluster_addr(map_to_rank(smem_u32(&bars->item_empty[slot]), 0));
+      if (!keep) free(bars, slot);
     }
-    if (++slot == MU_SLOTS) { slot = 0; par ^= 1; }
+    if (++slot == (uint32_t)slots) { slot = 0; par ^= 1; }
     return uniform(t);
+  }
+  __device__ __forceinline__ static void free(MuonBarriers* bars, uint32_t slot) {   // one lane
+    mbar_arrive_cluster_addr(map_to_rank(smem_u32(&bars->item_empty[slot]), 1));   // where the tickets are taken
   }
 };
 
-template <bool WIDE>
+// SPLIT: GRAM's reduction is (a.split > 1); VEC: a.vec.  Of their own, so that the usual kernel's epilogue keeps its registers.
+template <bool WIDE, bool SPLIT, bool VEC>
 __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __grid_constant__ MuonArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -309,33 +361,19 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
   pdl_wait();
 
   const MuonOrder order(a);
-  const int total = (int)order.total(a);
-  if (warp == 10) {
-    if (rank == 0 && lane == 0) {
-      uint32_t slot = 0, par = 1;
-      for (int t = 0; t < total;) {
-        if (!mbar_wait_cluster(&bars->item_empty[slot], par, wc, SITE_EMPTY, t, 50)) break;
-        t = atomicAdd(a.ctr + a.n, 1);
-        const uint32_t at = smem_u32(&bars->item[slot]), full = smem_u32(&bars->item_full[slot]);
-#pragma unroll
-        for (uint32_t r = 0; r < 2; ++r) {
-          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(at, r)), "r"(t) : "memory");
-          mbar_arrive_cluster_addr(map_to_rank(full, r));
-        }
-        if (++slot == MU_SLOTS) { slot = 0; par ^= 1; }
-      }
-    }
-  } else if (warp == 0) {
+  const int total = (int)order.total(a), slots = SPLIT ? 1 : MU_SLOTS;
+  if (warp == 0) {
     MuonTickets tk;
     uint32_t s = 0, par = (1u << MU_STAGES) - 1, dep = 0;
     for (bool ok = true; ok;) {
-      const int t = tk.next(bars, wc, 20);
+      const int t = tk.next(bars, slots, wc, 20);
       if (t < 0 || t >= total) break;
       const MuonItem it = order.decode(a, t);
       const MuonMajors<WIDE> mj(it);
       const int half = it.nt / 2, mat = uniform(it.mat), cur = it.step & 1;
       const int m0 = uniform(it.m0 + rank * 128), n0 = uniform(it.n0 + rank * half);
-      const int K = it.phase == MUON_GRAM ? max(a.rows, a.cols) : min(a.rows, a.cols), nkb = uniform((K + BK - 1) / BK);
+      const int2 blocks = muon_blocks(a, it);
+      const int kb0 = uniform(blocks.x), kb1 = uniform(blocks.y);
       // K-major and MN-major maps of both operands
       const CUtensorMap *a_k = &a.a128, *a_mn = &a.a64, *b_k = &a.a_part, *b_mn = &a.a64;
       if (it.phase == MUON_GRAM) {
@@ -354,8 +392,9 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       fence_proxy_async_global();   // what the counter announces was written by other CTAs' stores
       if (lane == 0) mbar_arrive_cta(&bars->dep[dep]);
       if (++dep == MU_DEPS) dep = 0;
+      if (SPLIT && it.phase == MUON_JOIN) continue;
       const int b_boxes = (half + 63) / 64;
-      for (int kb = 0; kb < nkb; ++kb) {
+      for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait_warp(&bars->empty[s], (par >> s) & 1, wc, SITE_EMPTY, t, 20)) { ok = false; break; }
         uint8_t* st = smem + s * MU_STAGE_BYTES;
         const bool amn = kb >= mj.a_from, bmn = kb >= mj.b_from;
@@ -377,44 +416,59 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
         if (++s == MU_STAGES) s = 0;
       }
     }
-  } else if (warp == 1) {
-    if (rank == 0) {
-      MuonTickets tk;
-      const uint32_t at0 = smem_u32(smem), bt0 = smem_u32(smem + A_STAGE_BYTES);
-      const uint32_t a_lo0[2] = {smem_desc_lo(at0, 16), smem_desc_lo(at0, MN_BOX_BYTES)}, b_lo0[2] = {smem_desc_lo(bt0, 16), smem_desc_lo(bt0, MN_BOX_BYTES)};
-      uint32_t s = 0, par = 0, acc = 0, acc_par = 3;
-      bool ok = true;
-      for (;;) {
-        const int t = tk.next(bars, wc, 0);
-        if (t < 0) ok = false;
-        if (t < 0 || t >= total) break;
-        const MuonItem it = order.decode(a, t);
-        const MuonMajors<WIDE> mj(it);
-        const int K = it.phase == MUON_GRAM ? max(a.rows, a.cols) : min(a.rows, a.cols), nkb = uniform((K + BK - 1) / BK);
-        const uint32_t idesc = uniform(make_idesc_f16(256, it.nt, 0, 0));
-        const int a_from = uniform(mj.a_from), b_from = uniform(mj.b_from);
-        if (!mbar_wait_warp(&bars->tmem_empty[acc], (acc_par >> acc) & 1, wc, SITE_TMEM_EMPTY, t)) { ok = false; break; }
-        acc_par ^= 1u << acc;
+  } else if (warp == 1 && rank == 0) {
+    MuonTickets tk;
+    const uint32_t at0 = smem_u32(smem), bt0 = smem_u32(smem + A_STAGE_BYTES);
+    const uint32_t a_lo0[2] = {smem_desc_lo(at0, 16), smem_desc_lo(at0, MN_BOX_BYTES)}, b_lo0[2] = {smem_desc_lo(bt0, 16), smem_desc_lo(bt0, MN_BOX_BYTES)};
+    uint32_t s = 0, par = 0, acc = 0, acc_par = 3;
+    bool ok = true;
+    for (;;) {
+      const int t = tk.next(bars, slots, wc, 0);
+      if (t < 0) ok = false;
+      if (t < 0 || t >= total) break;
+      const MuonItem it = order.decode(a, t);
+      if (SPLIT && it.phase == MUON_JOIN) continue;
+      const MuonMajors<WIDE> mj(it);
+      const int2 blocks = muon_blocks(a, it);
+      const int kb0 = uniform(blocks.x), kb1 = uniform(blocks.y);
+      const uint32_t idesc = uniform(make_idesc_f16(256, it.nt, 0, 0));
+      const int a_from = uniform(mj.a_from), b_from = uniform(mj.b_from);
+      if (!mbar_wait_warp(&bars->tmem_empty[acc], (acc_par >> acc) & 1, wc, SITE_TMEM_EMPTY, t)) { ok = false; break; }
+      acc_par ^= 1u << acc;
+      tc_fence_after_sync();
+      const uint32_t d_tmem = uniform(tmem_base + acc * 256);
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!mbar_wait_warp(&bars->full[s], (par >> s) & 1, wc, SITE_FULL, t)) { ok = false; break; }
+        par ^= 1u << s;
         tc_fence_after_sync();
-        const uint32_t d_tmem = uniform(tmem_base + acc * 256);
-        for (int kb = 0; kb < nkb; ++kb) {
-          if (!mbar_wait_warp(&bars->full[s], (par >> s) & 1, wc, SITE_FULL, t)) { ok = false; break; }
-          par ^= 1u << s;
-          tc_fence_after_sync();
-          const uint32_t at = s * (MU_STAGE_BYTES >> 4), amn = kb >= a_from, bmn = kb >= b_from;
-          tc_mma4_pair_steps(d_tmem, (amn ? a_lo0[1] : a_lo0[0]) + at, (bmn ? b_lo0[1] : b_lo0[0]) + at, smem_desc_hi(1024),
-                             idesc | amn << 15 | bmn << 16, kb != 0, amn ? 2048 >> 4 : 2, bmn ? 2048 >> 4 : 2);
-          tc_commit_pair(&bars->empty[s]);
-          if (++s == MU_STAGES) s = 0;
-        }
-        if (!ok) break;
-        tc_commit_pair(&bars->tmem_full[acc]);
-        acc ^= 1;
+        const uint32_t at = s * (MU_STAGE_BYTES >> 4), amn = kb >= a_from, bmn = kb >= b_from;
+        tc_mma4_pair_steps(d_tmem, (amn ? a_lo0[1] : a_lo0[0]) + at, (bmn ? b_lo0[1] : b_lo0[0]) + at, smem_desc_hi(1024),
+                           idesc | amn << 15 | bmn << 16, kb != kb0, amn ? 2048 >> 4 : 2, bmn ? 2048 >> 4 : 2);
+        tc_commit_pair(&bars->empty[s]);
+        if (++s == MU_STAGES) s = 0;
       }
-      if (uniform(!ok || *reinterpret_cast<volatile int*>(&a.status->abort) ? 1 : 0)) {
-        tc_commit_pair(&bars->drain);
-        const WaitCtl shortwc{a.status, 20ull * 1000 * 1000};
-        mbar_wait_warp(&bars->drain, 0, shortwc, SITE_DRAIN, 0);
+      if (!ok) break;
+      tc_commit_pair(&bars->tmem_full[acc]);
+      acc ^= 1;
+    }
+    if (uniform(!ok || *reinterpret_cast<volatile int*>(&a.status->abort) ? 1 : 0)) {
+      tc_commit_pair(&bars->drain);
+      const WaitCtl shortwc{a.status, 20ull * 1000 * 1000};
+      mbar_wait_warp(&bars->drain, 0, shortwc, SITE_DRAIN, 0);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {   // the odd CTA's
+      uint32_t slot = 0, par = 1;
+      for (int t = 0; t < total;) {
+        if (!mbar_wait_cluster(&bars->item_empty[slot], par, wc, SITE_EMPTY, t, 50)) break;
+        t = atomicAdd(a.ctr + a.n, 1);
+        const uint32_t at = smem_u32(&bars->item[slot]), full = smem_u32(&bars->item_full[slot]);
+#pragma unroll
+        for (uint32_t r = 0; r < 2; ++r) {
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(at, r)), "r"(t) : "memory");
+          mbar_arrive_cluster_addr(map_to_rank(full, r));
+        }
+        if (++slot == (uint32_t)slots) { slot = 0; par ^= 1; }
       }
     }
   } else {
@@ -425,19 +479,30 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
     uint64_t* in_full = &bars->in_full[ew];
     uint32_t acc = 0, full_par = 0, in_par = 0, dep = 0, dep_par = 0;
     for (bool ok = true; ok;) {
-      const int t = tk.next(bars, wc, 100);
-      if (t < 0 || t >= total) break;
+      const int t = tk.next(bars, slots, wc, 100, SPLIT);
+      if (t < 0 || t >= total) break;   // (a kept slot is the only one, and nobody waits for it any more)
       const MuonItem it = order.decode(a, t);
       const MuonArgs::Step k = a.step[it.step];   // (a copy: by reference the factors were read again for every chunk, 1.4 us a box)
       const int m = min(a.rows, a.cols), cur = it.step & 1;
       const int M = it.phase == MUON_APPLY ? a.rows : m, N = it.phase == MUON_APPLY ? a.cols : m;
       const bool last = it.phase == MUON_APPLY && it.step + 1 == a.steps;
       const bool lo = it.phase == MUON_APPLY && it.step < MUON_LATE, lo_out = it.phase == MUON_APPLY && !last && it.step + 1 < MUON_LATE;
-      const bool upd = last && !lo && a.vec && a.w_ptr;   // W comes with X
+      const bool upd = last && !lo && VEC && a.w_ptr;   // W comes with X
       const int r0 = it.m0 + rank * 128 + quad * 32;
       // the loader polls the counter for the CTA: with its eight epilogue warps polling too, 7 matrices 336 x 1176 took TODO us longer
       if (!mbar_wait_warp(&bars->dep[dep], dep_par, wc, SITE_DEP, t, 50)) break;
       if (++dep == MU_DEPS) { dep = 0; dep_par ^= 1; }
+      if (SPLIT && it.phase == MUON_JOIN) {
+        muon_join(a, it, order.tri, rank * MU_EPI_WARPS + ew, lane);
+        fence_proxy_async_global();   // every lane's stores, for the loads to come
+        __syncwarp();
+        if (lane == 0) {
+          if (SPLIT) MuonTickets::free(bars, 0);
+          counter_signal(a.ctr + it.mat, 1);
+        }
+        continue;
+      }
+      const bool parts = SPLIT && it.phase == MUON_GRAM;
       bool up = false;   // the accumulator has been seen complete
       for (int b = (ew >> 2) * 64; b < it.nt; b += 128) {
         const int c0 = it.n0 + b;
@@ -468,19 +533,8 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
         }
         if (!ok) break;
         const uint32_t tcol = tmem_base + acc * 256 + b + (static_cast<uint32_t>(quad * 32) << 16);
-        if (last && !a.vec) {
-          float v[64];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) tmem_ld16(tcol + 16 * q, v + 16 * q);
-          tmem_ld_wait();
-          if (lo) {
-            muon_box_apply<true, false, false>(k, v, box0, box1, lane, 0);
-            muon_box_apply<true, false, false>(k, v + 32, box0, box1, lane, 4);
-          } else {
-            muon_box_apply<false, false, false>(k, v, box0, box1, lane, 0);
-            muon_box_apply<false, false, false>(k, v + 32, box0, box1, lane, 4);
-          }
-          muon_rows_out(a, v, box0, lane, it.mat, r0, c0);
+        if (!VEC && last) {
+          muon_rows_out(a, a.step[it.step], tcol, box0, lo, lane, it.mat, r0, c0);
           continue;
         }
 #pragma unroll 1
@@ -489,7 +543,11 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
           tmem_ld16(tcol + 8 * j0, v);
           tmem_ld16(tcol + 8 * j0 + 16, v + 16);
           tmem_ld_wait();
-          if (it.phase == MUON_GRAM) {
+          if (parts) {   // 32 columns in fp32 a box
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              *reinterpret_cast<float4*>(box_chunk(j0 ? box1 : box0, lane, j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          } else if (it.phase == MUON_GRAM) {
             muon_box_gram(k, v, box0, lane, j0);
           } else if (it.phase == MUON_POLY) {
             muon_box_poly(k, v, box0, lane, j0, r0 + lane - c0 - 8 * j0);
@@ -497,14 +555,19 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
             if (lo_out) muon_box_apply<true, true, true>(k, v, box0, box1, lane, j0);
             else if (lo) muon_box_apply<true, true, false>(k, v, box0, box1, lane, j0);
             else muon_box_apply<false, true, false>(k, v, box0, box1, lane, j0);
-          } else {
+          } else if (VEC) {
             if (lo) muon_box_apply<true, false, false>(k, v, box0, box1, lane, j0);
             else muon_box_apply<false, false, false>(k, v, box0, box1, lane, j0);
             muon_box_out(a, v, box0, box1, lane, j0, lo, it.mat, r0 + lane, c0);
           }
         }
         staging_release();
-        if (lane == 0) {
+        if (lane == 0 && parts) {
+          const int y = ((it.mat * order.tri + it.tile) * a.split + it.part) * 256 + rank * 128 + quad * 32;
+          tma_store_2d(&a.part, b, y, box0);
+          tma_store_2d(&a.part, b + 32, y, box1);
+          tma_store_commit();
+        } else if (lane == 0) {
           const CUtensorMap* o = it.phase == MUON_GRAM ? &a.abox : it.phase == MUON_POLY ? &a.bbox : last ? &a.out : &a.xhi[cur ^ 1];
           tma_store_3d(o, c0, r0, last ? a.z0 + it.mat : it.mat, box0);
           if (lo_out) tma_store_3d(&a.xlo[cur ^ 1], c0, r0, it.mat, box1);
@@ -516,6 +579,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       __syncwarp();
       if (lane == 0) {
         mbar_arrive_leader(&bars->tmem_empty[acc]);
+        if (SPLIT) MuonTickets::free(bars, 0);
         if (!last && ok) {   // this warp's part of the tile is stored
           tma_store_wait_all();
           fence_proxy_async_global();
@@ -539,12 +603,20 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
   }
 }
 
+template <bool WIDE, bool SPLIT, bool VEC>
+static cudaError_t launch_one(const MuonArgs& a, int sms, cudaStream_t s) {
+  static PairLaunchState st;
+  return launch_on_pairs(st, muon_products_kernel<WIDE, SPLIT, VEC>, a, MU_THREADS, MU_SMEM, sms, s, true);
+}
+template <bool WIDE>
+static cudaError_t launch_of(const MuonArgs& a, int sms, cudaStream_t s) {
+  if (a.split > 1) return a.vec ? launch_one<WIDE, true, true>(a, sms, s) : launch_one<WIDE, true, false>(a, sms, s);
+  return a.vec ? launch_one<WIDE, false, true>(a, sms, s) : launch_one<WIDE, false, false>(a, sms, s);
+}
 cudaError_t launch_muon_products(bool wide, const MuonArgs& a, int num_sms, cudaStream_t s) {
-  static PairLaunchState st[2];
   const long tiles = MuonOrder(a).total(a);
   const int sms = (int)(2 * tiles < num_sms ? 2 * tiles : num_sms);
-  return wide ? launch_on_pairs(st[1], muon_products_kernel<true>, a, MU_THREADS, MU_SMEM, sms, s, true)
-              : launch_on_pairs(st[0], muon_products_kernel<false>, a, MU_THREADS, MU_SMEM, sms, s, true);
+  return wide ? launch_of<true>(a, sms, s) : launch_of<false>(a, sms, s);
 }
 
 }  // namespace moe
