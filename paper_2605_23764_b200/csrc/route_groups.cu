@@ -320,14 +320,22 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS<NPL>, ROUTE_BLOCKS<NPL>) rout
           kept = exact_groups(exact, c64, G, a.top_groups, a.group_top, lane);
       }
     }
-    // without a bias the experts' order is that of the logits, in v unless scores were needed for the groups
-    uint32_t key[NPL];
-    const bool mine_kept = kept >> (lane >> span_log) & 1;
+    if (scored && !a.bias) {   // the experts' order is that of the logits, scores were for the groups
 #pragma unroll
-    for (int i = 0; i < NPL; ++i) {
-      const int e = expert(i);
-      const bool in = (WHOLE || e < E) && (by_lanes ? mine_kept : (kept >> (e * per_gs >> 20 & 31) & 1) != 0);
-      key[i] = in ? float_key(a.bias || !scored ? v[i] : row[e]) : 0u;
+      for (int i = 0; i < NPL; ++i) v[i] = WHOLE || expert(i) < E ? row[expert(i)] : -INFINITY;
+    }
+    uint32_t key[NPL];
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) key[i] = WHOLE || expert(i) < E ? float_key(v[i]) : 0u;
+    if (pick) {
+      if (by_lanes) {
+        const bool in = kept >> (lane >> span_log) & 1;
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) key[i] = in ? key[i] : 0u;
+      } else {
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) key[i] = kept >> (expert(i) * per_gs >> 20 & 31) & 1 ? key[i] : 0u;
+      }
     }
     // a bound that the `want` largest reach and few others: the want-th largest of the lanes' largest
     uint32_t top = lane_max<NPL>(key), bound = 0;
