@@ -116,6 +116,39 @@ def test_spectra(rows, cols, kind):
     _near(MoeMuon(1, rows, cols).orthogonalize(G), _exact(G))
 
 
+def _noise(G):
+    """What roundings relative to the largest singular value can do to the smaller ones, in the norm, once steps enough have brought all of them
+    to 1: a step's 2^-11 / sqrt(3) x 2.75 of it (the norm of B) enters each, and a step later they are 3.4445 times as large, so what
+    enters adds up to 3.2e-4 of the largest, 3.2e-4 / tau of a value tau times as large."""
+    s = torch.linalg.svdvals(G.double())
+    return (3.2e-4 / (s / s[:, :1]).clamp(min=1e-30)).clamp(max=1.0).square().mean(1).sqrt().max().item()
+
+
+@pytest.mark.parametrize("n,rows,cols,steps", [(50, 300, 700, 5), (50, 700, 300, 5), (150, 200, 440, 6), (50, 264, 1056, 7), (150, 130, 401, 5), (25, 520, 1200, 9)])
+@pytest.mark.parametrize("kind", ["full", "low_rank"])
+def test_late_steps_together(n, rows, cols, steps, kind):
+    """Many matrices at least twice as long as wide: pairs of late steps go through the Gram matrix.  The products between round once more
+    where nothing is amplified any longer, within the same bound.  Gradients of fewer tokens than either side has, whose other singular values
+    are what bf16 makes of zero, 1e-3 of the largest, are brought to 1 by more than five steps: there what roundings do to those counts (_noise)."""
+    from paper_2605_23764_b200 import MoeMuon
+    G = _gradient(n, rows, cols, steps)
+    norm = NORM
+    if kind == "low_rank":
+        g = torch.Generator(device="cuda").manual_seed(9)
+        G = (torch.randn(n, rows, 100, device="cuda", generator=g) @ torch.randn(n, 100, cols, device="cuda", generator=g)).to(torch.bfloat16)
+        if steps > 5:
+            norm += _noise(G[:2])
+    muon = MoeMuon(n, rows, cols, steps=steps)
+    out = muon.orthogonalize(G)
+    assert muon.status() == (0, 0)
+    _near(out, _exact(G, steps=steps), norm)
+    W, M = _gradient(n, rows, cols, 1, scale=0.1), torch.zeros(n, rows, cols, device="cuda")
+    W1, _ = muon.step(W, M, G, lr=0.01, W_out=torch.empty_like(W), M_out=torch.empty_like(M))
+    x = _exact(1.95 * G.double(), steps=steps)
+    want = W.double() - 0.01 * x
+    assert bool(((W1.double() - want).abs() <= 0.01 * 10 * norm * x.abs().amax() + BF16 * (want.abs() + 0.01 * x.abs())).all())
+
+
 def _bits(t):
     return t.contiguous().view(torch.int16 if t.element_size() == 2 else torch.int32)
 
