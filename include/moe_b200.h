@@ -344,11 +344,15 @@ int moe_ffn_fwd_w4(moe_ctx* ctx, const uint16_t* x, const int32_t* topk_ids, con
  *   moe_muon_orthogonalize   u = G (bf16 or fp32, MOE_MUON_*) -> out bf16
  *   moe_muon_step            M_out = momentum M + dW;  u = dW + momentum M_out with nesterov, else M_out;
  *                            W_out = (1 - lr weight_decay) W - lr scale X;  W, dW, W_out bf16, M, M_out fp32; M_out may be M, W_out may be W
- * Products take fp16 operands (X to 11 significant bits) and sum in fp32; the linear term takes X to 22 bits.  For five such steps X is
- * 1e-3 off in the norm before it is rounded to bf16 (itself 1.7e-3).  A matrix with NaN or infinite elements gives NaN, the others are not affected.
+ * Products take fp16 operands (11 significant bits) and sum in fp32; the linear term a X keeps 22 bits of X or more while that counts (the
+ * first three steps; matrices up to 128 x 384 all along).  After five such steps X is 1e-3 off in the norm before it is rounded to bf16
+ * (itself 1.7e-3).  Singular values far below the largest, tau times it, carry noise of some 3e-4 / tau of their own by then: gradients of
+ * rank 256 of 512 are 2e-3 off, and more steps, which bring such values to 1, show more of it.
+ * A matrix with NaN or infinite elements gives NaN, the others are not affected.
  *
  * moe_muon_create: like moe_create; the workspace (moe_muon_workspace_bytes, 0 for an invalid shape; 256-byte aligned device memory, or
- * NULL) holds a batch of the matrices, about 1 GB at most unless a single one needs more.  Tensors need their type's alignment only;
+ * NULL) holds a batch of the matrices, about 1 GB at most unless a single one needs more (next to nothing for matrices up to 128 x 384,
+ * which stay on the chip).  Tensors need their type's alignment only;
  * 16-byte aligned ones with cols % 8 == 0 are read and written in vectors.  1 <= n, rows, cols <= MOE_MUON_MAX_SIZE,
  * 1 <= steps <= MOE_MUON_MAX_STEPS, eps >= 0.  Calls are asynchronous on `stream`; like a moe_ctx, a moe_muon serves one call at a
  * time, and two captured graphs that use one must not run at the same time. */

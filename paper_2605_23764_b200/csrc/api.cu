@@ -1649,6 +1649,7 @@ int moe_muon_step(moe_muon* u, const uint16_t* W, const float* M, const uint16_t
   if (!u || !W || !M || !dW || !W_out || !M_out) return MOE_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(W) | reinterpret_cast<uintptr_t>(dW) | reinterpret_cast<uintptr_t>(W_out)) & 1) return MOE_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(M) | reinterpret_cast<uintptr_t>(M_out)) & 3) return MOE_ERR_INVALID_ARG;
+  if (!std::isfinite(momentum) || !std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(scale)) return MOE_ERR_INVALID_ARG;
   if (!on_its_device(u)) return MOE_ERR_INVALID_ARG;
   u->last_stream = static_cast<cudaStream_t>(stream);
   u->launches = 0;

@@ -65,6 +65,14 @@ float real(PyObject* o) {
   }
   return (float)v;
 }
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) {
+    PyErr_Clear();
+    throw Slow();
+  }
+  return v != 0;
+}
 int64_t integer(PyObject* o) {
   if (!PyLong_CheckExact(o)) throw Slow();
   int over = 0;
@@ -359,7 +367,7 @@ PyObject* route_grouped_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t T = rows_of(l);
     const float *logits = here<float>(a[1], F32, T * s.E), *bias = here_or_null<float>(a[2], F32, s.E);
     const moe_route_groups g{(int32_t)integer(a[3]), (int32_t)integer(a[4]), (int32_t)integer(a[5]), real(a[6])};
-    const bool with_counts = a[7] == Py_True;
+    const bool with_counts = truth(a[7]);
     at::Tensor ids = empty({T, s.k}, I32, l), w = empty({T, s.k}, F32, l), counts;
     if (with_counts) counts = empty({s.E}, I32, l);
     int32_t *pi = ids.data_ptr<int32_t>(), *pc = with_counts ? counts.data_ptr<int32_t>() : nullptr;
@@ -445,7 +453,7 @@ PyObject* muon_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t ne = elems_of(m);
     const uint16_t *W = here<uint16_t>(a[1], BF, ne), *dW = here<uint16_t>(a[3], BF, ne);
     const float *M = here<float>(a[2], F32, ne), mu = real(a[4]), lr = real(a[6]), wd = real(a[7]), scale = real(a[8]);
-    const bool nesterov = a[5] == Py_True;
+    const bool nesterov = truth(a[5]);
     uint16_t* Wo = here<uint16_t>(a[9], BF, ne);
     float* Mo = here<float>(a[10], F32, ne);
     void* st = stream();

@@ -1,18 +1,23 @@
 // The products of an orthogonalisation (muon.cuh) on the tensor cores: one persistent launch for all steps of a batch of matrices.
 //
-// Where there are few tiles and a long reduction, GRAM sums parts of it and a phase more joins them (one matrix of 256 x 7168: 210 -> TODO us).
-// Items are tiles of 256 rows x 256 columns (fewer where there are not enough of them) of one matrix's product.  The phases of a matrix follow one another; an item
-// waits until all tiles of its matrix's phase before have been stored (a counter a matrix), which other matrices' tiles cover.
-// CTA pairs take items from a ticket in that order, so whichever pairs are resident make progress.  The accumulator is one of two in
-// TMEM: a tile's products run beside the epilogue of the one before.
+// Items are tiles of 256 rows x 256 columns (fewer where there are not enough of them) of one matrix's product.  The products of a matrix
+// follow one another; an item waits until all items of its matrix's product before have been stored (a counter a matrix), which other
+// matrices' tiles cover.  CTA pairs take items from a ticket in that order, so whichever pairs are resident make progress.  The accumulator
+// is one of two in TMEM: a tile's products run beside the epilogue of the one before.
 //
 // Operands come in as they lie: K-major where the reduction is contiguous, MN-major where it is the rows (X as the second operand of
-// B X, both of X^T X), so nothing is ever transposed in memory.  A and B are symmetric: tiles above the diagonal are neither computed
-// nor stored, and an operand's k-blocks that would lie there are read from their mirror image, MN-major -- the instruction descriptor
-// changes from k-block to k-block.  (Stored twice, as they are and mirrored, they cost the epilogue 2.3 times the shared-memory accesses.)
+// B X, both of X^T X), so nothing is ever transposed in memory.  A, B and their like are symmetric: tiles above the diagonal are neither
+// computed nor stored, and an operand's k-blocks that would lie there are read from their mirror image, MN-major -- the instruction
+// descriptor changes from k-block to k-block.  (Stored twice, as they are and mirrored, 132 matrices 1408 x 2048 took 14.2 ms instead of 12.0.)
 //
-// What bounds it: shared memory.  A k-block brings 32 KB into an SM and the products read 32 KB, 512 clocks' worth at 128 bytes a clock,
-// which is what the products take; the epilogue's boxes come on top.
+// Where there are few tiles and a long reduction, GRAM sums parts of it and JOIN adds them up in their order (one matrix of 256 x 7168:
+// 210 -> 155 us).
+//
+// What bounds it.  Large batches: power.  The tensor pipe is active 70 to 77 % of the clocks, at 1.4 GHz under the limit; 1.03 to 1.25 PFLOP/s
+// of executed products, where batched fp16 products of these shapes by the vendor's library sustain 1.07 and 1.16.  Without an epilogue
+// it is 78 to 85 %: a k-block brings 32 KB into an SM and the products read as much, near what shared memory gives in the products' 512 clocks.
+// Few matrices: latency, 3.7 us a product from the signal of the one before (poll 0.5, loads 0.8, products and commit 0.6 and up,
+// epilogue 0.5 to 2.5, stores and signal 0.8).
 //
 // Roles per CTA: warp 0 TMA producer, warp 1 MMA issuer (even CTA) or tickets (odd CTA) and TMEM owner, warps 2-9 epilogue.
 #include <cuda_fp16.h>
@@ -248,7 +253,7 @@ __device__ __forceinline__ void muon_box_out(const MuonArgs& a, float* v, uint8_
   }
 }
 // The same for rows that are no whole vectors: X' in fp32 through both boxes, so that a row's elements are next to one another when they
-// are written (a lane a row, 7 matrices 333 x 1171: 30 us more)
+// are written
 __device__ __forceinline__ void muon_rows_out(const MuonArgs& a, const MuonOp& op, uint32_t tcol, uint8_t* boxes, int lane, int mat, int r0, int c0) {
   float v[64];
 #pragma unroll
@@ -496,7 +501,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       const bool in = apply ? op.use : op.in >= 0;        // the epilogue's input: X, or a symmetric matrix
       const bool upd = last && !lo && VEC && a.w_ptr;     // W comes with it
       const int r0 = it.m0 + rank * 128 + quad * 32;
-      // the loader polls the counter for the CTA: with its eight epilogue warps polling too, 7 matrices 336 x 1176 took TODO us longer
+      // the loader polls the counter for the CTA
       if (!mbar_wait_warp(&bars->dep[dep], dep_par, wc, SITE_DEP, t, 50)) break;
       if (++dep == MU_DEPS) { dep = 0; dep_par ^= 1; }
       if (SPLIT && it.kind == MUON_JOIN) {

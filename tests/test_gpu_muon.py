@@ -49,7 +49,8 @@ def _near(got, want, norm=NORM):
 
 
 SHAPES = [(1, 1, 1), (3, 1, 8), (2, 9, 1), (4, 16, 16), (3, 28, 43), (2, 43, 28), (5, 64, 64), (16, 128, 256), (8, 256, 128), (2, 129, 257), (2, 257, 129),
-          (3, 130, 1000), (3, 1000, 130), (2, 333, 517), (1, 512, 512), (1, 700, 301), (2, 384, 640), (1, 256, 2056), (1, 2056, 264), (1, 1408, 2048), (40, 72, 200)]
+          (3, 130, 1000), (3, 1000, 130), (2, 333, 517), (1, 512, 512), (1, 700, 301), (2, 384, 640), (1, 256, 2056), (1, 2056, 264), (1, 1408, 2048), (40, 72, 200),
+          (2, 128, 384), (2, 384, 128), (1, 129, 384), (1, 128, 385), (1, 385, 65), (700, 24, 40), (150, 257, 260), (1, 64, 4096), (1, 3000, 136)]
 
 
 @pytest.mark.parametrize("n,rows,cols", SHAPES)
@@ -313,6 +314,11 @@ def test_refusals():
         muon.step(G, f, f, 0.1)
     with pytest.raises(MoeError, match="W_out"):
         muon.step(G, f, G, 0.1, W_out=G[:1])
+    for bad in (dict(lr=float("nan")), dict(lr=0.1, weight_decay=float("inf")), dict(lr=0.1, scale=float("nan"))):
+        with pytest.raises(MoeError):
+            muon.step(G, f, G, **bad)
+    keep = [binding.moe_muon_step(muon.handle, G, f, G, 0.9, n, 0.1, 0.0, 1.0, torch.empty_like(G), torch.empty_like(f)) for n in (1, True, 0, False)]
+    assert keep == [None] * 4
     muon.close()
     with pytest.raises(MoeError, match="unknown muon handle"):
         muon.orthogonalize(G)

@@ -267,6 +267,7 @@ def test_empty_batch_and_refusals():
         layer.route_grouped(torch.zeros(24, 16, device="cuda").t(), None)
     with pytest.raises(MoeError):
         layer.route_grouped(torch.zeros(17, 24, device="cuda"))          # more than T_max
+    assert len(layer.route_grouped(l, with_counts=1)) == 3 and len(layer.route_grouped(l, None, 1, 1, 1, 2, 0)) == 2
     with pytest.raises(MoeError, match="accumulate"):
         layer.route_grouped_bwd(l, torch.zeros(16, 4, dtype=torch.int32, device="cuda"), torch.zeros(16, 4, device="cuda"), accumulate=True)
     with pytest.raises(MoeError, match="counts"):
