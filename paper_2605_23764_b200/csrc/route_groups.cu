@@ -66,8 +66,10 @@ __device__ __forceinline__ float shifted_sigmoid(float l, float top) {
 struct RouteRow {
   const float* row;
   const float* bias;
-  int E;
+  int E, log;   // a lane's experts are 2^log neighbours
   bool sigmoid;
+  // Where an expert's bias lies: the lanes' first ones, their second ones, .. (as they come, 16 experts a lane were 16 lanes on a bank)
+  __device__ __forceinline__ static int place(int e, int log) { return (e & ((1 << log) - 1)) << 5 | e >> log; }
 };
 // the softmax's largest logit and sum
 __device__ __forceinline__ void row_sum64(const RouteRow& r, int lane, double& mx, double& den) {
@@ -77,7 +79,7 @@ __device__ __forceinline__ void row_sum64(const RouteRow& r, int lane, double& m
   for (int e = lane; e < r.E; e += 32) mx = fmax(mx, (double)r.row[e]);
 #pragma unroll
   for (int off = 16; off; off >>= 1) mx = fmax(mx, __shfl_xor_sync(ALL, mx, off));
-#pragma unroll 2
+#pragma unroll 4
   for (int e = lane; e < r.E; e += 32) den += exp((double)r.row[e] - mx);
 #pragma unroll
   for (int off = 16; off; off >>= 1) den += __shfl_xor_sync(ALL, den, off);
@@ -85,7 +87,7 @@ __device__ __forceinline__ void row_sum64(const RouteRow& r, int lane, double& m
 __device__ __forceinline__ double choice64(const RouteRow& r, int e, double mx, double den) {
   const double l = (double)r.row[e];
   double s = r.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - mx) / den;
-  if (r.bias) s += (double)r.bias[e];
+  if (r.bias) s += (double)r.bias[RouteRow::place(e, r.log)];
   return l == -INFINITY ? -INFINITY : isnan(s) ? -DBL_MAX : s;
 }
 
@@ -169,10 +171,10 @@ __device__ __noinline__ int exact_choice(RouteRow r, double* c, int k, int n_gro
 constexpr int ROUTE_POOL = 32;   // candidates of a token
 template <int NPL>
 constexpr int ROUTE_WARPS = NPL <= 8 ? 8 : 4;   // of a block: each has a row in 64 bits in shared memory
-// Blocks on an SM: 64 registers a thread, 255 from 1024 experts on.  256 experts in 104 registers: 95 us instead of 78 for 65536 tokens;
-// 512 in 96: 60 instead of 51 for 16384.
+// Blocks on an SM: 64 registers a thread, 80 with 512 experts, 255 with 1024.  256 experts in 104 registers: 95 us instead of 78 for 65536
+// tokens; 512 in 64 or 96: 4 to 9 us more for 16384.
 template <int NPL>
-constexpr int ROUTE_BLOCKS = NPL <= 8 ? 4 : NPL <= 16 ? 8 : 2;
+constexpr int ROUTE_BLOCKS = NPL <= 8 ? 4 : NPL <= 16 ? 6 : 2;
 
 // the two largest of two pairs, the larger first
 __device__ __forceinline__ void top2(float& m1, float& m2, float o1, float o2) {
@@ -194,6 +196,7 @@ __device__ __forceinline__ void top2_add(float& m1, float& m2, float x) {
 template <int NPL, bool WHOLE>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS<NPL>, ROUTE_BLOCKS<NPL>) route_groups_kernel(const RouteGroupsArgs a) {
   constexpr int WARPS = ROUTE_WARPS<NPL>;
+  constexpr int LOG = !WHOLE ? 0 : NPL == 1 ? 0 : NPL == 2 ? 1 : NPL == 4 ? 2 : NPL == 8 ? 3 : NPL == 16 ? 4 : 5;   // of a lane's neighbours
   extern __shared__ double route_smem[];   // [WARPS][E] doubles, bias [E], counts [E]
   __shared__ uint64_t pool_all[WARPS][ROUTE_POOL];
   const int E = WHOLE ? 32 * NPL : a.E, k = a.k, G = a.n_groups, gs = E / G;
@@ -211,7 +214,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS<NPL>, ROUTE_BLOCKS<NPL>) rout
   pdl_wait();
   float b_max = 0.f;
   for (int e = threadIdx.x; e < E; e += 32 * WARPS) {
-    sbias[e] = a.bias ? a.bias[e] : 0.f;
+    sbias[RouteRow::place(e, LOG)] = a.bias ? a.bias[e] : 0.f;
     hist[e] = 0;
   }
   __syncthreads();
@@ -227,11 +230,11 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS<NPL>, ROUTE_BLOCKS<NPL>) rout
   float bias_reg[NPL <= 8 ? NPL : 1];
   if constexpr (NPL <= 8) {
 #pragma unroll
-    for (int i = 0; i < NPL; ++i) bias_reg[i] = WHOLE || expert(i) < E ? sbias[expert(i)] : 0.f;
+    for (int i = 0; i < NPL; ++i) bias_reg[i] = WHOLE || expert(i) < E ? sbias[32 * i + lane] : 0.f;
   }
   auto bias_of = [&](int i) -> float {
     if constexpr (NPL <= 8) return bias_reg[i];
-    else return WHOLE || expert(i) < E ? sbias[expert(i)] : 0.f;
+    else return WHOLE || expert(i) < E ? sbias[32 * i + lane] : 0.f;
   };
 
   const uint32_t below = (1u << lane) - 1u;
@@ -256,7 +259,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS<NPL>, ROUTE_BLOCKS<NPL>) rout
       mx = warp_max(mx);
     }
     bool open = false;   // the token goes through exact_choice
-    const RouteRow exact{row, a.bias ? sbias : nullptr, E, sigmoid};
+    const RouteRow exact{row, a.bias ? sbias : nullptr, E, LOG, sigmoid};
     if (scored) {
       // v becomes c
       if (sigmoid) {
@@ -390,7 +393,11 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS<NPL>, ROUTE_BLOCKS<NPL>) rout
       if (__any_sync(ALL, lane + 1 < want && !(val - next > tol.expert))) {
         // the candidates' order is enough where none of the others can be among the k
         const float least = __shfl_sync(ALL, val, k - 1);
-        if (few && (bound == 1u || least - key_float(bound) > tol.expert)) mine = exact_order(exact, mine, n, reinterpret_cast<int*>(pool), lane);
+        uint32_t rest = 0;
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) rest = max(rest, key[i] < bound ? key[i] : 0u);
+        rest = __reduce_max_sync(ALL, rest);
+        if (few && (rest == 0u || least - key_float(rest) > tol.expert)) mine = exact_order(exact, mine, n, reinterpret_cast<int*>(pool), lane);
         else open = true;
       }
     }
