@@ -930,8 +930,7 @@ constexpr size_t MUON_BATCH_BYTES = size_t(1) << 30;
 struct MuonPlan {
   int m, l, ld, ldm;          // smaller and larger dimension; elements from row to row of X, of A and B
   int batch;                  // matrices of a turn
-  int syms;                   // symmetric matrices in use
-  size_t ctr, part, hi[2], lo[2], sym[MUON_SYMS], sums, total;
+  size_t ctr, part, hi[2], lo[2], A, B, sums, total;
   int nt_tri, nt_app, split;  // tile columns, parts of the reduction of A = X X^T
 };
 
@@ -942,26 +941,6 @@ bool muon_shape_ok(const moe_muon_shape* s) {
     for (int j = 0; j < 3; ++j)
       if (!std::isfinite(s->coefficients[i][j])) return false;
   return true;
-}
-
-// Whether steps k and k + 1 are better taken as one (plan_muon_ops).  That costs five products of m x m by m x m by half, one Gram matrix and one
-// product with X, 5 m^3 + 3 m^2 l, instead of 2 m^3 + 6 m^2 l: with l >= 2 m (2048 x 7168: 142 instead of 207 GFLOP) and tiles enough that nobody
-// waits for the products between.  Their factors' product, of norm under 48, stays in fp16's range.
-bool muon_pairs_steps(const moe_muon_shape& s, int k) {
-  const int m = std::min(s.rows, s.cols), l = std::max(s.rows, s.cols);
-  const long nb = (m + MUON_BLOCK - 1) / MUON_BLOCK;
-  if (k < MUON_LATE || k + 2 > s.steps || l < 2l * m || s.n * (nb * (nb + 1) / 2) < 2 * 74) return false;
-  double norm = 1.0;
-  for (int i = k; i < k + 2; ++i) {
-    const float* c = s.coefficients[i];
-    double most = 0.0;
-    for (int j = 0; j <= 150; ++j) {   // over the squares of the singular values
-      const double x = j * 0.01;
-      most = std::max(most, std::fabs(c[0] + x * (c[1] + x * (double)c[2])));
-    }
-    norm *= most;
-  }
-  return norm <= 48.0;
 }
 
 // Tile columns: the width whose turns over the pairs of SMs are over first.  A k-block takes what its operands' bytes take at 56 a clock (32 KB
@@ -1013,10 +992,7 @@ MuonPlan plan_muon(const moe_muon_shape& s) {
   p.ldm = row_ld(p.m);
   const size_t x = sizeof(uint16_t) * (size_t)s.rows * p.ld, a = sizeof(uint16_t) * (size_t)p.m * p.ldm;
   const long parts = muon_parts((long)s.rows * s.cols, false);
-  p.syms = 2;
-  for (int k = MUON_LATE; k < s.steps; ++k)
-    if (muon_pairs_steps(s, k)) p.syms = MUON_SYMS;
-  const size_t each = 4 * x + p.syms * a;
+  const size_t each = 4 * x + 2 * a;
   const size_t most = std::max<size_t>(1, MUON_BATCH_BYTES / each);
   const size_t turns = ((size_t)s.n + most - 1) / most;
   p.batch = (int)(((size_t)s.n + turns - 1) / turns);
@@ -1033,7 +1009,8 @@ MuonPlan plan_muon(const moe_muon_shape& s) {
     p.hi[i] = c.take(x * p.batch);
     p.lo[i] = c.take(x * p.batch);
   }
-  for (int i = 0; i < p.syms; ++i) p.sym[i] = c.take(a * p.batch);
+  p.A = c.take(a * p.batch);
+  p.B = c.take(a * p.batch);
   muon_tile_cols(s, p);
   if (p.split > 1) p.sums = c.take(sizeof(float) * p.batch * muon_tri_tiles(p) * p.split * 256 * p.nt_tri);
   p.total = c.off;
@@ -1075,71 +1052,25 @@ int muon_group(int m, int n, int num_sms) {
   return (int)((n + groups - 1) / groups);
 }
 
-// What a step adds to B's diagonal and takes off the linear term (muon.cuh)
-float muon_shift(const moe_muon_shape& s, int k) {
-  const float bc = s.coefficients[k][1] + s.coefficients[k][2];
-  return k >= MUON_LATE && bc < 0.f ? -0.75f * bc : 0.f;
-}
-
-// The products of all steps.  A step on its own:  A = X X^T;  B = b A + c A A + s I;  X <- (a - s) X + B X.
-// Two late steps as one (muon_pairs_steps) stay in m x m:  A = X X^T;  C = a I + b A + c A A;  A <- C A C;  B = a' I + b' A + c' A A;  X <- B C X.
-// All of these are polynomials of one symmetric matrix, so they commute and are symmetric too.  The singular values are near 1 by then, so
-// squaring them costs little: 1.0e-3 off in the norm instead of 0.9e-3.
-void plan_muon_ops(const moe_muon_shape& s, const MuonPlan& p, MuonArgs& a) {
-  enum { A, B, C, D };
-  int cur = 0;
-  auto add = [&](int kind, int pp, int r, int in, int out, float acc, float in_f, float diag) -> MuonOp& {
-    MuonOp& o = a.op[a.ops++];
-    o.kind = (int8_t)kind; o.p = (int8_t)pp; o.r = (int8_t)r; o.in = (int8_t)in; o.out = (int8_t)out;
-    o.acc_f = acc; o.in_f = in_f; o.diag_f = diag;
-    o.cur = (int8_t)cur;
-    return o;
-  };
-  auto gram = [&] {
-    const float f = MUON_SA / (MUON_SX * MUON_SX);
-    add(MUON_GRAM, A, A, -1, A, f, 0.f, 0.f);
-    if (p.split > 1) add(MUON_JOIN, A, A, -1, A, f, 0.f, 0.f);
-  };
-  auto poly = [&](int k, int out, float diag) {
-    const float* c = s.coefficients[k];
-    add(MUON_SYM, A, A, A, out, c[2] * (MUON_SB / (MUON_SA * MUON_SA)), c[1] * (MUON_SB / MUON_SA), diag * MUON_SB);
-  };
-  auto apply = [&](int k, int sym, float linear) {   // k: the last step that it takes
-    const bool last = k + 1 == s.steps;
-    const float scale = last ? 1.f / MUON_SX : 1.f;   // of the result
-    MuonOp& o = add(MUON_APPLY, sym, sym, -1, 0, scale / MUON_SB, linear * scale, 0.f);
-    o.use = linear != 0.f;
-    o.lo = o.use && k < MUON_LATE;
-    o.lo_out = !last && k + 1 < MUON_LATE;
-    o.last = last;
-    cur ^= 1;
-  };
-  for (int k = 0; k < s.steps;) {
-    gram();
-    if (!muon_pairs_steps(s, k)) {
-      const float shift = muon_shift(s, k);
-      poly(k, B, shift);
-      apply(k, B, s.coefficients[k][0] - shift);
-      ++k;
-      continue;
-    }
-    poly(k, C, s.coefficients[k][0]);
-    add(MUON_SYM, C, A, -1, D, 1.f / MUON_SA, 0.f, 0.f);
-    add(MUON_SYM, D, C, -1, A, MUON_SA / (MUON_SB * MUON_SB), 0.f, 0.f);
-    poly(k + 1, B, s.coefficients[k + 1][0]);
-    add(MUON_SYM, B, C, -1, D, 1.f / MUON_SB, 0.f, 0.f);
-    apply(k + 1, D, 0.f);
-    k += 2;
-  }
-}
-
 int plan_muon_args(moe_muon* u) {
   const MuonPlan& p = u->plan;
   const moe_muon_shape& s = u->shape;
+  const bool small = muon_is_small(s.rows, s.cols);
   MuonArgs& a = u->args;
   memset(&a, 0, sizeof a);
-  if (muon_is_small(s.rows, s.cols)) return MOE_OK;
-  plan_muon_ops(s, p, a);
+  for (int k = 0; k < s.steps; ++k) {
+    const float ca = s.coefficients[k][0], cb = s.coefficients[k][1], cc = s.coefficients[k][2];
+    const float shift = k >= MUON_LATE && cb + cc < 0.f ? -0.75f * (cb + cc) : 0.f;
+    const float scale = !small && k + 1 == s.steps ? 1.f / MUON_SX : 1.f;   // of the result
+    MuonArgs::Step& t = a.step[k];
+    t.gram_acc = MUON_SA / (MUON_SX * MUON_SX);
+    t.poly_acc = cc * (MUON_SB / (MUON_SA * MUON_SA));
+    t.poly_in = cb * (MUON_SB / MUON_SA);
+    t.poly_diag = shift * MUON_SB;
+    t.app_acc = scale / MUON_SB;
+    t.app_in = (ca - shift) * scale;
+  }
+  if (small) return MOE_OK;
   a.nt_tri = p.nt_tri; a.nt_app = p.nt_app; a.split = p.split;
   a.strips = 1;   // about an item a pair
   while (a.strips < 32 && 2 * a.strips * p.batch * muon_tri_tiles(p) <= 74) a.strips *= 2;
@@ -1153,14 +1084,15 @@ int plan_muon_args(moe_muon* u) {
     if (!rc) rc = encode_batch(&a.xhi[i], hi, n, rows, cols, p.ld, 32);
     if (!rc) rc = encode_batch(&a.xlo[i], lo, n, rows, cols, p.ld, 32);
   }
-  for (int i = 0; i < p.syms && !rc; ++i) {
-    const void* b = u->ws + p.sym[i];
-    rc = encode_batch(&a.s128[i], b, n, p.m, p.m, p.ldm, 128);
-    if (!rc) rc = encode_batch(&a.s_tri[i], b, n, p.m, p.m, p.ldm, p.nt_tri / 2);
-    if (!rc) rc = encode_batch(&a.s_app[i], b, n, p.m, p.m, p.ldm, p.nt_app / 2);
-    if (!rc) rc = encode_batch(&a.s64[i], b, n, p.m, p.m, p.ldm, 64);
-    if (!rc) rc = encode_batch(&a.sbox[i], b, n, p.m, p.m, p.ldm, 32);
-  }
+  const void *A = u->ws + p.A, *B = u->ws + p.B;
+  if (!rc) rc = encode_batch(&a.a128, A, n, p.m, p.m, p.ldm, 128);
+  if (!rc) rc = encode_batch(&a.a_part, A, n, p.m, p.m, p.ldm, a.nt_tri / 2);
+  if (!rc) rc = encode_batch(&a.a64, A, n, p.m, p.m, p.ldm, 64);
+  if (!rc) rc = encode_batch(&a.abox, A, n, p.m, p.m, p.ldm, 32);
+  if (!rc) rc = encode_batch(&a.b128, B, n, p.m, p.m, p.ldm, 128);
+  if (!rc) rc = encode_batch(&a.b_part, B, n, p.m, p.m, p.ldm, a.nt_app / 2);
+  if (!rc) rc = encode_batch(&a.b64, B, n, p.m, p.m, p.ldm, 64);
+  if (!rc) rc = encode_batch(&a.bbox, B, n, p.m, p.m, p.ldm, 32);
   if (!rc && p.split > 1) {
     const uint64_t dims[2] = {(uint64_t)p.nt_tri, (uint64_t)p.batch * muon_tri_tiles(p) * p.split * 256}, strides[1] = {(uint64_t)p.nt_tri * 4};
     const uint32_t box[2] = {32, 32};
@@ -1168,9 +1100,9 @@ int plan_muon_args(moe_muon* u) {
     a.part_ptr = u->at<float>(p.sums);
   }
   if (rc) return rc;
-  a.a_ptr = u->at<uint16_t>(p.sym[0]);
+  a.a_ptr = u->at<uint16_t>(p.A);
   a.lda = p.ldm;
-  a.rows = s.rows; a.cols = s.cols;
+  a.rows = s.rows; a.cols = s.cols; a.steps = s.steps;
   a.status = u->status();
   a.budget_ns = u->budget_ns;
   a.ctr = u->at<int>(p.ctr);
@@ -1189,11 +1121,7 @@ int run_muon(moe_muon* u, MuonElemArgs e, const uint16_t* W, uint16_t* out, floa
     b.e = e;
     b.e.n = s.n;
     b.steps = s.steps;
-    for (int k = 0; k < s.steps; ++k) {
-      const float* c = s.coefficients[k];
-      const float shift = muon_shift(s, k);
-      b.step[k] = {MUON_SA / (MUON_SX * MUON_SX), c[2] * (MUON_SB / (MUON_SA * MUON_SA)), c[1] * (MUON_SB / MUON_SA), shift * MUON_SB, c[0] - shift};
-    }
+    memcpy(b.step, u->args.step, sizeof b.step);
     b.out = out; b.W = W; b.keep = keep; b.rate = rate;
     b.vec = e.vec && aligned16(out) && aligned16(W);
     b.status = u->status();

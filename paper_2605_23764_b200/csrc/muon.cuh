@@ -22,48 +22,39 @@ constexpr float MUON_SX = 4096.f, MUON_SA = 4096.f, MUON_SB = 1024.f, MUON_SLO =
 constexpr int MUON_STEPS_MAX = 16;
 constexpr int MUON_LATE = 3;   // first step (from 0) with the shifted diagonal and X in one part
 
-// A matrix's steps are a program of products, one after the other:
-enum MuonKind : int {
+enum MuonPhase : int {
   MUON_GRAM = 0,    // A = X X^T or X^T X, or sums over parts of the reduction
   MUON_JOIN = 1,    // A from those
-  MUON_SYM = 2,     // of symmetric matrices that commute: acc P R + in I + diag
-  MUON_APPLY = 3,   // X' = acc P X (or X P) + in X; the last one's into the caller's tensors
+  MUON_POLY = 2,    // B = b A + c A A + s I
+  MUON_APPLY = 3,   // X' = (a - s) X + B X or X B; of the last step: into the caller's tensors
 };
+
 // A symmetric matrix is stored by blocks of 256 x 256, those on and below the diagonal.
 constexpr int MUON_BLOCK = 256;
-constexpr int MUON_SYMS = 4;                        // symmetric matrices: A, B, and two for steps taken together (plan_muon_ops, api.cu)
-constexpr int MUON_OPS_MAX = 4 * MUON_STEPS_MAX;
-struct MuonOp {
-  int8_t kind;
-  int8_t p, r, in, out;   // symmetric matrices; in < 0: none
-  int8_t cur;             // GRAM, APPLY: which buffer X is in
-  int8_t use, lo, lo_out, last;   // APPLY: X is read in the epilogue, its lo part too; lo is written; into the caller's tensors
-  float acc_f, in_f, diag_f;      // in the stored scalings
-};
 
 struct MuonArgs {
   // X, by buffer: K-major operands (128 rows x 64; half a tile's columns x 64), MN-major operand (64 x 64), epilogue boxes (32 rows x 64)
-  // of hi and lo; the symmetric matrices likewise, with half of either width
+  // of hi and lo; A and B likewise
   CUtensorMap x128[2], x_part[2], x64[2], xhi[2], xlo[2];
-  CUtensorMap s128[MUON_SYMS], s_tri[MUON_SYMS], s_app[MUON_SYMS], s64[MUON_SYMS], sbox[MUON_SYMS];
+  CUtensorMap a128, a_part, a64, abox, b128, b_part, b64, bbox;
   CUtensorMap out, w;          // the caller's tensors by epilogue boxes (vec)
   CUtensorMap part;            // GRAM's sums over parts [tile of a matrix][part][256][nt_tri] in fp32, boxes of 32 x 32
   int n, rows, cols;           // matrices of the batch
-  int ops;
-  MuonOp op[MUON_OPS_MAX];
+  int steps;
   int nt_tri, nt_app;          // columns of a tile: 64, 128 or 256; APPLY's also 192 in wide matrices
   int split, strips;           // parts of GRAM's reduction (1: no JOIN); strips of a tile's rows that JOIN's items are
   const float* part_ptr;
   uint16_t* a_ptr;             // A, rows lda apart
   int lda;
-  int sub;                     // matrices whose products follow one another
+  int sub;                     // matrices whose phases follow one another
   int z0;                      // the batch's first matrix in the caller's tensors
-  // the last X': out = X', or with W: out = keep W - rate X'
+  struct Step { float gram_acc, poly_acc, poly_in, poly_diag, app_acc, app_in; } step[MUON_STEPS_MAX];   // factors in the stored scalings
+  // the last step's X': out = X', or with W: out = keep W - rate X'
   uint16_t* out_ptr;           // bf16 [rows][cols] of the batch's first matrix
   const uint16_t* w_ptr;       // NULL: none
   float keep, rate;
   int vec;                     // rows of both are whole 16-byte vectors
-  int* ctr;                    // [n] finished warps' parts of items of each matrix, [n]: next item; zero before the launch
+  int* ctr;                    // [n] finished warps' parts of tiles of each matrix, [n]: next item; zero before the launch
   DevStatus* status;
   uint64_t budget_ns;
 };
@@ -102,8 +93,7 @@ inline bool muon_is_small(int rows, int cols) {
 struct MuonSmallArgs {
   MuonElemArgs e;
   int steps;
-  // factors of acc in A; of acc, A and on the diagonal in B; of X
-  struct Step { float gram_acc, poly_acc, poly_in, poly_diag, app_in; } step[MUON_STEPS_MAX];
+  MuonArgs::Step step[MUON_STEPS_MAX];   // app_in: a - s
   uint16_t* out;
   const uint16_t* W;    // NULL: out = X'
   float keep, rate;

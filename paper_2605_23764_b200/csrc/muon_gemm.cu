@@ -53,17 +53,15 @@ constexpr size_t MU_SMEM = 1024 + MU_STAGES * MU_STAGE_BYTES + MU_EPI_WARPS * 2 
 static_assert(MU_SMEM <= 227 * 1024, "shared memory budget");
 
 struct MuonItem {
-  int op, mat, m0, n0, nt;
-  int kind;         // of the op
+  int phase, step, mat, m0, n0, nt;
   int tile, part;   // GRAM, JOIN: of the matrix's symmetric tiles; part of the reduction, strip of the tile
-  int need;         // the matrix's counter when the op before is complete
+  int need;   // the matrix's counter when the phase before is complete
 };
 
-// Tiles of a matrix's products and how items go through them: `sub` matrices at a time, op by op, matrix by matrix.
+// Tiles of a matrix's phases and how items go through them: `sub` matrices at a time, step by step, phase by phase, matrix by matrix.
 struct MuonOrder {
   int blocks, per_block, tri, app, app_cols;   // rows of 256 of a symmetric matrix, tiles across one of its blocks; tiles
-  int gram, join, all;                         // items: of GRAM, of JOIN, of a matrix
-  __host__ __device__ int items(int kind) const { return kind == MUON_GRAM ? gram : kind == MUON_JOIN ? join : kind == MUON_SYM ? tri : app; }
+  int gram, join, per_step;                    // items
   __host__ __device__ explicit MuonOrder(const MuonArgs& a) {
     const int m = a.rows < a.cols ? a.rows : a.cols;
     blocks = (m + MUON_BLOCK - 1) / MUON_BLOCK;
@@ -72,37 +70,39 @@ struct MuonOrder {
     app_cols = (a.cols + a.nt_app - 1) / a.nt_app;
     app = (a.rows + 255) / 256 * app_cols;
     gram = tri * a.split;
-    join = tri * a.strips;
-    all = 0;
-    for (int i = 0; i < a.ops; ++i) all += items(a.op[i].kind);
+    join = a.split > 1 ? tri * a.strips : 0;
+    per_step = gram + join + tri + app;
   }
-  __host__ __device__ long total(const MuonArgs& a) const { return (long)a.n * all; }
+  __host__ __device__ long total(const MuonArgs& a) const { return (long)a.n * a.steps * per_step; }
   __device__ __forceinline__ MuonItem decode(const MuonArgs& a, int t) const {
     MuonItem r;
-    const int g = t / (a.sub * all);
-    t -= g * a.sub * all;
+    const int full = a.sub * a.steps * per_step, g = t / full;
+    t -= g * full;
     const int s = min(a.sub, a.n - g * a.sub);   // matrices of this group
-    int here = items(a.op[0].kind);              // a matrix's items of the op
-    r.op = r.need = 0;
-    while (t >= s * here) {
-      t -= s * here;
-      r.need += here;
-      here = items(a.op[++r.op].kind);
+    r.step = t / (s * per_step);
+    t -= r.step * s * per_step;
+    r.need = r.step * per_step;
+    int items = gram;   // of a matrix's phase
+    r.phase = MUON_GRAM;
+    while (t >= s * items) {
+      t -= s * items;
+      r.need += items;
+      ++r.phase;
+      items = r.phase == MUON_JOIN ? join : r.phase == MUON_POLY ? tri : app;
     }
-    r.kind = a.op[r.op].kind;
     r.need *= MU_PARTS;
-    const int q = t / here;
-    t -= q * here;
+    const int q = t / items;
+    t -= q * items;
     r.mat = g * a.sub + q;
     r.part = 0;
     int i = 0;
-    if (r.kind == MUON_APPLY) {
+    if (r.phase == MUON_APPLY) {
       i = t / app_cols;
       t -= i * app_cols;
       r.nt = a.nt_app;
     } else {
-      if (r.kind != MUON_SYM) {
-        const int parts = r.kind == MUON_GRAM ? a.split : a.strips;
+      if (r.phase != MUON_POLY) {
+        const int parts = r.phase == MUON_GRAM ? a.split : a.strips;
         r.part = t % parts;
         t /= parts;
       }
@@ -142,8 +142,8 @@ __device__ __forceinline__ void tc_mma4_pair_steps(uint32_t d_tmem, uint32_t a_l
 
 // k-blocks [first, end) of an item's products
 __device__ __forceinline__ int2 muon_blocks(const MuonArgs& a, const MuonItem& it) {
-  const int K = it.kind == MUON_GRAM ? max(a.rows, a.cols) : min(a.rows, a.cols), all = (K + BK - 1) / BK;
-  if (it.kind != MUON_GRAM) return make_int2(0, all);
+  const int K = it.phase == MUON_GRAM ? max(a.rows, a.cols) : min(a.rows, a.cols), all = (K + BK - 1) / BK;
+  if (it.phase != MUON_GRAM) return make_int2(0, all);
   return make_int2((int)((long)all * it.part / a.split), (int)((long)all * (it.part + 1) / a.split));
 }
 
@@ -154,9 +154,9 @@ struct MuonMajors {
   __device__ explicit MuonMajors(const MuonItem& it) {
     constexpr int NEVER = INT_MAX, BKS = MUON_BLOCK / BK;
     const int a_sym = it.m0 / BK + BKS, b_sym = it.n0 / MUON_BLOCK * BKS + BKS;
-    if (it.kind == MUON_GRAM) {
+    if (it.phase == MUON_GRAM) {
       a_from = b_from = WIDE ? NEVER : 0;
-    } else if (it.kind == MUON_SYM) {
+    } else if (it.phase == MUON_POLY) {
       a_from = a_sym;
       b_from = b_sym;
     } else {
@@ -167,17 +167,17 @@ struct MuonMajors {
 };
 
 // Half a box of 32 rows x 64 columns of the accumulator: v, 32 columns of the lane's row; j0: its first chunk of eight.
-__device__ __forceinline__ void muon_box_acc(float f, float* v, uint8_t* box, int lane, int j0) {
+__device__ __forceinline__ void muon_box_gram(const MuonArgs::Step k, float* v, uint8_t* box, int lane, int j0) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float* x = v + 8 * j;
-    *box_chunk(box, lane, j0 + j) = make_uint4(pack_h2(x[0] * f, x[1] * f), pack_h2(x[2] * f, x[3] * f),
-                                          pack_h2(x[4] * f, x[5] * f), pack_h2(x[6] * f, x[7] * f));
+    *box_chunk(box, lane, j0 + j) = make_uint4(pack_h2(x[0] * k.gram_acc, x[1] * k.gram_acc), pack_h2(x[2] * k.gram_acc, x[3] * k.gram_acc),
+                                          pack_h2(x[4] * k.gram_acc, x[5] * k.gram_acc), pack_h2(x[6] * k.gram_acc, x[7] * k.gram_acc));
   }
 }
 // (All chunks are read before the first is written: the compiler keeps reads behind writes that might meet them, a latency a chunk.)
 // diag: the column of v on the lane's diagonal, or none of 0 .. 31
-__device__ __forceinline__ void muon_box_sym(float acc_f, float in_f, float diag_f, float* v, uint8_t* box, int lane, int j0, int diag) {
+__device__ __forceinline__ void muon_box_poly(const MuonArgs::Step k, float* v, uint8_t* box, int lane, int j0, int diag) {
   uint4 in[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) in[j] = *box_chunk(box, lane, j0 + j);
@@ -188,21 +188,21 @@ __device__ __forceinline__ void muon_box_sym(float acc_f, float in_f, float diag
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const float2 y = unpack_h2(w[q]);
-      float x0 = fmaf(y.x, in_f, v[8 * j + 2 * q] * acc_f), x1 = fmaf(y.y, in_f, v[8 * j + 2 * q + 1] * acc_f);
-      if (diag == 8 * j + 2 * q) x0 += diag_f;
-      if (diag == 8 * j + 2 * q + 1) x1 += diag_f;
+      float x0 = fmaf(y.x, k.poly_in, v[8 * j + 2 * q] * k.poly_acc), x1 = fmaf(y.y, k.poly_in, v[8 * j + 2 * q + 1] * k.poly_acc);
+      if (diag == 8 * j + 2 * q) x0 += k.poly_diag;
+      if (diag == 8 * j + 2 * q + 1) x1 += k.poly_diag;
       o[q] = pack_h2(x0, x1);
     }
     *box_chunk(box, lane, j0 + j) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
-// X' (in v too) from, with IN, X hi in box0 and, with LO, lo in box1; written there as hi and lo
-template <bool IN, bool LO, bool HI_OUT, bool LO_OUT>
-__device__ __forceinline__ void muon_box_apply(float acc_f, float in_f, float* v, uint8_t* box0, uint8_t* box1, int lane, int j0) {
+// X' (in v too) from X hi in box0 and, with LO, lo in box1; written back as hi and, with KEEP, lo
+template <bool LO, bool HI_OUT, bool LO_OUT>
+__device__ __forceinline__ void muon_box_apply(const MuonArgs::Step k, float* v, uint8_t* box0, uint8_t* box1, int lane, int j0) {
   uint4 xh[4], xl[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    if (IN) xh[j] = *box_chunk(box0, lane, j0 + j);
+    xh[j] = *box_chunk(box0, lane, j0 + j);
     if (LO) xl[j] = *box_chunk(box1, lane, j0 + j);
   }
 #pragma unroll
@@ -211,15 +211,13 @@ __device__ __forceinline__ void muon_box_apply(float acc_f, float in_f, float* v
     uint32_t oh[4], ol[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      float2 y = make_float2(0.f, 0.f);
-      if (IN) y = unpack_h2(wh[q]);
+      float2 y = unpack_h2(wh[q]);
       if (LO) {
         const float2 yl = unpack_h2(wl[q]);
         y.x = fmaf(yl.x, 1.f / MUON_SLO, y.x);
         y.y = fmaf(yl.y, 1.f / MUON_SLO, y.y);
       }
-      const float a0 = v[8 * j + 2 * q] * acc_f, a1 = v[8 * j + 2 * q + 1] * acc_f;
-      const float x0 = IN ? fmaf(y.x, in_f, a0) : a0, x1 = IN ? fmaf(y.y, in_f, a1) : a1;
+      const float x0 = fmaf(y.x, k.app_in, v[8 * j + 2 * q] * k.app_acc), x1 = fmaf(y.y, k.app_in, v[8 * j + 2 * q + 1] * k.app_acc);
       v[8 * j + 2 * q] = x0;
       v[8 * j + 2 * q + 1] = x1;
       if (HI_OUT) oh[q] = pack_h2(x0, x1);
@@ -254,17 +252,17 @@ __device__ __forceinline__ void muon_box_out(const MuonArgs& a, float* v, uint8_
 }
 // The same for rows that are no whole vectors: X' in fp32 through both boxes, so that a row's elements are next to one another when they
 // are written
-__device__ __forceinline__ void muon_rows_out(const MuonArgs& a, const MuonOp& op, uint32_t tcol, uint8_t* boxes, int lane, int mat, int r0, int c0) {
+__device__ __forceinline__ void muon_rows_out(const MuonArgs& a, const MuonArgs::Step& k, uint32_t tcol, uint8_t* boxes, bool lo, int lane, int mat, int r0, int c0) {
   float v[64];
 #pragma unroll
   for (int q = 0; q < 4; ++q) tmem_ld16(tcol + 16 * q, v + 16 * q);
   tmem_ld_wait();
-  const float f = op.acc_f, g = op.in_f;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (op.lo) muon_box_apply<true, true, false, false>(f, g, v + 32 * h, boxes, boxes + MU_BOX, lane, 4 * h);
-    else if (op.use) muon_box_apply<true, false, false, false>(f, g, v + 32 * h, boxes, boxes + MU_BOX, lane, 4 * h);
-    else muon_box_apply<false, false, false, false>(f, g, v + 32 * h, boxes, boxes + MU_BOX, lane, 4 * h);
+  if (lo) {
+    muon_box_apply<true, false, false>(k, v, boxes, boxes + MU_BOX, lane, 0);
+    muon_box_apply<true, false, false>(k, v + 32, boxes, boxes + MU_BOX, lane, 4);
+  } else {
+    muon_box_apply<false, false, false>(k, v, boxes, boxes + MU_BOX, lane, 0);
+    muon_box_apply<false, false, false>(k, v + 32, boxes, boxes + MU_BOX, lane, 4);
   }
   __syncwarp();   // X has been read from the boxes
 #pragma unroll
@@ -287,7 +285,7 @@ __device__ __forceinline__ void muon_rows_out(const MuonArgs& a, const MuonOp& o
 // step's.
 __device__ __forceinline__ void muon_join(const MuonArgs& a, const MuonItem& it, int tri, int w, int lane) {
   const int m = min(a.rows, a.cols), rows = 256 / a.strips, quads = it.nt / 4, row0 = it.part * rows;
-  const float scale = a.op[it.op].acc_f;
+  const float scale = a.step[0].gram_acc;
   const size_t step = (size_t)256 * it.nt / 4;
   for (int u = w * 32 + lane; u < rows * quads; u += MU_PARTS * 32) {
     const int row = row0 + u / quads, c = u % quads * 4, r = it.m0 + row;
@@ -377,25 +375,21 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       if (t < 0 || t >= total) break;
       const MuonItem it = order.decode(a, t);
       const MuonMajors<WIDE> mj(it);
-      const int half = it.nt / 2, mat = uniform(it.mat);
+      const int half = it.nt / 2, mat = uniform(it.mat), cur = it.step & 1;
       const int m0 = uniform(it.m0 + rank * 128), n0 = uniform(it.n0 + rank * half);
       const int2 blocks = muon_blocks(a, it);
       const int kb0 = uniform(blocks.x), kb1 = uniform(blocks.y);
       // K-major and MN-major maps of both operands
-      const MuonOp& op = a.op[it.op];
-      const CUtensorMap *a_k = &a.s128[op.p], *a_mn = &a.s64[op.p], *b_k = &a.s_tri[op.r], *b_mn = &a.s64[op.r];
-      if (it.kind == MUON_GRAM) {
-        a_k = &a.x128[op.cur];
-        b_k = &a.x_part[op.cur];
-        a_mn = b_mn = &a.x64[op.cur];
-      } else if (it.kind == MUON_APPLY) {
-        if (WIDE) {
-          b_mn = &a.x64[op.cur];
-        } else {
-          a_k = &a.x128[op.cur];
-          b_k = &a.s_app[op.p];
-          b_mn = &a.s64[op.p];
-        }
+      const CUtensorMap *a_k = &a.a128, *a_mn = &a.a64, *b_k = &a.a_part, *b_mn = &a.a64;
+      if (it.phase == MUON_GRAM) {
+        a_k = &a.x128[cur];
+        b_k = &a.x_part[cur];
+        a_mn = b_mn = &a.x64[cur];
+      } else if (it.phase == MUON_APPLY) {
+        a_k = WIDE ? &a.b128 : &a.x128[cur];
+        a_mn = &a.b64;
+        b_k = &a.b_part;
+        b_mn = WIDE ? &a.x64[cur] : &a.b64;
       }
       int up = 1;
       if (it.need && lane == 0) up = counter_wait(a.ctr + mat, it.need, wc, t, 256) ? 1 : 0;
@@ -403,7 +397,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       fence_proxy_async_global();   // what the counter announces was written by other CTAs' stores
       if (lane == 0) mbar_arrive_cta(&bars->dep[dep]);
       if (++dep == MU_DEPS) dep = 0;
-      if (SPLIT && it.kind == MUON_JOIN) continue;
+      if (SPLIT && it.phase == MUON_JOIN) continue;
       const int b_boxes = (half + 63) / 64;
       for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait_warp(&bars->empty[s], (par >> s) & 1, wc, SITE_EMPTY, t, 20)) { ok = false; break; }
@@ -438,7 +432,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       if (t < 0) ok = false;
       if (t < 0 || t >= total) break;
       const MuonItem it = order.decode(a, t);
-      if (SPLIT && it.kind == MUON_JOIN) continue;
+      if (SPLIT && it.phase == MUON_JOIN) continue;
       const MuonMajors<WIDE> mj(it);
       const int2 blocks = muon_blocks(a, it);
       const int kb0 = uniform(blocks.x), kb1 = uniform(blocks.y);
@@ -493,18 +487,17 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       const int t = tk.next(bars, slots, wc, 100, SPLIT);
       if (t < 0 || t >= total) break;   // (a kept slot is the only one, and nobody waits for it any more)
       const MuonItem it = order.decode(a, t);
-      const MuonOp op = a.op[it.op];   // (a copy: by reference the factors were read again for every chunk, 1.4 us a box)
-      const int m = min(a.rows, a.cols);
-      const bool apply = it.kind == MUON_APPLY;
-      const int M = apply ? a.rows : m, N = apply ? a.cols : m;
-      const bool last = op.last, lo = op.lo, lo_out = op.lo_out;
-      const bool in = apply ? op.use : op.in >= 0;        // the epilogue's input: X, or a symmetric matrix
-      const bool upd = last && !lo && VEC && a.w_ptr;     // W comes with it
+      const MuonArgs::Step k = a.step[it.step];   // (a copy: by reference the factors were read again for every chunk, 1.4 us a box)
+      const int m = min(a.rows, a.cols), cur = it.step & 1;
+      const int M = it.phase == MUON_APPLY ? a.rows : m, N = it.phase == MUON_APPLY ? a.cols : m;
+      const bool last = it.phase == MUON_APPLY && it.step + 1 == a.steps;
+      const bool lo = it.phase == MUON_APPLY && it.step < MUON_LATE, lo_out = it.phase == MUON_APPLY && !last && it.step + 1 < MUON_LATE;
+      const bool upd = last && !lo && VEC && a.w_ptr;   // W comes with X
       const int r0 = it.m0 + rank * 128 + quad * 32;
       // the loader polls the counter for the CTA
       if (!mbar_wait_warp(&bars->dep[dep], dep_par, wc, SITE_DEP, t, 50)) break;
       if (++dep == MU_DEPS) { dep = 0; dep_par ^= 1; }
-      if (SPLIT && it.kind == MUON_JOIN) {
+      if (SPLIT && it.phase == MUON_JOIN) {
         muon_join(a, it, order.tri, rank * MU_EPI_WARPS + ew, lane);
         fence_proxy_async_global();   // every lane's stores, for the loads to come
         __syncwarp();
@@ -514,19 +507,19 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
         }
         continue;
       }
-      const bool parts = SPLIT && it.kind == MUON_GRAM;
+      const bool parts = SPLIT && it.phase == MUON_GRAM;
       bool up = false;   // the accumulator has been seen complete
       for (int b = (ew >> 2) * 64; b < it.nt; b += 128) {
         const int c0 = it.n0 + b;
         if (r0 >= M || c0 >= N) break;
         __syncwarp();   // every lane has read the boxes
-        if (in || upd) {
+        if (it.phase != MUON_GRAM) {
           if (lane == 0) {
             tma_store_wait_read();
             fence_proxy_async_global();
-            mbar_expect_tx(in_full, ((in ? 1 : 0) + (lo || upd ? 1 : 0)) * MU_BOX);
-            if (in) tma_load_3d_thread(box0, apply ? &a.xhi[op.cur] : &a.sbox[op.in], c0, r0, it.mat, in_full);
-            if (lo) tma_load_3d_thread(box1, &a.xlo[op.cur], c0, r0, it.mat, in_full);
+            mbar_expect_tx(in_full, lo || upd ? 2 * MU_BOX : MU_BOX);
+            tma_load_3d_thread(box0, it.phase == MUON_POLY ? &a.abox : &a.xhi[cur], c0, r0, it.mat, in_full);
+            if (lo) tma_load_3d_thread(box1, &a.xlo[cur], c0, r0, it.mat, in_full);
             else if (upd) tma_load_3d_thread(box1, &a.w, c0, r0, a.z0 + it.mat, in_full);
           }
           __syncwarp();
@@ -539,14 +532,14 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
           tc_fence_after_sync();
           up = true;
         }
-        if (in || upd) {
+        if (it.phase != MUON_GRAM) {
           if (!mbar_wait_warp(in_full, in_par, wc, SITE_FULL, t)) ok = false;
           in_par ^= 1;
         }
         if (!ok) break;
         const uint32_t tcol = tmem_base + acc * 256 + b + (static_cast<uint32_t>(quad * 32) << 16);
         if (!VEC && last) {
-          muon_rows_out(a, op, tcol, box0, lane, it.mat, r0, c0);
+          muon_rows_out(a, a.step[it.step], tcol, box0, lo, lane, it.mat, r0, c0);
           continue;
         }
 #pragma unroll 1
@@ -559,18 +552,17 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
 #pragma unroll
             for (int j = 0; j < 8; ++j)
               *reinterpret_cast<float4*>(box_chunk(j0 ? box1 : box0, lane, j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-          } else if (!apply) {
-            if (in) muon_box_sym(op.acc_f, op.in_f, op.diag_f, v, box0, lane, j0, r0 + lane - c0 - 8 * j0);
-            else muon_box_acc(op.acc_f, v, box0, lane, j0);
+          } else if (it.phase == MUON_GRAM) {
+            muon_box_gram(k, v, box0, lane, j0);
+          } else if (it.phase == MUON_POLY) {
+            muon_box_poly(k, v, box0, lane, j0, r0 + lane - c0 - 8 * j0);
           } else if (!last) {
-            if (lo_out) muon_box_apply<true, true, true, true>(op.acc_f, op.in_f, v, box0, box1, lane, j0);
-            else if (lo) muon_box_apply<true, true, true, false>(op.acc_f, op.in_f, v, box0, box1, lane, j0);
-            else if (in) muon_box_apply<true, false, true, false>(op.acc_f, op.in_f, v, box0, box1, lane, j0);
-            else muon_box_apply<false, false, true, false>(op.acc_f, op.in_f, v, box0, box1, lane, j0);
+            if (lo_out) muon_box_apply<true, true, true>(k, v, box0, box1, lane, j0);
+            else if (lo) muon_box_apply<true, true, false>(k, v, box0, box1, lane, j0);
+            else muon_box_apply<false, true, false>(k, v, box0, box1, lane, j0);
           } else if (VEC) {
-            if (lo) muon_box_apply<true, true, false, false>(op.acc_f, op.in_f, v, box0, box1, lane, j0);
-            else if (in) muon_box_apply<true, false, false, false>(op.acc_f, op.in_f, v, box0, box1, lane, j0);
-            else muon_box_apply<false, false, false, false>(op.acc_f, op.in_f, v, box0, box1, lane, j0);
+            if (lo) muon_box_apply<true, false, false>(k, v, box0, box1, lane, j0);
+            else muon_box_apply<false, false, false>(k, v, box0, box1, lane, j0);
             muon_box_out(a, v, box0, box1, lane, j0, lo, it.mat, r0 + lane, c0);
           }
         }
@@ -581,9 +573,9 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
           tma_store_2d(&a.part, b + 32, y, box1);
           tma_store_commit();
         } else if (lane == 0) {
-          const CUtensorMap* o = !apply ? &a.sbox[op.out] : last ? &a.out : &a.xhi[op.cur ^ 1];
+          const CUtensorMap* o = it.phase == MUON_GRAM ? &a.abox : it.phase == MUON_POLY ? &a.bbox : last ? &a.out : &a.xhi[cur ^ 1];
           tma_store_3d(o, c0, r0, last ? a.z0 + it.mat : it.mat, box0);
-          if (lo_out) tma_store_3d(&a.xlo[op.cur ^ 1], c0, r0, it.mat, box1);
+          if (lo_out) tma_store_3d(&a.xlo[cur ^ 1], c0, r0, it.mat, box1);
           tma_store_commit();
         }
       }

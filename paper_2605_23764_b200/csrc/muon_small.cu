@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(MS_THREADS, 1) muon_small_kernel(const __grid_
     tc_fence_after_sync();
   };
   for (int k = 0; k < a.steps; ++k) {
-    const MuonSmallArgs::Step st = a.step[k];
+    const MuonArgs::Step st = a.step[k];
     ready();
     if (warp == 0) {
       for (int kk = 0; kk < chunks * 4; ++kk) {

@@ -127,10 +127,9 @@ def _noise(G):
 
 @pytest.mark.parametrize("n,rows,cols,steps", [(50, 300, 700, 5), (50, 700, 300, 5), (150, 200, 440, 6), (50, 264, 1056, 7), (150, 130, 401, 5), (25, 520, 1200, 9)])
 @pytest.mark.parametrize("kind", ["full", "low_rank"])
-def test_late_steps_together(n, rows, cols, steps, kind):
-    """Many matrices at least twice as long as wide: pairs of late steps go through the Gram matrix.  The products between round once more
-    where nothing is amplified any longer, within the same bound.  Gradients of fewer tokens than either side has, whose other singular values
-    are what bf16 makes of zero, 1e-3 of the largest, are brought to 1 by more than five steps: there what roundings do to those counts (_noise)."""
+def test_many_matrices_and_steps(n, rows, cols, steps, kind):
+    """More tiles than pairs of SMs, five steps and more.  Gradients of fewer tokens than either side has, whose other singular values are what
+    bf16 makes of zero, 1e-3 of the largest, are brought to 1 by more than five steps: there what roundings do to those counts (_noise)."""
     from paper_2605_23764_b200 import MoeMuon
     G = _gradient(n, rows, cols, steps)
     norm = NORM
