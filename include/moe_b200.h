@@ -341,7 +341,7 @@ int moe_ffn_fwd_w4(moe_ctx* ctx, const uint16_t* x, const int32_t* topk_ids, con
  *   X = u / (|u| + eps), |u| the root of the sum of squares;   for each step:  X <- a X + (b A + c A A) X,  A = X X^T
  * with (a, b, c) = coefficients[step].  (3.4445, -4.7750, 2.0315) five times takes singular values above a hundredth of |u| to 0.7 .. 1.2.
  * The polynomials must keep singular values of at most 1 within 2.  A matrix of zeros (an expert without tokens) stays zero.
- *   moe_muon_orthogonalize   u = G (bf16 or fp32, MOE_MUON_*) -> out bf16
+ *   moe_muon_orthogonalize   u = G (bf16 or fp32, MOE_MUON_*) -> out bf16 (which may be a bf16 G)
  *   moe_muon_step            M_out = momentum M + dW;  u = dW + momentum M_out with nesterov, else M_out;
  *                            W_out = (1 - lr weight_decay) W - lr scale X;  W, dW, W_out bf16, M, M_out fp32; M_out may be M, W_out may be W
  * Products take fp16 operands (11 significant bits) and sum in fp32; the linear term a X keeps 22 bits of X or more while that counts (the

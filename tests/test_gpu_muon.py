@@ -50,7 +50,8 @@ def _near(got, want, norm=NORM):
 
 SHAPES = [(1, 1, 1), (3, 1, 8), (2, 9, 1), (4, 16, 16), (3, 28, 43), (2, 43, 28), (5, 64, 64), (16, 128, 256), (8, 256, 128), (2, 129, 257), (2, 257, 129),
           (3, 130, 1000), (3, 1000, 130), (2, 333, 517), (1, 512, 512), (1, 700, 301), (2, 384, 640), (1, 256, 2056), (1, 2056, 264), (1, 1408, 2048), (40, 72, 200),
-          (2, 128, 384), (2, 384, 128), (1, 129, 384), (1, 128, 385), (1, 385, 65), (700, 24, 40), (150, 257, 260), (1, 64, 4096), (1, 3000, 136)]
+          (2, 128, 384), (2, 384, 128), (1, 129, 384), (1, 128, 385), (1, 385, 65), (700, 24, 40), (150, 257, 260), (1, 64, 4096), (1, 3000, 136),
+          (1, 8, 65536), (1, 65536, 8), (3, 20000, 130), (1, 1, 5000), (2, 5001, 1), (1, 2049, 2047)]
 
 
 @pytest.mark.parametrize("n,rows,cols", SHAPES)
@@ -330,3 +331,39 @@ def test_refusals():
     torch.cuda.synchronize()
     assert not out.any()
     binding.moe_muon_destroy(h)
+
+
+def test_a_handle_serves_streams_in_turn_and_a_capture_beside_eager_calls():
+    """One handle on several streams, each waiting for the other; a graph captured from it between eager calls; memory of one's own."""
+    from paper_2605_23764_b200 import MoeMuon, binding
+    n, rows, cols = 6, 300, 520
+    G, H = _gradient(n, rows, cols, 1), _gradient(n, rows, cols, 2)
+    muon = MoeMuon(n, rows, cols)
+    want = muon.orthogonalize(G), muon.orthogonalize(H)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = []
+    a.wait_stream(torch.cuda.current_stream())
+    for i in range(6):
+        s, t = (a, b) if i % 2 == 0 else (b, a)
+        with torch.cuda.stream(s):
+            outs.append(muon.orthogonalize(G if i % 3 else H))
+        t.wait_stream(s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(_bits(o), _bits(want[0] if i % 3 else want[1])) for i, o in enumerate(outs))
+    out = torch.empty_like(G)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        muon.orthogonalize(G, out=out)
+    eager = muon.orthogonalize(H)
+    graph.replay()
+    again = muon.orthogonalize(H)
+    torch.cuda.synchronize()
+    assert torch.equal(_bits(out), _bits(want[0])) and torch.equal(_bits(eager), _bits(want[1])) and torch.equal(_bits(again), _bits(want[1]))
+    h = binding.moe_muon_create(binding.moe_muon_shape(n, rows, cols, COEF, 5, 1e-7))   # the library's own workspace
+    binding.moe_muon_orthogonalize(h, G, out.zero_())
+    assert binding.moe_muon_get_status(h) == (0, 0) and binding.moe_muon_last_launch_count(h) == 3
+    assert torch.equal(_bits(out), _bits(want[0]))
+    binding.moe_muon_destroy(h)
+    G2 = G.clone()   # in its own place
+    muon.orthogonalize(G2, out=G2)
+    assert torch.equal(_bits(G2), _bits(want[0]))
