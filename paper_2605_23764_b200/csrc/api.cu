@@ -68,9 +68,10 @@ EncodeTiledFn get_encode_fn() {
 }
 
 // bf16 (fp16, or another type's) tensor of `rank` dimensions (dims[0] innermost, strides in bytes for dims 1..), 128-byte
-// swizzle, zero fill outside the tensor on loads, clipping on stores.
+// swizzle unless stated, zero fill outside the tensor on loads, clipping on stores.
 int encode_tiled(CUtensorMap* tm, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
-                 const uint32_t* box, CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) {
+                 const uint32_t* box, CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                 CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) {
     g_cuda_error = "cuTensorMapEncodeTiled entry point not available";
@@ -81,7 +82,7 @@ int encode_tiled(CUtensorMap* tm, const void* base, int rank, const uint64_t* di
   for (int i = 0; i < rank; ++i) { gdim[i] = dims[i]; bx[i] = box[i]; }
   for (int i = 0; i + 1 < rank; ++i) gstr[i] = strides[i];
   CUresult r = fn(tm, type, rank, const_cast<void*>(base), gdim, gstr, bx, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
@@ -951,7 +952,7 @@ bool muon_shape_ok(const moe_muon_shape* s) {
 void muon_tile_cols(const moe_muon_shape& s, MuonPlan& p) {
   const int m = p.m, l = p.l, nkb = (l + 63) / 64;
   constexpr double pairs = 74;   // of a B200: the workspace's size is asked for without a device
-  auto turn = [](int nt, double blocks) { return blocks * (128 + nt / 2) * 128 / 56.0 + 2200.0 * ((nt + 127) / 128); };
+  auto turn = [](int nt, double blocks) { return blocks * (128 + nt / 2) * 128 / 56.0 + 1200.0 * (nt / 64); };
   auto cost = [&](double tiles, int nt, int K) {
     return (tiles <= 8 * pairs ? std::ceil(tiles / pairs) : tiles / pairs) * turn(nt, (K + 63) / 64);
   };
@@ -1036,11 +1037,16 @@ struct moe_muon {
 
 namespace {
 
-// [n][rows][cols] in 16 bits, rows ld elements apart
+// [n][rows][cols] in 16 bits, rows ld elements apart: boxes of 64 columns for operands, 32 x 32 for the epilogue (swizzled over their 64 bytes)
 int encode_batch(CUtensorMap* tm, const void* base, uint64_t n, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows) {
   const uint64_t dims[3] = {cols, rows, n}, strides[2] = {ld * 2, rows * ld * 2};
   const uint32_t box[3] = {64, box_rows, 1};
   return encode_tiled(tm, base, 3, dims, strides, box);
+}
+int encode_boxes(CUtensorMap* tm, const void* base, uint64_t n, uint64_t rows, uint64_t cols, uint64_t ld) {
+  const uint64_t dims[3] = {cols, rows, n}, strides[2] = {ld * 2, rows * ld * 2};
+  const uint32_t box[3] = {32, 32, 1};
+  return encode_tiled(tm, base, 3, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 // Matrices whose phases follow one another: four turns of symmetric tiles over the pairs, so that a phase's first tiles do not wait for
@@ -1081,18 +1087,18 @@ int plan_muon_args(moe_muon* u) {
     rc = encode_batch(&a.x128[i], hi, n, rows, cols, p.ld, 128);
     if (!rc) rc = encode_batch(&a.x_part[i], hi, n, rows, cols, p.ld, a.nt_tri / 2);
     if (!rc) rc = encode_batch(&a.x64[i], hi, n, rows, cols, p.ld, 64);
-    if (!rc) rc = encode_batch(&a.xhi[i], hi, n, rows, cols, p.ld, 32);
-    if (!rc) rc = encode_batch(&a.xlo[i], lo, n, rows, cols, p.ld, 32);
+    if (!rc) rc = encode_boxes(&a.xhi[i], hi, n, rows, cols, p.ld);
+    if (!rc) rc = encode_boxes(&a.xlo[i], lo, n, rows, cols, p.ld);
   }
   const void *A = u->ws + p.A, *B = u->ws + p.B;
   if (!rc) rc = encode_batch(&a.a128, A, n, p.m, p.m, p.ldm, 128);
   if (!rc) rc = encode_batch(&a.a_part, A, n, p.m, p.m, p.ldm, a.nt_tri / 2);
   if (!rc) rc = encode_batch(&a.a64, A, n, p.m, p.m, p.ldm, 64);
-  if (!rc) rc = encode_batch(&a.abox, A, n, p.m, p.m, p.ldm, 32);
+  if (!rc) rc = encode_boxes(&a.abox, A, n, p.m, p.m, p.ldm);
   if (!rc) rc = encode_batch(&a.b128, B, n, p.m, p.m, p.ldm, 128);
   if (!rc) rc = encode_batch(&a.b_part, B, n, p.m, p.m, p.ldm, a.nt_app / 2);
   if (!rc) rc = encode_batch(&a.b64, B, n, p.m, p.m, p.ldm, 64);
-  if (!rc) rc = encode_batch(&a.bbox, B, n, p.m, p.m, p.ldm, 32);
+  if (!rc) rc = encode_boxes(&a.bbox, B, n, p.m, p.m, p.ldm);
   if (!rc && p.split > 1) {
     const uint64_t dims[2] = {(uint64_t)p.nt_tri, (uint64_t)p.batch * muon_tri_tiles(p) * p.split * 256}, strides[1] = {(uint64_t)p.nt_tri * 4};
     const uint32_t box[2] = {32, 32};
@@ -1138,8 +1144,8 @@ int run_muon(moe_muon* u, MuonElemArgs e, const uint16_t* W, uint16_t* out, floa
   a.vec = s.cols % 8 == 0 && aligned16(out) && aligned16(W);
   a.keep = keep; a.rate = rate;
   if (a.vec) {
-    int rc = encode_batch(&a.out, out, s.n, s.rows, s.cols, s.cols, 32);
-    if (!rc && W) rc = encode_batch(&a.w, W, s.n, s.rows, s.cols, s.cols, 32);
+    int rc = encode_boxes(&a.out, out, s.n, s.rows, s.cols, s.cols);
+    if (!rc && W) rc = encode_boxes(&a.w, W, s.n, s.rows, s.cols, s.cols);
     if (rc) return rc;
   }
   for (int done = 0; done < s.n; done += p.batch) {

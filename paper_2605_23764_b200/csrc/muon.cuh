@@ -33,7 +33,7 @@ enum MuonPhase : int {
 constexpr int MUON_BLOCK = 256;
 
 struct MuonArgs {
-  // X, by buffer: K-major operands (128 rows x 64; half a tile's columns x 64), MN-major operand (64 x 64), epilogue boxes (32 rows x 64)
+  // X, by buffer: K-major operands (128 rows x 64; half a tile's columns x 64), MN-major operand (64 x 64), epilogue boxes (32 rows x 32)
   // of hi and lo; A and B likewise
   CUtensorMap x128[2], x_part[2], x64[2], xhi[2], xlo[2];
   CUtensorMap a128, a_part, a64, abox, b128, b_part, b64, bbox;

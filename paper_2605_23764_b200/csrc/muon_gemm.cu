@@ -33,7 +33,8 @@ namespace moe {
 constexpr int MU_STAGES = 5;
 constexpr int MU_STAGE_BYTES = A_STAGE_BYTES + HALF_B_BYTES;   // 128 rows of A, up to 128 of the tile's columns
 constexpr int MU_EPI_WARPS = 8, MU_THREADS = 32 * (2 + MU_EPI_WARPS);
-constexpr int MU_BOX = 32 * 64 * 2;
+constexpr int MU_BOX = 32 * 32 * 2;          // of the epilogue: 32 rows x 32 columns
+constexpr int MU_SLOT = 2 * MU_BOX;          // X hi and lo; as much is 32 x 32 in fp32
 constexpr int MU_SLOTS = 3;          // tickets taken ahead
 constexpr int MU_DEPS = MU_SLOTS + 1; // items that the loader can be ahead of the epilogue, and one
 constexpr int MU_READERS = 19;       // warps of the pair that read a ticket: two loaders, the issuer, sixteen of the epilogues
@@ -42,14 +43,14 @@ constexpr int MU_PARTS = 2 * MU_EPI_WARPS;   // signals of a tile
 struct MuonBarriers {
   uint64_t full[MU_STAGES], empty[MU_STAGES];
   uint64_t tmem_full[2], tmem_empty[2];
-  uint64_t in_full[MU_EPI_WARPS];
+  uint64_t in_full[MU_EPI_WARPS][2];
   uint64_t item_full[MU_SLOTS], item_empty[MU_SLOTS];
   uint64_t dep[MU_DEPS];            // the loader has seen what the item depends on complete
   uint64_t drain;
   uint32_t tmem_base;
   int item[MU_SLOTS];
 };
-constexpr size_t MU_SMEM = 1024 + MU_STAGES * MU_STAGE_BYTES + MU_EPI_WARPS * 2 * MU_BOX + sizeof(MuonBarriers);
+constexpr size_t MU_SMEM = 1024 + MU_STAGES * MU_STAGE_BYTES + MU_EPI_WARPS * 2 * MU_SLOT + sizeof(MuonBarriers);
 static_assert(MU_SMEM <= 227 * 1024, "shared memory budget");
 
 struct MuonItem {
@@ -121,7 +122,10 @@ __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ float2 unpack_h2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
-__device__ __forceinline__ uint4* box_chunk(uint8_t* box, int lane, int j) { return reinterpret_cast<uint4*>(box + lane * 128 + ((j ^ (lane & 7)) << 4)); }
+// 16-byte chunk j of the lane's row of a box, swizzled over 64 bytes
+__device__ __forceinline__ uint4* box_chunk(uint8_t* box, int lane, int j) { return reinterpret_cast<uint4*>(box + lane * 64 + ((j ^ (lane >> 1 & 3)) << 4)); }
+// the same of 32 columns in fp32, over 128 bytes
+__device__ __forceinline__ float4* wide_chunk(uint8_t* slot, int lane, int j) { return reinterpret_cast<float4*>(slot + lane * 128 + ((j ^ (lane & 7)) << 4)); }
 
 // Four 16-deep MMAs of a k-block; the operands' steps (16-byte units) follow how each lies.
 __device__ __forceinline__ void tc_mma4_pair_steps(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate,
@@ -166,21 +170,21 @@ struct MuonMajors {
   }
 };
 
-// Half a box of 32 rows x 64 columns of the accumulator: v, 32 columns of the lane's row; j0: its first chunk of eight.
-__device__ __forceinline__ void muon_box_gram(const MuonArgs::Step k, float* v, uint8_t* box, int lane, int j0) {
+// A box of the accumulator: v, 32 columns of the lane's row.
+__device__ __forceinline__ void muon_box_gram(const MuonArgs::Step k, float* v, uint8_t* box, int lane) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float* x = v + 8 * j;
-    *box_chunk(box, lane, j0 + j) = make_uint4(pack_h2(x[0] * k.gram_acc, x[1] * k.gram_acc), pack_h2(x[2] * k.gram_acc, x[3] * k.gram_acc),
+    *box_chunk(box, lane, j) = make_uint4(pack_h2(x[0] * k.gram_acc, x[1] * k.gram_acc), pack_h2(x[2] * k.gram_acc, x[3] * k.gram_acc),
                                           pack_h2(x[4] * k.gram_acc, x[5] * k.gram_acc), pack_h2(x[6] * k.gram_acc, x[7] * k.gram_acc));
   }
 }
 // (All chunks are read before the first is written: the compiler keeps reads behind writes that might meet them, a latency a chunk.)
 // diag: the column of v on the lane's diagonal, or none of 0 .. 31
-__device__ __forceinline__ void muon_box_poly(const MuonArgs::Step k, float* v, uint8_t* box, int lane, int j0, int diag) {
+__device__ __forceinline__ void muon_box_poly(const MuonArgs::Step k, float* v, uint8_t* box, int lane, int diag) {
   uint4 in[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) in[j] = *box_chunk(box, lane, j0 + j);
+  for (int j = 0; j < 4; ++j) in[j] = *box_chunk(box, lane, j);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint32_t w[4] = {in[j].x, in[j].y, in[j].z, in[j].w};
@@ -193,17 +197,17 @@ __device__ __forceinline__ void muon_box_poly(const MuonArgs::Step k, float* v, 
       if (diag == 8 * j + 2 * q + 1) x1 += k.poly_diag;
       o[q] = pack_h2(x0, x1);
     }
-    *box_chunk(box, lane, j0 + j) = make_uint4(o[0], o[1], o[2], o[3]);
+    *box_chunk(box, lane, j) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
 // X' (in v too) from X hi in box0 and, with LO, lo in box1; written back as hi and, with KEEP, lo
 template <bool LO, bool HI_OUT, bool LO_OUT>
-__device__ __forceinline__ void muon_box_apply(const MuonArgs::Step k, float* v, uint8_t* box0, uint8_t* box1, int lane, int j0) {
+__device__ __forceinline__ void muon_box_apply(const MuonArgs::Step k, float* v, uint8_t* box0, uint8_t* box1, int lane) {
   uint4 xh[4], xl[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    xh[j] = *box_chunk(box0, lane, j0 + j);
-    if (LO) xl[j] = *box_chunk(box1, lane, j0 + j);
+    xh[j] = *box_chunk(box0, lane, j);
+    if (LO) xl[j] = *box_chunk(box1, lane, j);
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -226,19 +230,19 @@ __device__ __forceinline__ void muon_box_apply(const MuonArgs::Step k, float* v,
         ol[q] = pack_h2((x0 - z.x) * MUON_SLO, (x1 - z.y) * MUON_SLO);
       }
     }
-    if (HI_OUT) *box_chunk(box0, lane, j0 + j) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
-    if (LO_OUT) *box_chunk(box1, lane, j0 + j) = make_uint4(ol[0], ol[1], ol[2], ol[3]);
+    if (HI_OUT) *box_chunk(box0, lane, j) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+    if (LO_OUT) *box_chunk(box1, lane, j) = make_uint4(ol[0], ol[1], ol[2], ol[3]);
   }
 }
 // The last step's X' in v: bf16, or the weights' update, into box0; W is in box1, or with `lo` (runs of up to three steps) still in memory
-__device__ __forceinline__ void muon_box_out(const MuonArgs& a, float* v, uint8_t* box0, uint8_t* box1, int lane, int j0, bool lo, int mat, int r, int c0) {
+__device__ __forceinline__ void muon_box_out(const MuonArgs& a, float* v, uint8_t* box0, uint8_t* box1, int lane, bool lo, int mat, int r, int c0) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     float* x = v + 8 * j;
     if (a.w_ptr) {
       uint4 w = make_uint4(0, 0, 0, 0);
-      const int c = c0 + 8 * (j0 + j);
-      if (!lo) w = *box_chunk(box1, lane, j0 + j);
+      const int c = c0 + 8 * j;
+      if (!lo) w = *box_chunk(box1, lane, j);
       else if (r < a.rows && c < a.cols) w = *reinterpret_cast<const uint4*>(a.w_ptr + ((size_t)mat * a.rows + r) * a.cols + c);
       const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -247,38 +251,26 @@ __device__ __forceinline__ void muon_box_out(const MuonArgs& a, float* v, uint8_
         x[2 * q + 1] = fmaf(a.keep, bf16hi(ww[q]), -a.rate * x[2 * q + 1]);
       }
     }
-    *box_chunk(box0, lane, j0 + j) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+    *box_chunk(box0, lane, j) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
   }
 }
-// The same for rows that are no whole vectors: X' in fp32 through both boxes, so that a row's elements are next to one another when they
-// are written
-__device__ __forceinline__ void muon_rows_out(const MuonArgs& a, const MuonArgs::Step& k, uint32_t tcol, uint8_t* boxes, bool lo, int lane, int mat, int r0, int c0) {
-  float v[64];
+// The same for rows that are no whole vectors: X' in fp32 through the slot, so that a row's elements are next to one another when they are written
+__device__ __forceinline__ void muon_rows_out(const MuonArgs& a, const MuonArgs::Step& k, float* v, uint8_t* slot, bool lo, int lane, int mat, int r0, int c0) {
+  if (lo) muon_box_apply<true, false, false>(k, v, slot, slot + MU_BOX, lane);
+  else muon_box_apply<false, false, false>(k, v, slot, slot + MU_BOX, lane);
+  __syncwarp();   // X has been read
 #pragma unroll
-  for (int q = 0; q < 4; ++q) tmem_ld16(tcol + 16 * q, v + 16 * q);
-  tmem_ld_wait();
-  if (lo) {
-    muon_box_apply<true, false, false>(k, v, boxes, boxes + MU_BOX, lane, 0);
-    muon_box_apply<true, false, false>(k, v + 32, boxes, boxes + MU_BOX, lane, 4);
-  } else {
-    muon_box_apply<false, false, false>(k, v, boxes, boxes + MU_BOX, lane, 0);
-    muon_box_apply<false, false, false>(k, v + 32, boxes, boxes + MU_BOX, lane, 4);
-  }
-  __syncwarp();   // X has been read from the boxes
-#pragma unroll
-  for (int j = 0; j < 16; ++j)
-    *reinterpret_cast<float4*>(boxes + lane * 256 + ((j ^ (lane & 7)) << 4)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+  for (int j = 0; j < 8; ++j) *wide_chunk(slot, lane, j) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
   __syncwarp();
+  const int c = c0 + lane;
 #pragma unroll 4
-  for (int i = 0; i < 64; ++i) {   // row i / 2, half a row at a time
-    const int r = i >> 1, c = (i & 1) * 32 + lane;
-    if (r0 + r < a.rows && c0 + c < a.cols) {
-      float x = *reinterpret_cast<const float*>(boxes + r * 256 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4);
-      const size_t at = ((size_t)mat * a.rows + r0 + r) * a.cols + c0 + c;
+  for (int i = 0; i < 32; ++i)
+    if (r0 + i < a.rows && c < a.cols) {
+      float x = reinterpret_cast<const float*>(wide_chunk(slot, i, lane >> 2))[lane & 3];
+      const size_t at = ((size_t)mat * a.rows + r0 + i) * a.cols + c;
       if (a.w_ptr) x = fmaf(a.keep, __uint_as_float((uint32_t)a.w_ptr[at] << 16), -a.rate * x);
       a.out_ptr[at] = (uint16_t)pack_bf16x2(x, 0.f);
     }
-  }
 }
 
 // JOIN: a strip of a tile's rows from the tile's parts, in their order; w: the warp of the pair.  Read past L1, which may hold an earlier
@@ -328,7 +320,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* boxes = smem + MU_STAGES * MU_STAGE_BYTES;
-  MuonBarriers* bars = reinterpret_cast<MuonBarriers*>(boxes + MU_EPI_WARPS * 2 * MU_BOX);
+  MuonBarriers* bars = reinterpret_cast<MuonBarriers*>(boxes + MU_EPI_WARPS * 2 * MU_SLOT);
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();
@@ -343,7 +335,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       mbar_init(&bars->tmem_full[s], 1);
       mbar_init(&bars->tmem_empty[s], MU_PARTS);
     }
-    for (int w = 0; w < MU_EPI_WARPS; ++w) mbar_init(&bars->in_full[w], 1);
+    for (int w = 0; w < 2 * MU_EPI_WARPS; ++w) mbar_init(&bars->in_full[w >> 1][w & 1], 1);
     for (int s = 0; s < MU_SLOTS; ++s) {
       mbar_init(&bars->item_full[s], 1);
       mbar_init(&bars->item_empty[s], MU_READERS);
@@ -479,10 +471,9 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
   } else {
     MuonTickets tk;
     const int ew = warp - 2, quad = warp & 3;
-    uint8_t* box0 = boxes + ew * 2 * MU_BOX;
-    uint8_t* box1 = box0 + MU_BOX;
-    uint64_t* in_full = &bars->in_full[ew];
-    uint32_t acc = 0, full_par = 0, in_par = 0, dep = 0, dep_par = 0;
+    uint8_t* slots_at = boxes + ew * 2 * MU_SLOT;
+    uint32_t sl = 0, in_par = 0;   // slot of the next box, parity of either slot's loads
+    uint32_t acc = 0, full_par = 0, dep = 0, dep_par = 0;
     for (bool ok = true; ok;) {
       const int t = tk.next(bars, slots, wc, 100, SPLIT);
       if (t < 0 || t >= total) break;   // (a kept slot is the only one, and nobody waits for it any more)
@@ -508,69 +499,76 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
         continue;
       }
       const bool parts = SPLIT && it.phase == MUON_GRAM;
+      const bool in = it.phase != MUON_GRAM;   // the box needs A or X
+      // this warp's boxes: every other one of its rows, those that lie in the product
+      const int b0 = (ew >> 2) * 32, left = min(it.nt, N - it.n0) - b0;
+      const int n_boxes = r0 < M && left > 0 ? (left + 63) / 64 : 0;
+      auto load = [&](int u, uint32_t s) {   // one lane
+        uint8_t* to = slots_at + s * MU_SLOT;
+        const int c = it.n0 + b0 + 64 * u;
+        fence_proxy_async_global();
+        mbar_expect_tx(&bars->in_full[ew][s], lo || upd ? 2 * MU_BOX : MU_BOX);
+        tma_load_3d_thread(to, it.phase == MUON_POLY ? &a.abox : &a.xhi[cur], c, r0, it.mat, &bars->in_full[ew][s]);
+        if (lo) tma_load_3d_thread(to + MU_BOX, &a.xlo[cur], c, r0, it.mat, &bars->in_full[ew][s]);
+        else if (upd) tma_load_3d_thread(to + MU_BOX, &a.w, c, r0, a.z0 + it.mat, &bars->in_full[ew][s]);
+      };
+      __syncwarp();   // every lane has read the slots
+      if (in && n_boxes && lane == 0) {
+        tma_store_wait_read();
+        load(0, sl);
+      }
       bool up = false;   // the accumulator has been seen complete
-      for (int b = (ew >> 2) * 64; b < it.nt; b += 128) {
-        const int c0 = it.n0 + b;
-        if (r0 >= M || c0 >= N) break;
-        __syncwarp();   // every lane has read the boxes
-        if (it.phase != MUON_GRAM) {
-          if (lane == 0) {
+      for (int u = 0; u < n_boxes; ++u, sl ^= 1) {
+        uint8_t *box0 = slots_at + sl * MU_SLOT, *box1 = box0 + MU_BOX;
+        const int b = b0 + 64 * u, c0 = it.n0 + b;
+        __syncwarp();
+        if (lane == 0) {
+          if (!in) {
+            tma_store_wait_read_but_one();   // this slot's, two boxes ago
+          } else if (u + 1 < n_boxes) {      // the next box's loads beside this one
             tma_store_wait_read();
-            fence_proxy_async_global();
-            mbar_expect_tx(in_full, lo || upd ? 2 * MU_BOX : MU_BOX);
-            tma_load_3d_thread(box0, it.phase == MUON_POLY ? &a.abox : &a.xhi[cur], c0, r0, it.mat, in_full);
-            if (lo) tma_load_3d_thread(box1, &a.xlo[cur], c0, r0, it.mat, in_full);
-            else if (upd) tma_load_3d_thread(box1, &a.w, c0, r0, a.z0 + it.mat, in_full);
+            load(u + 1, sl ^ 1);
           }
-          __syncwarp();
-        } else {
-          if (lane == 0) tma_store_wait_read();
-          __syncwarp();
         }
+        __syncwarp();
         if (!up) {
           if (!mbar_wait_warp(&bars->tmem_full[acc], (full_par >> acc) & 1, wc, SITE_TMEM_FULL, t, 100)) ok = false;
           tc_fence_after_sync();
           up = true;
         }
-        if (it.phase != MUON_GRAM) {
-          if (!mbar_wait_warp(in_full, in_par, wc, SITE_FULL, t)) ok = false;
-          in_par ^= 1;
+        if (in) {
+          if (!mbar_wait_warp(&bars->in_full[ew][sl], (in_par >> sl) & 1, wc, SITE_FULL, t)) ok = false;
+          in_par ^= 1u << sl;
         }
         if (!ok) break;
+        float v[32];
         const uint32_t tcol = tmem_base + acc * 256 + b + (static_cast<uint32_t>(quad * 32) << 16);
+        tmem_ld16(tcol, v);
+        tmem_ld16(tcol + 16, v + 16);
+        tmem_ld_wait();
         if (!VEC && last) {
-          muon_rows_out(a, a.step[it.step], tcol, box0, lo, lane, it.mat, r0, c0);
+          muon_rows_out(a, k, v, box0, lo, lane, it.mat, r0, c0);
           continue;
         }
-#pragma unroll 1
-        for (int j0 = 0; j0 < 8; j0 += 4) {
-          float v[32];
-          tmem_ld16(tcol + 8 * j0, v);
-          tmem_ld16(tcol + 8 * j0 + 16, v + 16);
-          tmem_ld_wait();
-          if (parts) {   // 32 columns in fp32 a box
+        if (parts) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              *reinterpret_cast<float4*>(box_chunk(j0 ? box1 : box0, lane, j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-          } else if (it.phase == MUON_GRAM) {
-            muon_box_gram(k, v, box0, lane, j0);
-          } else if (it.phase == MUON_POLY) {
-            muon_box_poly(k, v, box0, lane, j0, r0 + lane - c0 - 8 * j0);
-          } else if (!last) {
-            if (lo_out) muon_box_apply<true, true, true>(k, v, box0, box1, lane, j0);
-            else if (lo) muon_box_apply<true, true, false>(k, v, box0, box1, lane, j0);
-            else muon_box_apply<false, true, false>(k, v, box0, box1, lane, j0);
-          } else if (VEC) {
-            if (lo) muon_box_apply<true, false, false>(k, v, box0, box1, lane, j0);
-            else muon_box_apply<false, false, false>(k, v, box0, box1, lane, j0);
-            muon_box_out(a, v, box0, box1, lane, j0, lo, it.mat, r0 + lane, c0);
-          }
+          for (int j = 0; j < 8; ++j) *wide_chunk(box0, lane, j) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        } else if (it.phase == MUON_GRAM) {
+          muon_box_gram(k, v, box0, lane);
+        } else if (it.phase == MUON_POLY) {
+          muon_box_poly(k, v, box0, lane, r0 + lane - c0);
+        } else if (!last) {
+          if (lo_out) muon_box_apply<true, true, true>(k, v, box0, box1, lane);
+          else if (lo) muon_box_apply<true, true, false>(k, v, box0, box1, lane);
+          else muon_box_apply<false, true, false>(k, v, box0, box1, lane);
+        } else if (VEC) {
+          if (lo) muon_box_apply<true, false, false>(k, v, box0, box1, lane);
+          else muon_box_apply<false, false, false>(k, v, box0, box1, lane);
+          muon_box_out(a, v, box0, box1, lane, lo, it.mat, r0 + lane, c0);
         }
         staging_release();
         if (lane == 0 && parts) {
-          const int y = ((it.mat * order.tri + it.tile) * a.split + it.part) * 256 + rank * 128 + quad * 32;
-          tma_store_2d(&a.part, b, y, box0);
-          tma_store_2d(&a.part, b + 32, y, box1);
+          tma_store_2d(&a.part, b, ((it.mat * order.tri + it.tile) * a.split + it.part) * 256 + rank * 128 + quad * 32, box0);
           tma_store_commit();
         } else if (lane == 0) {
           const CUtensorMap* o = it.phase == MUON_GRAM ? &a.abox : it.phase == MUON_POLY ? &a.bbox : last ? &a.out : &a.xhi[cur ^ 1];
