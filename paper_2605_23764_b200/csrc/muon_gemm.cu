@@ -11,7 +11,7 @@
 // descriptor changes from k-block to k-block.  (Stored twice, as they are and mirrored, 132 matrices 1408 x 2048 took 14.2 ms instead of 12.0.)
 //
 // Where there are few tiles and a long reduction, GRAM sums parts of it and JOIN adds them up in their order (one matrix of 256 x 7168:
-// 210 -> 155 us).
+// 210 -> 140 us).
 //
 // What bounds it.  Large batches: power.  The tensor pipe is active 70 to 77 % of the clocks, at 1.4 GHz under the limit; 1.03 to 1.25 PFLOP/s
 // of executed products, where batched fp16 products of these shapes by the vendor's library sustain 1.07 and 1.16.  Without an epilogue
@@ -283,11 +283,13 @@ __device__ __forceinline__ void muon_join(const MuonArgs& a, const MuonItem& it,
     const int row = row0 + u / quads, c = u % quads * 4, r = it.m0 + row;
     if (r >= m) break;
     const float4* p = reinterpret_cast<const float4*>(a.part_ptr + (((size_t)it.mat * tri + it.tile) * a.split * 256 + row) * it.nt + c);
-    float4 s = __ldcg(p);
-#pragma unroll 8
-    for (int i = 1; i < a.split; ++i) {
-      const float4 x = __ldcg(p + i * step);
-      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < a.split; i += 16) {   // all loads of a turn under way together
+      float4 x[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[j] = i + j < a.split ? __ldcg(p + (i + j) * step) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) { s.x += x[j].x; s.y += x[j].y; s.z += x[j].z; s.w += x[j].w; }
     }
     if (it.n0 + c < a.lda)   // columns behind m are room
       *reinterpret_cast<uint2*>(a.a_ptr + ((size_t)it.mat * m + r) * a.lda + it.n0 + c) =
