@@ -598,6 +598,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
   }
 
   // ---------------------------------------------------------------- teardown
+  __syncwarp();
   if (*reinterpret_cast<volatile int*>(&a.status->abort)) __nanosleep(200000);
   tc_fence_before_sync();
   __syncthreads();
