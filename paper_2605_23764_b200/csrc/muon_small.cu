@@ -2,12 +2,16 @@
 // products and the weights' update, in one launch.
 //
 // X lies in TMEM in fp32, row i of its m rows on lane i, as V = X S_X S_B, and its fp16 image X S_X in shared memory.  A step is
-//   acc = X X^T;  A = fp16(acc);  acc = A A;  B = fp16(b A + c acc + s I);  V <- (a - s) V, then V += B X on the tensor cores
-// so the linear term never leaves fp32.  The image serves both products: as K-major operands of X X^T, and MN-major as the second of
-// B X.  Matrices taller than wide are turned while they are staged.
+//   acc = X X^T;  A = acc;  acc = A A;  B = b A + c acc + s I;  V <- (a - s) V, then V += B X on the tensor cores
+// so the linear term never leaves fp32.  The image serves both products: as K-major operands of X X^T, and MN-major as the second of B X.
+// Matrices taller than wide are turned while they are staged.  A A and B X sum over the m rows there are, in sixteens.
+// Up to 64 rows (MS_LO) A and B are two fp16 numbers each, hi + lo, and both products take lo too: there are few entries for roundings to
+// even out over (16 x 16, six steps: 1.4e-3 off in the norm instead of 2.0e-3; 128 x 256: 0.8e-3 instead of 1.2e-3), and their sums stay
+// short.  At 128 rows lo would cost 8 us of 31.
 //
-// What bounds it: latencies, some 2 us a step (three products of at most 0.3 us with what lies between them), and the loads in front.  By
-// the tiles of muon_gemm.cu every phase passes through L2 instead, with its stores, signal, poll and loads: 3.7 us.
+// What bounds it: latencies, 2.7 us a step at most (three products of at most 0.3 us with what lies between them), and some 9 us for the
+// loads in front and the stores behind: 28 us for five steps of 16 x 128 x 256.  By the tiles of muon_gemm.cu every phase passes through
+// L2 instead, with its stores, signal, poll and loads: 3.7 us.
 #include <cuda_fp16.h>
 
 #include "launch_pairs.cuh"
@@ -18,7 +22,8 @@ namespace moe {
 
 constexpr int MS_THREADS = 512, MS_WARPS = MS_THREADS / 32;
 constexpr int MS_BOX = 128 * 128;          // 128 rows x 64 columns in fp16, swizzled
-constexpr int MS_AB = 2 * MS_BOX;          // A or B, and 128 x 64 elements in fp32 on their way in and out
+constexpr int MS_LO = 64;                  // see above
+constexpr int MS_AB = 2 * MS_BOX;          // A's or B's hi, and 128 x 64 elements in fp32 on their way in and out; lo lies behind it
 
 struct MuonSmallShared {
   uint64_t done;           // the products issued last are complete
@@ -26,7 +31,7 @@ struct MuonSmallShared {
   float factor[2];
   double sums[MS_WARPS];
 };
-static size_t small_smem(int lp) { return 1024 + (size_t)(lp / 64) * MS_BOX + MS_AB + sizeof(MuonSmallShared); }
+static size_t small_smem(int lp) { return 1024 + (size_t)(lp / 64) * MS_BOX + 2 * MS_AB + sizeof(MuonSmallShared); }
 
 // tmem_ld16 the other way round; complete for other readers behind tmem_st_wait() and the fences.
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
@@ -37,6 +42,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// hi of two values, and what it leaves of them
+__device__ __forceinline__ uint32_t half2_rest(float& x, float& y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  const float2 f = __half22float2(h);
+  x -= f.x;
+  y -= f.y;
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
 __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
@@ -98,8 +111,10 @@ __global__ void __launch_bounds__(MS_THREADS, 1) muon_small_kernel(const __grid_
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const MuonElemArgs& e = a.e;
   const int l = WIDE ? e.cols : e.rows, chunks = (l + 63) / 64, lp = chunks * 64;
+  const int rows = WIDE ? e.rows : e.cols, ks = (rows + 15) / 16;
+  const bool with_lo = rows <= MS_LO;
   uint8_t* ab = smem + chunks * MS_BOX;
-  MuonSmallShared* sh = reinterpret_cast<MuonSmallShared*>(ab + MS_AB);
+  MuonSmallShared* sh = reinterpret_cast<MuonSmallShared*>(ab + 2 * MS_AB);
   const int warp = warp_index(), lane = threadIdx.x & 31, quad = warp & 3, group = warp >> 2;
   const int row = quad * 32 + lane;   // of X: this thread's TMEM lane
   const WaitCtl wc{a.status, a.budget_ns};
@@ -250,17 +265,37 @@ __global__ void __launch_bounds__(MS_THREADS, 1) muon_small_kernel(const __grid_
     tmem_ld16(acc + lanes + group * 32, v);
     tmem_ld16(acc + lanes + group * 32 + 16, v + 16);
     tmem_ld_wait();
-    uint32_t A[16];
+    float A[32];
 #pragma unroll
-    for (int q = 0; q < 16; ++q) A[q] = half2_of(v[2 * q] * st.gram_acc, v[2 * q + 1] * st.gram_acc);
+    for (int q = 0; q < 32; ++q) A[q] = v[q] * st.gram_acc;
+    // 32 columns of the lane's row into the boxes of hi and lo
+    auto put = [&](const float* x) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) *box8(box, row, j0 + j) = make_uint4(A[4 * j], A[4 * j + 1], A[4 * j + 2], A[4 * j + 3]);
+      for (int j = 0; j < 4; ++j) {
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float x0 = x[8 * j + 2 * q], x1 = x[8 * j + 2 * q + 1];
+          h[q] = half2_rest(x0, x1);
+          l[q] = half2_of(x0, x1);
+        }
+        *box8(box, row, j0 + j) = make_uint4(h[0], h[1], h[2], h[3]);
+        if (with_lo) *box8(box + MS_AB, row, j0 + j) = make_uint4(l[0], l[1], l[2], l[3]);
+      }
+    };
+    put(A);
+    if (!with_lo) {   // b A + c A A of one and the same A: with fp32's A in the first of them 1.8e-3 off instead of 1.2e-3 (100 x 120, six steps)
+#pragma unroll
+      for (int q = 0; q < 32; ++q) A[q] = __half2float(__float2half_rn(A[q]));
+    }
     ready();
     if (warp == 0) {
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {
-        const uint32_t at = ab_k + (kk >> 2) * (MS_BOX >> 4) + (kk & 3) * 2;
+      for (int kk = 0; kk < ks; ++kk) {
+        const uint32_t at = ab_k + (kk >> 2) * (MS_BOX >> 4) + (kk & 3) * 2, lo = at + (MS_AB >> 4);
         tc_mma1_f16_cta(acc, at, at, hi, sym, kk != 0);
+        if (!with_lo) continue;
+        tc_mma1_f16_cta(acc, lo, at, hi, sym, 1);
+        tc_mma1_f16_cta(acc, at, lo, hi, sym, 1);
       }
       tc_commit_cta(&sh->done);
     }
@@ -270,22 +305,20 @@ __global__ void __launch_bounds__(MS_THREADS, 1) muon_small_kernel(const __grid_
     tmem_ld_wait();
     const int diag = row - group * 32;
 #pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&A[q]));
-      float x0 = fmaf(y.x, st.poly_in, v[2 * q] * st.poly_acc), x1 = fmaf(y.y, st.poly_in, v[2 * q + 1] * st.poly_acc);
-      if (diag == 2 * q) x0 += st.poly_diag;
-      if (diag == 2 * q + 1) x1 += st.poly_diag;
-      A[q] = half2_of(x0, x1);
+    for (int q = 0; q < 32; ++q) {
+      A[q] = fmaf(A[q], st.poly_in, v[q] * st.poly_acc);
+      if (diag == q) A[q] += st.poly_diag;
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) *box8(box, row, j0 + j) = make_uint4(A[4 * j], A[4 * j + 1], A[4 * j + 2], A[4 * j + 3]);
+    put(A);
     ready();
     if (warp == 0) {
       for (int c = 0; c < lp; c += 256) {
         const uint32_t idesc = make_idesc_f16(128, min(256, lp - c), 0, 1);
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk)
-          tc_mma1_f16_cta(tmem + c, ab_k + (kk >> 2) * (MS_BOX >> 4) + (kk & 3) * 2, x_mn + (c / 64) * (MS_BOX >> 4) + kk * (2048 >> 4), hi, idesc, 1);
+        for (int kk = 0; kk < ks; ++kk) {
+          const uint32_t at = ab_k + (kk >> 2) * (MS_BOX >> 4) + (kk & 3) * 2, x = x_mn + (c / 64) * (MS_BOX >> 4) + kk * (2048 >> 4);
+          tc_mma1_f16_cta(tmem + c, at, x, hi, idesc, 1);
+          if (with_lo) tc_mma1_f16_cta(tmem + c, at + (MS_AB >> 4), x, hi, idesc, 1);
+        }
       }
       tc_commit_cta(&sh->done);
     }
