@@ -345,7 +345,7 @@ int moe_ffn_fwd_w4(moe_ctx* ctx, const uint16_t* x, const int32_t* topk_ids, con
  *   moe_muon_step            M_out = momentum M + dW;  u = dW + momentum M_out with nesterov, else M_out;
  *                            W_out = (1 - lr weight_decay) W - lr scale X;  W, dW, W_out bf16, M, M_out fp32; M_out may be M, W_out may be W
  * Products take fp16 operands (11 significant bits) and sum in fp32; the linear term a X keeps 22 bits of X or more while that counts (the
- * first three steps; matrices up to 128 x 384 all along).  After five such steps X is 1e-3 off in the norm before it is rounded to bf16
+ * first three steps; matrices up to 128 x 384 all along).  After five such steps X is 1e-3, tiny matrices 1.5e-3, off in the norm before it is rounded to bf16
  * (itself 1.7e-3).  Singular values far below the largest, tau times it, carry noise of some 3e-4 / tau of their own by then: gradients of
  * rank 256 of 512 are 2e-3 off, and more steps, which bring such values to 1, show more of it.
  * A matrix with NaN or infinite elements gives NaN, the others are not affected.

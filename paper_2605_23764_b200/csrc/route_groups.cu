@@ -171,7 +171,7 @@ __device__ __noinline__ int exact_choice(RouteRow r, double* c, int k, int n_gro
 constexpr int ROUTE_POOL = 32;   // candidates of a token
 template <int NPL>
 constexpr int ROUTE_WARPS = NPL <= 8 ? 8 : 4;   // of a block: each has a row in 64 bits in shared memory
-// Blocks on an SM: 64 registers a thread, 80 with 512 experts, 255 with 1024.  256 experts in 104 registers: 95 us instead of 78 for 65536
+// Blocks on an SM: 64 registers a thread, 80 with 512 experts, 255 with 1024.  256 experts in 104 registers: a fifth more time for 65536
 // tokens; 512 in 64 or 96: 4 to 9 us more for 16384.
 template <int NPL>
 constexpr int ROUTE_BLOCKS = NPL <= 8 ? 4 : NPL <= 16 ? 6 : 2;
@@ -190,7 +190,7 @@ __device__ __forceinline__ void top2_add(float& m1, float& m2, float x) {
 // A lane has NPL experts: with WHOLE (E = 32 NPL) neighbours, so that a row is read in vectors and a group that is a power of two of lanes
 // finds its score by shuffles; otherwise every 32nd, and groups are scanned in shared memory.
 //
-// What bounds it is instructions, 880 a token of 256 experts in 8 groups at 70 % of the issue slots (65536 tokens 78 us; 1150 with an IEEE
+// What bounds it is instructions, 880 a token of 256 experts in 8 groups at 70 % of the issue slots (65536 tokens 70 us; 1150 with an IEEE
 // division and expf for every expert, which the k chosen ones alone need, and a group found by dividing).  The rounds of a selection over
 // all keys go over the lanes' largest; who reaches the last of these finds its rank among a dozen.
 template <int NPL, bool WHOLE>
