@@ -550,6 +550,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
         tmem_ld_wait();
         if (!VEC && last) {
           muon_rows_out(a, k, v, box0, lo, lane, it.mat, r0, c0);
+          staging_release();   // the slot was written through; what comes into it next is loaded by TMA
           continue;
         }
         if (parts) {
