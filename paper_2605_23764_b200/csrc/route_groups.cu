@@ -20,15 +20,38 @@ namespace moe {
 
 constexpr unsigned ALL = 0xffffffffu;
 
-// How far apart two c, or two groups' scores, are for certain in the order that fp32 gives them.  2^(x log2 e) is off by 2 ulp and its
-// argument's rounding, ln 2 / 2 ulp of x log2 e: under (2 + 1.173 |x|) ulp; a sigmoid's share of that is at most s (1 - s) (2 + 1.173 |x|) < 0.77 ulp of 1; the addition and the reciprocal add 2.5 ulp of s: 3.3 x 2^-23
-// in all.  A softmax score's is at most 2.5 ulp of the largest score's, its sum's 10 ulp (the mean of d = max - logit weighted with e^-d is
-// under ln 1024) and 37 additions' roundings: under 2^-18 of the largest score.  The bias adds half an ulp of c, a group's sum the errors
-// of both and half an ulp.  Doubled, since two values are compared, and rounded up.
+// 2^x to 2 ulp, 1 / x to one, log2 x to 2^-22; results below 2^-126 as 0
+__device__ __forceinline__ float ex2_approx(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float lg2_approx(float x) {
+  float r;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float LOG2E = 1.4426950408889634f;
+
+// How far apart two c, or two groups' scores, are for certain in the order that fp32 gives them.  In units of 2^-23 of the value:
+//   2^y of y = -l log2 e is off by 2 and by what y's rounding and that of log2 e move it, ln 2 (0.5 + 0.12) |y| < 0.43 |y|;
+//   a sigmoid s = 1 / (1 + 2^y) takes the share 1 - s of that, the addition 0.5 and the reciprocal 1: at most 2.5 for l >= 0, and
+//   3.5 + 0.43 y for l < 0, which grows without limit as s falls.  s (3.5 + 0.43 y) falls with s, so no expert's error is above
+//   s_max (3.5 + 0.43 y) with the largest score's y, where that is positive; y < log2(1 + 2^y) = -log2 s_max.  One unit more is room for the
+//   roundings of the comparison itself and of that logarithm.
+//   A softmax score's is at most 2.5 of the largest score's, its sum's 10 (the mean of d = max - logit weighted with e^-d is under
+//   ln 1024) and 37 additions' roundings: under 32 of the largest score.
+// The bias adds half an ulp of c, a group's sum the errors of both and half an ulp.  Doubled, since two values are compared, and rounded up.
 struct RouteTol {
   float expert, group;
   __device__ RouteTol(bool sigmoid, float s_max, float b_max) {
-    const float s = s_max * (sigmoid ? 9.5367432e-7f /* 2^-20 */ : 7.6293945e-6f /* 2^-17 */), c = (s_max + b_max) * 1.1920929e-7f /* 2^-23 */;
+    constexpr float ULP = 1.1920929e-7f;   // 2^-23
+    const float s = s_max * (sigmoid ? fmaf(0.86f * ULP, -lg2_approx(fmaxf(s_max, FLT_MIN)), 9.f * ULP) : 64.f * ULP), c = (s_max + b_max) * ULP;
     constexpr float SUBNORMAL = 1e-37f;   // numbers below 2^-126 have steps of their own
     expert = s + c + SUBNORMAL;
     group = 2.f * (s + c) + 2.f * c + SUBNORMAL;
@@ -42,18 +65,6 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
-// 2^x to 2 ulp and 1 / x to one, results below 2^-126 as 0
-__device__ __forceinline__ float ex2_approx(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-__device__ __forceinline__ float rcp_approx(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-constexpr float LOG2E = 1.4426950408889634f;
 // INT_MAX: no expert, below all that there are
 __device__ __forceinline__ bool above(double a, int ia, double b, int ib) { return a > b || (a == b && ia < ib) || (ib == INT_MAX && ia != INT_MAX); }
 // sigmoid(l) or, where the largest l is far below 0, that over e^top: what such rows' sigmoids have in common is taken out
