@@ -344,10 +344,12 @@ int moe_ffn_fwd_w4(moe_ctx* ctx, const uint16_t* x, const int32_t* topk_ids, con
  *   moe_muon_orthogonalize   u = G (bf16 or fp32, MOE_MUON_*) -> out bf16 (which may be a bf16 G)
  *   moe_muon_step            M_out = momentum M + dW;  u = dW + momentum M_out with nesterov, else M_out;
  *                            W_out = (1 - lr weight_decay) W - lr scale X;  W, dW, W_out bf16, M, M_out fp32; M_out may be M, W_out may be W
- * Products take fp16 operands (11 significant bits) and sum in fp32; the linear term a X keeps 22 bits of X or more while that counts (the
- * first three steps; matrices up to 128 x 384 all along).  After five such steps X is 1e-3, tiny matrices 1.5e-3, off in the norm before it is rounded to bf16
- * (itself 1.7e-3).  Singular values far below the largest, tau times it, carry noise of some 3e-4 / tau of their own by then: gradients of
- * rank 256 of 512 are 2e-3 off, and more steps, which bring such values to 1, show more of it.
+ * Products take fp16 operands (11 significant bits) and sum in fp32; the linear term a X keeps 22 bits of X or more (matrices up to
+ * 128 x 384 all along; others in the first three steps, and in every step from which on the products of the |a| that are left sum up to more
+ * than 16: what a rounding adds beside large singular values grows by |a| a step).  After five such steps X is 1e-3, tiny matrices 1.5e-3, gradients of
+ * low rank up to 2.5e-3 off in the norm before it is rounded to bf16 (itself 1.7e-3).  Seven to nine such steps, or eight and more of
+ * (1.875, -1.25, 0.375) or (1.5, -0.5, 0), are 0.5e-3 to 2.5e-3 off, matrices of low rank among them; sixteen of the first triple, whose singular
+ * values do not settle, 3e-3 to 6e-3.
  * A matrix with NaN or infinite elements gives NaN, the others are not affected.
  *
  * moe_muon_create: like moe_create; the workspace (moe_muon_workspace_bytes, 0 for an invalid shape; 256-byte aligned device memory, or

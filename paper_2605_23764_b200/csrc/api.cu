@@ -1064,9 +1064,17 @@ int plan_muon_args(moe_muon* u) {
   const bool small = muon_is_small(s.rows, s.cols);
   MuonArgs& a = u->args;
   memset(&a, 0, sizeof a);
+  a.late = s.steps;
+  double grown = 1.0, sum = 0.0;   // the product of |a| from a step to the last, and of all those so far
+  while (a.late > std::min(MUON_SHIFT, s.steps)) {
+    grown *= std::fabs((double)s.coefficients[a.late - 1][0]);
+    sum += grown;
+    if (sum > MUON_GROWTH) break;
+    --a.late;
+  }
   for (int k = 0; k < s.steps; ++k) {
     const float ca = s.coefficients[k][0], cb = s.coefficients[k][1], cc = s.coefficients[k][2];
-    const float shift = k >= MUON_LATE && cb + cc < 0.f ? -0.75f * (cb + cc) : 0.f;
+    const float shift = k >= MUON_SHIFT && cb + cc < 0.f ? -0.75f * (cb + cc) : 0.f;
     const float scale = !small && k + 1 == s.steps ? 1.f / MUON_SX : 1.f;   // of the result
     MuonArgs::Step& t = a.step[k];
     t.gram_acc = MUON_SA / (MUON_SX * MUON_SX);
@@ -1075,6 +1083,7 @@ int plan_muon_args(moe_muon* u) {
     t.poly_diag = shift * MUON_SB;
     t.app_acc = scale / MUON_SB;
     t.app_in = (ca - shift) * scale;
+    t.app_rest = k < a.late ? shift * scale : 0.f;
   }
   if (small) return MOE_OK;
   a.nt_tri = p.nt_tri; a.nt_app = p.nt_app; a.split = p.split;

@@ -8,10 +8,15 @@
 // 2^-12 of the largest entries adds to a small singular value grows with it: matrices of rank 256 + rounding, 512 x 768, were 6.8e-3
 // off in the norm after five steps, with both 1.3e-3 (bf16 operands and X: 5.4e-2).
 //
-// Three steps on (MUON_LATE) the singular values have come near 1.  There X's lo part no longer counts and is left out (0.9e-3 instead of
-// 0.8e-3, 1.8e-3 instead of 1.3e-3 for the rank of 256).  B's diagonal is near b + c there, which a X mostly cancels: three quarters of it
-// move from B to the linear term, X <- (a - s) X + (B + s I) X with s = -3/4 (b + c).  Errors halve: 1.6e-3 -> 0.9e-3 on normally
-// distributed matrices.
+// From the fourth step on (MUON_SHIFT) the larger singular values have come near 1.  B's diagonal is near b + c there, which a X mostly cancels:
+// three quarters of it move from B to the linear term, X <- (a - s) X + (B + s I) X with s = -3/4 (b + c).  Errors halve: 1.6e-3 -> 0.9e-3
+// on normally distributed matrices, five steps.  The product takes s of X's hi alone, so lo enters the linear term with a.
+//
+// X's lo part is left out of the last steps (MuonArgs::late).  What rounding X to hi adds to a small singular value grows by |a| a step, so a
+// step can do without lo where the products of the |a| left, from its own and every later step's to the last's, sum up to MUON_GROWTH: two
+// of five steps of (3.4445, -4.7750, 2.0315), 15.3 (0.9e-3 instead of 0.8e-3, 1.8e-3 instead of 1.3e-3 for the rank of 256), never the first three.
+// Left out from the fourth step on whatever follows, with the shift's s of hi alone, matrices of rank 64, 256 x 400, were 1.6e-2 off
+// after seven such steps and 3.9e-2 after twelve of (1.875, -1.25, 0.375), 1.7e-3 and 1.3e-3 this way.
 #pragma once
 
 #include "moe_internal.h"
@@ -20,13 +25,14 @@ namespace moe {
 
 constexpr float MUON_SX = 4096.f, MUON_SA = 4096.f, MUON_SB = 1024.f, MUON_SLO = 2048.f;
 constexpr int MUON_STEPS_MAX = 16;
-constexpr int MUON_LATE = 3;   // first step (from 0) with the shifted diagonal and X in one part
+constexpr int MUON_SHIFT = 3;          // first step (from 0) with the shifted diagonal
+constexpr double MUON_GROWTH = 16.0;   // see above
 
 enum MuonPhase : int {
   MUON_GRAM = 0,    // A = X X^T or X^T X, or sums over parts of the reduction
   MUON_JOIN = 1,    // A from those
   MUON_POLY = 2,    // B = b A + c A A + s I
-  MUON_APPLY = 3,   // X' = (a - s) X + B X or X B; of the last step: into the caller's tensors
+  MUON_APPLY = 3,   // X' = (a - s) X + s lo + B X or X B; of the last step: into the caller's tensors
 };
 
 // A symmetric matrix is stored by blocks of 256 x 256, those on and below the diagonal.
@@ -48,7 +54,9 @@ struct MuonArgs {
   int lda;
   int sub;                     // matrices whose phases follow one another
   int z0;                      // the batch's first matrix in the caller's tensors
-  struct Step { float gram_acc, poly_acc, poly_in, poly_diag, app_acc, app_in; } step[MUON_STEPS_MAX];   // factors in the stored scalings
+  int late;                    // first step that goes by X's hi part alone
+  // factors in the stored scalings; app_in: of X (hi + lo), app_rest: of lo besides (0 without a shift)
+  struct Step { float gram_acc, poly_acc, poly_in, poly_diag, app_acc, app_in, app_rest; } step[MUON_STEPS_MAX];
   // the last step's X': out = X', or with W: out = keep W - rate X'
   uint16_t* out_ptr;           // bf16 [rows][cols] of the batch's first matrix
   const uint16_t* w_ptr;       // NULL: none
@@ -93,7 +101,7 @@ inline bool muon_is_small(int rows, int cols) {
 struct MuonSmallArgs {
   MuonElemArgs e;
   int steps;
-  MuonArgs::Step step[MUON_STEPS_MAX];   // app_in: a - s
+  MuonArgs::Step step[MUON_STEPS_MAX];   // app_in: a - s; app_rest: s in steps that are not late
   uint16_t* out;
   const uint16_t* W;    // NULL: out = X'
   float keep, rate;

@@ -215,13 +215,17 @@ __device__ __forceinline__ void muon_box_apply(const MuonArgs::Step k, float* v,
     uint32_t oh[4], ol[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      float2 y = unpack_h2(wh[q]);
+      float2 y = unpack_h2(wh[q]), yl = make_float2(0.f, 0.f);
       if (LO) {
-        const float2 yl = unpack_h2(wl[q]);
+        yl = unpack_h2(wl[q]);
         y.x = fmaf(yl.x, 1.f / MUON_SLO, y.x);
         y.y = fmaf(yl.y, 1.f / MUON_SLO, y.y);
       }
-      const float x0 = fmaf(y.x, k.app_in, v[8 * j + 2 * q] * k.app_acc), x1 = fmaf(y.y, k.app_in, v[8 * j + 2 * q + 1] * k.app_acc);
+      float x0 = fmaf(y.x, k.app_in, v[8 * j + 2 * q] * k.app_acc), x1 = fmaf(y.y, k.app_in, v[8 * j + 2 * q + 1] * k.app_acc);
+      if (LO) {
+        x0 = fmaf(yl.x, k.app_rest * (1.f / MUON_SLO), x0);
+        x1 = fmaf(yl.y, k.app_rest * (1.f / MUON_SLO), x1);
+      }
       v[8 * j + 2 * q] = x0;
       v[8 * j + 2 * q + 1] = x1;
       if (HI_OUT) oh[q] = pack_h2(x0, x1);
@@ -234,7 +238,7 @@ __device__ __forceinline__ void muon_box_apply(const MuonArgs::Step k, float* v,
     if (LO_OUT) *box_chunk(box1, lane, j) = make_uint4(ol[0], ol[1], ol[2], ol[3]);
   }
 }
-// The last step's X' in v: bf16, or the weights' update, into box0; W is in box1, or with `lo` (runs of up to three steps) still in memory
+// The last step's X' in v: bf16, or the weights' update, into box0; W is in box1, or with `lo` (no late step) still in memory
 __device__ __forceinline__ void muon_box_out(const MuonArgs& a, float* v, uint8_t* box0, uint8_t* box1, int lane, bool lo, int mat, int r, int c0) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -484,7 +488,7 @@ __global__ void __launch_bounds__(MU_THREADS, 1) muon_products_kernel(const __gr
       const int m = min(a.rows, a.cols), cur = it.step & 1;
       const int M = it.phase == MUON_APPLY ? a.rows : m, N = it.phase == MUON_APPLY ? a.cols : m;
       const bool last = it.phase == MUON_APPLY && it.step + 1 == a.steps;
-      const bool lo = it.phase == MUON_APPLY && it.step < MUON_LATE, lo_out = it.phase == MUON_APPLY && !last && it.step + 1 < MUON_LATE;
+      const bool lo = it.phase == MUON_APPLY && it.step < a.late, lo_out = it.phase == MUON_APPLY && !last && it.step + 1 < a.late;
       const bool upd = last && !lo && VEC && a.w_ptr;   // W comes with X
       const int r0 = it.m0 + rank * 128 + quad * 32;
       // the loader polls the counter for the CTA

@@ -2,8 +2,8 @@
 // products and the weights' update, in one launch.
 //
 // X lies in TMEM in fp32, row i of its m rows on lane i, as V = X S_X S_B, and its fp16 image X S_X in shared memory.  A step is
-//   acc = X X^T;  A = acc;  acc = A A;  B = b A + c acc + s I;  V <- (a - s) V, then V += B X on the tensor cores
-// so the linear term never leaves fp32.  The image serves both products: as K-major operands of X X^T, and MN-major as the second of B X.
+//   acc = X X^T;  A = acc;  acc = A A;  B = b A + c acc + s I;  V <- (a - s) V + s (V - image), then V += B X on the tensor cores
+// so the linear term never leaves fp32 (s (V - image) in steps that are not late: muon.cuh).  The image serves both products: as K-major operands of X X^T, and MN-major as the second of B X.
 // Matrices taller than wide are turned while they are staged.  A A and B X sum over the m rows there are, in sixteens.
 // Up to 64 rows (MS_LO) A and B are two fp16 numbers each, hi + lo, and both products take lo too: there are few entries for roundings to
 // even out over (16 x 16, six steps: 1.4e-3 off in the norm instead of 2.0e-3; 128 x 256: 0.8e-3 instead of 1.2e-3), and their sums stay
@@ -248,12 +248,17 @@ __global__ void __launch_bounds__(MS_THREADS, 1) muon_small_kernel(const __grid_
       tc_commit_cta(&sh->done);
     }
     // the linear term, beside the products
+    const bool rest = st.app_rest != 0.f;
     for (int c = group * 16; c < lp; c += 64) {
       float v[16];
       tmem_ld16(tmem + lanes + c, v);
       tmem_ld_wait();
 #pragma unroll
-      for (int q = 0; q < 16; ++q) v[q] *= st.app_in;
+      for (int q = 0; q < 16; ++q) {
+        float x = v[q] * st.app_in;
+        if (rest) x = fmaf(v[q] - __half2float(__float2half_rn(v[q] * (1.f / MUON_SB))) * MUON_SB, st.app_rest, x);   // what the image lacks of V
+        v[q] = x;
+      }
       tmem_st16(tmem + lanes + c, v);
     }
     tmem_st_wait();
