@@ -67,10 +67,11 @@ __device__ __forceinline__ float warp_sum(float x) {
 
 // INT_MAX: no expert, below all that there are
 __device__ __forceinline__ bool above(double a, int ia, double b, int ib) { return a > b || (a == b && ia < ib) || (ib == INT_MAX && ia != INT_MAX); }
-// sigmoid(l) or, where the largest l is far below 0, that over e^top: what such rows' sigmoids have in common is taken out
+// sigmoid(l) over e^min(top, 0), top the largest l: what a row's sigmoids have in common is taken out, so that none leaves fp32's range
+// while its share of the sum does not (logits of -50 and -95: 2.9e-20)
 __device__ __forceinline__ float shifted_sigmoid(float l, float top) {
-  if (top > -60.f) return __fdividef(1.f, 1.f + expf(-l));
-  return __fdividef(1.f, expf(top - l) + expf(top));
+  if (l >= 0.f) return __fdividef(1.f, 1.f + expf(-l));
+  return __fdividef(expf(l - fminf(top, 0.f)), 1.f + expf(l));
 }
 
 // One token in 64 bits, for the cases that fp32 leaves open.  bias: in shared memory, NULL: none.
