@@ -271,7 +271,8 @@ int moe_balance_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, 
 
 /* ---- Routing by groups, with a bias for balance -----------------------------------------------------------
  * Experts stand in n_groups groups of E / n_groups neighbours.  With s = softmax(logits) or, with MOE_FLAG_SIGMOID_GATE, the sigmoids:
- *   c[t][e] = s[t][e] + bias[e] (bias fp32 [E], NULL: none)         what decides; -infinity where the logit is
+ *   c[t][e] = s[t][e] + bias[e] (bias fp32 [E], NULL: none)         what decides; -infinity where the logit is, or the bias: such an
+ *                                                                   expert comes behind all others (which costs the others nothing)
  *   a group's score is the sum of its group_top (1 or 2) largest c; the top_groups groups of the largest scores stay
  *   topk_ids[t]: the k experts of the largest c in them, in descending order
  *   topk_w[t]: their scores s, without the bias -- over their sum with MOE_FLAG_RENORM_TOPK (0 where that is 0) -- times scale

@@ -46,16 +46,23 @@ constexpr float LOG2E = 1.4426950408889634f;
 //   roundings of the comparison itself and of that logarithm.
 //   A softmax score's is at most 2.5 of the largest score's, its sum's 10 (the mean of d = max - logit weighted with e^-d is under
 //   ln 1024) and 37 additions' roundings: under 32 of the largest score.
-// The bias adds half an ulp of c, a group's sum the errors of both and half an ulp.  Doubled, since two values are compared, and rounded up.
+// Doubled, since two values are compared, and rounded up; a group's score has two experts'.
+//   The bias adds half an ulp of c, a group's sum the errors of both c and half an ulp of its own: of every value by itself, so that a bias that
+//   keeps an expert out, -infinity or -1e9, leaves the others' comparisons what they are (by the largest bias of all, 65536 x 256 took 450 us
+//   instead of 66, every token in 64 bits).
 struct RouteTol {
+  static constexpr float ULP = 1.2e-7f;   // 2^-23, rounded up
   float expert, group;
-  __device__ RouteTol(bool sigmoid, float s_max, float b_max) {
-    constexpr float ULP = 1.1920929e-7f;   // 2^-23
-    const float s = s_max * (sigmoid ? fmaf(0.86f * ULP, -lg2_approx(fmaxf(s_max, FLT_MIN)), 9.f * ULP) : 64.f * ULP), c = (s_max + b_max) * ULP;
+  __device__ RouteTol(bool sigmoid, float s_max) {
+    const float s = s_max * (sigmoid ? fmaf(0.86f * ULP, -lg2_approx(fmaxf(s_max, FLT_MIN)), 9.f * ULP) : 64.f * ULP);
     constexpr float SUBNORMAL = 1e-37f;   // numbers below 2^-126 have steps of their own
-    expert = s + c + SUBNORMAL;
-    group = 2.f * (s + c) + 2.f * c + SUBNORMAL;
+    expert = s + SUBNORMAL;
+    group = 2.f * s + SUBNORMAL;
   }
+  // half an ulp of two values, of the magnitudes' sum or, doubled, of the larger one; infinities have none
+  __device__ __forceinline__ static float rounding(float magnitude) { return ULP * fminf(magnitude, FLT_MAX); }
+  // a >= b, and so they are for certain
+  __device__ __forceinline__ bool settled(float a, float b) const { return a - b > expert + rounding(fmaxf(fabsf(a), fabsf(b))); }
 };
 
 __device__ __forceinline__ float warp_max(float x) { return key_float(__reduce_max_sync(ALL, float_key(x))); }
@@ -224,16 +231,11 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS<NPL>, ROUTE_BLOCKS<NPL>) rout
   auto expert = [&](int i) { return WHOLE ? lane * NPL + i : 32 * i + lane; };
   pdl_trigger();
   pdl_wait();
-  float b_max = 0.f;
   for (int e = threadIdx.x; e < E; e += 32 * WARPS) {
     sbias[RouteRow::place(e, LOG)] = a.bias ? a.bias[e] : 0.f;
     hist[e] = 0;
   }
   __syncthreads();
-  if (a.bias) {
-    for (int e = lane; e < E; e += 32) b_max = fmaxf(b_max, fabsf(sbias[e]));
-    b_max = warp_max(b_max);
-  }
   const int avail = a.top_groups * gs, want = min(k + 1, min(avail, 32));
   int span_log = 5;   // 2^span_log lanes scan a group together
   while (G << span_log > 32) --span_log;
@@ -298,41 +300,41 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS<NPL>, ROUTE_BLOCKS<NPL>) rout
       // NaN among the scores; 32 experts have no lane left for the one behind them
       open = !(s_max <= FLT_MAX) || (a.bias && want <= k && avail > k);
     }
-    const RouteTol tol(sigmoid, s_max, b_max);
+    const RouteTol tol(sigmoid, s_max);
     uint32_t kept = ALL;
     if (pick) {
-      float score;
+      // `span` lanes a group: the two largest of their shares, then of one another's
+      float m1 = -INFINITY, m2 = -INFINITY;
       if (by_lanes) {
-        float m1 = v[0], m2 = -INFINITY;
+        m1 = v[0];
 #pragma unroll
         for (int i = 1; i < NPL; ++i) top2_add(m1, m2, v[i]);
-        for (int off = span >> 1; off; off >>= 1) top2(m1, m2, __shfl_xor_sync(ALL, m1, off), __shfl_xor_sync(ALL, m2, off));
-        score = a.group_top == 2 ? m1 + m2 : m1;
       } else {
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < NPL; ++i)
           if (WHOLE || expert(i) < E) c32[expert(i)] = v[i];
         __syncwarp();
-        // `span` lanes a group: the two largest of their shares, then of one another's
         const int g = lane >> span_log;
-        float m1 = -INFINITY, m2 = -INFINITY;
         if (g < G)
           for (int j = lane & (span - 1); j < gs; j += span) top2_add(m1, m2, c32[g * gs + j]);
-        for (int off = span >> 1; off; off >>= 1) top2(m1, m2, __shfl_xor_sync(ALL, m1, off), __shfl_xor_sync(ALL, m2, off));
-        score = a.group_top == 2 ? m1 + m2 : m1;
       }
-      score = __shfl_sync(ALL, score, min(lane << span_log, 31));   // from here on lane g has group g
+      for (int off = span >> 1; off; off >>= 1) top2(m1, m2, __shfl_xor_sync(ALL, m1, off), __shfl_xor_sync(ALL, m2, off));
+      const int from = min(lane << span_log, 31);   // from here on lane g has group g
+      const float score = __shfl_sync(ALL, a.group_top == 2 ? m1 + m2 : m1, from);
       int rank = 0;
       for (int o = 0; o < G; ++o) {
         const float x = __shfl_sync(ALL, score, o);
         rank += x > score || (x == score && o < lane) ? 1 : 0;
       }
-      kept = __ballot_sync(ALL, lane < G && rank < a.top_groups);
+      const bool stays = lane < G && rank < a.top_groups;
+      kept = __ballot_sync(ALL, stays);
       if (scored) {
-        const uint32_t low = __ballot_sync(ALL, lane < G && rank == a.top_groups - 1), high = __ballot_sync(ALL, lane < G && rank == a.top_groups);
-        if (!(__shfl_sync(ALL, score, __ffs(low) - 1) - __shfl_sync(ALL, score, __ffs(high) - 1) > tol.group))
-          kept = exact_groups(exact, c64, G, a.top_groups, a.group_top, lane);
+        // the least that a group that stays can have, and the most of one that does not
+        const float off = RouteTol::rounding(__shfl_sync(ALL, fabsf(m1) + (a.group_top == 2 ? fabsf(m2) : 0.f), from));
+        const float least = key_float(__reduce_min_sync(ALL, stays ? float_key(score - off) : ~0u));
+        const float most = key_float(__reduce_max_sync(ALL, lane < G && !stays ? float_key(score + off) : 0u));
+        if (!(least - most > tol.group)) kept = exact_groups(exact, c64, G, a.top_groups, a.group_top, lane);
       }
     }
     if (scored && !a.bias) {   // the experts' order is that of the logits, scores were for the groups
@@ -402,14 +404,14 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS<NPL>, ROUTE_BLOCKS<NPL>) rout
     }
     if (a.bias) {
       const float next = __shfl_down_sync(ALL, val, 1);
-      if (__any_sync(ALL, lane + 1 < want && !(val - next > tol.expert))) {
+      if (__any_sync(ALL, lane + 1 < want && !tol.settled(val, next))) {
         // the candidates' order is enough where none of the others can be among the k
         const float least = __shfl_sync(ALL, val, k - 1);
         uint32_t rest = 0;
 #pragma unroll
         for (int i = 0; i < NPL; ++i) rest = max(rest, key[i] < bound ? key[i] : 0u);
         rest = __reduce_max_sync(ALL, rest);
-        if (few && (rest == 0u || least - key_float(rest) > tol.expert)) mine = exact_order(exact, mine, n, reinterpret_cast<int*>(pool), lane);
+        if (few && (rest == 0u || tol.settled(least, key_float(rest)))) mine = exact_order(exact, mine, n, reinterpret_cast<int*>(pool), lane);
         else open = true;
       }
     }
