@@ -1592,7 +1592,10 @@ int moe_muon_step(moe_muon* u, const uint16_t* W, const float* M, const uint16_t
   if (!u || !W || !M || !dW || !W_out || !M_out) return MOE_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(W) | reinterpret_cast<uintptr_t>(dW) | reinterpret_cast<uintptr_t>(W_out)) & 1) return MOE_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(M) | reinterpret_cast<uintptr_t>(M_out)) & 3) return MOE_ERR_INVALID_ARG;
-  if (!std::isfinite(momentum) || !std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(scale)) return MOE_ERR_INVALID_ARG;
+  const float keep = (float)(1.0 - (double)lr * (double)weight_decay), rate = lr * scale;   // of W and of X
+  if (!std::isfinite(momentum) || !std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(scale) || !std::isfinite(keep) ||
+      !std::isfinite(rate))
+    return MOE_ERR_INVALID_ARG;
   if (!on_its_device(u)) return MOE_ERR_INVALID_ARG;
   u->last_stream = static_cast<cudaStream_t>(stream);
   u->launches = 0;
@@ -1605,7 +1608,7 @@ int moe_muon_step(moe_muon* u, const uint16_t* W, const float* M, const uint16_t
   e.nesterov = nesterov != 0;
   const bool rows8 = u->shape.cols % 8 == 0;
   e.vec = rows8 && aligned16(dW) && aligned16(M) && aligned16(M_out);
-  return run_muon(u, e, W, W_out, (float)(1.0 - (double)lr * (double)weight_decay), lr * scale, u->last_stream);
+  return run_muon(u, e, W, W_out, keep, rate, u->last_stream);
 }
 
 int moe_muon_get_status(moe_muon* u, int32_t* code, int32_t* detail) {
