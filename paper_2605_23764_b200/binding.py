@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import importlib.util
+import numbers
 import os
 import struct
 import sysconfig
@@ -530,13 +531,17 @@ def moe_muon_shape(n, rows, cols, coefficients, steps, eps):
     s.eps = float(eps)
     if not 1 <= s.steps <= MOE_MUON_MAX_STEPS:
         raise MoeError(f"steps: {s.steps}, expected 1 to {MOE_MUON_MAX_STEPS}")
-    triples = list(coefficients)
-    if len(triples) == 3 and all(isinstance(v, (int, float)) for v in triples):
-        triples = [triples] * s.steps
+    try:
+        triples = list(coefficients)
+        if len(triples) == 3 and all(isinstance(v, numbers.Real) for v in triples):   # NumPy's numbers too
+            triples = [triples] * s.steps
+        triples = [[float(v) for v in t] for t in triples]
+    except (TypeError, ValueError):
+        triples = []
     if len(triples) != s.steps or any(len(t) != 3 for t in triples):
         raise MoeError(f"coefficients: expected (a, b, c), or {s.steps} of them")
     for i, t in enumerate(triples):
-        s.coefficients[i][:] = [float(v) for v in t]
+        s.coefficients[i][:] = t
     return s
 
 
