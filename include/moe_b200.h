@@ -277,7 +277,8 @@ int moe_balance_bwd(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, 
  *   topk_ids[t]: the k experts of the largest c in them, in descending order
  *   topk_w[t]: their scores s, without the bias -- over their sum with MOE_FLAG_RENORM_TOPK (0 where that is 0) -- times scale
  * Values are compared as they are in 64 bits, equal ones go to the lower group or expert, so which experts come out does not hang on
- * an fp32 rounding (without a bias the experts' order is that of the logits).  n_groups = top_groups = 1: all experts.
+ * an fp32 rounding.  Without a bias experts go by their logits, and with group_top = 1 groups by their largest logit, also where scores are
+ * equal in 64 bits (sigmoids of 40 and 50).  n_groups = top_groups = 1: all experts.
  * counts[E] (may be NULL): slots of each expert.  Logits are finite or -infinity; NaN gives ids in range and unspecified weights.
  * Requirements: E % n_groups == 0, n_groups <= 32, 1 <= top_groups <= n_groups, group_top <= E / n_groups where groups are left
  * out, k <= top_groups * E / n_groups.

@@ -4,11 +4,11 @@
 //   groups of the largest scores stay, of their experts the k of the largest c; w = s (of the k over their sum), times scale.
 //
 // Which experts come out must not hang on a rounding: c is compared as it is in 64 bits, ties go to the lower index.  A warp has a
-// token.  It selects in fp32 and looks whether the selection is beyond doubt: the last group kept and the first one left out, and every
+// token.  It selects in fp32 and looks whether the selection is beyond doubt: the groups kept and those left out, and every
 // two neighbours in the order of the k + 1 largest, further apart than fp32 can have moved them (RouteTol).  Where the groups are not,
 // theirs are computed in 64 bits, where the experts are not, those of the candidates (one token in a thousand of normally distributed
 // logits, one in a hundred of a softmax over 512), and where that does not settle it, as with ties, everything is.  Without a bias the
-// experts' order is that of the logits, whose comparison is exact.
+// experts' order is that of the logits, whose comparison is exact, and so is that of groups by their best expert.
 #include <float.h>
 #include <limits.h>
 
