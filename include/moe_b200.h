@@ -354,8 +354,8 @@ int moe_ffn_fwd_w4(moe_ctx* ctx, const uint16_t* x, const int32_t* topk_ids, con
  * values do not settle, 3e-3 to 6e-3.
  * A matrix with NaN or infinite elements gives NaN, the others are not affected.
  *
- * moe_muon_create: like moe_create; the workspace (moe_muon_workspace_bytes, 0 for an invalid shape; 256-byte aligned device memory, or
- * NULL) holds a batch of the matrices, about 1 GB at most unless a single one needs more (next to nothing for matrices up to 128 x 384,
+ * moe_muon_create: like moe_create; the workspace (moe_muon_workspace_bytes, 0 for an invalid shape; 256-byte aligned device memory that
+ * nothing enqueued before still uses, or NULL) holds a batch of the matrices, about 1 GB at most unless a single one needs more (next to nothing for matrices up to 128 x 384,
  * which stay on the chip).  Tensors need their type's alignment only;
  * 16-byte aligned ones with cols % 8 == 0 are read and written in vectors.  1 <= n, rows, cols <= MOE_MUON_MAX_SIZE,
  * 1 <= steps <= MOE_MUON_MAX_STEPS, eps >= 0.  Calls are asynchronous on `stream`; like a moe_ctx, a moe_muon serves one call at a

@@ -1030,6 +1030,7 @@ class MoeMuon:
         if nbytes == 0:
             raise MoeError("invalid shape")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        torch.cuda.current_stream().synchronize()   # whose freed memory it may be; the handle's state is cleared beside all streams
         self.handle = moe_muon_create(shape, self.workspace)
 
     @classmethod
@@ -1088,6 +1089,7 @@ class MoeLayer:
         if nbytes == 0:
             raise MoeError("invalid shape")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        torch.cuda.current_stream().synchronize()   # as in MoeMuon
         self.ctx = moe_create(T_max, d, E, k, n_shared, F, self.flags, self.workspace)
 
     def close(self):
