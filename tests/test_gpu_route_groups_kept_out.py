@@ -42,7 +42,8 @@ def _open(l, b, k, n_groups, top_groups, group_top, sigmoid):
     on = np.flatnonzero(np.repeat(kept, len(l) // n_groups))
     o = on[np.argsort(-c[on], kind="stable")][:k + 1]
     x, y = o[:-1], o[1:]
-    near = c[x] - c[y] <= 2.0 ** -46 * s.max() + 2.0 ** -52 * np.maximum(big[x], big[y])   # (-infinity beside -infinity: the lower one, no doubt)
+    with np.errstate(invalid="ignore"):   # -infinity beside -infinity: the lower one, no doubt
+        near = c[x] - c[y] <= 2.0 ** -46 * s.max() + 2.0 ** -52 * np.maximum(big[x], big[y])
     return bool((near & ((l[x] != l[y]) | (b[x] != b[y]))).any())
 
 
