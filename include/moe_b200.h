@@ -342,7 +342,8 @@ int moe_ffn_fwd_w4(moe_ctx* ctx, const uint16_t* x, const int32_t* topk_ids, con
  * [F][d], the gate and the up projection each by itself; W_down: E + S matrices [d][F]):
  *   X = u / (|u| + eps), |u| the root of the sum of squares;   for each step:  X <- a X + (b A + c A A) X,  A = X X^T
  * with (a, b, c) = coefficients[step].  (3.4445, -4.7750, 2.0315) five times takes singular values above a hundredth of |u| to 0.7 .. 1.2.
- * The polynomials must keep singular values of at most 1 within 2.  A matrix of zeros (an expert without tokens) stays zero.
+ * The polynomials must keep singular values of at most 1 within 2, and |b x^2 + c x^4| of what they reach below 60 (fp16 operands).  A matrix of
+ * zeros (an expert without tokens) stays zero.
  *   moe_muon_orthogonalize   u = G (bf16 or fp32, MOE_MUON_*) -> out bf16 (which may be a bf16 G)
  *   moe_muon_step            M_out = momentum M + dW;  u = dW + momentum M_out with nesterov, else M_out;
  *                            W_out = (1 - lr weight_decay) W - lr scale X;  W, dW, W_out bf16, M, M_out fp32; M_out may be M, W_out may be W

@@ -1,5 +1,5 @@
 // The passes over single elements in front of an orthogonalisation (muon.cuh): momentum with the sum of squares, and X = u / norm.
-// Both are streams: 14 and 10 bytes an element of a training step (bf16 gradients, fp32 momentum), 2 and 6 of a plain bf16 input.
+// Both are streams: 10 and 10 bytes an element of a training step (bf16 gradients, fp32 momentum), 2 and 6 of a plain bf16 input.
 // Squares are summed in 64 bits in a fixed order, so that neither large nor small gradients leave fp32's range.
 #include <cuda_fp16.h>
 

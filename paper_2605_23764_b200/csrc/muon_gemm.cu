@@ -8,7 +8,7 @@
 // Operands come in as they lie: K-major where the reduction is contiguous, MN-major where it is the rows (X as the second operand of
 // B X, both of X^T X), so nothing is ever transposed in memory.  A, B and their like are symmetric: tiles above the diagonal are neither
 // computed nor stored, and an operand's k-blocks that would lie there are read from their mirror image, MN-major -- the instruction
-// descriptor changes from k-block to k-block.  (Stored twice, as they are and mirrored, 132 matrices 1408 x 2048 took 14.2 ms instead of 12.0.)
+// descriptor changes from k-block to k-block.  (Stored twice, as they are and mirrored, 132 matrices 1408 x 2048 took 18 % longer.)
 //
 // Where there are few tiles and a long reduction, GRAM sums parts of it and JOIN adds them up in their order (one matrix of 256 x 7168:
 // 210 -> 140 us).

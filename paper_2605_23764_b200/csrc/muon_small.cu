@@ -9,8 +9,8 @@
 // even out over (16 x 16, six steps: 1.4e-3 off in the norm instead of 2.0e-3; 128 x 256: 0.8e-3 instead of 1.2e-3), and their sums stay
 // short.  At 128 rows lo would cost 8 us of 31.
 //
-// What bounds it: latencies, 2.7 us a step at most (three products of at most 0.3 us with what lies between them), and some 9 us for the
-// loads in front and the stores behind: 28 us for five steps of 16 x 128 x 256.  By the tiles of muon_gemm.cu every phase passes through
+// What bounds it: latencies, 3.8 us a step of 16 x 128 x 256 (three products of at most 0.3 us with what lies between them; 4.2 us where V's
+// rest is added) and 14 us for the loads in front and the stores behind, 10 without momentum and weights: 33 us for five steps.  By the tiles of muon_gemm.cu every phase passes through
 // L2 instead, with its stores, signal, poll and loads: 3.7 us.
 #include <cuda_fp16.h>
 

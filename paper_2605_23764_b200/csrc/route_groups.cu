@@ -209,7 +209,7 @@ __device__ __forceinline__ void top2_add(float& m1, float& m2, float x) {
 // A lane has NPL experts: with WHOLE (E = 32 NPL) neighbours, so that a row is read in vectors and a group that is a power of two of lanes
 // finds its score by shuffles; otherwise every 32nd, and groups are scanned in shared memory.
 //
-// What bounds it is instructions, 880 a token of 256 experts in 8 groups at 70 % of the issue slots (65536 tokens 70 us; 1150 with an IEEE
+// What bounds it is instructions, 866 a token of 256 experts in 8 groups with a bias at 76 % of the issue slots (65536 tokens 68 us; 1150 with an IEEE
 // division and expf for every expert, which the k chosen ones alone need, and a group found by dividing).  The rounds of a selection over
 // all keys go over the lanes' largest; who reaches the last of these finds its rank among a dozen.
 template <int NPL, bool WHOLE>
