@@ -13,7 +13,7 @@
 // Where there are few tiles and a long reduction, GRAM sums parts of it and JOIN adds them up in their order (one matrix of 256 x 7168:
 // 210 -> 140 us).
 //
-// What bounds it.  Large batches: power.  The tensor pipe is active 70 to 77 % of the clocks, at 1.4 GHz under the limit; 1.03 to 1.25 PFLOP/s
+// What bounds it.  Large batches: power.  The tensor pipe is active 68 to 77 % of the clocks, at 1.4 GHz under the limit; 1.03 to 1.26 PFLOP/s
 // of executed products, where batched fp16 products of these shapes by the vendor's library sustain 1.07 and 1.16.  Without an epilogue
 // it is 78 to 85 %: a k-block brings 32 KB into an SM and the products read as much, near what shared memory gives in the products' 512 clocks.
 // Few matrices: latency, 3.7 us a product from the signal of the one before (poll 0.5, loads 0.8, products and commit 0.6 and up,
